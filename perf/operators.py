@@ -325,7 +325,7 @@ def _own(st):
     desc = dict(q=st["q"], k=st["k"], v=st["v"], log_decay=st["g"], scale=st["scale"], state_in=st["s_in"],
                 lengths=st["lengths"])
     if op == "la_bwd":
-        desc.update(do=st["do"], dq=st["dq"], dk=st["dk"], dv=st["dv"], dstate_out=st["ds_out"], dstate_in=st["ds_in"])
+        desc.update(dout=st["do"], dq=st["dq"], dk=st["dk"], dv=st["dv"], dstate_out=st["ds_out"], dstate_in=st["ds_in"])
         lp.lp_linear_attention_bf16(lp.LP_LINATTN_BACKWARD, desc, st["ws"], stream)
         out = [st["dq"], st["dk"], st["dv"]]
         return out + [st["ds_in"]] if st["ds_in"] is not None else out
