@@ -364,6 +364,88 @@ lp_status lp_attention_bf16(int form, const void* qkv, void* o, float* lse, cons
                             int batch, int seq_len, int n_heads, void* stream);
 
 /*
+ * Operators of language models, next to lp_attention_bf16: token embedding and its gradient, dropout, linear
+ * attention.  They work on the caller's buffers alone and keep nothing between calls: scratch memory is a workspace the
+ * caller owns (any content, 256-byte aligned, not shared by calls whose work may overlap on the GPU, a captured graph's
+ * replays among them).  All pointers are device pointers of the current device; outputs must not overlap inputs except
+ * where that is said.  The calls are asynchronous on `stream`, allocate nothing, do not synchronise and can be captured
+ * into a CUDA graph.  Sums are in fp32 in a fixed order: equal calls give equal bits.  Errors of all of them:
+ * INVALID_ARG (null or host pointer, unknown dtype or form, values out of range, workspace too small), SHAPE,
+ * UNSUPPORTED (alignment, another device's memory), CUDA; message: lp_last_error(NULL).  A refused call launches nothing.
+ */
+
+/*
+ * lp_embed_forward:  out[r] = scale * table[ids[r]] + pos[r mod seq_len].
+ *   dtype LP_FP32 or LP_BF16: type of table [vocab, d], pos [seq_len, d] and out [rows, d], row-major, any d, aligned to
+ *   their element.  ids: int32 [rows].  pos may be NULL (seq_len is then ignored).  One rounding, on storing.
+ *   An id outside [0, vocab) is clamped and, if out_of_range is not NULL, bit 0 of that device int is set (never cleared).
+ */
+lp_status lp_embed_forward(int dtype, const int* ids, const void* table, const void* pos, void* out, int rows, int vocab,
+                           int d, int seq_len, float scale, int* out_of_range, void* stream);
+
+/*
+ * lp_embed_backward: dtable[v] = scale * sum of dout[r] over the rows with ids[r] = v (0 where there is none),
+ * dpos[t] = sum of dout[r] over the rows with r mod seq_len = t.  dout [rows, d] in dtype; dtable [vocab, d] and dpos
+ * [seq_len, d] fp32, overwritten; dpos may be NULL.  The rows are sorted by token and every sum runs over its rows in
+ * increasing r (in pieces of fixed length, added in order, for a token with many rows): no atomics on floats.
+ * Ids out of range as in lp_embed_forward: their rows count for the clamped token.
+ * rows <= 2^30.  workspace: lp_embed_workspace_bytes(rows, vocab, d) (0: sizes not accepted).
+ */
+size_t lp_embed_workspace_bytes(int rows, int vocab, int d);
+lp_status lp_embed_backward(int dtype, const int* ids, const void* dout, float* dtable, float* dpos, int rows, int vocab,
+                            int d, int seq_len, float scale, int* out_of_range, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
+/*
+ * lp_dropout:  y[i] = resid[i] + (word(i) >= floor(p * 2^32) ? x[i] / (1 - p) : 0),  0 <= i < n,  0 <= p < 1.
+ *   word(i) is word i mod 4 of Philox4x32-10 with key = seed (low word, high word) and counter = (offset + i / 4) mod
+ *   2^64 (low word, high word, 0, 0).  offset_dev (device, nullable, 8-byte aligned): added to offset on the device, so
+ *   that a captured call can draw other words at every replay.  No mask is stored: the gradient of x is the same call on
+ *   dy with resid NULL and the same p, seed and offset; the gradient of resid is dy.  Advance offset by (n + 3) / 4 for
+ *   words that no other call uses.  A dropped element is selected away (a NaN or infinity there does not reach y).
+ *   dtype: type of x, resid (nullable) and y, aligned to their element.  y may be x or resid.
+ */
+lp_status lp_dropout(int dtype, const void* x, const void* resid, void* y, long long n, double p,
+                     unsigned long long seed, unsigned long long offset, const unsigned long long* offset_dev, void* stream);
+
+/*
+ * lp_linear_attention_bf16: causal linear attention with a decay for each head, heads of 64, bf16 tokens, fp32 states.
+ *   S_t = exp(log_decay[h]) * S_{t-1} + k_t v_t^T  (64 x 64: rows k, columns v),   o_t = scale * q_t S_t
+ *   log_decay: fp32 [n_heads], <= 0 (-infinity: a token sees itself only).
+ *   Tokens: element i of head h of token t of sequence b is p[b * batch_stride + t * token_stride + 64 h + i] (strides in
+ *   elements): separate tensors and slices of a packed [batch, seq_len, 3, n_heads, 64] tensor alike.  Pointers 16-byte
+ *   aligned, strides multiples of 8, token_stride >= 64 * n_heads (seq_len 1: ignored).
+ *   States: fp32 [batch, n_heads, 64, 64], contiguous, 16-byte aligned.
+ *   lengths (nullable): int32 [batch], sequence b has lengths[b] tokens (clamped to [0, seq_len]); tokens behind are not
+ *   read, and rows of outputs and gradients behind are left as they were.
+ *   LP_LINATTN_FORWARD:  q, k, v, [state_in] -> o, [state_out].  state_in NULL: zero.  state_out, if given, receives the
+ *       state behind the last token (state_in itself for an empty sequence) and may be state_in.
+ *   LP_LINATTN_BACKWARD: q, k, v, dout, [state_in], [dstate_out: gradient of state_out, NULL: zero] -> dq, dk, dv,
+ *       [dstate_in: gradient of state_in; may be dstate_out].  log_decay carries no gradient.
+ *   LP_LINATTN_STEP:     the recurrent form, seq_len 1: as FORWARD, all arithmetic in fp32; lengths[b] = 0 marks an idle
+ *       sequence.
+ *   FORWARD and BACKWARD form scores and state products on bf16 operands with fp32 accumulation; state_out and dstate_in
+ *   are accurate to about 2^-17 relative to the terms they add up.  A NaN or infinity in token t reaches the outputs from t
+ *   on, and may reach earlier ones of the same 16 tokens.
+ *   batch * n_heads <= 2^20.  workspace: lp_linear_attention_workspace_bytes (may be 0).
+ */
+enum { LP_LINATTN_FORWARD = 0, LP_LINATTN_BACKWARD = 1, LP_LINATTN_STEP = 2 };
+typedef struct { const void* p; long long batch_stride, token_stride; } lp_tokens;
+typedef struct {
+  lp_tokens q, k, v, o, dout, dq, dk, dv; /* o, dq, dk, dv are written */
+  const float* log_decay;
+  const float* state_in;
+  float* state_out;
+  const float* dstate_out;
+  float* dstate_in;
+  const int* lengths;
+  int batch, seq_len, n_heads;
+  float scale;
+} lp_linattn_desc;
+size_t lp_linear_attention_workspace_bytes(int form, int batch, int seq_len, int n_heads);
+lp_status lp_linear_attention_bf16(int form, const lp_linattn_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * lp_gemm_bf16_static: lp_gemm_bf16 for callers that cannot allocate device memory.  (The paper
  * has no counterpart to this entry point; it exists for the library's users.)
  *

@@ -62,7 +62,8 @@ EXPORTS = ["lp_create", "lp_step", "lp_step_host", "lp_forward", "lp_destroy", "
            "lp_tensor_info_get", "lp_get_tensor", "lp_set_tensor", "lp_reset_pipeline", "lp_status_poll",
            "lp_state_size", "lp_save_state", "lp_load_state", "lp_last_step_launches", "lp_device_bytes",
            "lp_last_error", "lp_gemm_bf16", "lp_profile_enable", "lp_profile_read",
-           "lp_attention_bf16", "lp_gemm_bf16_static", "lp_gemm_static_poll", "lp_gemm_static_last_error", "lp_conv3x3_bf16", "lp_conv2d_bf16", "lp_set_ramp", "lp_set_drain", "lp_set_fused_step", "lp_evaluate", "lp_set_overlap",
+           "lp_attention_bf16", "lp_embed_forward", "lp_embed_backward", "lp_embed_workspace_bytes", "lp_dropout",
+           "lp_linear_attention_bf16", "lp_linear_attention_workspace_bytes", "lp_gemm_bf16_static", "lp_gemm_static_poll", "lp_gemm_static_last_error", "lp_conv3x3_bf16", "lp_conv2d_bf16", "lp_set_ramp", "lp_set_drain", "lp_set_fused_step", "lp_evaluate", "lp_set_overlap",
            "lp_cost_model", "lp_mlp_layer_flops", "lp_mlp_aux_flops", "lp_chunk_output_bytes", "lp_chunk_output"]
 LP_KIND_NAMES = ["other", "gemm_tc", "gemm_alu", "norm", "xent", "attn", "optim", "reduce", "embed", "conv_aux"]
 
@@ -359,6 +360,104 @@ def lp_attention_bf16(form: int, qkv, o, lse, dout, dqkv, delta, batch: int, seq
     lse; backward reads them and dout and writes dqkv and delta.  Tensors may be torch tensors or raw pointers."""
     _check(None, _lib.lp_attention_bf16(form, _ptr(qkv), _ptr(o), _ptr(lse), _ptr(dout), _ptr(dqkv), _ptr(delta),
                                         batch, seq_len, n_heads, stream))
+
+
+def _dev(t):
+    """Device address of a CUDA tensor or raw address; anything on the host is refused before a kernel can see it."""
+    if t is None or isinstance(t, int):
+        return t
+    if not getattr(t, "is_cuda", False):
+        raise LpError(-1, "a host tensor was given where device memory is needed")
+    return t.data_ptr()
+
+
+_lib.lp_embed_forward.argtypes = [C.c_int] + [C.c_void_p] * 4 + [C.c_int] * 4 + [C.c_float, C.c_void_p, C.c_void_p]
+_lib.lp_embed_backward.argtypes = [C.c_int] + [C.c_void_p] * 4 + [C.c_int] * 4 + [C.c_float, C.c_void_p, C.c_void_p, C.c_size_t,
+                                                                                C.c_void_p]
+_lib.lp_embed_workspace_bytes.argtypes = [C.c_int] * 3
+_lib.lp_embed_workspace_bytes.restype = C.c_size_t
+
+
+def lp_embed_forward(dtype: int, ids, table, pos, out, rows: int, vocab: int, d: int, seq_len: int, scale: float = 1.0,
+                     out_of_range=None, stream=None) -> None:
+    """out[r] = scale * table[ids[r]] + pos[r mod seq_len] (see lp.h).  Tensors may be CUDA tensors or raw device
+    pointers; pos and out_of_range may be None."""
+    _check(None, _lib.lp_embed_forward(dtype, _dev(ids), _dev(table), _dev(pos), _dev(out), rows, vocab, d, seq_len, scale,
+                                       _dev(out_of_range), stream))
+
+
+def lp_embed_workspace_bytes(rows: int, vocab: int, d: int) -> int:
+    return _lib.lp_embed_workspace_bytes(rows, vocab, d)
+
+
+def lp_embed_backward(dtype: int, ids, dout, dtable, dpos, rows: int, vocab: int, d: int, seq_len: int, scale: float = 1.0,
+                      out_of_range=None, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    """Gradients of the token table (fp32 [vocab, d], written whole) and, if dpos is given, of the position table,
+    summed over the rows sorted by token (see lp.h)."""
+    _check(None, _lib.lp_embed_backward(dtype, _dev(ids), _dev(dout), _dev(dtable), _dev(dpos), rows, vocab, d, seq_len, scale,
+                                        _dev(out_of_range), _dev(workspace), workspace_bytes, stream))
+
+
+_lib.lp_dropout.argtypes = [C.c_int] + [C.c_void_p] * 3 + [C.c_longlong, C.c_double, C.c_ulonglong, C.c_ulonglong, C.c_void_p,
+                                                           C.c_void_p]
+
+
+def lp_dropout(dtype: int, x, resid, y, n: int, p: float, seed: int, offset: int = 0, offset_dev=None, stream=None) -> None:
+    """y = resid + dropout(x), the mask drawn from Philox4x32-10 and never stored (see lp.h); the gradient of x is the
+    same call on dy with resid None.  y may be x or resid."""
+    _check(None, _lib.lp_dropout(dtype, _dev(x), _dev(resid), _dev(y), n, p, seed, offset, _dev(offset_dev), stream))
+
+
+LP_LINATTN_FORWARD, LP_LINATTN_BACKWARD, LP_LINATTN_STEP = 0, 1, 2
+
+
+class lp_tokens(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("batch_stride", C.c_longlong), ("token_stride", C.c_longlong)]
+
+
+class lp_linattn_desc(C.Structure):
+    _fields_ = [(n, lp_tokens) for n in ("q", "k", "v", "o", "dout", "dq", "dk", "dv")] + \
+               [(n, C.c_void_p) for n in ("log_decay", "state_in", "state_out", "dstate_out", "dstate_in", "lengths")] + \
+               [("batch", C.c_int), ("seq_len", C.c_int), ("n_heads", C.c_int), ("scale", C.c_float)]
+
+
+_lib.lp_linear_attention_bf16.argtypes = [C.c_int, C.POINTER(lp_linattn_desc), C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.lp_linear_attention_workspace_bytes.argtypes = [C.c_int] * 4
+_lib.lp_linear_attention_workspace_bytes.restype = C.c_size_t
+
+
+def lp_linear_attention_workspace_bytes(form: int, batch: int, seq_len: int, n_heads: int) -> int:
+    return _lib.lp_linear_attention_workspace_bytes(form, batch, seq_len, n_heads)
+
+
+def lp_linear_attention_bf16(form: int, desc: dict, workspace=None, stream=None) -> None:
+    """Linear attention with a decay per head (see lp.h): forward, backward or the single-token step.  `desc` names the
+    tensors of lp_linattn_desc: q, k, v, o, dout, dq, dk, dv are bf16 CUDA tensors [batch, seq_len, n_heads, 64] (slices
+    of larger ones are fine: strides are read off), the states fp32 [batch, n_heads, 64, 64], log_decay fp32 [n_heads],
+    lengths int32 [batch]; `scale` a number.  Sizes come from q; the other tensors' shapes must agree."""
+    d = lp_linattn_desc()
+    shape = tuple(desc["q"].shape)
+    for name, value in desc.items():
+        if name == "scale":
+            d.scale = value
+        elif value is None:
+            continue
+        elif name in ("q", "k", "v", "o", "dout", "dq", "dk", "dv"):
+            if tuple(value.shape) != shape or len(shape) != 4 or shape[3] != 64 or value.element_size() != 2:
+                raise LpError(-2, f"lp_linear_attention_bf16: {name} must be bf16 [batch, seq_len, n_heads, 64], as q")
+            s = value.stride()
+            if s[3] != 1 or (shape[2] > 1 and s[2] != 64):
+                raise LpError(-3, f"lp_linear_attention_bf16: the heads of {name} must lie 64 elements apart")
+            t = getattr(d, name)
+            t.p, t.batch_stride, t.token_stride = _dev(value), s[0] if shape[0] > 1 else 0, s[1]
+        else:
+            want = {"log_decay": (shape[2],), "lengths": (shape[0],)}.get(name, (shape[0], shape[2], 64, 64))
+            if tuple(value.shape) != want or value.element_size() != 4 or not value.is_contiguous():
+                raise LpError(-2, f"lp_linear_attention_bf16: {name} must be contiguous {want} of four bytes each")
+            setattr(d, name, _dev(value))
+    d.batch, d.seq_len, d.n_heads = shape[:3]
+    nbytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(None, _lib.lp_linear_attention_bf16(form, C.byref(d), _dev(workspace) if nbytes else None, nbytes, stream))
 
 
 _lib.lp_conv2d_bf16.argtypes = [C.c_int, C.c_void_p, C.c_void_p, C.c_void_p] + [C.c_int] * 7 + [C.c_void_p]

@@ -776,6 +776,131 @@ lp_status lp_attention_bf16(int form, const void* qkv, void* o, float* lse, cons
   return LP_OK;
 }
 
+// ---- operators on the caller's buffers (embedding, dropout, linear attention)
+// The current device must be able to reach `out`: memory of another device, or of the host, is refused.
+static lp_status check_output(const char* what, const void* out) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return fail(nullptr, LP_ERR_CUDA, std::string(what) + ": no CUDA device"); }
+  cudaPointerAttributes at{};
+  if (cudaPointerGetAttributes(&at, out) != cudaSuccess) { cudaGetLastError(); return fail(nullptr, LP_ERR_CUDA, std::string(what) + ": cannot query a pointer"); }
+  if (at.type != cudaMemoryTypeDevice && at.type != cudaMemoryTypeManaged)
+    return fail(nullptr, LP_ERR_INVALID_ARG, std::string(what) + ": not a device pointer");
+  if (at.type == cudaMemoryTypeDevice && at.device != dev)
+    return fail(nullptr, LP_ERR_UNSUPPORTED, std::string(what) + ": memory of another device than the current one");
+  return LP_OK;
+}
+static lp_status launched(const char* what, cudaError_t e) {
+  if (e == cudaSuccess) return LP_OK;
+  cudaGetLastError();                            // this launch's own error: reported here, not by a later call
+  return fail(nullptr, LP_ERR_CUDA, std::string(what) + ": launch: " + cudaGetErrorString(e));
+}
+static bool aligned_to(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+static bool embed_sizes_ok(int rows, int vocab, int d) { return rows >= 1 && rows <= (1 << 30) && vocab >= 1 && d >= 1; }
+
+lp_status lp_embed_forward(int dtype, const int* ids, const void* table, const void* pos, void* out, int rows, int vocab,
+                           int d, int seq_len, float scale, int* out_of_range, void* stream) {
+  const char* me = "lp_embed_forward";
+  if (dtype != LP_FP32 && dtype != LP_BF16) return fail(nullptr, LP_ERR_INVALID_ARG, "lp_embed_forward: dtype");
+  if (!ids || !table || !out) return fail(nullptr, LP_ERR_INVALID_ARG, "lp_embed_forward: null pointer");
+  if (!embed_sizes_ok(rows, vocab, d) || (pos && seq_len < 1))
+    return fail(nullptr, LP_ERR_SHAPE, "lp_embed_forward: sizes must be positive (rows at most 2^30)");
+  const size_t es = dtype == LP_BF16 ? 2 : 4;
+  if (!aligned_to(ids, 4) || !aligned_to(table, es) || !aligned_to(pos, es) || !aligned_to(out, es) || !aligned_to(out_of_range, 4))
+    return fail(nullptr, LP_ERR_UNSUPPORTED, "lp_embed_forward: pointers must be aligned to their element");
+  lp_status st = check_output(me, out);
+  if (st != LP_OK) return st;
+  const EmbedProb p{ids, table, pos, out, rows, pos ? seq_len : 1, d, vocab, scale};
+  return launched(me, launch_embed_fwd(p, out_of_range, dtype == LP_BF16, (cudaStream_t)stream));
+}
+
+size_t lp_embed_workspace_bytes(int rows, int vocab, int d) { return embed_sizes_ok(rows, vocab, d) ? embed_bwd_workspace(rows, vocab, d) : 0; }
+
+lp_status lp_embed_backward(int dtype, const int* ids, const void* dout, float* dtable, float* dpos, int rows, int vocab,
+                            int d, int seq_len, float scale, int* out_of_range, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+  const char* me = "lp_embed_backward";
+  if (dtype != LP_FP32 && dtype != LP_BF16) return fail(nullptr, LP_ERR_INVALID_ARG, "lp_embed_backward: dtype");
+  if (!ids || !dout || !dtable || !workspace) return fail(nullptr, LP_ERR_INVALID_ARG, "lp_embed_backward: null pointer");
+  if (!embed_sizes_ok(rows, vocab, d) || (dpos && seq_len < 1))
+    return fail(nullptr, LP_ERR_SHAPE, "lp_embed_backward: sizes must be positive (rows at most 2^30)");
+  if (workspace_bytes < embed_bwd_workspace(rows, vocab, d)) return fail(nullptr, LP_ERR_INVALID_ARG, "lp_embed_backward: workspace too small");
+  if (!aligned_to(ids, 4) || !aligned_to(dout, dtype == LP_BF16 ? 2 : 4) || !aligned_to(dtable, 4) || !aligned_to(dpos, 4) ||
+      !aligned_to(out_of_range, 4) || !aligned_to(workspace, 256))
+    return fail(nullptr, LP_ERR_UNSUPPORTED, "lp_embed_backward: pointers must be aligned to their element, the workspace to 256 bytes");
+  lp_status st = check_output(me, dtable);
+  if (st != LP_OK) return st;
+  const EmbedBwdProb p{ids, dout, dtable, dpos, rows, dpos ? seq_len : 0, d, vocab, scale, nullptr, nullptr, nullptr, nullptr};
+  return launched(me, launch_embed_bwd(p, workspace, out_of_range, dtype == LP_BF16, (cudaStream_t)stream));
+}
+
+lp_status lp_dropout(int dtype, const void* x, const void* resid, void* y, long long n, double p, unsigned long long seed,
+                     unsigned long long offset, const unsigned long long* offset_dev, void* stream) {
+  const char* me = "lp_dropout";
+  if (dtype != LP_FP32 && dtype != LP_BF16) return fail(nullptr, LP_ERR_INVALID_ARG, "lp_dropout: dtype");
+  if (!(p >= 0.0 && p < 1.0)) return fail(nullptr, LP_ERR_INVALID_ARG, "lp_dropout: p must be in [0, 1)");
+  if (n < 0) return fail(nullptr, LP_ERR_SHAPE, "lp_dropout: n must not be negative");
+  if (n == 0) return LP_OK;
+  if (!x || !y) return fail(nullptr, LP_ERR_INVALID_ARG, "lp_dropout: null pointer");
+  const size_t es = dtype == LP_BF16 ? 2 : 4;
+  if (!aligned_to(x, es) || !aligned_to(resid, es) || !aligned_to(y, es) || !aligned_to(offset_dev, 8))
+    return fail(nullptr, LP_ERR_UNSUPPORTED, "lp_dropout: pointers must be aligned to their element");
+  lp_status st = check_output(me, y);
+  if (st != LP_OK) return st;
+  const DropoutArgs a{x, resid, y, n, dropout_threshold(p), (float)(1.0 / (1.0 - p)), seed, offset, offset_dev, 0, 0};
+  return launched(me, launch_dropout(a, dtype == LP_BF16, (cudaStream_t)stream));
+}
+
+size_t lp_linear_attention_workspace_bytes(int form, int batch, int seq_len, int n_heads) {
+  if (batch < 1 || seq_len < 1 || n_heads < 1 || (long long)batch * n_heads > (1 << 20)) return 0;
+  return form == LP_LINATTN_FORWARD || form == LP_LINATTN_BACKWARD ? linattn_workspace(form == LP_LINATTN_BACKWARD, batch, seq_len, n_heads) : 0;
+}
+
+lp_status lp_linear_attention_bf16(int form, const lp_linattn_desc* d, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* me = "lp_linear_attention_bf16";
+  auto bad = [&](lp_status code, const char* why) { return fail(nullptr, code, std::string(me) + ": " + why); };
+  if (form != LP_LINATTN_FORWARD && form != LP_LINATTN_BACKWARD && form != LP_LINATTN_STEP) return bad(LP_ERR_INVALID_ARG, "unknown form");
+  const bool back = form == LP_LINATTN_BACKWARD;
+  if (!d || !d->q.p || !d->k.p || !d->v.p || !d->log_decay) return bad(LP_ERR_INVALID_ARG, "null pointer");
+  if (back ? !d->dout.p || !d->dq.p || !d->dk.p || !d->dv.p : !d->o.p) return bad(LP_ERR_INVALID_ARG, "null pointer");
+  if (d->batch < 1 || d->seq_len < 1 || d->n_heads < 1) return bad(LP_ERR_SHAPE, "sizes must be positive");
+  if ((long long)d->batch * d->n_heads > (1 << 20)) return bad(LP_ERR_SHAPE, "batch * n_heads must be at most 2^20");
+  if (form == LP_LINATTN_STEP && d->seq_len != 1) return bad(LP_ERR_SHAPE, "the recurrent form takes one token");
+  const lp_tokens* all[8] = {&d->q, &d->k, &d->v, &d->o, &d->dout, &d->dq, &d->dk, &d->dv};
+  const bool used[8] = {true, true, true, !back, back, back, back, back};
+  for (int i = 0; i < 8; ++i) {
+    if (!used[i]) continue;
+    if (!aligned_to(all[i]->p, 16) || (all[i]->batch_stride & 7) || (all[i]->token_stride & 7))
+      return bad(LP_ERR_UNSUPPORTED, "tokens must be 16-byte aligned, their strides multiples of 8 elements");
+    if (all[i]->batch_stride < 0 || (d->seq_len > 1 && all[i]->token_stride < 64LL * d->n_heads))
+      return bad(LP_ERR_SHAPE, "token_stride must be at least 64 * n_heads, batch_stride not negative");
+    if (i >= 3 && i != 4 && d->batch > 1 && all[i]->batch_stride < 64LL * d->n_heads)
+      return bad(LP_ERR_SHAPE, "the sequences of an output overlap");
+  }
+  const void* outs[4] = {back ? d->dq.p : d->o.p, back ? d->dk.p : nullptr, back ? d->dv.p : nullptr, nullptr};
+  for (int i = 0; i < 3; ++i) {
+    if (!outs[i]) continue;
+    if (outs[i] == d->q.p || outs[i] == d->k.p || outs[i] == d->v.p || (back && outs[i] == d->dout.p)) return bad(LP_ERR_INVALID_ARG, "an output is an input");
+    for (int j = 0; j < i; ++j) if (outs[i] == outs[j]) return bad(LP_ERR_INVALID_ARG, "two outputs are the same");
+  }
+  if (!aligned_to(d->state_in, 16) || !aligned_to(d->log_decay, 4) || !aligned_to(d->lengths, 4) ||
+      (!back && !aligned_to(d->state_out, 16)) || (back && (!aligned_to(d->dstate_out, 16) || !aligned_to(d->dstate_in, 16))))
+    return bad(LP_ERR_UNSUPPORTED, "states must be 16-byte aligned");
+  if (back && d->dstate_in && d->dstate_in == d->state_in) return bad(LP_ERR_INVALID_ARG, "an output is an input");
+  if (d->scale != d->scale) return bad(LP_ERR_INVALID_ARG, "scale is not a number");
+  const size_t need = form == LP_LINATTN_STEP ? 0 : linattn_workspace(back, d->batch, d->seq_len, d->n_heads);
+  if (need && (!workspace || workspace_bytes < need)) return bad(LP_ERR_INVALID_ARG, "workspace too small");
+  if (need && !aligned_to(workspace, 256)) return bad(LP_ERR_UNSUPPORTED, "the workspace must be 256-byte aligned");
+  lp_status st = check_output(me, outs[0]);
+  if (st != LP_OK) return st;
+  auto tok = [](const lp_tokens& t) { return LinAttnTok{(const bf16*)t.p, t.token_stride, t.batch_stride}; };
+  LinAttnArgs a{tok(d->q), tok(d->k), tok(d->v), tok(d->o), tok(d->dout), tok(d->dq), tok(d->dk), tok(d->dv),
+                d->log_decay, d->state_in, back ? nullptr : d->state_out, back ? d->dstate_out : nullptr, back ? d->dstate_in : nullptr,
+                d->lengths, d->batch, d->seq_len, d->n_heads, d->scale, 1, 0, nullptr, nullptr};
+  // one token takes the recurrent kernel in either form: the chunked one would work on 63 empty rows
+  const cudaError_t e = !back && d->seq_len == 1 ? launch_linattn_step(a, (cudaStream_t)stream) : launch_linattn(a, back, workspace, (cudaStream_t)stream);
+  return launched(me, e);
+}
+
 lp_status lp_profile_enable(lp_handle hh, int on) {
   if (!hh) return LP_ERR_INVALID_ARG;
   hh->h.profiling = on != 0;

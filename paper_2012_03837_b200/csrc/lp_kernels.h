@@ -153,12 +153,38 @@ struct LossProb { const float* row_loss; const int* n_valid; int rows; int out_i
 void launch_loss_reduce(const LossProb* d_probs, int n, float* d_losses, int* d_status, cudaStream_t s);
 
 // ---------------------------------------------------------------------------- LM-specific
-struct EmbedProb { const int* ids; const void* tok; const void* pos; void* h; int rows, T, d, vocab; };
-void launch_embed_fwd(const EmbedProb& p, int* d_status, bool is_bf16, cudaStream_t s);
+struct EmbedProb { const int* ids; const void* tok; const void* pos; void* h; int rows, T, d, vocab; float scale; };
+cudaError_t launch_embed_fwd(const EmbedProb& p, int* d_status, bool is_bf16, cudaStream_t s);
+// Gradients of both tables (pos: T = 0 and dpos null if there is none); the last four pointers are set by the launcher,
+// inside a workspace of embed_bwd_workspace() bytes, 256-byte aligned.
 struct EmbedBwdProb {
-  const int* ids; const void* dh; float* dtok; float* dpos; int* next; int* first; int rows, T, d, vocab, B;
+  const int* ids; const void* dh; float* dtok; float* dpos; int rows, T, d, vocab; float scale;
+  int2* sorted; int2* seg; float* part; float* pos_part;
 };
-void launch_embed_bwd(const EmbedBwdProb& p, bool is_bf16, cudaStream_t s);
+size_t embed_bwd_workspace(int rows, int vocab, int d);
+cudaError_t launch_embed_bwd(EmbedBwdProb p, void* workspace, int* d_status, bool is_bf16, cudaStream_t s);
+
+// ---------------------------------------------------------------------------- dropout, linear attention
+struct DropoutArgs {
+  const void* x; const void* resid; void* y; long long n;
+  uint32_t threshold; float scale;               // word >= threshold keeps the element, times scale
+  unsigned long long seed, offset; const unsigned long long* offset_dev;
+  uint32_t w2, w3;                               // upper counter words
+};
+// floor(p 2^32) for p in [0, 1): the product is exact in 64 bits, the conversion truncates
+inline uint32_t dropout_threshold(double p) { return (uint32_t)(p * 4294967296.0); }
+cudaError_t launch_dropout(const DropoutArgs& a, bool is_bf16, cudaStream_t s);
+
+struct LinAttnTok { const bf16* p; long long ts, bs; };   // element (b, t, head h, i) at p[b * bs + t * ts + 64 h + i]
+struct LinAttnArgs {
+  LinAttnTok q, k, v, o, dout, dq, dk, dv;
+  const float* log_decay; const float* state_in; float* state_out; const float* dstate_out; float* dstate_in; const int* lengths;
+  int B, T, H; float scale;
+  int n_seg, seg_len; float* seg_states; float* seg_grads;   // set by the launcher
+};
+size_t linattn_workspace(bool backward, int B, int T, int H);
+cudaError_t launch_linattn(LinAttnArgs a, bool backward, void* workspace, cudaStream_t s);
+cudaError_t launch_linattn_step(const LinAttnArgs& a, cudaStream_t s);
 
 struct AttnProb {     // causal attention over qkv [B*T, 3d], heads of 64
   const void* qkv; void* o; float* lse; const void* dout; void* dqkv; float* delta; int B, T, H;

@@ -80,8 +80,7 @@ void build_lm(Handle& h) {
   h.x_in = h.dalloc(h.x_bytes);
   h.y_bytes = (size_t)M * sizeof(int);
   h.y_in = (int*)h.dalloc(h.y_bytes);
-  int* emb_next = (int*)h.dalloc((size_t)M * sizeof(int));
-  int* emb_first = (int*)h.dalloc((size_t)M * sizeof(int));
+  void* emb_ws = inner ? nullptr : h.dalloc(embed_bwd_workspace(M, V, d));
   auto fal = [&](size_t n) { return (float*)h.dalloc(n * sizeof(float)); };
   for (int k = 0; k < K; ++k) {
     h.bnd_bytes.push_back(md);
@@ -139,7 +138,7 @@ void build_lm(Handle& h) {
   auto forward = [&](Plan& p, const std::vector<int>& ks, int rd, int wr) {
     for (int k : ks)
       if (k == 0 && !inner) {
-        EmbedProb e{(const int*)h.x_in, h.W("c0.tok"), h.W("c0.pos"), cb[0].emb, M, T, d, V};
+        EmbedProb e{(const int*)h.x_in, h.W("c0.tok"), h.W("c0.pos"), cb[0].emb, M, T, d, V, 1.f};
         p.add(1, [e, st, bf](const RunCtx& c) { launch_embed_fwd(e, st, bf, c.stream); }, KIND_EMBED, 3.0 * M * d * es);
       }
     size_t maxb = 0;
@@ -387,8 +386,8 @@ void build_lm(Handle& h) {
       // chunk 0, first block: embedding tables
       for (auto& it : items)
         if (!inner && it.c == &cb[0] && it.b == &cb[0].blocks[0]) {
-          EmbedBwdProb e{(const int*)h.x_in, cb[0].G0, h.G("c0.tok"), h.G("c0.pos"), emb_next, emb_first, M, T, d, V, B};
-          p.add(6, [e, bf](const RunCtx& c) { launch_embed_bwd(e, bf, c.stream); }, KIND_EMBED, (double)M * d * es + 4.0 * V * d);
+          EmbedBwdProb e{(const int*)h.x_in, cb[0].G0, h.G("c0.tok"), h.G("c0.pos"), M, T, d, V, 1.f, nullptr, nullptr, nullptr, nullptr};
+          p.add(3, [e, emb_ws, bf](const RunCtx& c) { launch_embed_bwd(e, emb_ws, nullptr, bf, c.stream); }, KIND_EMBED, (double)M * d * es + 4.0 * V * d);
         }
     }
     // ---- overlapping updates (Sec. 3, Fig. 2 c): chunk k's loss, whose gradient at the chunk input now sits in

@@ -1,0 +1,365 @@
+"""Embedding and its gradient by sorted tokens, dropout, and linear attention on the GPU against their plain 64-bit
+forms (oracle/lm_ops.py), at the sizes, strides, masks and lengths where they can go wrong.
+
+Tolerances.  u(t) = finfo(t).eps / 2 is the largest relative error of one rounding: 2^-8 for bf16, 2^-24 for fp32.  A sum
+of n terms in fp32 is off by at most n * 2^-24 * sum |terms|; a stored bf16 value adds 2^-8 of itself."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import lm_ops as O
+from paper_2012_03837_b200 import binding as lp
+
+pytestmark = pytest.mark.gpu
+DT = {"fp32": (lp.LP_FP32, torch.float32, 2.0 ** -24), "bf16": (lp.LP_BF16, torch.bfloat16, 2.0 ** -8)}
+U16, U32 = 2.0 ** -8, 2.0 ** -24
+
+
+def cu(a, dtype=torch.float32):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda().to(dtype)
+
+
+def np64(t):
+    return t.double().cpu().numpy()
+
+
+def shifted(shape, dtype, off, fill=float("nan")):
+    """A tensor whose first element lies `off` elements behind an aligned address."""
+    n = int(np.prod(shape))
+    return torch.full((n + off,), fill, dtype=dtype, device="cuda")[off:off + n].view(shape)
+
+
+# ------------------------------------------------------------------------------------------------ embedding
+EMBED = [  # rows, vocab, d, T, tokens
+    (1, 2, 8, 0, "uniform"), (1, 1, 1, 1, "uniform"), (7, 5, 64, 3, "uniform"), (64, 500, 520, 0, "uniform"),
+    (300, 40, 33, 7, "uniform"), (513, 1000, 96, 512, "zipf"), (1000, 3, 24, 1, "uniform"), (700, 90, 1032, 50, "same"),
+    (33000, 129, 8, 100, "zipf"), (2049, 200000, 16, 0, "uniform"), (33000, 7, 40, 2, "same"), (17, 30, 2056, 4, "runs"),
+    (4000, 60, 12, 66, "runs"),
+]
+
+
+def make_ids(g, rows, vocab, kind):
+    if kind == "same":
+        return np.full(rows, vocab - 1, dtype=np.int32)
+    if kind == "runs":                              # counts 15, 16, 17, 32, 33: around the length of a stretch
+        runs = np.repeat(np.arange(5 * 40) % vocab, np.tile([15, 16, 17, 32, 33], 40))
+        return np.resize(runs, rows).astype(np.int32)
+    if kind == "zipf":
+        w = 1.0 / np.arange(1, vocab + 1)
+        return g.choice(vocab, rows, p=w / w.sum()).astype(np.int32)
+    return g.integers(0, vocab, rows).astype(np.int32)
+
+
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+@pytest.mark.parametrize("off", [0, 1])
+@pytest.mark.parametrize("rows,vocab,d,T,kind", EMBED)
+def test_embedding_forward_and_gradient(rows, vocab, d, T, kind, off, dt):
+    code, td, u = DT[dt]
+    g = np.random.default_rng(rows + d)
+    ids = make_ids(g, rows, vocab, kind)
+    scale = 1.7
+    table, pos, dout = (shifted(s, td, off) for s in ((vocab, d), (max(T, 1), d), (rows, d)))
+    for x in (table, pos, dout):
+        x.copy_(cu(g.standard_normal(x.shape)).to(td))
+    t_ids = cu(ids, torch.int32)
+    out = shifted((rows, d), td, off)
+    lp.lp_embed_forward(code, t_ids, table, pos if T else None, out, rows, vocab, d, T, scale)
+    p64 = np64(pos) if T else None
+    want = O.embed_fwd(ids, np64(table), p64, scale)
+    mag = scale * np.abs(np64(table)[ids]) + (np.abs(p64[np.arange(rows) % T]) if T else 0)
+    # scale itself rounds to fp32 once, the product and sum at most once each, the store once
+    assert (np.abs(np64(out) - want) <= 3 * U32 * mag + u * np.abs(want) * (1 + u)).all()
+
+    dtab, dpos = shifted((vocab, d), torch.float32, off), shifted((max(T, 1), d), torch.float32, off)
+    ws = torch.full((lp.lp_embed_workspace_bytes(rows, vocab, d),), 255, dtype=torch.uint8, device="cuda")
+    args = (code, t_ids, dout, dtab, dpos if T else None, rows, vocab, d, T, scale, None, ws, ws.numel())
+    lp.lp_embed_backward(*args)
+    x64 = np64(dout)
+    w_tab, w_pos = O.embed_bwd(ids, x64, vocab, T, scale)
+    m_tab, m_pos = O.embed_bwd(ids, np.abs(x64), vocab, T, scale)
+    n_tab = np.bincount(ids, minlength=vocab)[:, None]
+    got = np64(dtab)
+    assert (np.abs(got - w_tab) <= (n_tab + 2) * U32 * m_tab).all()
+    assert (got[n_tab[:, 0] == 0] == 0).all()
+    if T:
+        assert (np.abs(np64(dpos) - w_pos) <= (rows / T + 2) * U32 * m_pos).all()
+    first = dtab.clone(), dpos.clone()
+    dtab.fill_(float("nan"))
+    lp.lp_embed_backward(*args)                     # a used workspace; the same bits
+    assert torch.equal(dtab, first[0]) and (not T or torch.equal(dpos, first[1]))
+
+
+def test_embedding_ids_out_of_range_are_clamped_and_flagged():
+    ids = cu(np.array([0, -1, 9, 4, 2 ** 31 - 1, -2 ** 31]), torch.int32)
+    table = cu(np.arange(10.0).reshape(5, 2))
+    out, flag = torch.empty(6, 2, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    lp.lp_embed_forward(lp.LP_FP32, ids, table, None, out, 6, 5, 2, 0, 1.0, flag)
+    assert flag.item() == 1 and out[:, 0].tolist() == [0, 0, 8, 8, 8, 0]
+    flag.zero_()
+    dtab, ws = torch.empty(5, 2, device="cuda"), torch.empty(lp.lp_embed_workspace_bytes(6, 5, 2), dtype=torch.uint8, device="cuda")
+    lp.lp_embed_backward(lp.LP_FP32, ids, torch.ones(6, 2, device="cuda"), dtab, None, 6, 5, 2, 0, 1.0, flag, ws, ws.numel())
+    assert flag.item() == 1 and dtab[:, 0].tolist() == [3, 0, 0, 0, 3]
+    flag.zero_()
+    lp.lp_embed_forward(lp.LP_FP32, ids[:1], table, None, out, 1, 5, 2, 0, 1.0, flag)
+    assert flag.item() == 0
+
+
+# ------------------------------------------------------------------------------------------------ dropout
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,p,resid,off,offset", [
+    (1, 0.5, False, 0, 0), (3, 0.1, True, 0, 2 ** 32 - 1), (8, 0.0, True, 0, 5), (1027, 0.9, False, 1, 2 ** 33 + 7),
+    (4096, 0.1, True, 0, 2 ** 64 - 3), (100003, 0.25, True, 3, 11), (700001, 0.37, False, 0, 123456789012),
+    (1 << 20, 0.1, True, 8, 0)])
+def test_dropout_matches_the_generator(n, p, resid, off, offset, dt):
+    code, td, u = DT[dt]
+    g = np.random.default_rng(n)
+    seed = 0x9E3779B97F4A7C15
+    x, y = shifted((n,), td, off), shifted((n,), td, off)
+    x.copy_(cu(g.standard_normal(n)).to(td))
+    r = cu(g.standard_normal(n)).to(td) if resid else None
+    keep = O.dropout_keep(n, p, seed, offset)
+    if n > 8:
+        x[cu(np.flatnonzero(~keep)[:5], torch.int64)] = float("nan")      # dropped: must not reach y
+    lp.lp_dropout(code, x, r, y, n, p, seed, offset)
+    x64 = np.where(keep, np64(x), 0.0)
+    r64 = np64(r) if resid else np.zeros(n)
+    want = x64 / (1.0 - p) + r64
+    mag = np.abs(x64) / (1.0 - p) + np.abs(r64)
+    assert (np.abs(np64(y) - want) <= 3 * U32 * mag + u * np.abs(want) * (1 + u)).all()
+    if not resid:                                   # whole mask, exactly
+        assert np.array_equal(np64(y) != 0, keep & (x64 != 0))
+    half = torch.tensor([offset // 2 if offset < 2 ** 63 else 17], dtype=torch.int64, device="cuda")
+    y2 = x.clone() if not resid else r.clone()      # in place on x or on resid, the offset partly on the device
+    lp.lp_dropout(code, x if resid else y2, y2 if resid else None, y2, n, p, seed, (offset - int(half)) % 2 ** 64, half)
+    assert torch.equal(y, y2)
+
+
+def test_dropout_gradient_uses_the_forward_mask():
+    n, p = 5000, 0.3
+    x, dy = torch.randn(n, device="cuda"), torch.randn(n, device="cuda")
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    lp.lp_dropout(lp.LP_FP32, x, None, y, n, p, 42, 9)
+    lp.lp_dropout(lp.LP_FP32, dy, None, dx, n, p, 42, 9)
+    assert torch.equal(y != 0, dx != 0)
+    h = 2.0 ** -6                                   # y is linear in x: the difference quotient is exact up to rounding
+    y2 = torch.empty_like(x)
+    lp.lp_dropout(lp.LP_FP32, x + h * dy, None, y2, n, p, 42, 9)
+    assert ((y2 - y).double() / h - dx.double()).abs().max() <= 4 * U32 * (x.abs() + dy.abs()).max().item() / (1 - p) / h
+
+
+# ------------------------------------------------------------------------------------------------ linear attention
+def la_inputs(B, T, H, seed, packed=False, pad=0):
+    g = np.random.default_rng(seed)
+    t = {}
+    if packed:
+        base = cu(g.standard_normal((B, T, 3, H, 64)), torch.bfloat16)
+        t["q"], t["k"], t["v"] = base[:, :, 0], base[:, :, 1], base[:, :, 2]
+    else:
+        for n in ("q", "k", "v"):
+            t[n] = cu(g.standard_normal((B, T + pad, H, 64)), torch.bfloat16)[:, :T]
+    t["dout"] = cu(g.standard_normal((B, T, H, 64)), torch.bfloat16)
+    lg = np.log1p(-2.0 ** -g.uniform(1.0, 10.0, H))
+    lg[0] = 0.0 if seed % 2 else lg[0]
+    if H > 1:
+        lg[1] = -40.0 if seed % 3 else -np.inf      # powers underflow inside a chunk
+    t["log_decay"] = cu(lg)
+    s = cu(g.standard_normal((2, B, H, 64, 64)))
+    t["state_in"], t["dstate_out"] = s[0], s[1]
+    return t
+
+
+def la_workspace(form, B, T, H):
+    n = lp.lp_linear_attention_workspace_bytes(form, B, T, H)
+    return torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+
+
+def check_tokens(name, got, want, mag, lens, fill, decayed_state):
+    """|error| <= 2^-8 of the output, plus 2^-8 per rounded operand of the terms it adds up: one (the scores) or two
+    (the decayed k and the state), plus fp32 sums of at most 128 terms a chunk and 64 per product."""
+    got = np64(got)
+    for b, n in enumerate(lens):
+        err = np.abs(got[b, :n] - want[b, :n])
+        assert (err <= U16 * np.abs(want[b, :n]) + (2 * U16 + U16 * U16 + 2.0 ** -14) * mag[b, :n] + 1e-30).all(), (name, b, err.max())
+        # the roundings are independent: in norm the error stays near one rounding's (2^-8 / sqrt(3) at most each, three of them)
+        assert np.linalg.norm(err) <= U16 * np.linalg.norm(want[b, :n]) * np.sqrt(3) + 1e-30, (name, b)
+        assert (got[b, n:] == fill).all(), (name, b)
+
+
+LA = [  # B, T, H, packed, with states, lengths
+    (1, 2, 1, False, False, None), (2, 15, 2, False, True, [15, 0]), (1, 16, 1, True, False, None), (1, 17, 2, False, True, None),
+    (3, 63, 2, True, True, [63, 1, 40]), (1, 64, 3, False, False, None), (2, 65, 1, False, True, None), (1, 128, 2, True, False, None),
+    (2, 130, 2, False, True, [129, 64]), (1, 700, 2, False, True, None), (1, 1030, 1, True, False, None),
+    (2, 777, 3, False, True, [777, 300]), (150, 70, 2, False, False, None),
+]
+
+
+@pytest.mark.parametrize("B,T,H,packed,states,lengths", LA)
+def test_linear_attention_forward_and_backward(B, T, H, packed, states, lengths):
+    seed = B + T + H
+    t = la_inputs(B, T, H, seed, packed, pad=3)
+    lens = [T] * B if lengths is None else lengths
+    t_len = None if lengths is None else cu(np.array(lengths), torch.int32)
+    if lengths is not None:                          # what lies behind a sequence must not matter
+        for b, n in enumerate(lengths):
+            for x in ("q", "k", "v", "dout"):
+                t[x][b, n:] = float("nan")
+    q, k, v, do = (np.nan_to_num(np64(t[n])) for n in ("q", "k", "v", "dout"))
+    lg, s0, ds = np64(t["log_decay"]), np64(t["state_in"]), np64(t["dstate_out"])
+    scale = 0.125
+    sin, dsout = (s0, ds) if states else (None, None)
+    o_ref, S_ref = O.linear_attention_fwd(q, k, v, lg, scale, sin, lens)
+    o_mag, S_mag = O.linear_attention_fwd(abs(q), abs(k), abs(v), lg, scale, None if sin is None else abs(sin), lens)
+    o = torch.full((B, T, H, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    s_out = torch.full((B, H, 64, 64), float("nan"), device="cuda") if states else None
+    desc = dict(q=t["q"], k=t["k"], v=t["v"], o=o, log_decay=t["log_decay"], scale=scale, lengths=t_len,
+                state_in=t["state_in"] if states else None, state_out=s_out)
+    lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, desc, la_workspace(lp.LP_LINATTN_FORWARD, B, T, H))
+    check_tokens("o", o, o_ref, o_mag, lens, 7.0, True)
+    if states:                                       # two bf16 terms: 2^-8 * 2^-8; fp32 sums over the chunks and segments
+        tol = (2.0 ** -16 + (T / 64 + 70) * U32) * S_mag
+        assert (np.abs(np64(s_out) - S_ref) <= tol + 1e-30).all()
+        inplace = t["state_in"].clone()              # the state may be updated in place
+        lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, dict(desc, state_in=inplace, state_out=inplace),
+                                    la_workspace(lp.LP_LINATTN_FORWARD, B, T, H))
+        assert torch.equal(inplace, s_out)
+
+    refs = O.linear_attention_bwd(q, k, v, do, lg, scale, sin, dsout, lens)
+    mags = O.linear_attention_bwd(abs(q), abs(k), abs(v), abs(do), lg, scale, None if sin is None else abs(sin),
+                                  None if dsout is None else abs(dsout), lens)
+    if packed:
+        g = torch.full((B, T, 3, H, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+        grads = [g[:, :, i] for i in range(3)]
+    else:
+        grads = [torch.full((B, T, H, 64), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+    ds_in = torch.full((B, H, 64, 64), float("nan"), device="cuda") if states else None
+    bdesc = dict(q=t["q"], k=t["k"], v=t["v"], dout=t["dout"], dq=grads[0], dk=grads[1], dv=grads[2], log_decay=t["log_decay"],
+                 scale=scale, lengths=t_len, state_in=desc["state_in"], dstate_out=t["dstate_out"] if states else None, dstate_in=ds_in)
+    lp.lp_linear_attention_bf16(lp.LP_LINATTN_BACKWARD, bdesc, la_workspace(lp.LP_LINATTN_BACKWARD, B, T, H))
+    for name, got, want, mag in zip(("dq", "dk", "dv"), grads, refs, mags):
+        check_tokens(name, got, want, mag, lens, 7.0, True)
+    if states:
+        assert (np.abs(np64(ds_in) - refs[3]) <= (2.0 ** -16 + (T / 64 + 70) * U32) * mags[3] + 1e-30).all()
+
+
+@pytest.mark.parametrize("B,H,idle", [(1, 1, False), (5, 3, True), (40, 16, True)])
+def test_linear_attention_step(B, H, idle):
+    t = la_inputs(B, 1, H, 4 + B)
+    lens = None if not idle else (np.arange(B) % 3 != 1).astype(np.int32)
+    o = torch.full((B, 1, H, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    s_out = torch.full((B, H, 64, 64), float("nan"), device="cuda")
+    desc = dict(q=t["q"], k=t["k"], v=t["v"], o=o, log_decay=t["log_decay"], scale=0.3, state_in=t["state_in"], state_out=s_out,
+                lengths=None if lens is None else cu(lens, torch.int32))
+    lp.lp_linear_attention_bf16(lp.LP_LINATTN_STEP, desc)
+    args = [np64(t[n]) for n in ("q", "k", "v")]
+    lg, s0 = np64(t["log_decay"]), np64(t["state_in"])
+    o_ref, S_ref = O.linear_attention_fwd(*args, lg, 0.3, s0, lens)
+    o_mag, S_mag = O.linear_attention_fwd(*[abs(a) for a in args], lg, 0.3, abs(s0), lens)
+    assert (np.abs(np64(s_out) - S_ref) <= 4 * U32 * S_mag + 1e-30).all()
+    live = np.ones(B, bool) if lens is None else lens > 0
+    err = np.abs(np64(o) - o_ref)[live]
+    assert (err <= U16 * np.abs(o_ref[live]) * (1 + U16) + 70 * U32 * o_mag[live] + 1e-30).all()
+    assert (np64(o)[~live] == 7.0).all()
+    inplace = t["state_in"].clone()
+    lp.lp_linear_attention_bf16(lp.LP_LINATTN_STEP, dict(desc, state_in=inplace, state_out=inplace))
+    assert torch.equal(inplace, s_out)
+    o2 = torch.full_like(o, 7.0)                     # one token through the prompt's form: the same kernel
+    lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, dict(desc, o=o2, state_out=None))
+    assert torch.equal(o, o2)
+
+
+def test_linear_attention_later_tokens_do_not_matter():
+    B, T, H = 1, 300, 2
+    t = la_inputs(B, T, H, 8)
+    run = lambda: [lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, dict(q=t["q"], k=t["k"], v=t["v"], o=o, log_decay=t["log_decay"],
+                   scale=0.125), la_workspace(0, B, T, H)) or o for o in [torch.zeros(B, T, H, 64, dtype=torch.bfloat16, device="cuda")]][0]
+    a = run()
+    for n in ("q", "k", "v"):
+        t[n][:, 150:] *= -3
+    b = run()
+    assert torch.equal(a[:, :150], b[:, :150]) and not torch.equal(a[:, 150:], b[:, 150:])
+
+
+def test_a_prompt_then_single_tokens_equals_the_whole_sequence():
+    """The operators as a model uses them: embed, drop nothing, attend over the prompt, then answer token by token from
+    the state; against one pass over all tokens."""
+    B, T, P, H, V = 3, 90, 77, 2, 50
+    d = 64 * H
+    g = np.random.default_rng(3)
+    ids = cu(g.integers(0, V, (B, T)), torch.int32)
+    table = cu(g.standard_normal((V, d)), torch.bfloat16)
+    x = torch.empty(B, T, d, dtype=torch.bfloat16, device="cuda")
+    lp.lp_embed_forward(lp.LP_BF16, ids, table, None, x, B * T, V, d, 0, 1.0)
+    y = torch.empty_like(x)
+    lp.lp_dropout(lp.LP_BF16, x, None, y, x.numel(), 0.0, 1)
+    h = y.view(B, T, H, 64)
+    lg = cu(np.log([0.97, 0.8]))
+    whole, s_whole = torch.empty_like(h), torch.empty(B, H, 64, 64, device="cuda")
+    lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, dict(q=h, k=h, v=h, o=whole, log_decay=lg, scale=0.125, state_out=s_whole),
+                                la_workspace(0, B, T, H))
+    parts, state = torch.empty_like(h), torch.empty(B, H, 64, 64, device="cuda")
+    pre = h[:, :P]
+    lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, dict(q=pre, k=pre, v=pre, o=parts[:, :P], log_decay=lg, scale=0.125, state_out=state),
+                                la_workspace(0, B, P, H))
+    for i in range(P, T):
+        one = h[:, i:i + 1]
+        lp.lp_linear_attention_bf16(lp.LP_LINATTN_STEP, dict(q=one, k=one, v=one, o=parts[:, i:i + 1], log_decay=lg, scale=0.125,
+                                                             state_in=state, state_out=state))
+    x64 = np64(h)
+    ref, s_ref = O.linear_attention_fwd(x64, x64, x64, np64(lg), 0.125)
+    mag, s_mag = O.linear_attention_fwd(abs(x64), abs(x64), abs(x64), np64(lg), 0.125)
+    for o, s in ((whole, s_whole), (parts, state)):
+        check_tokens("o", o, ref, mag, [T] * B, None, True)
+        assert (np.abs(np64(s) - s_ref) <= (2.0 ** -16 + 90 * U32) * s_mag).all()
+
+
+# ------------------------------------------------------------------------------------------------ streams and graphs
+def test_calls_on_a_side_stream_and_replayed_from_a_graph():
+    B, T, H = 2, 600, 2
+    d, rows, V = 64 * H, B * T, 300
+    t = la_inputs(B, T, H, 12)
+    ids = torch.randint(0, V, (rows,), device="cuda", dtype=torch.int32)
+    out = dict(o=torch.zeros(B, T, H, 64, dtype=torch.bfloat16, device="cuda"), dtab=torch.zeros(V, d, device="cuda"),
+               y=torch.zeros(rows, d, dtype=torch.bfloat16, device="cuda"))
+    grads = {n: torch.zeros(B, T, H, 64, dtype=torch.bfloat16, device="cuda") for n in ("dq", "dk", "dv")}
+    ws = [la_workspace(0, B, T, H), la_workspace(1, B, T, H),
+          torch.empty(lp.lp_embed_workspace_bytes(rows, V, d), dtype=torch.uint8, device="cuda")]
+    counter = torch.zeros(1, dtype=torch.int64, device="cuda")
+    base = dict(q=t["q"], k=t["k"], v=t["v"], log_decay=t["log_decay"], scale=0.125)
+
+    def chain(s):
+        lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, dict(base, o=out["o"]), ws[0], s)
+        lp.lp_linear_attention_bf16(lp.LP_LINATTN_BACKWARD, dict(base, dout=out["o"], **grads), ws[1], s)
+        lp.lp_dropout(lp.LP_BF16, grads["dq"], grads["dk"], out["y"], rows * d, 0.2, 5, 0, counter, s)
+        lp.lp_embed_backward(lp.LP_BF16, ids, out["y"], out["dtab"], None, rows, V, d, 0, 1.0, None, ws[2], ws[2].numel(), s)
+
+    chain(None)
+    torch.cuda.synchronize()
+    want = {k: v.clone() for k, v in {**out, **grads}.items()}
+    side = torch.cuda.Stream()
+    for x in {**out, **grads}.values():
+        x.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    chain(side.cuda_stream)
+    side.synchronize()
+    assert all(torch.equal(want[k], v) for k, v in {**out, **grads}.items())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        chain(side.cuda_stream)
+    for x in {**out, **grads}.values():
+        x.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(want[k], v) for k, v in {**out, **grads}.items())
+    counter += (rows * d + 3) // 4                   # other words at the next replay
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(want["o"], out["o"]) and not torch.equal(want["y"], out["y"])
+
+
+def test_host_memory_is_refused():
+    x = torch.zeros(64, device="cuda")
+    host = np.zeros(64, dtype=np.float32)
+    with pytest.raises(lp.LpError) as e:
+        lp.lp_dropout(lp.LP_FP32, x, None, host.ctypes.data, 64, 0.1, 1)
+    assert e.value.code == -1
+    torch.cuda.synchronize()
