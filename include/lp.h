@@ -424,6 +424,8 @@ lp_status lp_dropout(int dtype, const void* x, const void* resid, void* y, long 
  *       [dstate_in: gradient of state_in; may be dstate_out].  log_decay carries no gradient.
  *   LP_LINATTN_STEP:     the recurrent form, seq_len 1: as FORWARD, all arithmetic in fp32; lengths[b] = 0 marks an idle
  *       sequence.
+ *   status (nullable): device int; bit 2 (4) is set, and never cleared, if a bounded device-side wait gave up (the outputs
+ *   are then not valid).
  *   FORWARD and BACKWARD form scores and state products on bf16 operands with fp32 accumulation; state_out and dstate_in
  *   are accurate to about 2^-17 relative to the terms they add up.  A NaN or infinity in token t reaches the outputs from t
  *   on, and may reach earlier ones of the same 16 tokens.
@@ -439,6 +441,7 @@ typedef struct {
   const float* dstate_out;
   float* dstate_in;
   const int* lengths;
+  int* status;
   int batch, seq_len, n_heads;
   float scale;
 } lp_linattn_desc;

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -364,11 +365,15 @@ def lp_attention_bf16(form: int, qkv, o, lse, dout, dqkv, delta, batch: int, seq
 
 def _dev(t):
     """Device address of a CUDA tensor or raw address; anything on the host is refused before a kernel can see it."""
-    if t is None or isinstance(t, int):
-        return t
-    if not getattr(t, "is_cuda", False):
-        raise LpError(-1, "a host tensor was given where device memory is needed")
-    return t.data_ptr()
+    if t is None:
+        return None
+    try:
+        if t.is_cuda:
+            return t.data_ptr()
+    except AttributeError:
+        if isinstance(t, int):
+            return t
+    raise LpError(-1, "host memory was given where device memory is needed")
 
 
 _lib.lp_embed_forward.argtypes = [C.c_int] + [C.c_void_p] * 4 + [C.c_int] * 4 + [C.c_float, C.c_void_p, C.c_void_p]
@@ -417,11 +422,17 @@ class lp_tokens(C.Structure):
 
 class lp_linattn_desc(C.Structure):
     _fields_ = [(n, lp_tokens) for n in ("q", "k", "v", "o", "dout", "dq", "dk", "dv")] + \
-               [(n, C.c_void_p) for n in ("log_decay", "state_in", "state_out", "dstate_out", "dstate_in", "lengths")] + \
+               [(n, C.c_void_p) for n in ("log_decay", "state_in", "state_out", "dstate_out", "dstate_in", "lengths", "status")] + \
                [("batch", C.c_int), ("seq_len", C.c_int), ("n_heads", C.c_int), ("scale", C.c_float)]
 
 
-_lib.lp_linear_attention_bf16.argtypes = [C.c_int, C.POINTER(lp_linattn_desc), C.c_void_p, C.c_size_t, C.c_void_p]
+_LINATTN_TOKENS = ("q", "k", "v", "o", "dout", "dq", "dk", "dv")
+_LINATTN_FLOATS = ("log_decay", "state_in", "state_out", "dstate_out", "dstate_in", "lengths", "status")
+_LINATTN_KEYS = {*_LINATTN_TOKENS, *_LINATTN_FLOATS, "scale"}
+_linattn_layout = struct.Struct("=24q7Q3if")      # lp_linattn_desc, filled in one go
+assert _linattn_layout.size == C.sizeof(lp_linattn_desc)
+_LINATTN_PACK = _linattn_layout.pack
+_lib.lp_linear_attention_bf16.argtypes = [C.c_int, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
 _lib.lp_linear_attention_workspace_bytes.argtypes = [C.c_int] * 4
 _lib.lp_linear_attention_workspace_bytes.restype = C.c_size_t
 
@@ -434,30 +445,37 @@ def lp_linear_attention_bf16(form: int, desc: dict, workspace=None, stream=None)
     """Linear attention with a decay per head (see lp.h): forward, backward or the single-token step.  `desc` names the
     tensors of lp_linattn_desc: q, k, v, o, dout, dq, dk, dv are bf16 CUDA tensors [batch, seq_len, n_heads, 64] (slices
     of larger ones are fine: strides are read off), the states fp32 [batch, n_heads, 64, 64], log_decay fp32 [n_heads],
-    lengths int32 [batch]; `scale` a number.  Sizes come from q; the other tensors' shapes must agree."""
-    d = lp_linattn_desc()
-    shape = tuple(desc["q"].shape)
-    for name, value in desc.items():
-        if name == "scale":
-            d.scale = value
-        elif value is None:
+    lengths int32 [batch]; `scale` a number (default 1).  Sizes come from q; the other tensors' shapes must agree."""
+    if not desc.keys() <= _LINATTN_KEYS:
+        raise LpError(-1, f"lp_linear_attention_bf16: unknown {sorted(desc.keys() - _LINATTN_KEYS)}")
+    get = desc.get
+    shape = desc["q"].shape
+    if len(shape) != 4 or shape[3] != 64:
+        raise LpError(-2, "lp_linear_attention_bf16: q must be [batch, seq_len, n_heads, 64]")
+    B, T, H, _ = shape
+    v = []
+    for name in _LINATTN_TOKENS:
+        t = get(name)
+        if t is None:
+            v += (0, 0, 0)
             continue
-        elif name in ("q", "k", "v", "o", "dout", "dq", "dk", "dv"):
-            if tuple(value.shape) != shape or len(shape) != 4 or shape[3] != 64 or value.element_size() != 2:
-                raise LpError(-2, f"lp_linear_attention_bf16: {name} must be bf16 [batch, seq_len, n_heads, 64], as q")
-            s = value.stride()
-            if s[3] != 1 or (shape[2] > 1 and s[2] != 64):
-                raise LpError(-3, f"lp_linear_attention_bf16: the heads of {name} must lie 64 elements apart")
-            t = getattr(d, name)
-            t.p, t.batch_stride, t.token_stride = _dev(value), s[0] if shape[0] > 1 else 0, s[1]
-        else:
-            want = {"log_decay": (shape[2],), "lengths": (shape[0],)}.get(name, (shape[0], shape[2], 64, 64))
-            if tuple(value.shape) != want or value.element_size() != 4 or not value.is_contiguous():
-                raise LpError(-2, f"lp_linear_attention_bf16: {name} must be contiguous {want} of four bytes each")
-            setattr(d, name, _dev(value))
-    d.batch, d.seq_len, d.n_heads = shape[:3]
+        if t.shape != shape or t.element_size() != 2:
+            raise LpError(-2, f"lp_linear_attention_bf16: {name} must be bf16 [batch, seq_len, n_heads, 64], as q")
+        sb, st, sh, se = t.stride()
+        if se != 1 or (sh != 64 and H > 1):
+            raise LpError(-3, f"lp_linear_attention_bf16: the heads of {name} must lie 64 elements apart")
+        v += (_dev(t), sb if B > 1 else 0, st)
+    for name in _LINATTN_FLOATS:
+        t = get(name)
+        if t is not None and (t.numel() != (H if name == "log_decay" else B if name == "lengths" else 1 if name == "status" else B * H * 4096) or
+                              t.element_size() != 4 or not t.is_contiguous()):
+            raise LpError(-2, f"lp_linear_attention_bf16: {name} has the wrong size or is not contiguous")
+        v.append(_dev(t) or 0)
     nbytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    _check(None, _lib.lp_linear_attention_bf16(form, C.byref(d), _dev(workspace) if nbytes else None, nbytes, stream))
+    code = _lib.lp_linear_attention_bf16(form, _LINATTN_PACK(*v, B, T, H, get("scale", 1.0)), _dev(workspace) if nbytes else None, nbytes,
+                                         stream)
+    if code:
+        _check(None, code)
 
 
 _lib.lp_conv2d_bf16.argtypes = [C.c_int, C.c_void_p, C.c_void_p, C.c_void_p] + [C.c_int] * 7 + [C.c_void_p]

@@ -7,6 +7,8 @@
 //
 // A dropped element is selected away, not multiplied by zero: a NaN or an infinity there does not reach y.
 // Sums and products are in fp32 and rounded once, on storing.
+#include <algorithm>
+
 #include "common.cuh"
 #include "launch.cuh"
 
@@ -36,6 +38,56 @@ __device__ __forceinline__ float drop(const DropoutArgs& a, uint32_t w, float x,
   return w >= a.threshold ? fmaf(x, a.scale, r) : r;
 }
 
+// 16 bytes per thread and load, U of them in flight (with the residual's); the generator's arithmetic fills the wait.
+// A block covers U * 256 consecutive vectors; the elements behind the last whole vector go one by one.
+template <typename T, bool RESID, int U>
+__global__ void __launch_bounds__(256) dropout_vec_kernel(DropoutArgs a) {
+  constexpr int VEC = 16 / sizeof(T);
+  const long long vecs = a.n / VEC, v0 = (long long)blockIdx.x * (256 * U) + threadIdx.x;
+  const unsigned long long first = a.offset + (a.offset_dev ? *a.offset_dev : 0ull);
+  uint4 x[U], r[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (v0 + 256 * u < vecs) {
+      x[u] = ((const uint4*)a.x)[v0 + 256 * u];
+      if (RESID) r[u] = ((const uint4*)a.resid)[v0 + 256 * u];
+    }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const long long v = v0 + 256 * u;
+    if (v >= vecs) break;
+    const uint32_t xs[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+    const uint32_t rs[4] = {r[u].x, r[u].y, r[u].z, r[u].w};
+    uint32_t ys[4];
+#pragma unroll
+    for (int k = 0; k < VEC / 4; ++k) {          // a counter per four elements
+      const uint4 w = words(a, first, v * (VEC / 4) + k);
+      const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+      if (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          ys[e] = __float_as_uint(drop(a, ww[e], __uint_as_float(xs[e]), RESID ? __uint_as_float(rs[e]) : 0.f));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t xx = xs[2 * k + e], rr = RESID ? rs[2 * k + e] : 0u;
+          const float lo = drop(a, ww[2 * e], __uint_as_float(xx << 16), __uint_as_float(rr << 16));
+          const float hi = drop(a, ww[2 * e + 1], __uint_as_float(xx & 0xffff0000u), __uint_as_float(rr & 0xffff0000u));
+          __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+          ys[2 * k + e] = *(uint32_t*)&b;
+        }
+      }
+    }
+    ((uint4*)a.y)[v] = make_uint4(ys[0], ys[1], ys[2], ys[3]);
+  }
+  const long long i = vecs * VEC + threadIdx.x;
+  if (blockIdx.x == 0 && i < a.n) {
+    const uint4 w = words(a, first, i >> 2);
+    const uint32_t ww = (i & 3) == 0 ? w.x : (i & 3) == 1 ? w.y : (i & 3) == 2 ? w.z : w.w;
+    ((T*)a.y)[i] = from_f<T>(drop(a, ww, to_f(((const T*)a.x)[i]), RESID ? to_f(((const T*)a.resid)[i]) : 0.f));
+  }
+}
+
 // One thread per group of four elements; any alignment.
 template <typename T>
 __global__ void __launch_bounds__(256) dropout_kernel(DropoutArgs a) {
@@ -55,10 +107,20 @@ __global__ void __launch_bounds__(256) dropout_kernel(DropoutArgs a) {
   }
 }
 
+template <typename T>
+cudaError_t run_vec(const DropoutArgs& a, cudaStream_t s) {
+  const long long vecs = a.n / (16 / (int)sizeof(T));
+  const bool many = vecs >= 148LL * 8 * 256 * 2;   // more than two waves of single loads: four in flight per thread
+  const unsigned blocks = (unsigned)std::max<long long>(1, many ? (vecs + 1023) / 1024 : (vecs + 255) / 256);
+  if (a.resid) return many ? launch_kernel(dropout_vec_kernel<T, true, 4>, dim3(blocks), 256, 0, s, a) : launch_kernel(dropout_vec_kernel<T, true, 1>, dim3(blocks), 256, 0, s, a);
+  return many ? launch_kernel(dropout_vec_kernel<T, false, 4>, dim3(blocks), 256, 0, s, a) : launch_kernel(dropout_vec_kernel<T, false, 1>, dim3(blocks), 256, 0, s, a);
+}
+
 }  // namespace
 
 cudaError_t launch_dropout(const DropoutArgs& a, bool is_bf16, cudaStream_t s) {
   if (a.n <= 0) return cudaSuccess;
+  if ((((uintptr_t)a.x | (uintptr_t)a.resid | (uintptr_t)a.y) & 15) == 0) return is_bf16 ? run_vec<bf16>(a, s) : run_vec<float>(a, s);
   const long long groups = (a.n + 3) / 4;
   const unsigned blocks = (unsigned)std::min<long long>((groups + 255) / 256, 148 * 16);
   return is_bf16 ? launch_kernel(dropout_kernel<bf16>, dim3(blocks), 256, 0, s, a)

@@ -17,6 +17,7 @@
 //             sums go to the workspace.  Further blocks of the launch write the zero rows and the position gradient.
 //   combine : adds the pieces of every such token in order (a launch of its own, only if more than P rows exist).
 #include <algorithm>
+#include <climits>
 
 #include "common.cuh"
 #include "launch.cuh"
@@ -25,29 +26,44 @@ namespace lp {
 namespace {
 
 constexpr int SORT_WARPS = 32;
-constexpr int SORT_MAX_LOCAL = 1536;             // tokens of one sorting block: (32 + 2) * 1536 counters fit its shared memory
+constexpr int SORT_MAX_LOCAL = 1024;             // tokens of one sorting block: (32 + 2) * 1024 counters and the lists fit its shared memory
+constexpr int SORT_LIST = 512;                   // rows of this block that a warp remembers
+constexpr int SORT_BATCH = 8;                    // loads of ids in flight
 constexpr int SUM_THREADS = 128;
+constexpr int PIECES = 4;                        // rows of a piece of a long token, in stretches
 constexpr int ZERO_ROWS = 16;                    // table rows a zero-filling block looks at
 constexpr int POS_PIECE = 64;                    // rows one position worker sums
 constexpr uint32_t HEAVY = 0x80000000u;
 
-template <typename T, int VEC> struct Pack;
-template <> struct Pack<float, 1> { float v[1]; __device__ void load(const float* p) { v[0] = *p; } };
-template <> struct Pack<bf16, 1> { float v[1]; __device__ void load(const bf16* p) { v[0] = to_f(*p); } };
+template <typename T, int VEC> struct Pack;      // VEC elements as loaded; get(i) converts
+template <> struct Pack<float, 1> {
+  float x;
+  __device__ void load(const float* p) { x = *p; }
+  __device__ float get(int) const { return x; }
+};
+template <> struct Pack<bf16, 1> {
+  bf16 x;
+  __device__ void load(const bf16* p) { x = *p; }
+  __device__ float get(int) const { return to_f(x); }
+};
 template <> struct Pack<float, 4> {
-  float v[4];
-  __device__ void load(const float* p) { const float4 x = *(const float4*)p; v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; }
+  float x[4];
+  __device__ void load(const float* p) { *(float4*)x = *(const float4*)p; }
+  __device__ float get(int i) const { return x[i]; }
 };
 template <> struct Pack<bf16, 8> {
-  float v[8];
-  __device__ void load(const bf16* p) {
-    const uint4 x = *(const uint4*)p;
-    const uint32_t u[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(u[i] << 16); v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
-  }
+  uint32_t x[4];
+  __device__ void load(const bf16* p) { *(uint4*)x = *(const uint4*)p; }
+  __device__ float get(int i) const { return __uint_as_float(i & 1 ? x[i >> 1] & 0xffff0000u : x[i >> 1] << 16); }
 };
 template <typename T> __device__ __forceinline__ void store_vec(T* p, const float (&v)[1]) { *p = from_f<T>(v[0]); }
+// The gradients leave past the caches' resident set: dh, which several blocks read, is to stay there.
+__device__ __forceinline__ void stream_vec(float* p, const float (&v)[1]) { __stcs(p, v[0]); }
+__device__ __forceinline__ void stream_vec(float* p, const float (&v)[4]) { __stcs((float4*)p, make_float4(v[0], v[1], v[2], v[3])); }
+__device__ __forceinline__ void stream_vec(float* p, const float (&v)[8]) {
+  __stcs((float4*)p, make_float4(v[0], v[1], v[2], v[3]));
+  __stcs((float4*)(p + 4), make_float4(v[4], v[5], v[6], v[7]));
+}
 __device__ __forceinline__ void store_vec(float* p, const float (&v)[4]) { *(float4*)p = make_float4(v[0], v[1], v[2], v[3]); }
 __device__ __forceinline__ void store_vec(float* p, const float (&v)[8]) {
   *(float4*)p = make_float4(v[0], v[1], v[2], v[3]);
@@ -84,92 +100,172 @@ __global__ void __launch_bounds__(128) embed_fwd_kernel(EmbedProb p, int lanes_l
 #pragma unroll 4
   for (int c = lane * VEC; c < p.d; c += VEC << lanes_log2) {
     Pack<T, VEC> a, b;
+    float v[VEC];
     a.load(tok + c);
     if (pos) {
       b.load(pos + c);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) a.v[i] = fmaf(p.scale, a.v[i], b.v[i]);
+      for (int i = 0; i < VEC; ++i) v[i] = fmaf(p.scale, a.get(i), b.get(i));
     } else {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) a.v[i] *= p.scale;
+      for (int i = 0; i < VEC; ++i) v[i] = p.scale * a.get(i);
     }
-    store_vec(h + c, a.v);
+    store_vec(h + c, v);
+  }
+}
+
+// Position gradient: 2^split_log2 groups of 2^lanes_log2 threads sum one piece of one position's rows together; the first
+// of them adds their sums in order.  buf: a float per thread and element.
+template <typename T, int VEC>
+__device__ void pos_sums(const EmbedBwdProb& p, int lanes_log2, int split_log2, int block, int pos_pieces, float* buf) {
+  const int lanes = 1 << lanes_log2, lane = threadIdx.x & (lanes - 1), split = 1 << split_log2, sub = (threadIdx.x >> lanes_log2) & (split - 1);
+  const long long wk = ((long long)block * blockDim.x + threadIdx.x) >> (lanes_log2 + split_log2);
+  const bool real = wk < (long long)p.T * pos_pieces;
+  const int t = real ? (int)(wk / pos_pieces) : 0, piece = real ? (int)(wk % pos_pieces) : 0;
+  const long long step = p.T, i0 = (long long)piece * POS_PIECE;
+  const long long rows = real && t < p.rows ? (p.rows - 1 - t) / step + 1 : 0;          // of this position
+  const long long n = max(0LL, pos_pieces == 1 ? rows : min(rows - i0, (long long)POS_PIECE));
+  const long long per = (n + split - 1) >> split_log2, k0 = min(n, sub * per), k1 = min(n, k0 + per);
+  float* out = pos_pieces == 1 ? p.dpos + (size_t)t * p.d : p.pos_part + (size_t)wk * p.d;
+  constexpr int U = 4;                           // rows in flight
+  for (int c0 = 0; c0 < p.d; c0 += lanes * VEC) {
+    const int c = c0 + lane * VEC;
+    const T* dh = (const T*)p.dh + (size_t)(t + i0 * step) * p.d + c;
+    float acc[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
+    if (c < p.d)
+      for (long long k = k0; k < k1; k += U) {
+        Pack<T, VEC> x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) if (k + u < k1) x[u].load(dh + (size_t)((k + u) * step) * p.d);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (k + u < k1) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) acc[i] += x[u].get(i);
+          }
+      }
+    if (split > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) buf[threadIdx.x + i * blockDim.x] = acc[i];
+      __syncthreads();
+      if (sub == 0)
+        for (int k = 1; k < split; ++k)
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) acc[i] += buf[threadIdx.x + k * lanes + i * blockDim.x];
+    }
+    if (real && sub == 0 && c < p.d) store_vec(out + c, acc);
   }
 }
 
 // Rows by token.  Block j owns the tokens t with t mod n = j (n a power of two), local index t div n.
 // sorted[p] = {row, token | HEAVY if the token has more than `piece` rows}; seg[t] = {first p, number of rows}.
-__global__ void __launch_bounds__(SORT_WARPS * 32) embed_sort_kernel(EmbedBwdProb p, int n_log2, int local, int piece, int* status) {
+// First sweep: every warp counts its stretch's rows per token and lists those of this block; second sweep: over the list
+// (or over the stretch again, if the list overflowed).  The blocks behind the n sorting ones sum the position gradient.
+template <typename T, int VEC>
+__global__ void __launch_bounds__(SORT_WARPS * 32, 1) embed_sort_kernel(EmbedBwdProb p, int n_log2, int local, int piece, int* status, int lanes_log2,
+                                                                     int split_log2, int pos_pieces) {
   extern __shared__ int sm[];
-  const int pitch = local | 1;                   // odd: a warp that reads one token's 32 counters meets 32 banks
+  if ((int)blockIdx.x >> n_log2) {
+    pos_sums<T, VEC>(p, lanes_log2, split_log2, (int)blockIdx.x - (1 << n_log2), pos_pieces, (float*)sm);
+    return;
+  }
+  const int pitch = local | 1;
   int* cnt = sm;                                 // [SORT_WARPS][pitch]
   int* start = cnt + SORT_WARPS * pitch;         // [local]
   int* total = start + local;                    // [local]
-  __shared__ int less_sum;
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, j = blockIdx.x, mask = (1 << n_log2) - 1;
+  int* list = total + local + w * SORT_LIST;     // [SORT_LIST] rows
+  __shared__ int less_sum, carry_of[SORT_WARPS];
   for (int i = tid; i < SORT_WARPS * pitch; i += blockDim.x) cnt[i] = 0;
   if (tid == 0) less_sum = 0;
   __syncthreads();
   const int stretch = ((p.rows + SORT_WARPS * 32 - 1) / (SORT_WARPS * 32)) * 32;
   const long long lo = (long long)w * stretch;
   const int r0 = (int)min(lo, (long long)p.rows), r1 = (int)min(lo + stretch, (long long)p.rows);
-  int less = 0;
+  int* mine = cnt + w * pitch;
+  const unsigned below = (1u << lane) - 1;
+  int less = 0, listed = 0;
   bool bad = false;
-#pragma unroll 4
-  for (int r = r0 + lane; r < r1; r += 32) {
-    const int id = p.ids[r], t = clamp_id(id, p.vocab);
-    bad |= id != t;
-    less += (t & mask) < j;
-    if ((t & mask) == j) atomicAdd(&cnt[w * pitch + (t >> n_log2)], 1);
+  auto take = [&](int id, int r, bool real) {
+    const int t = clamp_id(id, p.vocab), cls = real ? t & mask : INT_MAX;
+    bad |= real && id != t;
+    less += cls < j;
+    const unsigned hits = __ballot_sync(0xffffffffu, cls == j);
+    if (hits) {
+      if (cls == j) {
+        atomicAdd(&mine[t >> n_log2], 1);
+        const int at = listed + __popc(hits & below);
+        if (at < SORT_LIST) list[at] = r;
+      }
+      listed += __popc(hits);
+    }
+  };
+  int rb = r0;
+  for (; rb + 32 * SORT_BATCH <= r1; rb += 32 * SORT_BATCH) {
+    int id[SORT_BATCH];
+#pragma unroll
+    for (int u = 0; u < SORT_BATCH; ++u) id[u] = p.ids[rb + 32 * u + lane];
+#pragma unroll
+    for (int u = 0; u < SORT_BATCH; ++u) take(id[u], rb + 32 * u + lane, true);
   }
+  for (; rb < r1; rb += 32) take(rb + lane < r1 ? p.ids[rb + lane] : 0, rb + lane, rb + lane < r1);
   less = __reduce_add_sync(0xffffffffu, less);
   if (lane == 0 && less) atomicAdd(&less_sum, less);
   if (bad && status && j == 0) atomicOr(status, ST_LABEL_RANGE);
   __syncthreads();
-  for (int lt = w; lt < local; lt += SORT_WARPS) {        // per token: where each warp's rows begin
-    const int c = cnt[lane * pitch + lt];
-    int s = c;
+  // per token: where each warp's rows begin; over the tokens: where each token's rows begin
+  int carry = less_sum;
+  for (int l0 = 0; l0 < local; l0 += blockDim.x) {
+    const int lt = l0 + tid;
+    int sum = 0;
+    if (lt < local)
+      for (int k0 = 0; k0 < SORT_WARPS; k0 += 16) {
+        int c[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) c[k] = cnt[(k0 + k) * pitch + lt];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) { cnt[(k0 + k) * pitch + lt] = sum; sum += c[k]; }
+      }
+    int s = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) { const int u = __shfl_up_sync(0xffffffffu, s, o); if (lane >= o) s += u; }
-    cnt[lane * pitch + lt] = s - c;
-    if (lane == 31) total[lt] = s;
-  }
-  __syncthreads();
-  if (w == 0) {
-    int carry = less_sum;
-    for (int i0 = 0; i0 < local; i0 += 32) {
-      const int lt = i0 + lane, c = lt < local ? total[lt] : 0;
-      int s = c;
+    if (lane == 31) carry_of[w] = s;
+    __syncthreads();
+    int before = 0, all = 0;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) { const int u = __shfl_up_sync(0xffffffffu, s, o); if (lane >= o) s += u; }
-      if (lt < local) {
-        start[lt] = carry + s - c;
-        const long long t = ((long long)lt << n_log2) | j;
-        if (t < p.vocab) p.seg[t] = make_int2(carry + s - c, c);
-      }
-      carry += __shfl_sync(0xffffffffu, s, 31);
+    for (int k = 0; k < SORT_WARPS; ++k) { const int c = carry_of[k]; before += k < w ? c : 0; all += c; }
+    if (lt < local) {
+      const int at = carry + before + s - sum;
+      start[lt] = at;
+      total[lt] = sum;
+      const long long t = ((long long)lt << n_log2) | j;
+      if (t < p.vocab) p.seg[t] = make_int2(at, sum);
     }
+    carry += all;
+    __syncthreads();
   }
-  __syncthreads();
-  for (int rb = r0; rb < r1; rb += 32) {
-    const int r = rb + lane;
-    const int t = r < r1 ? clamp_id(p.ids[r], p.vocab) : 0;
-    const bool in = r < r1 && (t & mask) == j;
+  const bool fits = listed <= SORT_LIST;
+  const int steps = fits ? listed : r1 - r0;
+  for (int b = 0; b < steps; b += 32) {
+    const int i = b + lane;
+    const int r = i < steps ? (fits ? list[i] : r0 + i) : 0, t = i < steps ? clamp_id(p.ids[r], p.vocab) : 0;
+    const bool in = i < steps && (t & mask) == j;
     if (__ballot_sync(0xffffffffu, in) == 0) continue;
-    const int lt = in ? t >> n_log2 : 0;
-    const unsigned peers = __match_any_sync(0xffffffffu, in ? lt : ~lane);
-    if (in) {
-      const int at = start[lt] + cnt[w * pitch + lt] + __popc(peers & ((1u << lane) - 1));
-      p.sorted[at] = make_int2(r, (int)((uint32_t)t | (total[lt] > piece ? HEAVY : 0u)));
-    }
+    const int lt = in ? t >> n_log2 : ~lane;
+    const unsigned peers = __match_any_sync(0xffffffffu, lt);
+    if (in) p.sorted[start[lt] + mine[lt] + __popc(peers & below)] = make_int2(r, (int)((uint32_t)t | (total[lt] > piece ? HEAVY : 0u)));
     __syncwarp();
-    if (in && (peers & ((1u << lane) - 1)) == 0) cnt[w * pitch + lt] += __popc(peers);
+    if (in && (peers & below) == 0) mine[lt] += __popc(peers);
     __syncwarp();
   }
 }
 
 // First sorted position that stretch c owns: the first start of a token, or of a piece of a long one, at or behind
-// c * P.  (A token of at most P rows is summed whole by the stretch it starts in.)
+// c * P.  (A token of at most PIECES * P rows is summed whole by the stretch it starts in; a longer one is cut into pieces
+// of that length, of which at most one that is not the token's first starts in a stretch.)
 __device__ __forceinline__ int stretch_begin(const EmbedBwdProb& p, long long c, int P) {
   if (c * P >= p.rows) return p.rows;
   const int q = (int)(c * P);
@@ -178,15 +274,20 @@ __device__ __forceinline__ int stretch_begin(const EmbedBwdProb& p, long long c,
   const int off = q - sg.x;
   if (off == 0) return q;
   if (!((uint32_t)e.y & HEAVY)) return sg.x + sg.y;
-  const int up = (P - off % P) % P;
+  const int piece = PIECES * P, up = (piece - off % piece) % piece;
   return min(q + up, sg.x + sg.y);
 }
 
 template <typename T, int VEC>
 __global__ void __launch_bounds__(SUM_THREADS) embed_sum_kernel(EmbedBwdProb p, int lanes_log2, int P, int sum_blocks, int pos_blocks,
                                                                 int pos_pieces) {
+  cudaGridDependencySynchronize();
   const int lanes = 1 << lanes_log2, per_block = SUM_THREADS >> lanes_log2;
   const int grp = threadIdx.x >> lanes_log2, lane = threadIdx.x & (lanes - 1);
+  if ((int)blockIdx.x >= sum_blocks && (int)blockIdx.x < sum_blocks + pos_blocks) {
+    if (blockIdx.y == 0) pos_sums<T, VEC>(p, lanes_log2, 0, (int)blockIdx.x - sum_blocks, pos_pieces, nullptr);
+    return;
+  }
   const int c = (blockIdx.y * lanes + lane) * VEC;
   if (c >= p.d) return;
   const T* dh = (const T*)p.dh + c;
@@ -205,110 +306,115 @@ __global__ void __launch_bounds__(SUM_THREADS) embed_sum_kernel(EmbedBwdProb p, 
       } else {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) acc[i] *= p.scale;
-        store_vec(p.dtok + (size_t)cur * p.d + c, acc);
+        stream_vec(p.dtok + (size_t)cur * p.d + c, acc);
       }
 #pragma unroll
       for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
     };
-    for (int q = b0; q < b1; q += 4) {           // four rows in flight, whatever tokens they belong to
-      int2 e[4];
-      Pack<T, VEC> x[4];
+    constexpr int U = VEC == 1 ? 4 : 8;          // rows in flight, whatever tokens they belong to
+    int2 e[U], next[U];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) if (q + u < b1) e[u] = p.sorted[q + u];
+    for (int u = 0; u < U; ++u) next[u] = b0 + u < b1 ? p.sorted[b0 + u] : make_int2(0, 0);
+    for (int q = b0; q < b1; q += U) {
+      Pack<T, VEC> x[U];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) if (q + u < b1) x[u].load(dh + (size_t)e[u].x * p.d);
+      for (int u = 0; u < U; ++u) {
+        e[u] = next[u];
+        if (q + u < b1) x[u].load(dh + (size_t)e[u].x * p.d);
+      }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < U; ++u) if (q + U + u < b1) next[u] = p.sorted[q + U + u];   // the next rows' numbers meanwhile
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
         if (q + u >= b1) break;
         if ((uint32_t)e[u].y != cur) { flush(); cur = (uint32_t)e[u].y; first = true; }
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) acc[i] += x[u].v[i];
+        for (int i = 0; i < VEC; ++i) acc[i] += x[u].get(i);
       }
     }
     flush();
-  } else if ((int)blockIdx.x < sum_blocks + pos_blocks) {
-    const long long wk = (long long)(blockIdx.x - sum_blocks) * per_block + grp;
-    if (wk >= (long long)p.T * pos_pieces) return;
-    const int t = (int)(wk / pos_pieces), piece = (int)(wk % pos_pieces);
-    long long r = t + (long long)piece * POS_PIECE * p.T;
-    float acc[VEC];
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
-    for (int k = 0; k < POS_PIECE; k += 4, r += 4LL * p.T) {
-      if (r >= p.rows) break;
-      Pack<T, VEC> x[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) if (r + (long long)u * p.T < p.rows) x[u].load(dh + (size_t)(r + (long long)u * p.T) * p.d);
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (r + (long long)u * p.T < p.rows) {
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) acc[i] += x[u].v[i];
-        }
-    }
-    store_vec((pos_pieces == 1 ? p.dpos + (size_t)t * p.d : p.pos_part + (size_t)wk * p.d) + c, acc);
   } else {
     const long long t0 = (long long)(blockIdx.x - sum_blocks - pos_blocks) * ZERO_ROWS;
     float z[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) z[i] = 0.f;
     for (int i = grp; i < ZERO_ROWS; i += per_block)
-      if (t0 + i < p.vocab && p.seg[t0 + i].y == 0) store_vec(p.dtok + (size_t)(t0 + i) * p.d + c, z);
+      if (t0 + i < p.vocab && p.seg[t0 + i].y == 0) stream_vec(p.dtok + (size_t)(t0 + i) * p.d + c, z);
   }
 }
 
-// Pieces of long tokens (and of positions with many rows): eight warps take every eighth piece of 128 columns, the
-// eight sums are added in order.
-__global__ void __launch_bounds__(256) embed_combine_kernel(EmbedBwdProb p, int P, int chunks, int pos_pieces) {
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const float* base;
-  float* out;
-  float scale = 1.f;
-  int pieces;
-  long long stride;                              // floats between consecutive pieces behind the first
-  long long first;                               // offset of piece 0 relative to `base`; piece i > 0 at i * stride
-  if ((int)blockIdx.x < chunks) {
-    const long long c = blockIdx.x;
-    const int last = (int)min((c + 1) * P, (long long)p.rows) - 1;
-    const uint32_t e = (uint32_t)p.sorted[last].y;
-    if (!(e & HEAVY)) return;
-    const int2 sg = p.seg[e & ~HEAVY];
-    if (sg.x < c * P) return;                    // that token started in an earlier stretch
-    pieces = (sg.y + P - 1) / P;
-    base = p.part + (size_t)(2 * c) * p.d;
-    first = p.d;
-    stride = 2LL * p.d;
-    out = p.dtok + (size_t)(e & ~HEAVY) * p.d;
-    scale = p.scale;
-  } else {
-    const int t = (int)blockIdx.x - chunks;
-    pieces = (int)(((long long)p.rows - t + (long long)POS_PIECE * p.T - 1) / ((long long)POS_PIECE * p.T));
-    if (p.rows <= t) pieces = 0;
-    base = p.pos_part + (size_t)t * pos_pieces * p.d;
-    first = 0;
-    stride = p.d;
-    out = p.dpos + (size_t)t * p.d;
-  }
-  const int c0 = blockIdx.y * 128 + lane;
-  float acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int i = w; i < pieces; i += 8) {
-    const float* src = base + (i == 0 ? first : (long long)i * stride);
+// Adds `pieces` rows of d floats (piece 0 at base + first, piece i > 0 at base + i * stride) and stores the sum times
+// scale.  A block has 256 columns: eight warps per 128 of them, each with every eighth piece, whose sums are added in
+// order.  (One block for all columns of the commonest token of natural text read its pieces at 44 GB/s: 17 us.)
+constexpr int COMBINE_COLS = 256, SLICES = 8, COMBINE_WARPS = SLICES * COMBINE_COLS / 128;
+__device__ __forceinline__ void add_pieces(const float* base, long long first, long long stride, int pieces, int d, float* out, float scale,
+                                           float (*red)[128]) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, tile = w / SLICES, slice = w % SLICES, c0 = blockIdx.y * COMBINE_COLS + tile * 128 + lane;
+  int col[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) if (c0 + 32 * u < p.d) acc[u] += src[c0 + 32 * u];
+  for (int u = 0; u < 4; ++u) col[u] = min(c0 + 32 * u, d - 1);
+  float acc[4] = {0.f, 0.f, 0.f, 0.f};
+  constexpr int BATCH = 8;                       // pieces in flight
+  for (int i0 = slice; i0 < pieces; i0 += SLICES * BATCH) {
+    float x[BATCH][4];
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const int i = min(i0 + k * SLICES, pieces - 1);
+      const float* src = base + (i == 0 ? first : (long long)i * stride);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x[k][u] = src[col[u]];
+    }
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k)
+      if (i0 + k * SLICES < pieces) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) acc[u] += x[k][u];
+      }
   }
-  __shared__ float red[8][128];
+  __syncthreads();
 #pragma unroll
   for (int u = 0; u < 4; ++u) red[w][lane + 32 * u] = acc[u];
   __syncthreads();
-  if (threadIdx.x < 128) {
-    const int cc = blockIdx.y * 128 + threadIdx.x;
-    if (cc < p.d) {
-      float s = red[0][threadIdx.x];
+  if (slice == 0) {
 #pragma unroll
-      for (int i = 1; i < 8; ++i) s += red[i][threadIdx.x];
-      out[cc] = s * scale;
+    for (int u = 0; u < 4; ++u) {
+      float s = acc[u];
+#pragma unroll
+      for (int i = 1; i < SLICES; ++i) s += red[w + i][lane + 32 * u];
+      if (c0 + 32 * u < d) out[c0 + 32 * u] = s * scale;
     }
+  }
+}
+// A block looks at COMBINE stretches for long tokens that start there, or takes one position with several pieces.
+constexpr int COMBINE = 8;
+__global__ void __launch_bounds__(COMBINE_WARPS * 32) embed_combine_kernel(EmbedBwdProb p, int P, int chunks, int pos_pieces) {
+  __shared__ float red[COMBINE_WARPS][128];
+  __shared__ int2 found[COMBINE];                // token and number of rows
+  const int blocks = (chunks + COMBINE - 1) / COMBINE;
+  cudaGridDependencySynchronize();
+  if ((int)blockIdx.x < blocks) {
+    if (threadIdx.x < COMBINE) {
+      const long long c = (long long)blockIdx.x * COMBINE + threadIdx.x;
+      int2 f = make_int2(0, 0);
+      if (c < chunks) {
+        const uint32_t e = (uint32_t)p.sorted[(int)min((c + 1) * P, (long long)p.rows) - 1].y;
+        if (e & HEAVY) {
+          const int2 sg = p.seg[e & ~HEAVY];
+          if (sg.x >= c * P) f = make_int2((int)(e & ~HEAVY), sg.y);   // else it started in an earlier stretch
+        }
+      }
+      found[threadIdx.x] = f;
+    }
+    __syncthreads();
+    for (int i = 0; i < COMBINE; ++i) {
+      const int2 f = found[i];
+      const long long c = (long long)blockIdx.x * COMBINE + i;
+      if (f.y) add_pieces(p.part + (size_t)(2 * c) * p.d, p.d, 2LL * PIECES * p.d, (f.y + PIECES * P - 1) / (PIECES * P), p.d, p.dtok + (size_t)f.x * p.d, p.scale, red);
+    }
+  } else {
+    const int t = (int)blockIdx.x - blocks;
+    const long long per = (long long)POS_PIECE * p.T;
+    add_pieces(p.pos_part + (size_t)t * pos_pieces * p.d, 0, p.d, (int)(((long long)p.rows - t + per - 1) / per), p.d, p.dpos + (size_t)t * p.d, 1.f, red);
   }
 }
 
@@ -321,19 +427,40 @@ bool aligned16(const void* a, const void* b, const void* c) { return (((uintptr_
 
 // Rows of a stretch.  Few rows: short stretches, so that there are enough workers; many: long ones, so that the
 // pieces of frequent tokens stay few.
-int piece_rows(int rows) { return rows <= 32768 ? 16 : 64; }
-int pos_pieces_for(int rows, int T) { return T > 0 ? (int)(((rows + T - 1) / T + POS_PIECE - 1) / POS_PIECE) : 0; }
+int piece_rows(int rows) { return rows <= 16384 ? 16 : rows <= 131072 ? 32 : 64; }
+// Pieces of a position's rows: only where the positions alone would not give every SM two workers.
+int pos_pieces_for(int rows, int T) { return T >= 296 ? 1 : (int)(((rows + T - 1) / T + POS_PIECE - 1) / POS_PIECE); }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 template <typename T, int VEC>
-cudaError_t run_sum(const EmbedBwdProb& p, int P, int chunks, int pos_pieces, cudaStream_t s) {
+cudaError_t run_sort_and_sum(const EmbedBwdProb& p, int P, int chunks, int pos_pieces, int* d_status, cudaStream_t s) {
   const int vecs = (p.d + VEC - 1) / VEC, ll = lanes_log2_for(vecs, 7), per_block = SUM_THREADS >> ll;
+  int n_log2 = 0;
+  while (n_log2 < 7 && (1 << n_log2) < p.vocab) ++n_log2;
+  while ((((long long)p.vocab + (1 << n_log2) - 1) >> n_log2) > SORT_MAX_LOCAL) ++n_log2;
+  const int local = (int)(((long long)p.vocab + (1 << n_log2) - 1) >> n_log2);
+  const size_t smem = ((size_t)SORT_WARPS * (local | 1) + 2 * (size_t)local + SORT_WARPS * SORT_LIST) * sizeof(int);
+  static SmemLimit limit;
+  cudaError_t e = limit.raise((const void*)embed_sort_kernel<T, VEC>,
+                              (SORT_WARPS * (SORT_MAX_LOCAL | 1) + 2 * SORT_MAX_LOCAL + SORT_WARPS * SORT_LIST) * (int)sizeof(int));
+  if (e != cudaSuccess) return e;
+  // The position gradient reads dh a second time.  While dh stays in the L2 cache (126 MB) that is cheap, and it rides with
+  // the sums; a larger one is read under the sort, which leaves the memory idle.  ([8192, 512]: 15 against 20 us with
+  // the sort; [65536, 1024]: 104 against 93.)
+  const long long pos_work = p.dpos ? (long long)p.T * pos_pieces : 0;
+  const bool early = (size_t)p.rows * p.d * sizeof(T) > ((size_t)64 << 20);
+  const int groups_log2 = 10 - ll;               // of a block of 1024 threads
+  int split = 0;                                 // groups per sum: until there is a block for every SM
+  while (split < groups_log2 && (pos_work << split >> groups_log2) < 148) ++split;
+  const long long pos_blocks = early ? ((pos_work << split) + (1 << groups_log2) - 1) >> groups_log2 : 0;
+  const long long pos_late = early ? 0 : (pos_work + per_block - 1) / per_block;
+  e = launch_kernel(embed_sort_kernel<T, VEC>, dim3((unsigned)((1 << n_log2) + pos_blocks)), SORT_WARPS * 32, smem, s, p, n_log2, local, PIECES * P, d_status, ll,
+                    split, pos_pieces);
+  if (e != cudaSuccess) return e;
   const int sum_blocks = (chunks + per_block - 1) / per_block;
-  const long long pos_workers = p.dpos ? (long long)p.T * pos_pieces : 0;
-  const long long pos_blocks = (pos_workers + per_block - 1) / per_block;
   const long long zero_blocks = ((long long)p.vocab + ZERO_ROWS - 1) / ZERO_ROWS;
-  const dim3 grid((unsigned)(sum_blocks + pos_blocks + zero_blocks), (unsigned)((vecs + (1 << ll) - 1) >> ll));
-  return launch_kernel(embed_sum_kernel<T, VEC>, grid, SUM_THREADS, 0, s, p, ll, P, sum_blocks, (int)pos_blocks, pos_pieces);
+  const dim3 grid((unsigned)(sum_blocks + pos_late + zero_blocks), (unsigned)((vecs + (1 << ll) - 1) >> ll));
+  return launch_after(embed_sum_kernel<T, VEC>, grid, SUM_THREADS, 0, s, p, ll, P, sum_blocks, (int)pos_late, pos_pieces);
 }
 
 }  // namespace
@@ -366,24 +493,15 @@ cudaError_t launch_embed_bwd(EmbedBwdProb p, void* workspace, int* d_status, boo
   p.seg = (int2*)w;     w += up256((size_t)p.vocab * sizeof(int2));
   p.part = (float*)w;   w += up256(2 * (size_t)chunks * p.d * sizeof(float));
   p.pos_part = (float*)w;
-  int n_log2 = 0;
-  while (n_log2 < 7 && (1 << n_log2) < p.vocab) ++n_log2;
-  while ((((long long)p.vocab + (1 << n_log2) - 1) >> n_log2) > SORT_MAX_LOCAL) ++n_log2;
-  const int local = (int)(((long long)p.vocab + (1 << n_log2) - 1) >> n_log2);
-  const size_t smem = ((size_t)SORT_WARPS * (local | 1) + 2 * (size_t)local) * sizeof(int);
-  static SmemLimit limit;
-  cudaError_t e = limit.raise((const void*)embed_sort_kernel, (SORT_WARPS * (SORT_MAX_LOCAL | 1) + 2 * SORT_MAX_LOCAL) * (int)sizeof(int));
-  if (e != cudaSuccess) return e;
-  e = launch_kernel(embed_sort_kernel, dim3(1u << n_log2), SORT_WARPS * 32, smem, s, p, n_log2, local, P, d_status);
-  if (e != cudaSuccess) return e;
   const int full = is_bf16 ? 8 : 4;
   const bool vec = p.d % full == 0 && aligned16(p.dh, p.dtok, p.dpos);
-  if (is_bf16) e = vec ? run_sum<bf16, 8>(p, P, chunks, pos_pieces, s) : run_sum<bf16, 1>(p, P, chunks, pos_pieces, s);
-  else e = vec ? run_sum<float, 4>(p, P, chunks, pos_pieces, s) : run_sum<float, 1>(p, P, chunks, pos_pieces, s);
+  cudaError_t e;
+  if (is_bf16) e = vec ? run_sort_and_sum<bf16, 8>(p, P, chunks, pos_pieces, d_status, s) : run_sort_and_sum<bf16, 1>(p, P, chunks, pos_pieces, d_status, s);
+  else e = vec ? run_sort_and_sum<float, 4>(p, P, chunks, pos_pieces, d_status, s) : run_sort_and_sum<float, 1>(p, P, chunks, pos_pieces, d_status, s);
   if (e != cudaSuccess) return e;
-  const int long_chunks = p.rows > P ? chunks : 0, long_pos = pos_pieces > 1 ? p.T : 0;
+  const int long_chunks = p.rows > PIECES * P ? chunks : 0, long_pos = pos_pieces > 1 ? p.T : 0;
   if (long_chunks + long_pos == 0) return cudaSuccess;
-  return launch_kernel(embed_combine_kernel, dim3((unsigned)(long_chunks + long_pos), (unsigned)((p.d + 127) / 128)), 256, 0, s, p, P,
+  return launch_after(embed_combine_kernel, dim3((unsigned)((long_chunks + COMBINE - 1) / COMBINE + long_pos), (unsigned)((p.d + COMBINE_COLS - 1) / COMBINE_COLS)), COMBINE_WARPS * 32, 0, s, p, P,
                        long_chunks, pos_pieces);
 }
 

@@ -882,7 +882,7 @@ lp_status lp_linear_attention_bf16(int form, const lp_linattn_desc* d, void* wor
     if (outs[i] == d->q.p || outs[i] == d->k.p || outs[i] == d->v.p || (back && outs[i] == d->dout.p)) return bad(LP_ERR_INVALID_ARG, "an output is an input");
     for (int j = 0; j < i; ++j) if (outs[i] == outs[j]) return bad(LP_ERR_INVALID_ARG, "two outputs are the same");
   }
-  if (!aligned_to(d->state_in, 16) || !aligned_to(d->log_decay, 4) || !aligned_to(d->lengths, 4) ||
+  if (!aligned_to(d->state_in, 16) || !aligned_to(d->log_decay, 4) || !aligned_to(d->lengths, 4) || !aligned_to(d->status, 4) ||
       (!back && !aligned_to(d->state_out, 16)) || (back && (!aligned_to(d->dstate_out, 16) || !aligned_to(d->dstate_in, 16))))
     return bad(LP_ERR_UNSUPPORTED, "states must be 16-byte aligned");
   if (back && d->dstate_in && d->dstate_in == d->state_in) return bad(LP_ERR_INVALID_ARG, "an output is an input");
@@ -895,7 +895,7 @@ lp_status lp_linear_attention_bf16(int form, const lp_linattn_desc* d, void* wor
   auto tok = [](const lp_tokens& t) { return LinAttnTok{(const bf16*)t.p, t.token_stride, t.batch_stride}; };
   LinAttnArgs a{tok(d->q), tok(d->k), tok(d->v), tok(d->o), tok(d->dout), tok(d->dq), tok(d->dk), tok(d->dv),
                 d->log_decay, d->state_in, back ? nullptr : d->state_out, back ? d->dstate_out : nullptr, back ? d->dstate_in : nullptr,
-                d->lengths, d->batch, d->seq_len, d->n_heads, d->scale, 1, 0, nullptr, nullptr};
+                d->lengths, d->status, d->batch, d->seq_len, d->n_heads, d->scale, 1, 0, nullptr, nullptr};
   // one token takes the recurrent kernel in either form: the chunked one would work on 63 empty rows
   const cudaError_t e = !back && d->seq_len == 1 ? launch_linattn_step(a, (cudaStream_t)stream) : launch_linattn(a, back, workspace, (cudaStream_t)stream);
   return launched(me, e);
