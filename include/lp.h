@@ -414,10 +414,11 @@ lp_status lp_dropout(int dtype, const void* x, const void* resid, void* y, long 
  *   log_decay: fp32 [n_heads], <= 0 (-infinity: a token sees itself only).
  *   Tokens: element i of head h of token t of sequence b is p[b * batch_stride + t * token_stride + 64 h + i] (strides in
  *   elements): separate tensors and slices of a packed [batch, seq_len, 3, n_heads, 64] tensor alike.  Pointers 16-byte
- *   aligned, strides multiples of 8, token_stride >= 64 * n_heads (seq_len 1: ignored).
+ *   aligned, strides multiples of 8 and at most 2^38, token_stride >= 64 * n_heads (seq_len 1: ignored), batch_stride > 0
+ *   (batch 1: ignored).
  *   States: fp32 [batch, n_heads, 64, 64], contiguous, 16-byte aligned.
- *   lengths (nullable): int32 [batch], sequence b has lengths[b] tokens (clamped to [0, seq_len]); tokens behind are not
- *   read, and rows of outputs and gradients behind are left as they were.
+ *   lengths (nullable): int32 [batch], sequence b has lengths[b] tokens (clamped to [0, seq_len]); tokens behind may
+ *   hold anything, and rows of outputs and gradients behind are left as they were.
  *   LP_LINATTN_FORWARD:  q, k, v, [state_in] -> o, [state_out].  state_in NULL: zero.  state_out, if given, receives the
  *       state behind the last token (state_in itself for an empty sequence) and may be state_in.
  *   LP_LINATTN_BACKWARD: q, k, v, dout, [state_in], [dstate_out: gradient of state_out, NULL: zero] -> dq, dk, dv,

@@ -43,9 +43,30 @@ __device__ __forceinline__ void stsm(uint32_t a, uint32_t x, uint32_t y, uint32_
   asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// The same with zeros in place of the accumulator.
+__device__ __forceinline__ void mma0(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+// Two products (or sums) at a time.
+__device__ __forceinline__ void mul2(float& x, float& y, float a, float b) {
+  asm("{\n\t.reg .b64 u, v;\n\tmov.b64 u, {%0, %1};\n\tmov.b64 v, {%2, %3};\n\tmul.rn.f32x2 u, u, v;\n\tmov.b64 {%0, %1}, u;\n\t}"
+      : "+f"(x), "+f"(y) : "f"(a), "f"(b));
+}
+__device__ __forceinline__ void sub2(float& x, float& y, float a, float b) {
+  asm("{\n\t.reg .b64 u, v, m;\n\tmov.b64 u, {%0, %1};\n\tmov.b64 v, {%2, %3};\n\tmov.b64 m, {%4, %4};\n\tfma.rn.f32x2 u, v, m, u;\n\tmov.b64 {%0, %1}, u;\n\t}"
+      : "+f"(x), "+f"(y) : "f"(a), "f"(b), "f"(-1.f));
+}
+// The bf16 pair nearest to (x, y); x and y become what is left.
+__device__ __forceinline__ uint32_t split(float& x, float& y) {
+  const uint32_t h = la_pack(x, y);
+  sub2(x, y, la_lo(h), la_hi(h));
+  return h;
+}
+
 // What a lane adds to a tile's address.  lane_rows: rows lane % 16, unit lane / 16 -- ldsm gives the A fragment of 16 rows
 // and 16 columns, ldsm_t the B fragments B(k, n) = tile[k][n] of 16 k and 16 n.  lane_cols: rows and units the other way
 // round -- ldsm gives B(k, n) = tile[n][k], ldsm_t the A fragment A(m, k) = tile[k][m].
@@ -123,9 +144,10 @@ __device__ __forceinline__ void state_mma(float (&d)[N / 8][4], const uint32_t (
   uint32_t term[TERMS][4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {                  // registers 0, 1: tokens 2t, 2t+1; registers 2, 3: tokens 2t+8, 2t+9
-    float x = la_lo(bt[e]) * wt[(e >> 1) * 2], y = la_hi(bt[e]) * wt[(e >> 1) * 2 + 1];
+    float x = la_lo(bt[e]), y = la_hi(bt[e]);
+    mul2(x, y, wt[(e >> 1) * 2], wt[(e >> 1) * 2 + 1]);
 #pragma unroll
-    for (int k = 0; k + 1 < TERMS; ++k) term[k][e] = la_take(x, y);
+    for (int k = 0; k + 1 < TERMS; ++k) term[k][e] = split(x, y);
     term[TERMS - 1][e] = la_pack(x, y);
   }
 #pragma unroll
@@ -264,51 +286,248 @@ __global__ void __launch_bounds__(128) la_backward_short_kernel(LinAttnArgs p) {
   else scan_short<3, true>(p, sp, p.k, p.q, p.dout, p.dv, r_in, false, p.dstate_in ? p.dstate_in + so : nullptr, smem);
 }
 
-// The state a segment leaves when it starts from zero: sum_j l^(end-1-j) b_j c_j^T, or backwards in time
-// sum_j l^(j+1) scale b_j c_j^T.
-template <int TERMS, bool REV>
-__device__ __forceinline__ void segment_state(const LinAttnArgs& p, const LaSpan& sp, const LinAttnTok& B, const LinAttnTok& Cc, float* out, char* smem) {
+// Tokens in the order of a scan: the first one, and the distance to the next (negative backwards in time).
+struct Run { const bf16* p; long long ts; };
+__device__ __forceinline__ Run run_of(const LinAttnTok& x, const LaSpan& sp, bool rev) {
+  return rev ? Run{la_at(x, sp, sp.t1 - 1), -x.ts} : Run{la_at(x, sp, sp.t0), x.ts};
+}
+
+// Fetches a run's tokens tile by tile, in order; 128 threads.  Rows behind the end read as zero.
+struct Loader {
+  const bf16* g;                                 // this thread's unit of the next tile
+  long long step;                                // 16 rows on
+  const bf16* any;                               // an address that may be named where nothing is fetched
+  int left;                                      // rows from this thread's first one to the end
+  __device__ __forceinline__ Loader(const Run& r, int len)
+      : g(r.p + (threadIdx.x >> 3) * r.ts + (threadIdx.x & 7) * 8), step(16 * r.ts), any(r.p), left(len - (int)(threadIdx.x >> 3)) {}
+  __device__ __forceinline__ void next(uint32_t tile) {
+    const uint32_t d = tile + (threadIdx.x >> 3) * PITCH + (threadIdx.x & 7) * 16;
+    if (left > 48) {                             // all four rows of this thread
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d + i * 16 * PITCH), "l"(g) : "memory");
+        g += step;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool in = 16 * i < left;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d + i * 16 * PITCH), "l"(in ? g : any), "r"(in ? 16 : 0) : "memory");
+        g += step;
+      }
+    }
+    left -= C;
+  }
+};
+
+// The scan of a span (see the head of the file): four warps, 16 rows of y and of the state each.  TERMS: bf16 terms of the
+// decayed b.  Backwards in time the tokens are taken in reversed order, so that both directions are one and the same
+// code (three copies of it, one per gradient, kept the warps waiting for instructions for a quarter of their time); the
+// state is then the one right at the first token, not a step before it, and carries the scale.
+template <int TERMS>
+__device__ __forceinline__ void scan(int len, const Run A, const Run B, const Run Cc, const Run Y, bool rev, float lg, float scale, const float* s_in,
+                                     bool transposed, float* s_out, char* smem) {
+  constexpr int BUF = 4 * TILE_B;                // two buffers of a, b, c and the state
+  float *pw = (float*)smem + 64, *sc = (float*)smem + 160;
+  const uint32_t tiles = smem_addr(smem + TAB);
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const int n_chunks = (len + C - 1) / C;
+  Loader la(A, len), lb(B, len), lc(Cc, len);
+  auto fetch = [&](uint32_t buf) {
+    la.next(buf);
+    lb.next(buf + TILE_B);
+    lc.next(buf + 2 * TILE_B);
+  };
+  if (n_chunks > 0) fetch(tiles);
+  cp_commit();
+  decay_tables(pw, sc, lg, scale);
+  float s[8][4];
+  state_load<64>(s, s_in, transposed, 0, w, lane);
+  const uint32_t rows = lane_rows(lane), own = rows + w * 16 * PITCH, cols = lane_cols(lane);
+  put_rows<64>(tiles + 3 * TILE_B + own, s);
+  const float* from_state = (rev ? pw : sc + 1) + 16 * w + g;            // weights of the rows' products with the state
+  bf16* y = const_cast<bf16*>(Y.p) + (16 * w + (lane >> 3)) * Y.ts + (lane & 7) * 8;
+  const uint32_t y_at = (16 * w + (lane >> 3)) * PITCH + (lane & 7) * 16;
+  for (int it = 0; it < n_chunks; ++it) {
+    const uint32_t buf = tiles + (it & 1) * BUF, other = tiles + ((it & 1) ^ 1) * BUF;
+    cp_wait<0>();
+    __syncthreads();                             // this chunk's tiles and state are in place; the other buffer is free
+    if (it + 1 < n_chunks) fetch(other);
+    cp_commit();
+    const int n = min(C, len - it * C);
+    const uint32_t ba = buf + own, bs = buf + 3 * TILE_B + rows;
+    uint32_t af[4][4];
+    float acc[8][4];
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      ldsm(af[ks], ba + ks * 32);
+#pragma unroll
+      for (int np = 0; np < 4; ++np) {
+        uint32_t b[4];
+        ldsm_t(b, bs + ks * 16 * PITCH + np * 32);
+        if (ks == 0) {
+          mma0(acc[2 * np], af[ks], b[0], b[1]);
+          mma0(acc[2 * np + 1], af[ks], b[2], b[3]);
+        } else {
+          mma(acc[2 * np], af[ks], b[0], b[1]);
+          mma(acc[2 * np + 1], af[ks], b[2], b[3]);
+        }
+      }
+    }
+    const float w0 = from_state[0], w1 = from_state[8], ln = pw[n];
+    float d[TERMS == 3 ? 8 : 1][4] = {};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      mul2(acc[j][0], acc[j][1], w0, w0);
+      mul2(acc[j][2], acc[j][3], w1, w1);
+      if (TERMS < 3) {
+        mul2(s[j][0], s[j][1], ln, ln);
+        mul2(s[j][2], s[j][3], ln, ln);
+      }
+    }
+    uint32_t bb = buf + TILE_B + cols, bc = buf + 2 * TILE_B + rows;
+    const float* wp = sc + 16 * w + g - 2 * t;   // ages of the pair (row g of this warp, column 2t of a step): rows lie 8 apart
+    const float* wj = (rev ? sc + n : pw + n - 1) - 2 * t;               // weights of the tokens in the state
+#pragma unroll 1
+    for (int kk = 0; kk < 4; ++kk) {
+      uint32_t cf[4][4], bt[4];
+      ldsm_t(bt, bb + w * 32);
+#pragma unroll
+      for (int np = 0; np < 4; ++np) ldsm_t(cf[np], bc + np * 32);
+      const float wt[4] = {wj[0], wj[-1], wj[-8], wj[-9]};
+      // The state's products stand in both branches: beside the scores' they fill the waits of that chain.
+      if (kk <= w) {
+        float x[2][4];
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          uint32_t b[4];
+          ldsm(b, bb + ks * 32);
+          if (ks == 0) {
+            mma0(x[0], af[ks], b[0], b[1]);
+            mma0(x[1], af[ks], b[2], b[3]);
+          } else {
+            mma(x[0], af[ks], b[0], b[1]);
+            mma(x[1], af[ks], b[2], b[3]);
+          }
+        }
+        if constexpr (TERMS == 3) state_mma<64, 3>(d, bt, cf, wt);
+        else state_mma<64, TERMS>(s, bt, cf, wt);
+        uint32_t pf[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int up = (e & 1) * 8, left = (e >> 1) * 8;
+          float u = x[e >> 1][(e & 1) * 2], v = x[e >> 1][(e & 1) * 2 + 1];
+          mul2(u, v, wp[up - left], wp[up - left - 1]);
+          pf[e] = la_pack(u, v);
+        }
+#pragma unroll
+        for (int np = 0; np < 4; ++np) {
+          mma(acc[2 * np], pf, cf[np][0], cf[np][1]);
+          mma(acc[2 * np + 1], pf, cf[np][2], cf[np][3]);
+        }
+      } else {
+        if constexpr (TERMS == 3) state_mma<64, 3>(d, bt, cf, wt);
+        else state_mma<64, TERMS>(s, bt, cf, wt);
+      }
+      bb += 16 * PITCH;
+      bc += 16 * PITCH;
+      wp -= 16;
+      wj -= 16;
+    }
+    if constexpr (TERMS == 3) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[j][e] = fmaf(ln, s[j][e], d[j][e]);
+    }
+    put_rows<64>(other + 3 * TILE_B + own, s);
+    // y leaves through this warp's own rows of a: no other warp reads them
+    __syncwarp();
+    put_rows<64>(ba, acc);
+    __syncwarp();
+    const int left = n - 16 * w - (lane >> 3);   // rows 4 i of this warp with 4 i < left exist
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint4 v;
+      asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(buf + y_at + i * 4 * PITCH) : "memory");
+      if (4 * i < left) *(uint4*)(y + i * 4 * Y.ts) = v;
+    }
+    y += C * Y.ts;
+  }
+  if (s_out) state_store<64>(s_out, s, 0, w, lane);
+}
+
+// Entry states: from the workspace where segments were formed, else from the caller.
+template <int TERMS>
+__global__ void __launch_bounds__(128, TERMS == 3 ? 2 : 3) la_forward_kernel(LinAttnArgs p) {
+  extern __shared__ __align__(128) char smem[];
+  cudaGridDependencySynchronize();
+  const LaSpan sp = la_span(p, blockIdx.x);
+  const size_t so = ((size_t)sp.b * p.H + sp.h) * TILE;
+  const float* in = p.seg_states ? p.seg_states + (size_t)blockIdx.x * TILE : p.state_in ? p.state_in + so : nullptr;
+  scan<TERMS>(sp.t1 - sp.t0, run_of(p.q, sp, false), run_of(p.k, sp, false), run_of(p.v, sp, false), run_of(p.o, sp, false), false, p.log_decay[sp.h],
+              p.scale, in, false, p.seg_states || !p.state_out ? nullptr : p.state_out + so, smem);
+}
+// Three scans of every segment: dq, dk, dv.
+template <int TERMS>
+__global__ void __launch_bounds__(128, TERMS == 3 ? 2 : 3) la_backward_kernel(LinAttnArgs p) {
+  extern __shared__ __align__(128) char smem[];
+  cudaGridDependencySynchronize();
+  const int which = blockIdx.x % 3, item = blockIdx.x / 3;
+  const LaSpan sp = la_span(p, item);
+  const size_t so = ((size_t)sp.b * p.H + sp.h) * TILE;
+  const float* s_in = p.seg_states ? p.seg_states + (size_t)item * TILE : p.state_in ? p.state_in + so : nullptr;
+  const float* r_in = p.seg_states ? p.seg_grads + (size_t)item * TILE : p.dstate_out ? p.dstate_out + so : nullptr;
+  const LinAttnTok &a = which == 0 ? p.dout : which == 1 ? p.v : p.k, &b = which == 0 ? p.v : which == 1 ? p.dout : p.q,
+                   &c = which == 0 ? p.k : which == 1 ? p.q : p.dout, &y = which == 0 ? p.dq : which == 1 ? p.dk : p.dv;
+  const bool rev = which != 0;
+  scan<TERMS>(sp.t1 - sp.t0, run_of(a, sp, rev), run_of(b, sp, rev), run_of(c, sp, rev), run_of(y, sp, rev), rev, p.log_decay[sp.h], p.scale,
+              rev ? r_in : s_in, which != 2, which != 2 || p.seg_states || !p.dstate_in ? nullptr : p.dstate_in + so, smem);
+}
+constexpr int SCAN_SMEM = TAB + 8 * TILE_B;
+
+// The state a run of tokens leaves when it starts from zero: sum_j l^(n-1-j) b_j c_j^T, or backwards in time
+// sum_j l^(n-j) scale b_j c_j^T.
+template <int TERMS>
+__device__ __forceinline__ void run_state(int len, const Run B, const Run Cc, bool rev, float lg, float scale, float* out, char* smem) {
   float *pw = (float*)smem + 64, *sc = (float*)smem + 160;
   const uint32_t tiles = smem_addr(smem + TAB);
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, t = lane & 3;
   float s[8][4] = {};
-  const int n_chunks = (sp.t1 - sp.t0 + C - 1) / C;
-  auto begin = [&](int it) { return sp.t0 + (long long)(REV ? n_chunks - 1 - it : it) * C; };
+  const int n_chunks = (len + C - 1) / C;
+  Loader lb(B, len), lc(Cc, len);
   auto fetch = [&](int it) {
-    const long long tb = begin(it);
-    const int n = min(C, (int)(sp.t1 - tb));
     const uint32_t buf = tiles + (it % 3) * 2 * TILE_B;
-    load_tile<128>(buf, la_at(B, sp, tb), B.ts, n);
-    load_tile<128>(buf + TILE_B, la_at(Cc, sp, tb), Cc.ts, n);
+    lb.next(buf);
+    lc.next(buf + TILE_B);
   };
   if (n_chunks > 0) fetch(0);
   cp_commit();
   if (n_chunks > 1) fetch(1);
   cp_commit();
-  decay_tables(pw, sc, p.log_decay[sp.h], p.scale);
+  decay_tables(pw, sc, lg, scale);
   for (int it = 0; it < n_chunks; ++it) {
     cp_wait<1>();
     __syncthreads();
     if (it + 2 < n_chunks) fetch(it + 2);
     cp_commit();
-    const int n = min(C, (int)(sp.t1 - begin(it)));
-    const uint32_t buf = tiles + (it % 3) * 2 * TILE_B, bt_at = buf + lane_cols(lane) + w * 32, bc = buf + TILE_B + lane_rows(lane);
+    const int n = min(C, len - it * C);
+    const uint32_t buf = tiles + (it % 3) * 2 * TILE_B;
+    uint32_t bt_at = buf + lane_cols(lane) + w * 32, bc = buf + TILE_B + lane_rows(lane);
     const float ln = pw[n];
-    const float* wj = REV ? sc + 1 + 2 * t : pw + n - 1 - 2 * t;
+    const float* wj = (rev ? sc + n : pw + n - 1) - 2 * t;
     float d[8][4] = {};
-#pragma unroll
+#pragma unroll 1
     for (int kk = 0; kk < 4; ++kk) {
       uint32_t cf[4][4], bt[4];
 #pragma unroll
-      for (int np = 0; np < 4; ++np) ldsm_t(cf[np], bc + kk * 16 * PITCH + np * 32);
-      ldsm_t(bt, bt_at + kk * 16 * PITCH);
-      float wt[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int j = 16 * kk + (e & 1) + (e >> 1) * 8;
-        wt[e] = REV ? wj[j] : wj[-j];
-      }
+      for (int np = 0; np < 4; ++np) ldsm_t(cf[np], bc + np * 32);
+      ldsm_t(bt, bt_at);
+      const float wt[4] = {wj[0], wj[-1], wj[-8], wj[-9]};
       state_mma<64, TERMS>(d, bt, cf, wt);
+      bt_at += 16 * PITCH;
+      bc += 16 * PITCH;
+      wj -= 16;
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -324,12 +543,15 @@ template <int TERMS>
 __global__ void __launch_bounds__(128, 4) la_segment_kernel(LinAttnArgs p) {
   extern __shared__ __align__(128) char smem[];
   const LaSpan sp = la_span(p, blockIdx.x);
-  if (blockIdx.y == 0) segment_state<TERMS, false>(p, sp, p.k, p.v, p.seg_states + (size_t)blockIdx.x * TILE, smem);
-  else segment_state<TERMS, true>(p, sp, p.q, p.dout, p.seg_grads + (size_t)blockIdx.x * TILE, smem);
+  const bool rev = blockIdx.y != 0;
+  const LinAttnTok &b = rev ? p.q : p.k, &c = rev ? p.dout : p.v;
+  run_state<TERMS>(sp.t1 - sp.t0, run_of(b, sp, rev), run_of(c, sp, rev), rev, p.log_decay[sp.h], p.scale,
+                   (rev ? p.seg_grads : p.seg_states) + (size_t)blockIdx.x * TILE, smem);
 }
 
 // Turns every segment's own state into the state at its entry, and forms the last state.
 __global__ void __launch_bounds__(256) la_join_kernel(LinAttnArgs p) {
+  cudaGridDependencySynchronize();
   const bool reverse = blockIdx.y != 0;
   const int bh = blockIdx.x, h = bh % p.H, b = bh / p.H, len = p.lengths ? min(max(p.lengths[b], 0), p.T) : p.T;
   float* seg = (reverse ? p.seg_grads : p.seg_states) + (size_t)bh * p.n_seg * TILE;
@@ -404,30 +626,25 @@ __global__ void __launch_bounds__(256) la_step_kernel(LinAttnArgs p) {
   }
 }
 
-// How the scans of bh sequences and heads are laid over the GPU: 148 SMs, two blocks each.  scans: how many scans of every
-// sequence run in the launch (1, or 3 in the backward pass).
+// Whether sequences are cut into segments whose entry states are formed ahead of the scans (k, v -- and q, do -- are then
+// read twice, in two more launches).  One block alone takes 1.7 us a chunk, three on an SM 3.4, so cutting pays where there
+// are fewer scans than SMs, and more segments than would fill the GPU even out its last wave.  Measured, whole / cut:
+// forward of 16 sequences and heads x 8192 tokens 209 / 38 us, 96 x 8192 212 / 165, 128 x 8192 212 / 200, 192 x 2048
+// 79 / 94; backward of 16 x 8192 212 / 80, 48 x 2048 56 / 64, 96 x 8192 308 / 383; of 16 x 512 either way 16 / 17.
+// scans: how many scans of every sequence run in the launch (1, or 3 in the backward pass).
 struct Layout { int n_seg, seg_len; };
 Layout choose_layout(long long bh, int T, int scans) {
-  Layout l;
-  constexpr int CH = 2 * C;                      // tokens of a chunk of the long form
-  const int chunks = (T + CH - 1) / CH;
-  const long long items = bh * scans;
-  long long want = items >= 148 ? 1 : (296 + items - 1) / items;
-  want = std::min<long long>(want, std::max(1, chunks / 2));
+  const int chunks = (T + C - 1) / C;
+  const long long want = bh * scans < 112 && chunks >= 16 ? std::min<long long>((1024 + bh - 1) / bh, chunks / 4) : 1;
   const int per = (int)((chunks + want - 1) / want);
-  l.n_seg = (chunks + per - 1) / per;
-  l.seg_len = per * CH;
-  return l;
+  return Layout{(chunks + per - 1) / per, per * C};
 }
-// Whether the states between segments (or the one that leaves the operator) are formed on their own, ahead of the scans.
-bool forms_states(const Layout& l, int T, bool state_leaves) { return T > C && (l.n_seg > 1 || state_leaves); }
 
 }  // namespace
 
-// Sized for a call that hands out a state, whether this one does or not.
 size_t linattn_workspace(bool backward, int B, int T, int H) {
   const Layout l = choose_layout((long long)B * H, T, backward ? 3 : 1);
-  return forms_states(l, T, true) ? (size_t)B * H * l.n_seg * TILE * sizeof(float) * (backward ? 2 : 1) : 0;
+  return l.n_seg > 1 ? (size_t)B * H * l.n_seg * TILE * sizeof(float) * (backward ? 2 : 1) : 0;
 }
 
 cudaError_t launch_linattn_step(const LinAttnArgs& a, cudaStream_t s) {
@@ -436,26 +653,31 @@ cudaError_t launch_linattn_step(const LinAttnArgs& a, cudaStream_t s) {
 
 cudaError_t launch_linattn(LinAttnArgs a, bool backward, void* workspace, cudaStream_t s) {
   const int bh = a.B * a.H;
-  const Layout l = choose_layout(bh, a.T, backward ? 3 : 1);
   if (a.T <= C) {
     a.n_seg = 1;
     a.seg_len = C;
     return launch_kernel(backward ? la_backward_short_kernel : la_forward_short_kernel, dim3((unsigned)(backward ? 3 * bh : bh)), 128, SHORT_SMEM, s, a);
   }
+  const Layout l = choose_layout(bh, a.T, backward ? 3 : 1);
   a.n_seg = l.n_seg;
   a.seg_len = l.seg_len;
   const bool leaves = backward ? a.dstate_in != nullptr : a.state_out != nullptr;
-  if (forms_states(l, a.T, leaves)) {
+  cudaError_t e;
+  if (a.n_seg > 1) {
     a.seg_states = (float*)workspace;
     a.seg_grads = a.seg_states + (size_t)bh * a.n_seg * TILE;
     static SmemLimit limit[2];
     auto seg = leaves ? la_segment_kernel<3> : la_segment_kernel<2>;
-    cudaError_t e = limit[leaves].raise((const void*)seg, SEG_SMEM);
+    e = limit[leaves].raise((const void*)seg, SEG_SMEM);
     if (e == cudaSuccess) e = launch_kernel(seg, dim3((unsigned)(bh * a.n_seg), backward ? 2 : 1), 128, SEG_SMEM, s, a);
-    if (e == cudaSuccess) e = launch_kernel(la_join_kernel, dim3((unsigned)bh, backward ? 2 : 1, 4), 256, 0, s, a);
+    if (e == cudaSuccess) e = launch_after(la_join_kernel, dim3((unsigned)bh, backward ? 2 : 1, 4), 256, 0, s, a);
     if (e != cudaSuccess) return e;
   }
-  return launch_linattn_scan_tc(a, backward, s);
+  const bool three = leaves && a.n_seg == 1;     // otherwise the state that leaves comes from the segments
+  static SmemLimit limit[4];
+  auto kernel = backward ? (three ? la_backward_kernel<3> : la_backward_kernel<2>) : three ? la_forward_kernel<3> : la_forward_kernel<2>;
+  e = limit[backward * 2 + three].raise((const void*)kernel, SCAN_SMEM);
+  return e != cudaSuccess ? e : launch_after(kernel, dim3((unsigned)((long long)bh * a.n_seg * (backward ? 3 : 1))), 128, (size_t)SCAN_SMEM, s, a);
 }
 
 }  // namespace lp

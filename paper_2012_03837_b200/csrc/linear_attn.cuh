@@ -44,7 +44,4 @@ __device__ __forceinline__ uint32_t la_take(float& x, float& y) {
   return h;
 }
 
-// The scan on tcgen05 (linear_attn_tc.cu) of a.n_seg segments of every sequence and head.
-cudaError_t launch_linattn_scan_tc(const LinAttnArgs& a, bool backward, cudaStream_t s);
-
 }  // namespace lp

@@ -871,6 +871,8 @@ lp_status lp_linear_attention_bf16(int form, const lp_linattn_desc* d, void* wor
     if (!used[i]) continue;
     if (!aligned_to(all[i]->p, 16) || (all[i]->batch_stride & 7) || (all[i]->token_stride & 7))
       return bad(LP_ERR_UNSUPPORTED, "tokens must be 16-byte aligned, their strides multiples of 8 elements");
+    if (all[i]->batch_stride > 1LL << 38 || all[i]->token_stride > 1LL << 38) return bad(LP_ERR_SHAPE, "strides must be at most 2^38 elements");
+    if (d->batch > 1 && all[i]->batch_stride < 8) return bad(LP_ERR_SHAPE, "batch_stride must be positive");
     if (all[i]->batch_stride < 0 || (d->seq_len > 1 && all[i]->token_stride < 64LL * d->n_heads))
       return bad(LP_ERR_SHAPE, "token_stride must be at least 64 * n_heads, batch_stride not negative");
     if (i >= 3 && i != 4 && d->batch > 1 && all[i]->batch_stride < 64LL * d->n_heads)
