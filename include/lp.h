@@ -97,6 +97,16 @@ typedef struct {
   int block_kind;
   /* RESNET, nullable: [K] blocks per stage (a ResNet-50 has 3, 4, 6, 3); NULL: blocks_per_stage in every stage. */
   const int* stage_blocks;
+  /* LM: probability, in [0, 1), with which the training steps drop elements of the embedding and of every attention and
+     feed-forward branch before it joins the residual stream (0, default: nothing is dropped).  The mask is lp_dropout's,
+     never stored: key dropout_seed, counter {i / 4 (low, high word), site, step} for element i of the [batch, seq_len,
+     d_model] tensor; site 0 is the embedding, 1 + 2 n the attention branch and 2 + 2 n the feed-forward branch of the
+     model's n-th block; step is the number of lp_step calls before this one (mod 2^32), which a checkpoint carries on.
+     lp_forward and lp_evaluate drop nothing.  Pieces of a chain on several GPUs take seeds of their own. */
+  float dropout;
+  unsigned long long dropout_seed;
+  /* LM: factor of the token embedding before the position is added (0: 1). */
+  float embed_scale;
 } lp_model_spec;
 
 /* Auxiliary head of every chunk (Sec. 3: same form as the global objective): softmax

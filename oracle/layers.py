@@ -198,15 +198,17 @@ def attention_bwd(dout, cache):
     return np.concatenate(parts, axis=-1).astype(dout.dtype)
 
 
-def embedding_fwd(ids, tok, pos):
-    """h[b, t] = tok[ids[b, t]] + pos[t]."""
-    return tok[ids] + pos[None, :ids.shape[1], :], (ids, tok.shape, pos.shape)
+def embedding_fwd(ids, tok, pos, scale=1.0):
+    """h[b, t] = scale * tok[ids[b, t]] + pos[t]."""
+    scale = tok.dtype.type(scale)
+    return scale * tok[ids] + pos[None, :ids.shape[1], :], (ids, tok.shape, pos.shape, scale)
 
 
 def embedding_bwd(dh, cache):
-    ids, tshape, pshape = cache
+    ids, tshape, pshape, scale = cache
     dtok = np.zeros(tshape, dtype=dh.dtype)
     np.add.at(dtok, ids.reshape(-1), dh.reshape(-1, dh.shape[-1]))
+    dtok *= scale
     dpos = np.zeros(pshape, dtype=dh.dtype)
     dpos[:ids.shape[1]] = dh.sum(axis=0)
     return dtok, dpos

@@ -40,6 +40,7 @@ import numpy as np
 
 import lp_synth
 from . import layers as L
+from . import lm_ops
 from . import optim as O
 
 
@@ -60,6 +61,8 @@ class LocalUpdateOracle:
         self.overlap = overlap   # overlapping local parallelism (Sec. 3, Fig. 2 c): synchronous schedule only
         self.buf = None          # pipelined: buf[k] = (activation, labels) chunk k+1 reads next
         self.t = 0               # pipelined steps taken since the last reset
+        self.steps = 0           # steps taken: the last counter word of dropout masks
+        self.drop_step = None    # that word inside a training step with dropout, else None (nothing is dropped)
         self.last_grads = {}
 
     # ---------------------------------------------------------------- chunk forward / backward
@@ -147,11 +150,22 @@ class LocalUpdateOracle:
         first = sum(self.cfg["blocks_per_chunk"][:k])
         return [f"c{k}.b{first + j}" for j in range(self.cfg["blocks_per_chunk"][k])]
 
+    def _drop(self, x, site):
+        """x with the elements that this step drops at `site` set to 0 and the others divided by 1 - p; and the
+        factors, which the gradient is multiplied by.  Sites: 0 embedding, 1 + 2n and 2 + 2n the branches of block n."""
+        if self.drop_step is None:
+            return x, None
+        pr = float(np.float32(self.cfg["dropout"]))      # the specification holds it in 32 bits
+        keep = lm_ops.dropout_keep(x.size, pr, self.cfg.get("dropout_seed", 0), 0, site, self.drop_step)
+        f = np.where(keep, 1.0 / (1.0 - pr), 0.0).astype(x.dtype).reshape(x.shape)
+        return x * f, f
+
     def _lm_fwd(self, k, inp):
         p = self.p
         cache = {}
         if k == 0:
-            h, cache["emb"] = L.embedding_fwd(inp, p["c0.tok"], p["c0.pos"])
+            h, cache["emb"] = L.embedding_fwd(inp, p["c0.tok"], p["c0.pos"], self.cfg.get("embed_scale") or 1.0)
+            h, cache["emb_drop"] = self._drop(h, 0)
         else:
             h = inp
         b, t, d = h.shape
@@ -161,26 +175,30 @@ class LocalUpdateOracle:
             qkv, cq = L.linear_fwd(a1.reshape(b * t, d), p[n + ".Wqkv"], p[n + ".bqkv"])
             o, ca = L.attention_fwd(qkv.reshape(b, t, 3 * d), self.cfg["n_heads"])
             r1, co = L.linear_fwd(o.reshape(b * t, d), p[n + ".Wo"], p[n + ".bo"])
+            site = 1 + 2 * int(n.split(".b")[1])
+            r1, f1 = self._drop(r1, site)
             h = h + r1.reshape(b, t, d)
             a2, cl2 = L.layernorm_fwd(h, p[n + ".ln2.g"], p[n + ".ln2.b"])
             u, c1 = L.linear_fwd(a2.reshape(b * t, d), p[n + ".W1"], p[n + ".b1"])
             gl, cg = L.gelu_fwd(u)
             r2, c2 = L.linear_fwd(gl, p[n + ".W2"], p[n + ".b2"])
+            r2, f2 = self._drop(r2, site + 1)
             h = h + r2.reshape(b, t, d)
-            cache["blocks"].append((n, cl1, cq, ca, co, cl2, c1, cg, c2))
+            cache["blocks"].append((n, cl1, cq, ca, co, cl2, c1, cg, c2, f1, f2))
         return h, cache
 
     def _lm_block_bwd(self, dh, block_cache, g):
         """Backward of one transformer block: fills g with its parameter gradients, returns the gradient
         at the block input."""
-        (n, cl1, cq, ca, co, cl2, c1, cg, c2) = block_cache
+        (n, cl1, cq, ca, co, cl2, c1, cg, c2, f1, f2) = block_cache
         b, t, d = dh.shape
-        dgl, g[n + ".W2"], g[n + ".b2"] = L.linear_bwd(dh.reshape(b * t, d), c2)
+        dropped = lambda x, f: x if f is None else x * f
+        dgl, g[n + ".W2"], g[n + ".b2"] = L.linear_bwd(dropped(dh.reshape(b * t, d), f2), c2)
         du = L.gelu_bwd(dgl, cg)
         da2, g[n + ".W1"], g[n + ".b1"] = L.linear_bwd(du, c1)
         dx, g[n + ".ln2.g"], g[n + ".ln2.b"] = L.layernorm_bwd(da2.reshape(b, t, d), cl2)
         dh = dh + dx
-        do, g[n + ".Wo"], g[n + ".bo"] = L.linear_bwd(dh.reshape(b * t, d), co)
+        do, g[n + ".Wo"], g[n + ".bo"] = L.linear_bwd(dropped(dh.reshape(b * t, d), f1), co)
         dqkv = L.attention_bwd(do.reshape(b, t, d), ca)
         da1, g[n + ".Wqkv"], g[n + ".bqkv"] = L.linear_bwd(dqkv.reshape(b * t, 3 * d), cq)
         dx, g[n + ".ln1.g"], g[n + ".ln1.b"] = L.layernorm_bwd(da1.reshape(b, t, d), cl1)
@@ -192,7 +210,8 @@ class LocalUpdateOracle:
             dh = self._lm_block_bwd(dh, block_cache, g)
         self._dx_in = dh         # gradient at the chunk input: used only by the overlapping variant
         if k == 0:
-            g["c0.tok"], g["c0.pos"] = L.embedding_bwd(dh, cache["emb"])
+            f = cache["emb_drop"]
+            g["c0.tok"], g["c0.pos"] = L.embedding_bwd(dh if f is None else dh * f, cache["emb"])
         return g
 
     # ResNet chunk: one stage of BasicBlocks or bottleneck blocks (stem convolution in chunk 0), App. B.3.
@@ -371,6 +390,7 @@ class LocalUpdateOracle:
         x = self._cast_input(x)
         losses = np.full(K, np.nan, dtype=np.float64)
         all_grads = [None] * K
+        self.drop_step = self.steps if self.cfg.get("dropout") else None
         if self.overlap and schedule != "sync":
             raise ValueError("overlapping updates are defined for the synchronous schedule")
         if schedule == "sync":
@@ -402,6 +422,8 @@ class LocalUpdateOracle:
                     new_buf[k] = (h, src[1])
             self.buf = new_buf
             self.t += 1
+        self.drop_step = None
+        self.steps += 1
         for k in range(K):
             if all_grads[k] is not None:
                 self.apply_update(k, all_grads[k])

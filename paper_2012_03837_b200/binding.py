@@ -42,7 +42,8 @@ class lp_model_spec(C.Structure):
                 ("in_channels", C.c_int), ("height", C.c_int), ("width", C.c_int),
                 ("stem_channels", C.c_int), ("stage_channels", C.POINTER(C.c_int)),
                 ("blocks_per_stage", C.c_int), ("gemm_backend", C.c_int), ("input_is_activation", C.c_int),
-                ("block_kind", C.c_int), ("stage_blocks", C.POINTER(C.c_int))]
+                ("block_kind", C.c_int), ("stage_blocks", C.POINTER(C.c_int)), ("dropout", C.c_float),
+                ("dropout_seed", C.c_ulonglong), ("embed_scale", C.c_float)]
 
 
 class lp_head_spec(C.Structure):
@@ -152,6 +153,8 @@ def specs_from_config(cfg: dict, gemm_backend: int = 0):
         m.family = LP_FAMILY_LM
         m.vocab, m.seq_len, m.d_model = cfg["vocab"], cfg["seq_len"], cfg["d_model"]
         m.n_heads, m.d_ffn = cfg["n_heads"], cfg["d_ffn"]
+        m.dropout, m.dropout_seed = cfg.get("dropout", 0.0), cfg.get("dropout_seed", 0)
+        m.embed_scale = cfg.get("embed_scale", 0.0)
         a = _ints(cfg["blocks_per_chunk"])
         keep.append(a)
         m.blocks_per_chunk = a
@@ -427,8 +430,10 @@ class lp_linattn_desc(C.Structure):
 
 
 _LINATTN_TOKENS = ("q", "k", "v", "o", "dout", "dq", "dk", "dv")
-_LINATTN_FLOATS = ("log_decay", "state_in", "state_out", "dstate_out", "dstate_in", "lengths", "status")
-_LINATTN_KEYS = {*_LINATTN_TOKENS, *_LINATTN_FLOATS, "scale"}
+_LINATTN_FLOATS = (("log_decay", 0), ("state_in", 4096), ("state_out", 4096), ("dstate_out", 4096), ("dstate_in", 4096),
+                   ("lengths", 0), ("status", 0))   # elements per sequence and head of the states
+_LINATTN_KEYS = {*_LINATTN_TOKENS, *(n for n, _ in _LINATTN_FLOATS), "scale"}
+_NO_TOKENS = (0, 0, 0)
 _linattn_layout = struct.Struct("=24q7Q3if")      # lp_linattn_desc, filled in one go
 assert _linattn_layout.size == C.sizeof(lp_linattn_desc)
 _LINATTN_PACK = _linattn_layout.pack
@@ -448,29 +453,36 @@ def lp_linear_attention_bf16(form: int, desc: dict, workspace=None, stream=None)
     lengths int32 [batch]; `scale` a number (default 1).  Sizes come from q; the other tensors' shapes must agree."""
     if not desc.keys() <= _LINATTN_KEYS:
         raise LpError(-1, f"lp_linear_attention_bf16: unknown {sorted(desc.keys() - _LINATTN_KEYS)}")
-    get = desc.get
-    shape = desc["q"].shape
-    if len(shape) != 4 or shape[3] != 64:
-        raise LpError(-2, "lp_linear_attention_bf16: q must be [batch, seq_len, n_heads, 64]")
+    get, q = desc.get, desc["q"]
+    shape, bf16 = q.shape, q.dtype
+    if len(shape) != 4 or shape[3] != 64 or str(bf16) != "torch.bfloat16":
+        raise LpError(-2, "lp_linear_attention_bf16: q must be bf16 [batch, seq_len, n_heads, 64]")
     B, T, H, _ = shape
     v = []
     for name in _LINATTN_TOKENS:
         t = get(name)
         if t is None:
-            v += (0, 0, 0)
+            v += _NO_TOKENS
             continue
-        if t.shape != shape or t.element_size() != 2:
-            raise LpError(-2, f"lp_linear_attention_bf16: {name} must be bf16 [batch, seq_len, n_heads, 64], as q")
+        if t.shape != shape or t.dtype is not bf16:
+            raise LpError(-2, f"lp_linear_attention_bf16: {name} must be bf16 and of q's shape")
         sb, st, sh, se = t.stride()
         if se != 1 or (sh != 64 and H > 1):
             raise LpError(-3, f"lp_linear_attention_bf16: the heads of {name} must lie 64 elements apart")
-        v += (_dev(t), sb if B > 1 else 0, st)
-    for name in _LINATTN_FLOATS:
+        if not t.is_cuda:
+            raise LpError(-1, f"lp_linear_attention_bf16: {name} is in host memory")
+        v += (t.data_ptr(), sb if B > 1 else 0, st)
+    for name, per in _LINATTN_FLOATS:
         t = get(name)
-        if t is not None and (t.numel() != (H if name == "log_decay" else B if name == "lengths" else 1 if name == "status" else B * H * 4096) or
-                              t.element_size() != 4 or not t.is_contiguous()):
+        if t is None:
+            v.append(0)
+            continue
+        if t.numel() != (per * B * H if per else H if name == "log_decay" else B if name == "lengths" else 1) or \
+                t.element_size() != 4 or not t.is_contiguous():
             raise LpError(-2, f"lp_linear_attention_bf16: {name} has the wrong size or is not contiguous")
-        v.append(_dev(t) or 0)
+        if not t.is_cuda:
+            raise LpError(-1, f"lp_linear_attention_bf16: {name} is in host memory")
+        v.append(t.data_ptr())
     nbytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     code = _lib.lp_linear_attention_bf16(form, _LINATTN_PACK(*v, B, T, H, get("scale", 1.0)), _dev(workspace) if nbytes else None, nbytes,
                                          stream)

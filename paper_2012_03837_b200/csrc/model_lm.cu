@@ -17,6 +17,7 @@ namespace {
 
 struct BlockBufs {
   std::string name;
+  int index;                   // of the block in the model
   const void* hin = nullptr;   // set per plan
   void *a1, *qkv, *o, *h1, *a2, *u, *g;
   void* hout_internal;         // output when this is not the chunk's last block
@@ -29,6 +30,7 @@ struct ChunkBufs {
   float *meanh, *rstdh, *row_loss;
   float2* zstats = nullptr;    // per-row softmax statistics of the logits' column groups (training, tensor-core path)
   void *G0, *G1, *G2, *Gf, *Gq;   // gradient scratch: [M,d] x3, [M,ffn], [M,3d]
+  void* Gd = nullptr;             // with dropout: the gradient of a dropped branch, [M,d]
 };
 
 std::string hn(int k, const char* s) { return "c" + std::to_string(k) + ".head." + s; }
@@ -52,6 +54,7 @@ void build_lm(Handle& h) {
     for (int j = 0; j < h.per_chunk[k]; ++j, ++blk) {
       BlockBufs bb;
       bb.name = "c" + std::to_string(k) + ".b" + std::to_string(blk);
+      bb.index = blk;
       const std::string& n = bb.name;
       h.add_tensor(n + ".ln1.g", k, {d}, false);
       h.add_tensor(n + ".ln1.b", k, {d}, false);
@@ -104,6 +107,7 @@ void build_lm(Handle& h) {
     c.meanh = fal(M); c.rstdh = fal(M); c.row_loss = fal(M);
     c.G0 = h.dalloc(md); c.G1 = h.dalloc(md); c.G2 = h.dalloc(md);
     c.Gf = h.dalloc((size_t)M * F * es); c.Gq = h.dalloc(3 * md);
+    if (h.spec.dropout > 0.f) c.Gd = h.dalloc(md);
   }
 
   std::vector<int> all;
@@ -134,12 +138,34 @@ void build_lm(Handle& h) {
     return (!pipelined || k == 0) ? h.y_in : h.lab[rd][k - 1];
   };
 
+  // Dropout of [M, d] tensors (training passes only): y = resid + dropped x, a launch per chunk.  The mask follows from
+  // the site and the step's number alone, so the backward pass forms it again.
+  struct DropItem { const void* x; const void* resid; void* y; int site; };
+  const float drop_p = h.spec.dropout;
+  const unsigned long long drop_seed = h.spec.dropout_seed;
+  const float tok_scale = h.spec.embed_scale == 0.f ? 1.f : h.spec.embed_scale;
+  auto emit_dropout = [&](Plan& p, const std::vector<DropItem>& items) {
+    if (items.empty()) return;
+    std::vector<DropoutArgs> args;
+    double bytes = 0;
+    for (auto& it : items) {
+      args.push_back(DropoutArgs{it.x, it.resid, it.y, (long long)M * d, dropout_threshold((double)drop_p), (float)(1.0 / (1.0 - (double)drop_p)),
+                                 drop_seed, 0, nullptr, (uint32_t)it.site, 0});
+      bytes += (it.resid ? 3.0 : 2.0) * md;
+    }
+    p.add((int)args.size(), [args, bf](const RunCtx& c) {
+      for (DropoutArgs a : args) { a.w3 = c.step; launch_dropout(a, bf, c.stream); }
+    }, KIND_OTHER, bytes);
+  };
+
   // ---- forward of the trunks of chunks `ks`
-  auto forward = [&](Plan& p, const std::vector<int>& ks, int rd, int wr) {
+  auto forward = [&](Plan& p, const std::vector<int>& ks, int rd, int wr, bool train) {
+    const bool drop = train && drop_p > 0.f;
     for (int k : ks)
       if (k == 0 && !inner) {
-        EmbedProb e{(const int*)h.x_in, h.W("c0.tok"), h.W("c0.pos"), cb[0].emb, M, T, d, V, 1.f};
+        EmbedProb e{(const int*)h.x_in, h.W("c0.tok"), h.W("c0.pos"), cb[0].emb, M, T, d, V, tok_scale};
         p.add(1, [e, st, bf](const RunCtx& c) { launch_embed_fwd(e, st, bf, c.stream); }, KIND_EMBED, 3.0 * M * d * es);
+        if (drop) emit_dropout(p, {DropItem{cb[0].emb, nullptr, cb[0].emb, 0}});
       }
     size_t maxb = 0;
     for (int k : ks) maxb = std::max(maxb, cb[k].blocks.size());
@@ -159,16 +185,19 @@ void build_lm(Handle& h) {
       emit_gemm(h, p, g);
       emit_attention(h, p, at, false);
       g.clear(); ln.clear();
+      std::vector<DropItem> di;                  // with dropout a branch leaves its product alone and joins the stream here
       for (int k : act) {
         BlockBufs& b = cb[k].blocks[j];
         GemmProb q = gemm_fwd(b.o, h.W(b.name + ".Wo"), b.h1, M, d, d, h.P32(b.name + ".bo"), EPI_NONE);
-        q.resid = block_in(k, j, rd);
+        if (drop) di.push_back(DropItem{b.h1, block_in(k, j, rd), b.h1, 1 + 2 * b.index});
+        else q.resid = block_in(k, j, rd);
         g.push_back(q);
         ln.push_back(LnProb{b.h1, b.a2, h.P32(b.name + ".ln2.g"), h.P32(b.name + ".ln2.b"), b.mean2, b.rstd2, M, d});
       }
       emit_gemm(h, p, g);
+      emit_dropout(p, di);
       emit_ln_fwd(h, p, ln);
-      g.clear();
+      g.clear(); di.clear();
       for (int k : act) {
         BlockBufs& b = cb[k].blocks[j];
         GemmProb q = gemm_fwd(b.a2, h.W(b.name + ".W1"), b.g, M, F, d, h.P32(b.name + ".b1"), EPI_GELU);
@@ -181,10 +210,12 @@ void build_lm(Handle& h) {
       for (int k : act) {
         BlockBufs& b = cb[k].blocks[j];
         GemmProb q = gemm_fwd(b.g, h.W(b.name + ".W2"), block_out(k, j, wr), M, d, F, h.P32(b.name + ".b2"), EPI_NONE);
-        q.resid = b.h1;
+        if (drop) di.push_back(DropItem{block_out(k, j, wr), b.h1, block_out(k, j, wr), 2 + 2 * b.index});
+        else q.resid = b.h1;
         g.push_back(q);
       }
       emit_gemm(h, p, g);
+      emit_dropout(p, di);
     }
   };
 
@@ -252,13 +283,18 @@ void build_lm(Handle& h) {
     std::vector<GemmProb> g;
     std::vector<ColSumProb> cs;
     std::vector<float*> outs;
-    // 1. feed-forward second matrix: dW2, db2, du = (dout W2) * gelu'(u)
+    // 1. feed-forward second matrix: dW2, db2, du = (dout W2) * gelu'(u); with dropout dout is dropped on its way there
+    const bool drop = drop_p > 0.f;
+    std::vector<DropItem> di;
+    for (auto& it : items) if (drop) di.push_back(DropItem{it.c->G0, nullptr, it.c->Gd, 2 + 2 * it.b->index});
+    emit_dropout(p, di);
     for (auto& it : items) {
       ChunkBufs& c = *it.c; BlockBufs& b = *it.b;
-      g.push_back(gemm_wgrad(c.G0, b.g, GR(it, b.name + ".W2"), M, d, F));
-      g.push_back(gemm_dgrad(c.G0, h.W(b.name + ".W2"), c.Gf, M, d, F, EPI_GELU_GRAD, b.u));
+      const void* dr = drop ? c.Gd : c.G0;
+      g.push_back(gemm_wgrad(dr, b.g, GR(it, b.name + ".W2"), M, d, F));
+      g.push_back(gemm_dgrad(dr, h.W(b.name + ".W2"), c.Gf, M, d, F, EPI_GELU_GRAD, b.u));
       g.back().aux_blocked = u_blocked ? 1 : 0;
-      cs.push_back(ColSumProb{c.G0, nullptr, M, d, d});
+      cs.push_back(ColSumProb{dr, nullptr, M, d, d});
       outs.push_back(GR(it, b.name + ".b2"));
     }
     emit_gemm(h, p, g); emit_colsum(h, p, cs, outs);
@@ -286,11 +322,15 @@ void build_lm(Handle& h) {
       emit_ln_bwd(h, p, lb, dgs, dbs);
     }
     // 4. attention output projection: dWo, dbo, do -> G1
+    di.clear();
+    for (auto& it : items) if (drop) di.push_back(DropItem{it.c->G2, nullptr, it.c->Gd, 1 + 2 * it.b->index});
+    emit_dropout(p, di);
     for (auto& it : items) {
       ChunkBufs& c = *it.c; BlockBufs& b = *it.b;
-      g.push_back(gemm_wgrad(c.G2, b.o, GR(it, b.name + ".Wo"), M, d, d));
-      g.push_back(gemm_dgrad(c.G2, h.W(b.name + ".Wo"), c.G1, M, d, d, EPI_NONE, nullptr));
-      cs.push_back(ColSumProb{c.G2, nullptr, M, d, d});
+      const void* dr = drop ? c.Gd : c.G2;
+      g.push_back(gemm_wgrad(dr, b.o, GR(it, b.name + ".Wo"), M, d, d));
+      g.push_back(gemm_dgrad(dr, h.W(b.name + ".Wo"), c.G1, M, d, d, EPI_NONE, nullptr));
+      cs.push_back(ColSumProb{dr, nullptr, M, d, d});
       outs.push_back(GR(it, b.name + ".bo"));
     }
     emit_gemm(h, p, g); emit_colsum(h, p, cs, outs);
@@ -338,8 +378,8 @@ void build_lm(Handle& h) {
       lps.push_back(LabelProb{labels_of(k, pipelined, rd), (pipelined && k < K - 1) ? h.lab[wr][k] : nullptr, M, V,
                               h.n_valid[k]});
     emit_labels(h, p, lps);
-    if (pipelined) forward(p, all, rd, wr);
-    else for (int k = 0; k < K; ++k) forward(p, {k}, rd, wr);
+    if (pipelined) forward(p, all, rd, wr, true);
+    else for (int k = 0; k < K; ++k) forward(p, {k}, rd, wr, true);
     heads_forward(p, wr, pipelined, rd, false, true);
 
     // ---- head backward -> gradient at the trunk output in G0
@@ -386,7 +426,8 @@ void build_lm(Handle& h) {
       // chunk 0, first block: embedding tables
       for (auto& it : items)
         if (!inner && it.c == &cb[0] && it.b == &cb[0].blocks[0]) {
-          EmbedBwdProb e{(const int*)h.x_in, cb[0].G0, h.G("c0.tok"), h.G("c0.pos"), M, T, d, V, 1.f, nullptr, nullptr, nullptr, nullptr};
+          EmbedBwdProb e{(const int*)h.x_in, cb[0].G0, h.G("c0.tok"), h.G("c0.pos"), M, T, d, V, tok_scale, nullptr, nullptr, nullptr, nullptr};
+          if (drop_p > 0.f) emit_dropout(p, {DropItem{cb[0].G0, nullptr, cb[0].G0, 0}});
           p.add(3, [e, emb_ws, bf](const RunCtx& c) { launch_embed_bwd(e, emb_ws, nullptr, bf, c.stream); }, KIND_EMBED, (double)M * d * es + 4.0 * V * d);
         }
     }
@@ -426,7 +467,7 @@ void build_lm(Handle& h) {
   };
 
   auto build_forward = [&](Plan& p, int wr, bool heads) {
-    for (int k = 0; k < K; ++k) forward(p, {k}, wr, wr);
+    for (int k = 0; k < K; ++k) forward(p, {k}, wr, wr, !heads);   // without heads: the priming pass of a training step
     if (!heads) return;
     std::vector<LabelProb> lps;
     for (int k = 0; k < K; ++k) lps.push_back(LabelProb{h.y_in, nullptr, M, V, h.n_valid[k]});

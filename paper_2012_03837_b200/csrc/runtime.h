@@ -34,6 +34,7 @@ struct RunCtx {
   int* out_correct = nullptr;            // lp_evaluate only: per-chunk count of correct predictions
   const void* x = nullptr;               // training step: where the caller holds the step's inputs (device), when the
   const int* y = nullptr;                // step may read them in place; null: the handle's own input buffers
+  uint32_t step = 0;                     // training steps before this one: the last counter word of dropout masks
 };
 
 struct PlanOp {

@@ -158,3 +158,48 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         with pytest.raises(lp.LpError) as e:
             lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, dict(q=t, k=bad, v=t, o=t, scale=1.0))
         assert e.value.code in (ERR["SHAPE"], ERR["INVALID_ARG"])
+
+
+# ---- the training step with dropout: the oracle's gradients against differences, and its refusals
+def test_oracle_gradients_with_dropout_match_differences():
+    import lp_synth
+    from oracle.local_step import LocalUpdateOracle
+    cfg = lp_synth.config("c3", batch=2, seq_len=5, vocab=11, d_model=8, n_heads=2, d_ffn=12, blocks_per_chunk=[1, 2], dropout=0.4,
+                          dropout_seed=77, embed_scale=2.5)
+    g = np.random.default_rng(9)
+    params = {n: a.astype(np.float64) + 0.3 * g.standard_normal(a.shape) for n, a in lp_synth.init_params(dict(cfg, dtype="fp32")).items()}
+    x, y = lp_synth.minibatch(cfg, 0)
+    orc = LocalUpdateOracle(cfg, params, dtype=np.float64)
+    orc.drop_step = 3
+    inp = x
+    dropped = 0
+    for k in range(2):
+        loss, h, grads = orc.local_grads(k, inp, y)
+        for n in orc.names_of_chunk[k]:
+            flat = orc.p[n].reshape(-1)
+            for idx in g.choice(flat.size, size=min(4, flat.size), replace=False):
+                old, eps = flat[idx], 1e-6
+                flat[idx] = old + eps
+                up = orc.local_grads(k, inp, y)[0]
+                flat[idx] = old - eps
+                dn = orc.local_grads(k, inp, y)[0]
+                flat[idx] = old
+                num = (up - dn) / (2 * eps)
+                assert abs(num - grads[n].reshape(-1)[idx]) <= 1e-5 * max(1.0, abs(num)), (n, idx)
+        dropped += sum(int((f == 0).sum()) for b in orc._last_cache["blocks"] for f in b[-2:])
+        inp = h
+    assert dropped > 0
+    a = orc.local_grads(0, x, y)[0]
+    orc.drop_step = 4
+    assert orc.local_grads(0, x, y)[0] != a                     # another step, another mask
+    orc.drop_step = None
+    assert LocalUpdateOracle(dict(cfg, dropout=0.0), params, dtype=np.float64).local_grads(0, x, y)[0] == orc.local_grads(0, x, y)[0]
+
+
+def test_create_refuses_bad_dropout():
+    import lp_synth
+    for kw in (dict(dropout=1.0), dict(dropout=-0.1), dict(dropout=float("nan")), dict(embed_scale=float("inf"))):
+        m, K, hd, op = lp.specs_from_config(lp_synth.config("c3", **kw))
+        with pytest.raises(lp.LpError) as e:
+            lp.lp_create(m, K, hd, op)
+        assert lp.LP_ERR[e.value.code] == "INVALID_ARG", kw
