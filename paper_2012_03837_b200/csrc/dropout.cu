@@ -15,33 +15,46 @@
 namespace lp {
 namespace {
 
-__device__ __forceinline__ uint4 philox10(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1) {
+// The arguments and the ten rounds' keys, formed on the host: as kernel parameters they are operands of the rounds' own
+// instructions.
+struct Args : DropoutArgs {
+  uint32_t k0[10], k1[10];
+  explicit Args(const DropoutArgs& a) : DropoutArgs(a) {
+    for (uint32_t r = 0; r < 10; ++r) {
+      k0[r] = (uint32_t)seed + r * 0x9E3779B9u;
+      k1[r] = (uint32_t)(seed >> 32) + r * 0xBB67AE85u;
+    }
+  }
+};
+
+__device__ __forceinline__ uint4 words(const Args& a, unsigned long long first, long long group) {
+  const unsigned long long c = first + (unsigned long long)group;
+  uint32_t c0 = (uint32_t)c, c1 = (uint32_t)(c >> 32), c2 = a.w2, c3 = a.w3;
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
-    const unsigned long long a = (unsigned long long)c0 * 0xD2511F53u, b = (unsigned long long)c2 * 0xCD9E8D57u;
-    c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
-    c1 = (uint32_t)b;
-    c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
-    c3 = (uint32_t)a;
-    k0 += 0x9E3779B9u;
-    k1 += 0xBB67AE85u;
+    const unsigned long long x = (unsigned long long)c0 * 0xD2511F53u, y = (unsigned long long)c2 * 0xCD9E8D57u;
+    c0 = (uint32_t)(y >> 32) ^ c1 ^ a.k0[r];
+    c1 = (uint32_t)y;
+    c2 = (uint32_t)(x >> 32) ^ c3 ^ a.k1[r];
+    c3 = (uint32_t)x;
   }
   return make_uint4(c0, c1, c2, c3);
 }
 
-__device__ __forceinline__ uint4 words(const DropoutArgs& a, unsigned long long first, long long group) {
-  const unsigned long long c = first + (unsigned long long)group;
-  return philox10((uint32_t)c, (uint32_t)(c >> 32), a.w2, a.w3, (uint32_t)a.seed, (uint32_t)(a.seed >> 32));
+__device__ __forceinline__ float drop(const Args& a, uint32_t w, float x, float r) {
+  return w >= a.threshold ? fmaf(x, a.scale, r) : r;
 }
 
-__device__ __forceinline__ float drop(const DropoutArgs& a, uint32_t w, float x, float r) {
-  return w >= a.threshold ? fmaf(x, a.scale, r) : r;
+// x = x * s + a, y = y * s + b in one instruction.
+__device__ __forceinline__ void scale_add(float& x, float& y, float s, float a, float b) {
+  asm("{\n\t.reg .b64 u, v, m;\n\tmov.b64 u, {%0, %1};\n\tmov.b64 m, {%2, %2};\n\tmov.b64 v, {%3, %4};\n\tfma.rn.f32x2 u, u, m, v;\n\tmov.b64 {%0, %1}, u;\n\t}"
+      : "+f"(x), "+f"(y) : "f"(s), "f"(a), "f"(b));
 }
 
 // 16 bytes per thread and load, U of them in flight (with the residual's); the generator's arithmetic fills the wait.
 // A block covers U * 256 consecutive vectors; the elements behind the last whole vector go one by one.
 template <typename T, bool RESID, int U>
-__global__ void __launch_bounds__(256) dropout_vec_kernel(DropoutArgs a) {
+__global__ void __launch_bounds__(256) dropout_vec_kernel(const __grid_constant__ Args a) {
   constexpr int VEC = 16 / sizeof(T);
   const long long vecs = a.n / VEC, v0 = (long long)blockIdx.x * (256 * U) + threadIdx.x;
   const unsigned long long first = a.offset + (a.offset_dev ? *a.offset_dev : 0ull);
@@ -69,10 +82,11 @@ __global__ void __launch_bounds__(256) dropout_vec_kernel(DropoutArgs a) {
           ys[e] = __float_as_uint(drop(a, ww[e], __uint_as_float(xs[e]), RESID ? __uint_as_float(rs[e]) : 0.f));
       } else {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t xx = xs[2 * k + e], rr = RESID ? rs[2 * k + e] : 0u;
-          const float lo = drop(a, ww[2 * e], __uint_as_float(xx << 16), __uint_as_float(rr << 16));
-          const float hi = drop(a, ww[2 * e + 1], __uint_as_float(xx & 0xffff0000u), __uint_as_float(rr & 0xffff0000u));
+        for (int e = 0; e < 2; ++e) {            // dropped elements are cleared in the packed pair
+          const uint32_t keep = (ww[2 * e] >= a.threshold ? 0xffffu : 0u) | (ww[2 * e + 1] >= a.threshold ? 0xffff0000u : 0u);
+          const uint32_t xx = xs[2 * k + e] & keep, rr = RESID ? rs[2 * k + e] : 0u;
+          float lo = __uint_as_float(xx << 16), hi = __uint_as_float(xx & 0xffff0000u);
+          scale_add(lo, hi, a.scale, __uint_as_float(rr << 16), __uint_as_float(rr & 0xffff0000u));
           __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
           ys[2 * k + e] = *(uint32_t*)&b;
         }
@@ -90,7 +104,7 @@ __global__ void __launch_bounds__(256) dropout_vec_kernel(DropoutArgs a) {
 
 // One thread per group of four elements; any alignment.
 template <typename T>
-__global__ void __launch_bounds__(256) dropout_kernel(DropoutArgs a) {
+__global__ void __launch_bounds__(256) dropout_kernel(const __grid_constant__ Args a) {
   const long long groups = (a.n + 3) / 4;
   const unsigned long long first = a.offset + (a.offset_dev ? *a.offset_dev : 0ull);
   for (long long g = (long long)blockIdx.x * blockDim.x + threadIdx.x; g < groups; g += (long long)gridDim.x * blockDim.x) {
@@ -108,7 +122,7 @@ __global__ void __launch_bounds__(256) dropout_kernel(DropoutArgs a) {
 }
 
 template <typename T>
-cudaError_t run_vec(const DropoutArgs& a, cudaStream_t s) {
+cudaError_t run_vec(const Args& a, cudaStream_t s) {
   const long long vecs = a.n / (16 / (int)sizeof(T));
   const bool many = vecs >= 148LL * 8 * 256 * 2;   // more than two waves of single loads: four in flight per thread
   const unsigned blocks = (unsigned)std::max<long long>(1, many ? (vecs + 1023) / 1024 : (vecs + 255) / 256);
@@ -118,7 +132,8 @@ cudaError_t run_vec(const DropoutArgs& a, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t launch_dropout(const DropoutArgs& a, bool is_bf16, cudaStream_t s) {
+cudaError_t launch_dropout(const DropoutArgs& in, bool is_bf16, cudaStream_t s) {
+  const Args a(in);
   if (a.n <= 0) return cudaSuccess;
   if ((((uintptr_t)a.x | (uintptr_t)a.resid | (uintptr_t)a.y) & 15) == 0) return is_bf16 ? run_vec<bf16>(a, s) : run_vec<float>(a, s);
   const long long groups = (a.n + 3) / 4;

@@ -180,7 +180,10 @@ __global__ void __launch_bounds__(SORT_WARPS * 32, 1) embed_sort_kernel(EmbedBwd
   int* list = total + local + w * SORT_LIST;     // [SORT_LIST] rows
   __shared__ int less_sum, carry_of[SORT_WARPS];
   for (int i = tid; i < SORT_WARPS * pitch; i += blockDim.x) cnt[i] = 0;
-  if (tid == 0) less_sum = 0;
+  if (tid == 0) {
+    less_sum = 0;
+    if (j == 0) *p.n_long = 0;
+  }
   __syncthreads();
   const int stretch = ((p.rows + SORT_WARPS * 32 - 1) / (SORT_WARPS * 32)) * 32;
   const long long lo = (long long)w * stretch;
@@ -302,6 +305,7 @@ __global__ void __launch_bounds__(SUM_THREADS) embed_sum_kernel(EmbedBwdProb p, 
     for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
     auto flush = [&]() {
       if (cur & HEAVY) {
+        if (first && lane == 0 && blockIdx.y == 0) p.long_list[atomicAdd(p.n_long, 1)] = make_int2((int)ch, (int)(cur & ~HEAVY));
         store_vec(p.part + (size_t)(2 * ch + (first ? 1 : 0)) * p.d + c, acc);
       } else {
 #pragma unroll
@@ -385,36 +389,22 @@ __device__ __forceinline__ void add_pieces(const float* base, long long first, l
     }
   }
 }
-// A block looks at COMBINE stretches for long tokens that start there, or takes one position with several pieces.
-constexpr int COMBINE = 8;
-__global__ void __launch_bounds__(COMBINE_WARPS * 32) embed_combine_kernel(EmbedBwdProb p, int P, int chunks, int pos_pieces) {
+// The long tokens of the list, then the positions with several pieces, dealt out to the blocks.
+__global__ void __launch_bounds__(COMBINE_WARPS * 32) embed_combine_kernel(EmbedBwdProb p, int P, int positions, int pos_pieces) {
   __shared__ float red[COMBINE_WARPS][128];
-  __shared__ int2 found[COMBINE];                // token and number of rows
-  const int blocks = (chunks + COMBINE - 1) / COMBINE;
   cudaGridDependencySynchronize();
-  if ((int)blockIdx.x < blocks) {
-    if (threadIdx.x < COMBINE) {
-      const long long c = (long long)blockIdx.x * COMBINE + threadIdx.x;
-      int2 f = make_int2(0, 0);
-      if (c < chunks) {
-        const uint32_t e = (uint32_t)p.sorted[(int)min((c + 1) * P, (long long)p.rows) - 1].y;
-        if (e & HEAVY) {
-          const int2 sg = p.seg[e & ~HEAVY];
-          if (sg.x >= c * P) f = make_int2((int)(e & ~HEAVY), sg.y);   // else it started in an earlier stretch
-        }
-      }
-      found[threadIdx.x] = f;
+  const int n_long = *p.n_long;
+  for (int i = blockIdx.x; i < n_long + positions; i += gridDim.x) {
+    if (i < n_long) {
+      const int2 e = p.long_list[i];             // stretch of the first piece, token
+      const int rows = p.seg[e.y].y;
+      add_pieces(p.part + (size_t)(2 * (long long)e.x) * p.d, p.d, 2LL * PIECES * p.d, (rows + PIECES * P - 1) / (PIECES * P), p.d,
+                 p.dtok + (size_t)e.y * p.d, p.scale, red);
+    } else {
+      const int t = i - n_long;
+      const long long per = (long long)POS_PIECE * p.T;
+      add_pieces(p.pos_part + (size_t)t * pos_pieces * p.d, 0, p.d, (int)(((long long)p.rows - t + per - 1) / per), p.d, p.dpos + (size_t)t * p.d, 1.f, red);
     }
-    __syncthreads();
-    for (int i = 0; i < COMBINE; ++i) {
-      const int2 f = found[i];
-      const long long c = (long long)blockIdx.x * COMBINE + i;
-      if (f.y) add_pieces(p.part + (size_t)(2 * c) * p.d, p.d, 2LL * PIECES * p.d, (f.y + PIECES * P - 1) / (PIECES * P), p.d, p.dtok + (size_t)f.x * p.d, p.scale, red);
-    }
-  } else {
-    const int t = (int)blockIdx.x - blocks;
-    const long long per = (long long)POS_PIECE * p.T;
-    add_pieces(p.pos_part + (size_t)t * pos_pieces * p.d, 0, p.d, (int)(((long long)p.rows - t + per - 1) / per), p.d, p.dpos + (size_t)t * p.d, 1.f, red);
   }
 }
 
@@ -477,13 +467,14 @@ cudaError_t launch_embed_fwd(const EmbedProb& p, int* d_status, bool is_bf16, cu
                   : launch_kernel(embed_fwd_kernel<float, 1>, grid, 128, 0, s, p, ll, d_status);
 }
 
-// Workspace: sorted rows, token segments, pieces of long tokens, pieces of the position sums.  Pieces of positions are
+// Workspace: sorted rows, token segments, pieces of long tokens, pieces of the position sums, the list of long
+// tokens.  Pieces of positions are
 // stored only if a position has more than POS_PIECE rows; then T < rows / POS_PIECE and T * pieces(T) < 3 rows / POS_PIECE.
 size_t embed_bwd_workspace(int rows, int vocab, int d) {
   const size_t chunks = ((size_t)rows + piece_rows(rows) - 1) / piece_rows(rows);
   const size_t pos_rows = 3 * ((size_t)rows / POS_PIECE) + 3;
   return up256((size_t)rows * sizeof(int2)) + up256((size_t)vocab * sizeof(int2)) + up256(2 * chunks * d * sizeof(float)) +
-         up256(pos_rows * d * sizeof(float));
+         up256(pos_rows * d * sizeof(float)) + 256 + up256(chunks * sizeof(int2));
 }
 
 cudaError_t launch_embed_bwd(EmbedBwdProb p, void* workspace, int* d_status, bool is_bf16, cudaStream_t s) {
@@ -493,16 +484,19 @@ cudaError_t launch_embed_bwd(EmbedBwdProb p, void* workspace, int* d_status, boo
   p.seg = (int2*)w;     w += up256((size_t)p.vocab * sizeof(int2));
   p.part = (float*)w;   w += up256(2 * (size_t)chunks * p.d * sizeof(float));
   p.pos_part = (float*)w;
+  w = (char*)workspace + embed_bwd_workspace(p.rows, p.vocab, p.d) - up256((size_t)chunks * sizeof(int2)) - 256;
+  p.n_long = (int*)w;   w += 256;
+  p.long_list = (int2*)w;
   const int full = is_bf16 ? 8 : 4;
   const bool vec = p.d % full == 0 && aligned16(p.dh, p.dtok, p.dpos);
   cudaError_t e;
   if (is_bf16) e = vec ? run_sort_and_sum<bf16, 8>(p, P, chunks, pos_pieces, d_status, s) : run_sort_and_sum<bf16, 1>(p, P, chunks, pos_pieces, d_status, s);
   else e = vec ? run_sort_and_sum<float, 4>(p, P, chunks, pos_pieces, d_status, s) : run_sort_and_sum<float, 1>(p, P, chunks, pos_pieces, d_status, s);
   if (e != cudaSuccess) return e;
-  const int long_chunks = p.rows > PIECES * P ? chunks : 0, long_pos = pos_pieces > 1 ? p.T : 0;
-  if (long_chunks + long_pos == 0) return cudaSuccess;
-  return launch_after(embed_combine_kernel, dim3((unsigned)((long_chunks + COMBINE - 1) / COMBINE + long_pos), (unsigned)((p.d + COMBINE_COLS - 1) / COMBINE_COLS)), COMBINE_WARPS * 32, 0, s, p, P,
-                       long_chunks, pos_pieces);
+  const int most_long = p.rows / (PIECES * P + 1), positions = pos_pieces > 1 ? p.T : 0;
+  if (most_long + positions == 0) return cudaSuccess;
+  return launch_after(embed_combine_kernel, dim3((unsigned)std::min(most_long + positions, 148), (unsigned)((p.d + COMBINE_COLS - 1) / COMBINE_COLS)),
+                      COMBINE_WARPS * 32, 0, s, p, P, positions, pos_pieces);
 }
 
 }  // namespace lp

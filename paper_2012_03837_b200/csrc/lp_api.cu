@@ -832,7 +832,7 @@ lp_status lp_embed_backward(int dtype, const int* ids, const void* dout, float* 
     return fail(nullptr, LP_ERR_UNSUPPORTED, "lp_embed_backward: pointers must be aligned to their element, the workspace to 256 bytes");
   lp_status st = check_output(me, dtable);
   if (st != LP_OK) return st;
-  const EmbedBwdProb p{ids, dout, dtable, dpos, rows, dpos ? seq_len : 0, d, vocab, scale, nullptr, nullptr, nullptr, nullptr};
+  const EmbedBwdProb p{ids, dout, dtable, dpos, rows, dpos ? seq_len : 0, d, vocab, scale, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
   return launched(me, launch_embed_bwd(p, workspace, out_of_range, dtype == LP_BF16, (cudaStream_t)stream));
 }
 

@@ -155,11 +155,11 @@ void launch_loss_reduce(const LossProb* d_probs, int n, float* d_losses, int* d_
 // ---------------------------------------------------------------------------- LM-specific
 struct EmbedProb { const int* ids; const void* tok; const void* pos; void* h; int rows, T, d, vocab; float scale; };
 cudaError_t launch_embed_fwd(const EmbedProb& p, int* d_status, bool is_bf16, cudaStream_t s);
-// Gradients of both tables (pos: T = 0 and dpos null if there is none); the last four pointers are set by the launcher,
+// Gradients of both tables (pos: T = 0 and dpos null if there is none); the last six pointers are set by the launcher,
 // inside a workspace of embed_bwd_workspace() bytes, 256-byte aligned.
 struct EmbedBwdProb {
   const int* ids; const void* dh; float* dtok; float* dpos; int rows, T, d, vocab; float scale;
-  int2* sorted; int2* seg; float* part; float* pos_part;
+  int2* sorted; int2* seg; float* part; float* pos_part; int* n_long; int2* long_list;
 };
 size_t embed_bwd_workspace(int rows, int vocab, int d);
 cudaError_t launch_embed_bwd(EmbedBwdProb p, void* workspace, int* d_status, bool is_bf16, cudaStream_t s);
