@@ -388,7 +388,7 @@ __device__ __forceinline__ void scan(int len, const Run A, const Run B, const Ru
     uint32_t bb = buf + TILE_B + cols, bc = buf + 2 * TILE_B + rows;
     const float* wp = sc + 16 * w + g - 2 * t;   // ages of the pair (row g of this warp, column 2t of a step): rows lie 8 apart
     const float* wj = (rev ? sc + n : pw + n - 1) - 2 * t;               // weights of the tokens in the state
-#pragma unroll 1
+#pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
       uint32_t cf[4][4], bt[4];
       ldsm_t(bt, bb + w * 32);

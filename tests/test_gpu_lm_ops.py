@@ -363,3 +363,130 @@ def test_host_memory_is_refused():
         lp.lp_dropout(lp.LP_FP32, x, None, host.ctypes.data, 64, 0.1, 1)
     assert e.value.code == -1
     torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------------------------------------------ sizes beyond 32 bits
+def test_dropout_beyond_two_to_the_31_elements():
+    n, p, seed, tail = 2 ** 31 + 19, 0.25, 7, 4096
+    x = torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    lp.lp_dropout(lp.LP_BF16, x, None, x, n, p, seed, 3)
+    first = (n - tail) // 4 * 4                      # a whole counter
+    keep = O.dropout_keep(n - first, p, seed, 3 + first // 4)
+    assert np.array_equal(np64(x[first:]) != 0, keep)
+    assert np.array_equal(np64(x[:tail]) != 0, O.dropout_keep(tail, p, seed, 3))
+
+
+def test_embedding_tables_beyond_two_to_the_31_elements():
+    V, d, rows = 2 ** 22 + 5, 520, 40                # 2.2e9 elements
+    table = torch.empty(V, d, dtype=torch.bfloat16, device="cuda")
+    g = np.random.default_rng(0)
+    ids = np.concatenate([[0, V - 1, V - 1, 5, V - 2], g.integers(V - 1000, V, rows - 5)]).astype(np.int32)
+    t_ids = cu(ids, torch.int32)
+    used = torch.unique(t_ids).long()
+    table[used] = torch.randn(len(used), d, device="cuda").to(torch.bfloat16)
+    out = torch.empty(rows, d, dtype=torch.bfloat16, device="cuda")
+    lp.lp_embed_forward(lp.LP_BF16, t_ids, table, None, out, rows, V, d, 0, 1.0)
+    assert torch.equal(out, table[t_ids.long()])
+    del table
+    dtab = torch.full((V, d), float("nan"), device="cuda")
+    ws = torch.empty(lp.lp_embed_workspace_bytes(rows, V, d), dtype=torch.uint8, device="cuda")
+    lp.lp_embed_backward(lp.LP_BF16, t_ids, out, dtab, None, rows, V, d, 0, 1.0, None, ws, ws.numel())
+    want = torch.zeros(len(used), d, device="cuda", dtype=torch.float64)
+    want.index_add_(0, torch.searchsorted(used, t_ids.long()), out.double())
+    assert ((dtab[used].double() - want).abs() <= 1e-6 * want.abs() + 1e-6).all()
+    assert not torch.isnan(dtab).any() and int((dtab != 0).any(dim=1).sum()) == len(used)
+
+
+def test_linear_attention_strides_beyond_two_to_the_31_elements():
+    T, H, ts = 100, 1, 2 ** 25                       # the last token lies 3.3e9 elements behind the first
+    t = la_inputs(1, T, H, 21)
+    big = torch.empty(T * ts, dtype=torch.bfloat16, device="cuda").view(1, T, ts)
+    far = {}
+    for i, n in enumerate(("q", "k", "v", "dout", "o", "dq", "dk", "dv")):
+        far[n] = big[:, :, 64 * i:64 * i + 64].view(1, T, 1, 64)
+        if n in t:
+            far[n].copy_(t[n])
+    near = {n: torch.empty(1, T, H, 64, dtype=torch.bfloat16, device="cuda") for n in ("o", "dq", "dk", "dv")}
+    for src, outs in ((far, far), (t, near)):
+        base = dict(q=src["q"], k=src["k"], v=src["v"], log_decay=t["log_decay"], scale=0.125)
+        lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, dict(base, o=outs["o"]), la_workspace(0, 1, T, H))
+        lp.lp_linear_attention_bf16(lp.LP_LINATTN_BACKWARD, dict(base, dout=src["dout"], dq=outs["dq"], dk=outs["dk"], dv=outs["dv"]),
+                                    la_workspace(1, 1, T, H))
+    for n in near:
+        assert torch.equal(far[n], near[n]), n
+
+
+# ------------------------------------------------------------------------------------------------ two calls at once, layouts
+def test_two_streams_with_workspaces_of_their_own():
+    B, T, H, rows, V, d = 1, 3000, 2, 9000, 700, 136
+    t = la_inputs(B, T, H, 30)
+    ids = torch.randint(0, V, (rows,), device="cuda", dtype=torch.int32)
+    dh = torch.randn(rows, d, device="cuda").to(torch.bfloat16)
+    res = []
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for s in streams:
+        o, st = torch.zeros(B, T, H, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(B, H, 64, 64, device="cuda")
+        dtab = torch.zeros(V, d, device="cuda")
+        res.append((o, st, dtab, la_workspace(0, B, T, H), torch.empty(lp.lp_embed_workspace_bytes(rows, V, d), dtype=torch.uint8, device="cuda")))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, (o, st, dtab, w1, w2) in zip(streams, res):
+            lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, dict(q=t["q"], k=t["k"], v=t["v"], o=o, state_out=st, log_decay=t["log_decay"],
+                                        scale=0.125), w1, s.cuda_stream)
+            lp.lp_embed_backward(lp.LP_BF16, ids, dh, dtab, None, rows, V, d, 0, 1.0, None, w2, w2.numel(), s.cuda_stream)
+    torch.cuda.synchronize()
+    for a, b in zip(res[0][:3], res[1][:3]):
+        assert torch.equal(a, b) and a.abs().sum() > 0
+
+
+def test_linear_attention_on_sequence_first_tensors():
+    """[seq_len, batch, n_heads, 64] storage: the batch stride is smaller than a token's."""
+    B, T, H = 3, 150, 2
+    t = la_inputs(B, T, H, 5)
+    seq = {n: t[n].transpose(0, 1).contiguous().transpose(0, 1) for n in ("q", "k", "v")}
+    o1 = torch.zeros(T, B, H, 64, dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+    o2 = torch.zeros(B, T, H, 64, dtype=torch.bfloat16, device="cuda")
+    for src, o in ((seq, o1), (t, o2)):
+        lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, dict(q=src["q"], k=src["k"], v=src["v"], o=o, log_decay=t["log_decay"], scale=0.1),
+                                    la_workspace(0, B, T, H))
+    assert torch.equal(o1, o2)
+
+
+def test_a_state_updated_in_place_through_segments_and_a_backward_in_a_graph():
+    """Long prompts of few heads are cut into segments; the state is read and written in place, and the gradient with
+    respect to the incoming state overwrites the outgoing one's, in a captured call that is replayed."""
+    B, T, H = 1, 2100, 2
+    t = la_inputs(B, T, H, 17)
+    state, grad = t["state_in"].clone(), t["dstate_out"].clone()
+    o = torch.zeros(B, T, H, 64, dtype=torch.bfloat16, device="cuda")
+    g = {n: torch.zeros_like(o) for n in ("dq", "dk", "dv")}
+    ws = la_workspace(0, B, T, H), la_workspace(1, B, T, H)
+    assert ws[0].numel() > 0 and ws[1].numel() > 0
+    base = dict(q=t["q"], k=t["k"], v=t["v"], log_decay=t["log_decay"], scale=0.125)
+    keep = state.clone()
+
+    def calls(s):
+        lp.lp_linear_attention_bf16(lp.LP_LINATTN_BACKWARD, dict(base, dout=t["dout"], state_in=state, dstate_out=grad, dstate_in=grad, **g), ws[1], s)
+        lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, dict(base, o=o, state_in=state, state_out=state), ws[0], s)
+
+    q, k, v, do = (np64(t[n]) for n in ("q", "k", "v", "dout"))
+    lg = np64(t["log_decay"])
+    refs = O.linear_attention_bwd(q, k, v, do, lg, 0.125, np64(state), np64(grad))
+    mags = O.linear_attention_bwd(abs(q), abs(k), abs(v), abs(do), lg, 0.125, abs(np64(state)), abs(np64(grad)))
+    s_ref = O.linear_attention_fwd(q, k, v, lg, 0.125, np64(state))[1]
+    s_mag = O.linear_attention_fwd(abs(q), abs(k), abs(v), lg, 0.125, abs(np64(state)))[1]
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        calls(stream.cuda_stream)
+    for _ in range(2):
+        state.copy_(keep)
+        grad.copy_(t["dstate_out"])
+        graph.replay()
+    torch.cuda.synchronize()
+    assert (np.abs(np64(grad) - refs[3]) <= (2.0 ** -16 + (T / 64 + 70) * U32) * mags[3] + 1e-30).all()
+    assert (np.abs(np64(state) - s_ref) <= (2.0 ** -16 + (T / 64 + 70) * U32) * s_mag + 1e-30).all()
+    for n, r, m in zip(("dq", "dk", "dv"), refs, mags):
+        check_tokens(n, g[n], r, m, [T], None, True)
