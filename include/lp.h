@@ -399,7 +399,7 @@ lp_status lp_embed_forward(int dtype, const int* ids, const void* table, const v
  * [seq_len, d] fp32, overwritten; dpos may be NULL.  The rows are sorted by token and every sum runs over its rows in
  * increasing r (in pieces of fixed length, added in order, for a token with many rows): no atomics on floats.
  * Ids out of range as in lp_embed_forward: their rows count for the clamped token.
- * rows <= 2^30.  workspace: lp_embed_workspace_bytes(rows, vocab, d) (0: sizes not accepted).
+ * rows <= 2^30, d <= 2^22 (lp_embed_forward too).  workspace: lp_embed_workspace_bytes(rows, vocab, d) (0: sizes not accepted).
  */
 size_t lp_embed_workspace_bytes(int rows, int vocab, int d);
 lp_status lp_embed_backward(int dtype, const int* ids, const void* dout, float* dtable, float* dpos, int rows, int vocab,
@@ -435,8 +435,6 @@ lp_status lp_dropout(int dtype, const void* x, const void* resid, void* y, long 
  *       [dstate_in: gradient of state_in; may be dstate_out].  log_decay carries no gradient.
  *   LP_LINATTN_STEP:     the recurrent form, seq_len 1: as FORWARD, all arithmetic in fp32; lengths[b] = 0 marks an idle
  *       sequence.
- *   status (nullable): device int; bit 2 (4) is set, and never cleared, if a bounded device-side wait gave up (the outputs
- *   are then not valid).
  *   FORWARD and BACKWARD form scores and state products on bf16 operands with fp32 accumulation; state_out and dstate_in
  *   are accurate to about 2^-17 relative to the terms they add up.  A NaN or infinity in token t reaches the outputs from t
  *   on, and may reach earlier ones of the same 16 tokens.
@@ -452,7 +450,6 @@ typedef struct {
   const float* dstate_out;
   float* dstate_in;
   const int* lengths;
-  int* status;
   int batch, seq_len, n_heads;
   float scale;
 } lp_linattn_desc;

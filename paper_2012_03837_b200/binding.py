@@ -425,16 +425,16 @@ class lp_tokens(C.Structure):
 
 class lp_linattn_desc(C.Structure):
     _fields_ = [(n, lp_tokens) for n in ("q", "k", "v", "o", "dout", "dq", "dk", "dv")] + \
-               [(n, C.c_void_p) for n in ("log_decay", "state_in", "state_out", "dstate_out", "dstate_in", "lengths", "status")] + \
+               [(n, C.c_void_p) for n in ("log_decay", "state_in", "state_out", "dstate_out", "dstate_in", "lengths")] + \
                [("batch", C.c_int), ("seq_len", C.c_int), ("n_heads", C.c_int), ("scale", C.c_float)]
 
 
 _LINATTN_TOKENS = ("q", "k", "v", "o", "dout", "dq", "dk", "dv")
 _LINATTN_FLOATS = (("log_decay", 0), ("state_in", 4096), ("state_out", 4096), ("dstate_out", 4096), ("dstate_in", 4096),
-                   ("lengths", 0), ("status", 0))   # elements per sequence and head of the states
+                   ("lengths", 0))   # elements per sequence and head of the states
 _LINATTN_KEYS = {*_LINATTN_TOKENS, *(n for n, _ in _LINATTN_FLOATS), "scale"}
 _NO_TOKENS = (0, 0, 0)
-_linattn_layout = struct.Struct("=24q7Q3if")      # lp_linattn_desc, filled in one go
+_linattn_layout = struct.Struct("=24q6Q3if")      # lp_linattn_desc, filled in one go
 assert _linattn_layout.size == C.sizeof(lp_linattn_desc)
 _LINATTN_PACK = _linattn_layout.pack
 _lib.lp_linear_attention_bf16.argtypes = [C.c_int, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
@@ -477,7 +477,7 @@ def lp_linear_attention_bf16(form: int, desc: dict, workspace=None, stream=None)
         if t is None:
             v.append(0)
             continue
-        if t.numel() != (per * B * H if per else H if name == "log_decay" else B if name == "lengths" else 1) or \
+        if t.numel() != (per * B * H if per else H if name == "log_decay" else B) or \
                 t.element_size() != 4 or not t.is_contiguous():
             raise LpError(-2, f"lp_linear_attention_bf16: {name} has the wrong size or is not contiguous")
         if not t.is_cuda:

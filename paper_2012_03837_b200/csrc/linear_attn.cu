@@ -17,20 +17,61 @@
 // operand of a S are rounded once (2^-8 of a term, of the size of the output's own rounding, and at random; in
 // sequences of one chunk, where few terms average out, the scores too are split).  A state that is handed out in fp32
 // is formed from three terms and summed chunk by chunk in fp32, as exact as fp32 products would be.
+//
+// What bounds it: per token and head 512 bytes (forward) stand against 4.25 products of 64 x 64 (the triangles, and the two
+// terms of b), so the memory's time (82 us for [128, 512, 16 heads]) lies above that of the products on mma.sync (74 us at
+// 8 cycles per m16n8k16, measured) only by a little, and neither alone is met: 122 us forward, 0.36 of the memory's rate
+// backward ([64, 512, 16]: 178 us; the scans of dq, dk and dv each read three tensors).  Half of the tensor pipe's time is
+// used, with three blocks of four warps per SM; the rest are the waits of the chains ldmatrix, mma, scaling, mma.  Four
+// blocks (one buffer of tiles, 128 registers) were no faster, eight warps with half of the columns each slower (14.4
+// against 12.0 us on [32, 256, 8]).
+// On tcgen05 (chunks of 128, accumulators in tensor memory, TMA, eight row warps and two issuing ones, two blocks per
+// SM) the same scan was right and slower: 154 / 243 us on the two cases above.  Every chunk is a chain of four short
+// products with row work between them; a product of N = 64 and K = 128 took its issuing thread 2000 to 2600 clocks with
+// two blocks on the SM, and the tensor pipe was busy for a sixth of the time.
 #include <algorithm>
 
-#include "linear_attn.cuh"
+#include "common.cuh"
+#include "launch.cuh"
 
 namespace lp {
 namespace {
 
+// l^n for n >= 0, l = exp(lg), l^0 = 1 also for l = 0.  n lg is formed as a product and its rounding error, so that
+// the error of the result stays that of one expf.
+__device__ __forceinline__ float decay_pow(float lg, float n) {
+  if (n == 0.f) return 1.f;
+  const float x = n * lg, r = fmaf(n, lg, -x), e = expf(x);
+  return r == r ? fmaf(e, r, e) : e;             // lg = -infinity: no correction
+}
+
+// Tokens [t0, t1) of sequence (b, h) that a block covers.
+struct Span { int b, h, t0, t1; };
+__device__ __forceinline__ Span span_of(const LinAttnArgs& a, int item) {
+  Span s;
+  const int seg = item % a.n_seg, bh = item / a.n_seg;
+  s.h = bh % a.H;
+  s.b = bh / a.H;
+  const int len = a.lengths ? min(max(a.lengths[s.b], 0), a.T) : a.T;
+  s.t0 = (int)min((long long)seg * a.seg_len, (long long)len);
+  s.t1 = (int)min((long long)s.t0 + a.seg_len, (long long)len);
+  return s;
+}
+__device__ __forceinline__ const bf16* at(const LinAttnTok& x, const Span& s, long long t) { return x.p + s.b * x.bs + t * x.ts + s.h * 64; }
+
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+  __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *(uint32_t*)&v;
+}
+__device__ __forceinline__ float lo_f(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float hi_f(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
 constexpr int C = 64;                            // tokens of a chunk = width of a head
-constexpr int TILE = LA_STATE;
+constexpr int TILE = C * C;                      // elements of a state
 // Tiles in shared memory are 64 rows of 64 bf16, 144 bytes apart: the 16-byte units of eight consecutive rows lie in eight
 // different groups of banks, and every address of a fragment is one register plus a constant.
 constexpr int PITCH = 144;
 constexpr int TILE_B = C * PITCH;
-constexpr int TAB = 1024;                        // bytes of the tables of powers
+constexpr int TAB = 1280;                        // bytes of the tables of powers
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void ldsm(uint32_t (&r)[4], uint32_t a) {
@@ -62,8 +103,8 @@ __device__ __forceinline__ void sub2(float& x, float& y, float a, float b) {
 }
 // The bf16 pair nearest to (x, y); x and y become what is left.
 __device__ __forceinline__ uint32_t split(float& x, float& y) {
-  const uint32_t h = la_pack(x, y);
-  sub2(x, y, la_lo(h), la_hi(h));
+  const uint32_t h = pack(x, y);
+  sub2(x, y, lo_f(h), hi_f(h));
   return h;
 }
 
@@ -77,7 +118,7 @@ template <int N>
 __device__ __forceinline__ void put_rows(uint32_t at, const float (&x)[N / 8][4]) {
 #pragma unroll
   for (int j = 0; j < N / 8; j += 2)
-    stsm(at + j * 16, la_pack(x[j][0], x[j][1]), la_pack(x[j][2], x[j][3]), la_pack(x[j + 1][0], x[j + 1][1]), la_pack(x[j + 1][2], x[j + 1][3]));
+    stsm(at + j * 16, pack(x[j][0], x[j][1]), pack(x[j][2], x[j][3]), pack(x[j + 1][0], x[j + 1][1]), pack(x[j + 1][2], x[j + 1][3]));
 }
 
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -103,11 +144,10 @@ __device__ __forceinline__ void load_tile(uint32_t tile, const bf16* src, long l
   }
 }
 
-// pw[n] = l^n for 0 <= n <= 64, 0 for -64 <= n < 0 (tokens that do not exist); sc[n] = scale * l^n, 0 for -16 < n < 0 (not seen)
+// pw[n] = l^n and sc[n] = scale * l^n for 0 <= n <= 64; 0 for -64 <= n < 0 (tokens that do not exist, or are not seen)
 __device__ __forceinline__ void decay_tables(float* pw, float* sc, float lg, float scale) {
   const int x = threadIdx.x;
-  if (x < C) pw[x - C] = 0.f;
-  if (x < 16) sc[x - 16] = 0.f;
+  if (x < C) pw[x - C] = sc[x - C] = 0.f;
   if (x <= C) {
     const float p = decay_pow(lg, (float)x);
     pw[x] = p;
@@ -144,11 +184,11 @@ __device__ __forceinline__ void state_mma(float (&d)[N / 8][4], const uint32_t (
   uint32_t term[TERMS][4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {                  // registers 0, 1: tokens 2t, 2t+1; registers 2, 3: tokens 2t+8, 2t+9
-    float x = la_lo(bt[e]), y = la_hi(bt[e]);
+    float x = lo_f(bt[e]), y = hi_f(bt[e]);
     mul2(x, y, wt[(e >> 1) * 2], wt[(e >> 1) * 2 + 1]);
 #pragma unroll
     for (int k = 0; k + 1 < TERMS; ++k) term[k][e] = split(x, y);
-    term[TERMS - 1][e] = la_pack(x, y);
+    term[TERMS - 1][e] = pack(x, y);
   }
 #pragma unroll
   for (int k = TERMS - 1; k >= 0; --k)
@@ -162,14 +202,14 @@ __device__ __forceinline__ void state_mma(float (&d)[N / 8][4], const uint32_t (
 // The scan of a sequence of at most one chunk (see the head of the file): four warps, 16 rows of y and of the state each.
 // TERMS: bf16 terms of the decayed b.
 template <int TERMS, bool REV>
-__device__ __forceinline__ void scan_short(const LinAttnArgs& p, const LaSpan& sp, const LinAttnTok& A, const LinAttnTok& B, const LinAttnTok& Cc,
+__device__ __forceinline__ void scan_short(const LinAttnArgs& p, const Span& sp, const LinAttnTok& A, const LinAttnTok& B, const LinAttnTok& Cc,
                                            const LinAttnTok& Y, const float* s_in, bool transposed, float* s_out, char* smem) {
-  float *pw = (float*)smem + 64, *sc = (float*)smem + 160;
+  float *pw = (float*)smem + 64, *sc = (float*)smem + 193;
   const uint32_t tiles = smem_addr(smem + TAB);  // a, b, c, the state
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, t = lane & 3, n = sp.t1 - sp.t0;
-  load_tile<128>(tiles, la_at(A, sp, sp.t0), A.ts, n);
-  load_tile<128>(tiles + TILE_B, la_at(B, sp, sp.t0), B.ts, n);
-  load_tile<128>(tiles + 2 * TILE_B, la_at(Cc, sp, sp.t0), Cc.ts, n);
+  load_tile<128>(tiles, at(A, sp, sp.t0), A.ts, n);
+  load_tile<128>(tiles + TILE_B, at(B, sp, sp.t0), B.ts, n);
+  load_tile<128>(tiles + 2 * TILE_B, at(Cc, sp, sp.t0), Cc.ts, n);
   cp_commit();
   decay_tables(pw, sc, p.log_decay[sp.h], p.scale);
   float s[8][4];
@@ -223,8 +263,8 @@ __device__ __forceinline__ void scan_short(const LinAttnArgs& p, const LaSpan& s
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float u = x[e >> 1][(e & 1) * 2], v = x[e >> 1][(e & 1) * 2 + 1];
-        hi[e] = la_take(u, v);
-        lo[e] = la_pack(u, v);
+        hi[e] = split(u, v);
+        lo[e] = pack(u, v);
       }
 #pragma unroll
       for (int np = 0; np < 4; ++np) {
@@ -256,7 +296,7 @@ __device__ __forceinline__ void scan_short(const LinAttnArgs& p, const LaSpan& s
   __syncwarp();
   put_rows<64>(ba, acc);                         // y leaves through this warp's own rows of a: no other warp reads them
   __syncwarp();
-  bf16* y = const_cast<bf16*>(la_at(Y, sp, sp.t0));
+  bf16* y = const_cast<bf16*>(at(Y, sp, sp.t0));
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int e = lane + 32 * i, row = 16 * w + (e >> 3), u = e & 7;
@@ -269,7 +309,7 @@ constexpr int SHORT_SMEM = TAB + 4 * TILE_B;
 
 __global__ void __launch_bounds__(128) la_forward_short_kernel(LinAttnArgs p) {
   extern __shared__ __align__(128) char smem[];
-  const LaSpan sp = la_span(p, blockIdx.x);
+  const Span sp = span_of(p, blockIdx.x);
   const size_t so = (size_t)blockIdx.x * TILE;
   scan_short<3, false>(p, sp, p.q, p.k, p.v, p.o, p.state_in ? p.state_in + so : nullptr, false, p.state_out ? p.state_out + so : nullptr, smem);
 }
@@ -278,7 +318,7 @@ __global__ void __launch_bounds__(128) la_forward_short_kernel(LinAttnArgs p) {
 __global__ void __launch_bounds__(128) la_backward_short_kernel(LinAttnArgs p) {
   extern __shared__ __align__(128) char smem[];
   const int which = blockIdx.x % 3;
-  const LaSpan sp = la_span(p, blockIdx.x / 3);
+  const Span sp = span_of(p, blockIdx.x / 3);
   const size_t so = (size_t)(blockIdx.x / 3) * TILE;
   const float* r_in = p.dstate_out ? p.dstate_out + so : nullptr;
   if (which == 0) scan_short<1, false>(p, sp, p.dout, p.v, p.k, p.dq, p.state_in ? p.state_in + so : nullptr, true, nullptr, smem);
@@ -288,8 +328,8 @@ __global__ void __launch_bounds__(128) la_backward_short_kernel(LinAttnArgs p) {
 
 // Tokens in the order of a scan: the first one, and the distance to the next (negative backwards in time).
 struct Run { const bf16* p; long long ts; };
-__device__ __forceinline__ Run run_of(const LinAttnTok& x, const LaSpan& sp, bool rev) {
-  return rev ? Run{la_at(x, sp, sp.t1 - 1), -x.ts} : Run{la_at(x, sp, sp.t0), x.ts};
+__device__ __forceinline__ Run run_of(const LinAttnTok& x, const Span& sp, bool rev) {
+  return rev ? Run{at(x, sp, sp.t1 - 1), -x.ts} : Run{at(x, sp, sp.t0), x.ts};
 }
 
 // Fetches a run's tokens tile by tile, in order; 128 threads.  Rows behind the end read as zero.
@@ -328,7 +368,7 @@ template <int TERMS>
 __device__ __forceinline__ void scan(int len, const Run A, const Run B, const Run Cc, const Run Y, bool rev, float lg, float scale, const float* s_in,
                                      bool transposed, float* s_out, char* smem) {
   constexpr int BUF = 4 * TILE_B;                // two buffers of a, b, c and the state
-  float *pw = (float*)smem + 64, *sc = (float*)smem + 160;
+  float *pw = (float*)smem + 64, *sc = (float*)smem + 193;
   const uint32_t tiles = smem_addr(smem + TAB);
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int n_chunks = (len + C - 1) / C;
@@ -418,7 +458,7 @@ __device__ __forceinline__ void scan(int len, const Run A, const Run B, const Ru
           const int up = (e & 1) * 8, left = (e >> 1) * 8;
           float u = x[e >> 1][(e & 1) * 2], v = x[e >> 1][(e & 1) * 2 + 1];
           mul2(u, v, wp[up - left], wp[up - left - 1]);
-          pf[e] = la_pack(u, v);
+          pf[e] = pack(u, v);
         }
 #pragma unroll
         for (int np = 0; np < 4; ++np) {
@@ -462,7 +502,7 @@ template <int TERMS>
 __global__ void __launch_bounds__(128, TERMS == 3 ? 2 : 3) la_forward_kernel(LinAttnArgs p) {
   extern __shared__ __align__(128) char smem[];
   cudaGridDependencySynchronize();
-  const LaSpan sp = la_span(p, blockIdx.x);
+  const Span sp = span_of(p, blockIdx.x);
   const size_t so = ((size_t)sp.b * p.H + sp.h) * TILE;
   const float* in = p.seg_states ? p.seg_states + (size_t)blockIdx.x * TILE : p.state_in ? p.state_in + so : nullptr;
   scan<TERMS>(sp.t1 - sp.t0, run_of(p.q, sp, false), run_of(p.k, sp, false), run_of(p.v, sp, false), run_of(p.o, sp, false), false, p.log_decay[sp.h],
@@ -474,7 +514,7 @@ __global__ void __launch_bounds__(128, TERMS == 3 ? 2 : 3) la_backward_kernel(Li
   extern __shared__ __align__(128) char smem[];
   cudaGridDependencySynchronize();
   const int which = blockIdx.x % 3, item = blockIdx.x / 3;
-  const LaSpan sp = la_span(p, item);
+  const Span sp = span_of(p, item);
   const size_t so = ((size_t)sp.b * p.H + sp.h) * TILE;
   const float* s_in = p.seg_states ? p.seg_states + (size_t)item * TILE : p.state_in ? p.state_in + so : nullptr;
   const float* r_in = p.seg_states ? p.seg_grads + (size_t)item * TILE : p.dstate_out ? p.dstate_out + so : nullptr;
@@ -490,7 +530,7 @@ constexpr int SCAN_SMEM = TAB + 8 * TILE_B;
 // sum_j l^(n-j) scale b_j c_j^T.
 template <int TERMS>
 __device__ __forceinline__ void run_state(int len, const Run B, const Run Cc, bool rev, float lg, float scale, float* out, char* smem) {
-  float *pw = (float*)smem + 64, *sc = (float*)smem + 160;
+  float *pw = (float*)smem + 64, *sc = (float*)smem + 193;
   const uint32_t tiles = smem_addr(smem + TAB);
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, t = lane & 3;
   float s[8][4] = {};
@@ -542,7 +582,7 @@ constexpr int SEG_SMEM = TAB + 6 * TILE_B;
 template <int TERMS>
 __global__ void __launch_bounds__(128, 4) la_segment_kernel(LinAttnArgs p) {
   extern __shared__ __align__(128) char smem[];
-  const LaSpan sp = la_span(p, blockIdx.x);
+  const Span sp = span_of(p, blockIdx.x);
   const bool rev = blockIdx.y != 0;
   const LinAttnTok &b = rev ? p.q : p.k, &c = rev ? p.dout : p.v;
   run_state<TERMS>(sp.t1 - sp.t0, run_of(b, sp, rev), run_of(c, sp, rev), rev, p.log_decay[sp.h], p.scale,
@@ -603,7 +643,7 @@ __global__ void __launch_bounds__(256) la_step_kernel(LinAttnArgs p) {
   const bf16* k = p.k.p + b * p.k.bs + h * C;
   const uint2 vv = *(const uint2*)(p.v.p + b * p.v.bs + h * C + c4);
   const float l = expf(p.log_decay[h]);
-  const float4 v = make_float4(la_lo(vv.x), la_hi(vv.x), la_lo(vv.y), la_hi(vv.y));
+  const float4 v = make_float4(lo_f(vv.x), hi_f(vv.x), lo_f(vv.y), hi_f(vv.y));
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -622,7 +662,7 @@ __global__ void __launch_bounds__(256) la_step_kernel(LinAttnArgs p) {
 #pragma unroll
     for (int i = 1; i < 8; ++i) { a.x += red[i][tid].x; a.y += red[i][tid].y; a.z += red[i][tid].z; a.w += red[i][tid].w; }
     *(uint2*)(const_cast<bf16*>(p.o.p) + b * p.o.bs + h * C + c4) =
-        make_uint2(la_pack(a.x * p.scale, a.y * p.scale), la_pack(a.z * p.scale, a.w * p.scale));
+        make_uint2(pack(a.x * p.scale, a.y * p.scale), pack(a.z * p.scale, a.w * p.scale));
   }
 }
 

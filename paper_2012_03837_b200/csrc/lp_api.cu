@@ -798,7 +798,7 @@ static lp_status launched(const char* what, cudaError_t e) {
   return fail(nullptr, LP_ERR_CUDA, std::string(what) + ": launch: " + cudaGetErrorString(e));
 }
 static bool aligned_to(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
-static bool embed_sizes_ok(int rows, int vocab, int d) { return rows >= 1 && rows <= (1 << 30) && vocab >= 1 && d >= 1; }
+static bool embed_sizes_ok(int rows, int vocab, int d) { return rows >= 1 && rows <= (1 << 30) && vocab >= 1 && d >= 1 && d <= (1 << 22); }
 
 lp_status lp_embed_forward(int dtype, const int* ids, const void* table, const void* pos, void* out, int rows, int vocab,
                            int d, int seq_len, float scale, int* out_of_range, void* stream) {
@@ -806,7 +806,7 @@ lp_status lp_embed_forward(int dtype, const int* ids, const void* table, const v
   if (dtype != LP_FP32 && dtype != LP_BF16) return fail(nullptr, LP_ERR_INVALID_ARG, "lp_embed_forward: dtype");
   if (!ids || !table || !out) return fail(nullptr, LP_ERR_INVALID_ARG, "lp_embed_forward: null pointer");
   if (!embed_sizes_ok(rows, vocab, d) || (pos && seq_len < 1))
-    return fail(nullptr, LP_ERR_SHAPE, "lp_embed_forward: sizes must be positive (rows at most 2^30)");
+    return fail(nullptr, LP_ERR_SHAPE, "lp_embed_forward: sizes must be positive (rows at most 2^30, d at most 2^22)");
   const size_t es = dtype == LP_BF16 ? 2 : 4;
   if (!aligned_to(ids, 4) || !aligned_to(table, es) || !aligned_to(pos, es) || !aligned_to(out, es) || !aligned_to(out_of_range, 4))
     return fail(nullptr, LP_ERR_UNSUPPORTED, "lp_embed_forward: pointers must be aligned to their element");
@@ -825,7 +825,7 @@ lp_status lp_embed_backward(int dtype, const int* ids, const void* dout, float* 
   if (dtype != LP_FP32 && dtype != LP_BF16) return fail(nullptr, LP_ERR_INVALID_ARG, "lp_embed_backward: dtype");
   if (!ids || !dout || !dtable || !workspace) return fail(nullptr, LP_ERR_INVALID_ARG, "lp_embed_backward: null pointer");
   if (!embed_sizes_ok(rows, vocab, d) || (dpos && seq_len < 1))
-    return fail(nullptr, LP_ERR_SHAPE, "lp_embed_backward: sizes must be positive (rows at most 2^30)");
+    return fail(nullptr, LP_ERR_SHAPE, "lp_embed_backward: sizes must be positive (rows at most 2^30, d at most 2^22)");
   if (workspace_bytes < embed_bwd_workspace(rows, vocab, d)) return fail(nullptr, LP_ERR_INVALID_ARG, "lp_embed_backward: workspace too small");
   if (!aligned_to(ids, 4) || !aligned_to(dout, dtype == LP_BF16 ? 2 : 4) || !aligned_to(dtable, 4) || !aligned_to(dpos, 4) ||
       !aligned_to(out_of_range, 4) || !aligned_to(workspace, 256))
@@ -887,7 +887,7 @@ lp_status lp_linear_attention_bf16(int form, const lp_linattn_desc* d, void* wor
     if (outs[i] == d->q.p || outs[i] == d->k.p || outs[i] == d->v.p || (back && outs[i] == d->dout.p)) return bad(LP_ERR_INVALID_ARG, "an output is an input");
     for (int j = 0; j < i; ++j) if (outs[i] == outs[j]) return bad(LP_ERR_INVALID_ARG, "two outputs are the same");
   }
-  if (!aligned_to(d->state_in, 16) || !aligned_to(d->log_decay, 4) || !aligned_to(d->lengths, 4) || !aligned_to(d->status, 4) ||
+  if (!aligned_to(d->state_in, 16) || !aligned_to(d->log_decay, 4) || !aligned_to(d->lengths, 4) ||
       (!back && !aligned_to(d->state_out, 16)) || (back && (!aligned_to(d->dstate_out, 16) || !aligned_to(d->dstate_in, 16))))
     return bad(LP_ERR_UNSUPPORTED, "states must be 16-byte aligned");
   if (back && d->dstate_in && d->dstate_in == d->state_in) return bad(LP_ERR_INVALID_ARG, "an output is an input");
@@ -900,7 +900,7 @@ lp_status lp_linear_attention_bf16(int form, const lp_linattn_desc* d, void* wor
   auto tok = [](const lp_tokens& t) { return LinAttnTok{(const bf16*)t.p, t.token_stride, t.batch_stride}; };
   LinAttnArgs a{tok(d->q), tok(d->k), tok(d->v), tok(d->o), tok(d->dout), tok(d->dq), tok(d->dk), tok(d->dv),
                 d->log_decay, d->state_in, back ? nullptr : d->state_out, back ? d->dstate_out : nullptr, back ? d->dstate_in : nullptr,
-                d->lengths, d->status, d->batch, d->seq_len, d->n_heads, d->scale, 1, 0, nullptr, nullptr};
+                d->lengths, d->batch, d->seq_len, d->n_heads, d->scale, 1, 0, nullptr, nullptr};
   // one token takes the recurrent kernel in either form: the chunked one would work on 63 empty rows
   const cudaError_t e = !back && d->seq_len == 1 ? launch_linattn_step(a, (cudaStream_t)stream) : launch_linattn(a, back, workspace, (cudaStream_t)stream);
   return launched(me, e);

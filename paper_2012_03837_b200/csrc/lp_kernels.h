@@ -179,7 +179,6 @@ struct LinAttnTok { const bf16* p; long long ts, bs; };   // element (b, t, head
 struct LinAttnArgs {
   LinAttnTok q, k, v, o, dout, dq, dk, dv;
   const float* log_decay; const float* state_in; float* state_out; const float* dstate_out; float* dstate_in; const int* lengths;
-  int* status;                                   // nullable: ST_TIMEOUT if a device-side wait gave up
   int B, T, H; float scale;
   int n_seg, seg_len; float* seg_states; float* seg_grads;   // set by the launcher
 };

@@ -490,3 +490,24 @@ def test_a_state_updated_in_place_through_segments_and_a_backward_in_a_graph():
     assert (np.abs(np64(state) - s_ref) <= (2.0 ** -16 + (T / 64 + 70) * U32) * s_mag + 1e-30).all()
     for n, r, m in zip(("dq", "dk", "dv"), refs, mags):
         check_tokens(n, g[n], r, m, [T], None, True)
+
+
+def test_linear_attention_does_not_depend_on_what_shared_memory_held():
+    """Backwards in time the last chunk of a length that is no multiple of 64 has absent tokens; their weights come from a
+    table, and what an earlier kernel left in shared memory must not pass for one."""
+    a = torch.full((4096, 4096), float("nan"), device="cuda")
+    for B, T, H in ((2, 70, 2), (1, 1029, 1), (2, 2, 1)):
+        t = la_inputs(B, T, H, 3)
+        outs = []
+        for dirty in (False, True):
+            if dirty:
+                torch.matmul(a, a)
+                torch.softmax(a, dim=1)
+                torch.matmul(a.to(torch.bfloat16), a.to(torch.bfloat16))
+            g = [torch.zeros(B, T, H, 64, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+            ds = torch.zeros(B, H, 64, 64, device="cuda")
+            lp.lp_linear_attention_bf16(lp.LP_LINATTN_BACKWARD, dict(q=t["q"], k=t["k"], v=t["v"], dout=t["dout"], dq=g[0], dk=g[1], dv=g[2],
+                                        log_decay=t["log_decay"], scale=0.125, state_in=t["state_in"], dstate_out=t["dstate_out"], dstate_in=ds),
+                                        la_workspace(1, B, T, H))
+            outs.append(g + [ds])
+        assert all(torch.equal(x, y) and torch.isfinite(x).all() for x, y in zip(*outs))
