@@ -464,14 +464,12 @@ def lp_linear_attention_bf16(form: int, desc: dict, workspace=None, stream=None)
         if t is None:
             v += _NO_TOKENS
             continue
-        if t.shape != shape or t.dtype is not bf16:
+        if t.dtype is not bf16 or t.shape != shape:
             raise LpError(-2, f"lp_linear_attention_bf16: {name} must be bf16 and of q's shape")
         sb, st, sh, se = t.stride()
         if se != 1 or (sh != 64 and H > 1):
             raise LpError(-3, f"lp_linear_attention_bf16: the heads of {name} must lie 64 elements apart")
-        if not t.is_cuda:
-            raise LpError(-1, f"lp_linear_attention_bf16: {name} is in host memory")
-        v += (t.data_ptr(), sb if B > 1 else 0, st)
+        v += (t.data_ptr(), sb, st)
     for name, per in _LINATTN_FLOATS:
         t = get(name)
         if t is None:
@@ -480,10 +478,8 @@ def lp_linear_attention_bf16(form: int, desc: dict, workspace=None, stream=None)
         if t.numel() != (per * B * H if per else H if name == "log_decay" else B) or \
                 t.element_size() != 4 or not t.is_contiguous():
             raise LpError(-2, f"lp_linear_attention_bf16: {name} has the wrong size or is not contiguous")
-        if not t.is_cuda:
-            raise LpError(-1, f"lp_linear_attention_bf16: {name} is in host memory")
         v.append(t.data_ptr())
-    nbytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    nbytes = workspace.nbytes if workspace is not None else 0
     code = _lib.lp_linear_attention_bf16(form, _LINATTN_PACK(*v, B, T, H, get("scale", 1.0)), _dev(workspace) if nbytes else None, nbytes,
                                          stream)
     if code:

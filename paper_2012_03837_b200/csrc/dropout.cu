@@ -55,6 +55,7 @@ __device__ __forceinline__ void scale_add(float& x, float& y, float s, float a, 
 // A block covers U * 256 consecutive vectors; the elements behind the last whole vector go one by one.
 template <typename T, bool RESID, int U>
 __global__ void __launch_bounds__(256) dropout_vec_kernel(const __grid_constant__ Args a) {
+  cudaGridDependencySynchronize();
   constexpr int VEC = 16 / sizeof(T);
   const long long vecs = a.n / VEC, v0 = (long long)blockIdx.x * (256 * U) + threadIdx.x;
   const unsigned long long first = a.offset + (a.offset_dev ? *a.offset_dev : 0ull);
@@ -105,6 +106,7 @@ __global__ void __launch_bounds__(256) dropout_vec_kernel(const __grid_constant_
 // One thread per group of four elements; any alignment.
 template <typename T>
 __global__ void __launch_bounds__(256) dropout_kernel(const __grid_constant__ Args a) {
+  cudaGridDependencySynchronize();
   const long long groups = (a.n + 3) / 4;
   const unsigned long long first = a.offset + (a.offset_dev ? *a.offset_dev : 0ull);
   for (long long g = (long long)blockIdx.x * blockDim.x + threadIdx.x; g < groups; g += (long long)gridDim.x * blockDim.x) {
@@ -126,8 +128,8 @@ cudaError_t run_vec(const Args& a, cudaStream_t s) {
   const long long vecs = a.n / (16 / (int)sizeof(T));
   const bool many = vecs >= 148LL * 8 * 256 * 2;   // more than two waves of single loads: four in flight per thread
   const unsigned blocks = (unsigned)std::max<long long>(1, many ? (vecs + 1023) / 1024 : (vecs + 255) / 256);
-  if (a.resid) return many ? launch_kernel(dropout_vec_kernel<T, true, 4>, dim3(blocks), 256, 0, s, a) : launch_kernel(dropout_vec_kernel<T, true, 1>, dim3(blocks), 256, 0, s, a);
-  return many ? launch_kernel(dropout_vec_kernel<T, false, 4>, dim3(blocks), 256, 0, s, a) : launch_kernel(dropout_vec_kernel<T, false, 1>, dim3(blocks), 256, 0, s, a);
+  if (a.resid) return many ? launch_after(dropout_vec_kernel<T, true, 4>, dim3(blocks), 256, 0, s, a) : launch_after(dropout_vec_kernel<T, true, 1>, dim3(blocks), 256, 0, s, a);
+  return many ? launch_after(dropout_vec_kernel<T, false, 4>, dim3(blocks), 256, 0, s, a) : launch_after(dropout_vec_kernel<T, false, 1>, dim3(blocks), 256, 0, s, a);
 }
 
 }  // namespace
@@ -138,8 +140,8 @@ cudaError_t launch_dropout(const DropoutArgs& in, bool is_bf16, cudaStream_t s) 
   if ((((uintptr_t)a.x | (uintptr_t)a.resid | (uintptr_t)a.y) & 15) == 0) return is_bf16 ? run_vec<bf16>(a, s) : run_vec<float>(a, s);
   const long long groups = (a.n + 3) / 4;
   const unsigned blocks = (unsigned)std::min<long long>((groups + 255) / 256, 148 * 16);
-  return is_bf16 ? launch_kernel(dropout_kernel<bf16>, dim3(blocks), 256, 0, s, a)
-                 : launch_kernel(dropout_kernel<float>, dim3(blocks), 256, 0, s, a);
+  return is_bf16 ? launch_after(dropout_kernel<bf16>, dim3(blocks), 256, 0, s, a)
+                 : launch_after(dropout_kernel<float>, dim3(blocks), 256, 0, s, a);
 }
 
 }  // namespace lp

@@ -85,6 +85,7 @@ __device__ __forceinline__ int clamp_id(int id, int vocab) { return min(max(id, 
 // `lanes` threads (a power of two) per row, VEC elements each.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(128) embed_fwd_kernel(EmbedProb p, int lanes_log2, int* status) {
+  cudaGridDependencySynchronize();
   const long long gt = (long long)blockIdx.x * blockDim.x + threadIdx.x;
   const long long row = gt >> lanes_log2;
   const int lane = (int)(gt & ((1 << lanes_log2) - 1));
@@ -168,6 +169,7 @@ template <typename T, int VEC>
 __global__ void __launch_bounds__(SORT_WARPS * 32, 1) embed_sort_kernel(EmbedBwdProb p, int n_log2, int local, int piece, int* status, int lanes_log2,
                                                                      int split_log2, int pos_pieces) {
   extern __shared__ int sm[];
+  cudaGridDependencySynchronize();
   if ((int)blockIdx.x >> n_log2) {
     pos_sums<T, VEC>(p, lanes_log2, split_log2, (int)blockIdx.x - (1 << n_log2), pos_pieces, (float*)sm);
     return;
@@ -444,7 +446,7 @@ cudaError_t run_sort_and_sum(const EmbedBwdProb& p, int P, int chunks, int pos_p
   while (split < groups_log2 && (pos_work << split >> groups_log2) < 148) ++split;
   const long long pos_blocks = early ? ((pos_work << split) + (1 << groups_log2) - 1) >> groups_log2 : 0;
   const long long pos_late = early ? 0 : (pos_work + per_block - 1) / per_block;
-  e = launch_kernel(embed_sort_kernel<T, VEC>, dim3((unsigned)((1 << n_log2) + pos_blocks)), SORT_WARPS * 32, smem, s, p, n_log2, local, PIECES * P, d_status, ll,
+  e = launch_after(embed_sort_kernel<T, VEC>, dim3((unsigned)((1 << n_log2) + pos_blocks)), SORT_WARPS * 32, smem, s, p, n_log2, local, PIECES * P, d_status, ll,
                     split, pos_pieces);
   if (e != cudaSuccess) return e;
   const int sum_blocks = (chunks + per_block - 1) / per_block;
@@ -461,10 +463,10 @@ cudaError_t launch_embed_fwd(const EmbedProb& p, int* d_status, bool is_bf16, cu
   const int ll = lanes_log2_for((p.d + vec - 1) / vec, 5);
   const dim3 grid((unsigned)((((long long)p.rows << ll) + 127) / 128));
   if (is_bf16)
-    return vec == 8 ? launch_kernel(embed_fwd_kernel<bf16, 8>, grid, 128, 0, s, p, ll, d_status)
-                    : launch_kernel(embed_fwd_kernel<bf16, 1>, grid, 128, 0, s, p, ll, d_status);
-  return vec == 4 ? launch_kernel(embed_fwd_kernel<float, 4>, grid, 128, 0, s, p, ll, d_status)
-                  : launch_kernel(embed_fwd_kernel<float, 1>, grid, 128, 0, s, p, ll, d_status);
+    return vec == 8 ? launch_after(embed_fwd_kernel<bf16, 8>, grid, 128, 0, s, p, ll, d_status)
+                    : launch_after(embed_fwd_kernel<bf16, 1>, grid, 128, 0, s, p, ll, d_status);
+  return vec == 4 ? launch_after(embed_fwd_kernel<float, 4>, grid, 128, 0, s, p, ll, d_status)
+                  : launch_after(embed_fwd_kernel<float, 1>, grid, 128, 0, s, p, ll, d_status);
 }
 
 // Workspace: sorted rows, token segments, pieces of long tokens, pieces of the position sums, the list of long

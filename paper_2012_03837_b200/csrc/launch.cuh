@@ -23,18 +23,8 @@ struct SmemLimit {
   }
 };
 
-template <typename... KArgs, typename... Args>
-cudaError_t launch_kernel(void (*kernel)(KArgs...), dim3 grid, int threads, size_t smem, cudaStream_t s, Args&&... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3((unsigned)threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
-}
-
-// The same for a kernel that waits for its predecessor on the stream itself (cudaGridDependencySynchronize): its blocks
-// are set up while the predecessor drains.
+// Launches a kernel that waits for its predecessor on the stream itself: cudaGridDependencySynchronize() before anything
+// else, so its blocks are set up while the predecessor drains.
 template <typename... KArgs, typename... Args>
 cudaError_t launch_after(void (*kernel)(KArgs...), dim3 grid, int threads, size_t smem, cudaStream_t s, Args&&... args) {
   cudaLaunchConfig_t cfg{};

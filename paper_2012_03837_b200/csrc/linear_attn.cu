@@ -309,6 +309,7 @@ constexpr int SHORT_SMEM = TAB + 4 * TILE_B;
 
 __global__ void __launch_bounds__(128) la_forward_short_kernel(LinAttnArgs p) {
   extern __shared__ __align__(128) char smem[];
+  cudaGridDependencySynchronize();
   const Span sp = span_of(p, blockIdx.x);
   const size_t so = (size_t)blockIdx.x * TILE;
   scan_short<3, false>(p, sp, p.q, p.k, p.v, p.o, p.state_in ? p.state_in + so : nullptr, false, p.state_out ? p.state_out + so : nullptr, smem);
@@ -317,6 +318,7 @@ __global__ void __launch_bounds__(128) la_forward_short_kernel(LinAttnArgs p) {
 // Three scans of every sequence and head: dq, dk, dv.
 __global__ void __launch_bounds__(128) la_backward_short_kernel(LinAttnArgs p) {
   extern __shared__ __align__(128) char smem[];
+  cudaGridDependencySynchronize();
   const int which = blockIdx.x % 3;
   const Span sp = span_of(p, blockIdx.x / 3);
   const size_t so = (size_t)(blockIdx.x / 3) * TILE;
@@ -582,6 +584,7 @@ constexpr int SEG_SMEM = TAB + 6 * TILE_B;
 template <int TERMS>
 __global__ void __launch_bounds__(128, 4) la_segment_kernel(LinAttnArgs p) {
   extern __shared__ __align__(128) char smem[];
+  cudaGridDependencySynchronize();
   const Span sp = span_of(p, blockIdx.x);
   const bool rev = blockIdx.y != 0;
   const LinAttnTok &b = rev ? p.q : p.k, &c = rev ? p.dout : p.v;
@@ -625,6 +628,7 @@ __global__ void __launch_bounds__(256) la_join_kernel(LinAttnArgs p) {
 
 // One token: a block per sequence and head.  The state is read and written once (32 KB), all in fp32.
 __global__ void __launch_bounds__(256) la_step_kernel(LinAttnArgs p) {
+  cudaGridDependencySynchronize();
   const int h = blockIdx.x % p.H, b = blockIdx.x / p.H, tid = threadIdx.x;
   const float* in = p.state_in ? p.state_in + (size_t)blockIdx.x * TILE : nullptr;
   float* out = p.state_out ? p.state_out + (size_t)blockIdx.x * TILE : nullptr;
@@ -688,7 +692,7 @@ size_t linattn_workspace(bool backward, int B, int T, int H) {
 }
 
 cudaError_t launch_linattn_step(const LinAttnArgs& a, cudaStream_t s) {
-  return launch_kernel(la_step_kernel, dim3((unsigned)(a.B * a.H)), 256, 0, s, a);
+  return launch_after(la_step_kernel, dim3((unsigned)(a.B * a.H)), 256, 0, s, a);
 }
 
 cudaError_t launch_linattn(LinAttnArgs a, bool backward, void* workspace, cudaStream_t s) {
@@ -696,7 +700,7 @@ cudaError_t launch_linattn(LinAttnArgs a, bool backward, void* workspace, cudaSt
   if (a.T <= C) {
     a.n_seg = 1;
     a.seg_len = C;
-    return launch_kernel(backward ? la_backward_short_kernel : la_forward_short_kernel, dim3((unsigned)(backward ? 3 * bh : bh)), 128, SHORT_SMEM, s, a);
+    return launch_after(backward ? la_backward_short_kernel : la_forward_short_kernel, dim3((unsigned)(backward ? 3 * bh : bh)), 128, SHORT_SMEM, s, a);
   }
   const Layout l = choose_layout(bh, a.T, backward ? 3 : 1);
   a.n_seg = l.n_seg;
@@ -709,7 +713,7 @@ cudaError_t launch_linattn(LinAttnArgs a, bool backward, void* workspace, cudaSt
     static SmemLimit limit[2];
     auto seg = leaves ? la_segment_kernel<3> : la_segment_kernel<2>;
     e = limit[leaves].raise((const void*)seg, SEG_SMEM);
-    if (e == cudaSuccess) e = launch_kernel(seg, dim3((unsigned)(bh * a.n_seg), backward ? 2 : 1), 128, SEG_SMEM, s, a);
+    if (e == cudaSuccess) e = launch_after(seg, dim3((unsigned)(bh * a.n_seg), backward ? 2 : 1), 128, SEG_SMEM, s, a);
     if (e == cudaSuccess) e = launch_after(la_join_kernel, dim3((unsigned)bh, backward ? 2 : 1, 4), 256, 0, s, a);
     if (e != cudaSuccess) return e;
   }

@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <stdexcept>
 
 #include "runtime.h"
@@ -780,16 +781,19 @@ lp_status lp_attention_bf16(int form, const void* qkv, void* o, float* lse, cons
 }
 
 // ---- operators on the caller's buffers (embedding, dropout, linear attention)
-// The current device must be able to reach `out`: memory of another device, or of the host, is refused.
-static lp_status check_output(const char* what, const void* out) {
+// The current device must be able to reach every (non-null) pointer: memory of another device, or of the host, is refused.
+static lp_status check_memory(const char* what, std::initializer_list<const void*> pointers) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return fail(nullptr, LP_ERR_CUDA, std::string(what) + ": no CUDA device"); }
-  cudaPointerAttributes at{};
-  if (cudaPointerGetAttributes(&at, out) != cudaSuccess) { cudaGetLastError(); return fail(nullptr, LP_ERR_CUDA, std::string(what) + ": cannot query a pointer"); }
-  if (at.type != cudaMemoryTypeDevice && at.type != cudaMemoryTypeManaged)
-    return fail(nullptr, LP_ERR_INVALID_ARG, std::string(what) + ": not a device pointer");
-  if (at.type == cudaMemoryTypeDevice && at.device != dev)
-    return fail(nullptr, LP_ERR_UNSUPPORTED, std::string(what) + ": memory of another device than the current one");
+  for (const void* p : pointers) {
+    if (!p) continue;
+    cudaPointerAttributes at{};
+    if (cudaPointerGetAttributes(&at, p) != cudaSuccess) { cudaGetLastError(); return fail(nullptr, LP_ERR_CUDA, std::string(what) + ": cannot query a pointer"); }
+    if (at.type != cudaMemoryTypeDevice && at.type != cudaMemoryTypeManaged)
+      return fail(nullptr, LP_ERR_INVALID_ARG, std::string(what) + ": not a device pointer");
+    if (at.type == cudaMemoryTypeDevice && at.device != dev)
+      return fail(nullptr, LP_ERR_UNSUPPORTED, std::string(what) + ": memory of another device than the current one");
+  }
   return LP_OK;
 }
 static lp_status launched(const char* what, cudaError_t e) {
@@ -810,7 +814,7 @@ lp_status lp_embed_forward(int dtype, const int* ids, const void* table, const v
   const size_t es = dtype == LP_BF16 ? 2 : 4;
   if (!aligned_to(ids, 4) || !aligned_to(table, es) || !aligned_to(pos, es) || !aligned_to(out, es) || !aligned_to(out_of_range, 4))
     return fail(nullptr, LP_ERR_UNSUPPORTED, "lp_embed_forward: pointers must be aligned to their element");
-  lp_status st = check_output(me, out);
+  lp_status st = check_memory(me, {ids, table, pos, out, out_of_range});
   if (st != LP_OK) return st;
   const EmbedProb p{ids, table, pos, out, rows, pos ? seq_len : 1, d, vocab, scale};
   return launched(me, launch_embed_fwd(p, out_of_range, dtype == LP_BF16, (cudaStream_t)stream));
@@ -830,7 +834,7 @@ lp_status lp_embed_backward(int dtype, const int* ids, const void* dout, float* 
   if (!aligned_to(ids, 4) || !aligned_to(dout, dtype == LP_BF16 ? 2 : 4) || !aligned_to(dtable, 4) || !aligned_to(dpos, 4) ||
       !aligned_to(out_of_range, 4) || !aligned_to(workspace, 256))
     return fail(nullptr, LP_ERR_UNSUPPORTED, "lp_embed_backward: pointers must be aligned to their element, the workspace to 256 bytes");
-  lp_status st = check_output(me, dtable);
+  lp_status st = check_memory(me, {ids, dout, dtable, dpos, out_of_range, workspace});
   if (st != LP_OK) return st;
   const EmbedBwdProb p{ids, dout, dtable, dpos, rows, dpos ? seq_len : 0, d, vocab, scale, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
   return launched(me, launch_embed_bwd(p, workspace, out_of_range, dtype == LP_BF16, (cudaStream_t)stream));
@@ -847,7 +851,7 @@ lp_status lp_dropout(int dtype, const void* x, const void* resid, void* y, long 
   const size_t es = dtype == LP_BF16 ? 2 : 4;
   if (!aligned_to(x, es) || !aligned_to(resid, es) || !aligned_to(y, es) || !aligned_to(offset_dev, 8))
     return fail(nullptr, LP_ERR_UNSUPPORTED, "lp_dropout: pointers must be aligned to their element");
-  lp_status st = check_output(me, y);
+  lp_status st = check_memory(me, {x, resid, y, offset_dev});
   if (st != LP_OK) return st;
   const DropoutArgs a{x, resid, y, n, dropout_threshold(p), (float)(1.0 / (1.0 - p)), seed, offset, offset_dev, 0, 0};
   return launched(me, launch_dropout(a, dtype == LP_BF16, (cudaStream_t)stream));
@@ -872,14 +876,13 @@ lp_status lp_linear_attention_bf16(int form, const lp_linattn_desc* d, void* wor
   const bool used[8] = {true, true, true, !back, back, back, back, back};
   for (int i = 0; i < 8; ++i) {
     if (!used[i]) continue;
-    if (!aligned_to(all[i]->p, 16) || (all[i]->batch_stride & 7) || (all[i]->token_stride & 7))
+    // strides that no second sequence or token uses are not looked at (and multiplied by 0 only)
+    const long long bs = d->batch > 1 ? all[i]->batch_stride : 64LL * d->n_heads, ts = d->seq_len > 1 ? all[i]->token_stride : 64LL * d->n_heads;
+    if (!aligned_to(all[i]->p, 16) || (bs & 7) || (ts & 7))
       return bad(LP_ERR_UNSUPPORTED, "tokens must be 16-byte aligned, their strides multiples of 8 elements");
-    if (all[i]->batch_stride > 1LL << 38 || all[i]->token_stride > 1LL << 38) return bad(LP_ERR_SHAPE, "strides must be at most 2^38 elements");
-    if (d->batch > 1 && all[i]->batch_stride < 8) return bad(LP_ERR_SHAPE, "batch_stride must be positive");
-    if (all[i]->batch_stride < 0 || (d->seq_len > 1 && all[i]->token_stride < 64LL * d->n_heads))
-      return bad(LP_ERR_SHAPE, "token_stride must be at least 64 * n_heads, batch_stride not negative");
-    if (i >= 3 && i != 4 && d->batch > 1 && all[i]->batch_stride < 64LL * d->n_heads)
-      return bad(LP_ERR_SHAPE, "the sequences of an output overlap");
+    if (bs > 1LL << 38 || ts > 1LL << 38) return bad(LP_ERR_SHAPE, "strides must be at most 2^38 elements");
+    if (bs < 8 || ts < 64LL * d->n_heads) return bad(LP_ERR_SHAPE, "token_stride must be at least 64 * n_heads, batch_stride positive");
+    if (i >= 3 && i != 4 && bs < 64LL * d->n_heads) return bad(LP_ERR_SHAPE, "the sequences of an output overlap");
   }
   const void* outs[4] = {back ? d->dq.p : d->o.p, back ? d->dk.p : nullptr, back ? d->dv.p : nullptr, nullptr};
   for (int i = 0; i < 3; ++i) {
@@ -895,9 +898,13 @@ lp_status lp_linear_attention_bf16(int form, const lp_linattn_desc* d, void* wor
   const size_t need = form == LP_LINATTN_STEP ? 0 : linattn_workspace(back, d->batch, d->seq_len, d->n_heads);
   if (need && (!workspace || workspace_bytes < need)) return bad(LP_ERR_INVALID_ARG, "workspace too small");
   if (need && !aligned_to(workspace, 256)) return bad(LP_ERR_UNSUPPORTED, "the workspace must be 256-byte aligned");
-  lp_status st = check_output(me, outs[0]);
+  lp_status st = back ? check_memory(me, {d->q.p, d->k.p, d->v.p, d->dout.p, d->dq.p, d->dk.p, d->dv.p, d->log_decay, d->lengths, d->state_in,
+                                          d->dstate_out, d->dstate_in, need ? workspace : nullptr})
+                      : check_memory(me, {d->q.p, d->k.p, d->v.p, d->o.p, d->log_decay, d->lengths, d->state_in, d->state_out, need ? workspace : nullptr});
   if (st != LP_OK) return st;
-  auto tok = [](const lp_tokens& t) { return LinAttnTok{(const bf16*)t.p, t.token_stride, t.batch_stride}; };
+  auto tok = [&](const lp_tokens& t) {
+    return LinAttnTok{(const bf16*)t.p, d->seq_len > 1 ? t.token_stride : 0, d->batch > 1 ? t.batch_stride : 0};
+  };
   LinAttnArgs a{tok(d->q), tok(d->k), tok(d->v), tok(d->o), tok(d->dout), tok(d->dq), tok(d->dk), tok(d->dv),
                 d->log_decay, d->state_in, back ? nullptr : d->state_out, back ? d->dstate_out : nullptr, back ? d->dstate_in : nullptr,
                 d->lengths, d->batch, d->seq_len, d->n_heads, d->scale, 1, 0, nullptr, nullptr};
