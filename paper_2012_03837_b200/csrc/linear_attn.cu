@@ -592,38 +592,34 @@ __global__ void __launch_bounds__(128, 4) la_segment_kernel(LinAttnArgs p) {
                    (rev ? p.seg_grads : p.seg_states) + (size_t)blockIdx.x * TILE, smem);
 }
 
-// Turns every segment's own state into the state at its entry, and forms the last state.
+// Turns every segment's own state into the state at its entry, and forms the last state.  A thread per element, sixteen
+// segments in flight.
 __global__ void __launch_bounds__(256) la_join_kernel(LinAttnArgs p) {
   cudaGridDependencySynchronize();
   const bool reverse = blockIdx.y != 0;
   const int bh = blockIdx.x, h = bh % p.H, b = bh / p.H, len = p.lengths ? min(max(p.lengths[b], 0), p.T) : p.T;
-  float* seg = (reverse ? p.seg_grads : p.seg_states) + (size_t)bh * p.n_seg * TILE;
+  const int e = blockIdx.z * blockDim.x + threadIdx.x;
+  float* seg = (reverse ? p.seg_grads : p.seg_states) + (size_t)bh * p.n_seg * TILE + e;
   const float* in = reverse ? p.dstate_out : p.state_in;
   float* out = reverse ? p.dstate_in : p.state_out;
-  const float lg = p.log_decay[h];
-  const int e = (blockIdx.z * blockDim.x + threadIdx.x) * 4;
-  float4 run = in ? *(const float4*)(in + (size_t)bh * TILE + e) : make_float4(0.f, 0.f, 0.f, 0.f);
-  const float lfull = decay_pow(lg, (float)p.seg_len);
-  constexpr int BATCH = 8;                       // segments in flight
+  const float lg = p.log_decay[h], lfull = decay_pow(lg, (float)p.seg_len);
+  float run = in ? in[(size_t)bh * TILE + e] : 0.f;
+  constexpr int BATCH = 16;
   for (int i0 = 0; i0 < p.n_seg; i0 += BATCH) {
-    float4 own[BATCH];
-    float4* at[BATCH];
+    float own[BATCH];
 #pragma unroll
-    for (int u = 0; u < BATCH; ++u) {
-      at[u] = (float4*)(seg + (size_t)(reverse ? p.n_seg - 1 - i0 - u : i0 + u) * TILE + e);
-      if (i0 + u < p.n_seg) own[u] = *at[u];
-    }
+    for (int u = 0; u < BATCH; ++u)
+      if (i0 + u < p.n_seg) own[u] = seg[(size_t)(reverse ? p.n_seg - 1 - i0 - u : i0 + u) * TILE];
 #pragma unroll
     for (int u = 0; u < BATCH; ++u) {
       if (i0 + u >= p.n_seg) break;
       const int sidx = reverse ? p.n_seg - 1 - i0 - u : i0 + u;
       const int n = (int)min(max((long long)len - (long long)sidx * p.seg_len, 0LL), (long long)p.seg_len);
-      const float l = n == p.seg_len ? lfull : decay_pow(lg, (float)n);
-      *at[u] = run;
-      run.x = fmaf(l, run.x, own[u].x); run.y = fmaf(l, run.y, own[u].y); run.z = fmaf(l, run.z, own[u].z); run.w = fmaf(l, run.w, own[u].w);
+      seg[(size_t)sidx * TILE] = run;
+      run = fmaf(n == p.seg_len ? lfull : decay_pow(lg, (float)n), run, own[u]);
     }
   }
-  if (out) *(float4*)(out + (size_t)bh * TILE + e) = run;
+  if (out) out[(size_t)bh * TILE + e] = run;
 }
 
 // One token: a block per sequence and head.  The state is read and written once (32 KB), all in fp32.
@@ -714,7 +710,7 @@ cudaError_t launch_linattn(LinAttnArgs a, bool backward, void* workspace, cudaSt
     auto seg = leaves ? la_segment_kernel<3> : la_segment_kernel<2>;
     e = limit[leaves].raise((const void*)seg, SEG_SMEM);
     if (e == cudaSuccess) e = launch_after(seg, dim3((unsigned)(bh * a.n_seg), backward ? 2 : 1), 128, SEG_SMEM, s, a);
-    if (e == cudaSuccess) e = launch_after(la_join_kernel, dim3((unsigned)bh, backward ? 2 : 1, 4), 256, 0, s, a);
+    if (e == cudaSuccess) e = launch_after(la_join_kernel, dim3((unsigned)bh, backward ? 2 : 1, TILE / 256), 256, 0, s, a);
     if (e != cudaSuccess) return e;
   }
   const bool three = leaves && a.n_seg == 1;     // otherwise the state that leaves comes from the segments
