@@ -7,6 +7,11 @@
 //
 // A dropped element is selected away, not multiplied by zero: a NaN or an infinity there does not reach y.
 // Sums and products are in fp32 and rounded once, on storing.
+//
+// What bounds it: memory where three tensors pass (33.5 M bf16 with residual: 31 us, 6.5 TB/s, as fast as a copy), the
+// generator's instructions where two bf16 tensors do (30 us against 20 for the bytes: twenty wide products and twenty
+// three-way exclusive-ors per four elements, about 150 instructions per eight).  Sixteen random bits per element would
+// halve that and tie p to multiples of 2^-16; a loop over blocks that fetches ahead was slower (35 to 41 us).
 #include <algorithm>
 
 #include "common.cuh"
@@ -41,14 +46,10 @@ __device__ __forceinline__ uint4 words(const Args& a, unsigned long long first, 
   return make_uint4(c0, c1, c2, c3);
 }
 
+// A predicated multiply-add: selecting an operand would go through the pipe that the generator's rounds keep busy.
 __device__ __forceinline__ float drop(const Args& a, uint32_t w, float x, float r) {
-  return w >= a.threshold ? fmaf(x, a.scale, r) : r;
-}
-
-// x = x * s + a, y = y * s + b in one instruction.
-__device__ __forceinline__ void scale_add(float& x, float& y, float s, float a, float b) {
-  asm("{\n\t.reg .b64 u, v, m;\n\tmov.b64 u, {%0, %1};\n\tmov.b64 m, {%2, %2};\n\tmov.b64 v, {%3, %4};\n\tfma.rn.f32x2 u, u, m, v;\n\tmov.b64 {%0, %1}, u;\n\t}"
-      : "+f"(x), "+f"(y) : "f"(s), "f"(a), "f"(b));
+  if (w >= a.threshold) r = fmaf(x, a.scale, r);
+  return r;
 }
 
 // 16 bytes per thread and load, U of them in flight (with the residual's); the generator's arithmetic fills the wait.
@@ -83,11 +84,11 @@ __global__ void __launch_bounds__(256) dropout_vec_kernel(const __grid_constant_
           ys[e] = __float_as_uint(drop(a, ww[e], __uint_as_float(xs[e]), RESID ? __uint_as_float(rs[e]) : 0.f));
       } else {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {            // dropped elements are cleared in the packed pair
-          const uint32_t keep = (ww[2 * e] >= a.threshold ? 0xffffu : 0u) | (ww[2 * e + 1] >= a.threshold ? 0xffff0000u : 0u);
-          const uint32_t xx = xs[2 * k + e] & keep, rr = RESID ? rs[2 * k + e] : 0u;
-          float lo = __uint_as_float(xx << 16), hi = __uint_as_float(xx & 0xffff0000u);
-          scale_add(lo, hi, a.scale, __uint_as_float(rr << 16), __uint_as_float(rr & 0xffff0000u));
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t xx = xs[2 * k + e], rr = RESID ? rs[2 * k + e] : 0u;
+          float lo = __uint_as_float(rr << 16), hi = __uint_as_float(rr & 0xffff0000u);
+          if (ww[2 * e] >= a.threshold) lo = fmaf(__uint_as_float(xx << 16), a.scale, lo);
+          if (ww[2 * e + 1] >= a.threshold) hi = fmaf(__uint_as_float(xx & 0xffff0000u), a.scale, hi);
           __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
           ys[2 * k + e] = *(uint32_t*)&b;
         }
