@@ -435,8 +435,8 @@ lp_status lp_dropout(int dtype, const void* x, const void* resid, void* y, long 
  *       [dstate_in: gradient of state_in; may be dstate_out].  log_decay carries no gradient.
  *   LP_LINATTN_STEP:     the recurrent form, seq_len 1: as FORWARD, all arithmetic in fp32; lengths[b] = 0 marks an idle
  *       sequence.
- *   FORWARD and BACKWARD form scores and state products on bf16 operands with fp32 accumulation; state_out and dstate_in
- *   are accurate to about 2^-17 relative to the terms they add up.  A NaN or infinity in token t reaches the outputs from t
+ *   FORWARD and BACKWARD form scores and state products on bf16 operands with fp32 accumulation; the operands of state_out
+ *   and dstate_in are split into as many terms as they need, so those are as exact as sums in fp32.  A NaN or infinity in token t reaches the outputs from t
  *   on, and may reach earlier ones of the same 16 tokens.
  *   batch * n_heads <= 2^20.  workspace: lp_linear_attention_workspace_bytes (may be 0).
  */

@@ -429,11 +429,9 @@ class lp_linattn_desc(C.Structure):
                [("batch", C.c_int), ("seq_len", C.c_int), ("n_heads", C.c_int), ("scale", C.c_float)]
 
 
-_LINATTN_TOKENS = ("q", "k", "v", "o", "dout", "dq", "dk", "dv")
-_LINATTN_FLOATS = (("log_decay", 0), ("state_in", 4096), ("state_out", 4096), ("dstate_out", 4096), ("dstate_in", 4096),
-                   ("lengths", 0))   # elements per sequence and head of the states
-_LINATTN_KEYS = {*_LINATTN_TOKENS, *(n for n, _ in _LINATTN_FLOATS), "scale"}
-_NO_TOKENS = (0, 0, 0)
+_LINATTN_SLOTS = {n: 3 * i for i, n in enumerate(("q", "k", "v", "o", "dout", "dq", "dk", "dv"))}      # three values each
+_LINATTN_SLOTS |= {n: 24 + i for i, n in enumerate(("log_decay", "state_in", "state_out", "dstate_out", "dstate_in", "lengths"))}
+_linattn_types = None                              # torch's bfloat16, float32, int32 (torch is there once a tensor is)
 _linattn_layout = struct.Struct("=24q6Q3if")      # lp_linattn_desc, filled in one go
 assert _linattn_layout.size == C.sizeof(lp_linattn_desc)
 _LINATTN_PACK = _linattn_layout.pack
@@ -451,36 +449,41 @@ def lp_linear_attention_bf16(form: int, desc: dict, workspace=None, stream=None)
     tensors of lp_linattn_desc: q, k, v, o, dout, dq, dk, dv are bf16 CUDA tensors [batch, seq_len, n_heads, 64] (slices
     of larger ones are fine: strides are read off), the states fp32 [batch, n_heads, 64, 64], log_decay fp32 [n_heads],
     lengths int32 [batch]; `scale` a number (default 1).  Sizes come from q; the other tensors' shapes must agree."""
-    if not desc.keys() <= _LINATTN_KEYS:
-        raise LpError(-1, f"lp_linear_attention_bf16: unknown {sorted(desc.keys() - _LINATTN_KEYS)}")
-    get, q = desc.get, desc["q"]
-    shape, bf16 = q.shape, q.dtype
-    if len(shape) != 4 or shape[3] != 64 or str(bf16) != "torch.bfloat16":
+    global _linattn_types
+    if _linattn_types is None:
+        import torch
+        _linattn_types = torch.bfloat16, torch.float32, torch.int32
+    bf16, f32, i32 = _linattn_types
+    q, scale = desc.get("q"), 1.0
+    if q is None or q.dtype is not bf16 or q.ndim != 4:
         raise LpError(-2, "lp_linear_attention_bf16: q must be bf16 [batch, seq_len, n_heads, 64]")
-    B, T, H, _ = shape
-    v = []
-    for name in _LINATTN_TOKENS:
-        t = get(name)
-        if t is None:
-            v += _NO_TOKENS
+    shape = q.shape
+    B, T, H, width = shape
+    if width != 64:
+        raise LpError(-2, "lp_linear_attention_bf16: q must be bf16 [batch, seq_len, n_heads, 64]")
+    v = [0] * 30                                   # lp_linattn_desc up to the sizes; 0: not given
+    for name, t in desc.items():
+        at = _LINATTN_SLOTS.get(name)
+        if at is None:
+            if name != "scale":
+                raise LpError(-1, f"lp_linear_attention_bf16: unknown {name}")
+            scale = t
+        elif t is None:
             continue
-        if t.dtype is not bf16 or t.shape != shape:
-            raise LpError(-2, f"lp_linear_attention_bf16: {name} must be bf16 and of q's shape")
-        sb, st, sh, se = t.stride()
-        if se != 1 or (sh != 64 and H > 1):
-            raise LpError(-3, f"lp_linear_attention_bf16: the heads of {name} must lie 64 elements apart")
-        v += (t.data_ptr(), sb, st)
-    for name, per in _LINATTN_FLOATS:
-        t = get(name)
-        if t is None:
-            v.append(0)
-            continue
-        if t.numel() != (per * B * H if per else H if name == "log_decay" else B) or \
-                t.element_size() != 4 or not t.is_contiguous():
-            raise LpError(-2, f"lp_linear_attention_bf16: {name} has the wrong size or is not contiguous")
-        v.append(t.data_ptr())
+        elif at < 24:
+            if t is not q and (t.dtype is not bf16 or t.shape != shape):
+                raise LpError(-2, f"lp_linear_attention_bf16: {name} must be bf16 and of q's shape")
+            sb, st, sh, se = t.stride()
+            if se != 1 or (sh != 64 and H > 1):
+                raise LpError(-3, f"lp_linear_attention_bf16: the heads of {name} must lie 64 elements apart")
+            v[at], v[at + 1], v[at + 2] = t.data_ptr(), sb, st
+        else:
+            n, kind = (H, f32) if at == 24 else (B, i32) if at == 29 else (4096 * B * H, f32)
+            if t.dtype is not kind or t.numel() != n or not t.is_contiguous():
+                raise LpError(-2, f"lp_linear_attention_bf16: {name} has the wrong type or size or is not contiguous")
+            v[at] = t.data_ptr()
     nbytes = workspace.nbytes if workspace is not None else 0
-    code = _lib.lp_linear_attention_bf16(form, _LINATTN_PACK(*v, B, T, H, get("scale", 1.0)), _dev(workspace) if nbytes else None, nbytes,
+    code = _lib.lp_linear_attention_bf16(form, _LINATTN_PACK(*v, B, T, H, scale), _dev(workspace) if nbytes else None, nbytes,
                                          stream)
     if code:
         _check(None, code)

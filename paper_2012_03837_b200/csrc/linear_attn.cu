@@ -113,21 +113,19 @@ __device__ __forceinline__ uint32_t split(float& x, float& y) {
 // round -- ldsm gives B(k, n) = tile[n][k], ldsm_t the A fragment A(m, k) = tile[k][m].
 __device__ __forceinline__ uint32_t lane_rows(int lane) { return (lane & 15) * PITCH + (lane >> 4) * 16; }
 __device__ __forceinline__ uint32_t lane_cols(int lane) { return ((lane & 7) + ((lane >> 4) << 3)) * PITCH + ((lane >> 3) & 1) * 16; }
-// A warp's 16 x N accumulators as bf16 rows of a tile; at: address of the first row and column plus lane_rows.
-template <int N>
-__device__ __forceinline__ void put_rows(uint32_t at, const float (&x)[N / 8][4]) {
+// A warp's 16 x 64 accumulators as bf16 rows of a tile; at: address of the first row plus lane_rows.
+__device__ __forceinline__ void put_rows(uint32_t at, const float (&x)[8][4]) {
 #pragma unroll
-  for (int j = 0; j < N / 8; j += 2)
+  for (int j = 0; j < 8; j += 2)
     stsm(at + j * 16, pack(x[j][0], x[j][1]), pack(x[j][2], x[j][3]), pack(x[j + 1][0], x[j + 1][1]), pack(x[j + 1][2], x[j + 1][3]));
 }
 
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// 64 token rows into a tile; rows at or behind n read as zero (nothing is fetched for them).
-template <int THREADS>
+// 64 token rows into a tile, by 128 threads; rows at or behind n read as zero (nothing is fetched for them).
 __device__ __forceinline__ void load_tile(uint32_t tile, const bf16* src, long long ts, int n) {
-  constexpr int STEP = THREADS / 8;              // rows of one round
+  constexpr int STEP = 16;                       // rows of one round
   const int row = threadIdx.x >> 3, u = threadIdx.x & 7;
   const uint32_t d = tile + row * PITCH + u * 16;
   const bf16* g = src + row * ts + u * 8;
@@ -155,32 +153,30 @@ __device__ __forceinline__ void decay_tables(float* pw, float* sc, float lg, flo
   }
 }
 
-// The state of a warp: rows 16 w + g (+8), columns col0 + 8 j + 2 t (+1), g = lane / 4, t = lane % 4.
-template <int N>
-__device__ __forceinline__ void state_load(float (&s)[N / 8][4], const float* src, bool transposed, int col0, int w, int lane) {
+// The state of a warp: rows 16 w + g (+8), columns 8 j + 2 t (+1), g = lane / 4, t = lane % 4.
+__device__ __forceinline__ void state_load(float (&s)[8][4], const float* src, bool transposed, int w, int lane) {
   const int g = lane >> 2, t = lane & 3;
 #pragma unroll
-  for (int j = 0; j < N / 8; ++j)
+  for (int j = 0; j < 8; ++j)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int r = 16 * w + g + (e >> 1) * 8, c = col0 + 8 * j + 2 * t + (e & 1);
+      const int r = 16 * w + g + (e >> 1) * 8, c = 8 * j + 2 * t + (e & 1);
       s[j][e] = src ? src[transposed ? c * C + r : r * C + c] : 0.f;
     }
 }
-template <int N>
-__device__ __forceinline__ void state_store(float* dst, const float (&s)[N / 8][4], int col0, int w, int lane) {
+__device__ __forceinline__ void state_store(float* dst, const float (&s)[8][4], int w, int lane) {
   const int g = lane >> 2, t = lane & 3;
 #pragma unroll
-  for (int j = 0; j < N / 8; ++j) {
-    *(float2*)(dst + (16 * w + g) * C + col0 + 8 * j + 2 * t) = make_float2(s[j][0], s[j][1]);
-    *(float2*)(dst + (16 * w + g + 8) * C + col0 + 8 * j + 2 * t) = make_float2(s[j][2], s[j][3]);
+  for (int j = 0; j < 8; ++j) {
+    *(float2*)(dst + (16 * w + g) * C + 8 * j + 2 * t) = make_float2(s[j][0], s[j][1]);
+    *(float2*)(dst + (16 * w + g + 8) * C + 8 * j + 2 * t) = make_float2(s[j][2], s[j][3]);
   }
 }
 
 // d += (weights . B)^T C over the 16 tokens of a step: `bt` is the fragment of B^T, cf the fragments of C.  The decayed
 // b goes in as TERMS bf16 terms, the smallest first.
-template <int N, int TERMS>
-__device__ __forceinline__ void state_mma(float (&d)[N / 8][4], const uint32_t (&bt)[4], const uint32_t (&cf)[N / 16][4], const float (&wt)[4]) {
+template <int TERMS>
+__device__ __forceinline__ void state_mma(float (&d)[8][4], const uint32_t (&bt)[4], const uint32_t (&cf)[4][4], const float (&wt)[4]) {
   uint32_t term[TERMS][4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {                  // registers 0, 1: tokens 2t, 2t+1; registers 2, 3: tokens 2t+8, 2t+9
@@ -193,7 +189,7 @@ __device__ __forceinline__ void state_mma(float (&d)[N / 8][4], const uint32_t (
 #pragma unroll
   for (int k = TERMS - 1; k >= 0; --k)
 #pragma unroll
-    for (int np = 0; np < N / 16; ++np) {
+    for (int np = 0; np < 4; ++np) {
       mma(d[2 * np], term[k], cf[np][0], cf[np][1]);
       mma(d[2 * np + 1], term[k], cf[np][2], cf[np][3]);
     }
@@ -207,15 +203,15 @@ __device__ __forceinline__ void scan_short(const LinAttnArgs& p, const Span& sp,
   float *pw = (float*)smem + 64, *sc = (float*)smem + 193;
   const uint32_t tiles = smem_addr(smem + TAB);  // a, b, c, the state
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, t = lane & 3, n = sp.t1 - sp.t0;
-  load_tile<128>(tiles, at(A, sp, sp.t0), A.ts, n);
-  load_tile<128>(tiles + TILE_B, at(B, sp, sp.t0), B.ts, n);
-  load_tile<128>(tiles + 2 * TILE_B, at(Cc, sp, sp.t0), Cc.ts, n);
+  load_tile(tiles, at(A, sp, sp.t0), A.ts, n);
+  load_tile(tiles + TILE_B, at(B, sp, sp.t0), B.ts, n);
+  load_tile(tiles + 2 * TILE_B, at(Cc, sp, sp.t0), Cc.ts, n);
   cp_commit();
   decay_tables(pw, sc, p.log_decay[sp.h], p.scale);
   float s[8][4];
-  state_load<64>(s, s_in, transposed, 0, w, lane);
+  state_load(s, s_in, transposed, w, lane);
   const uint32_t rows = lane_rows(lane), own = rows + w * 16 * PITCH, cols = lane_cols(lane);
-  put_rows<64>(tiles + 3 * TILE_B + own, s);
+  put_rows(tiles + 3 * TILE_B + own, s);
   cp_wait<0>();
   __syncthreads();
   // ages of the pair (row g of this warp, first column of a step): rows lie 8 apart, columns 8 and 1 apart
@@ -283,7 +279,7 @@ __device__ __forceinline__ void scan_short(const LinAttnArgs& p, const Span& sp,
         const int j = 16 * kk + (e & 1) + (e >> 1) * 8;
         wt[e] = REV ? wj[j] : wj[-j];
       }
-      state_mma<64, TERMS>(d, bt, cf, wt);
+      state_mma<TERMS>(d, bt, cf, wt);
     }
   }
   if (s_out) {
@@ -291,10 +287,10 @@ __device__ __forceinline__ void scan_short(const LinAttnArgs& p, const Span& sp,
     for (int j = 0; j < 8; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[j][e] = fmaf(ln, s[j][e], d[j][e]);
-    state_store<64>(s_out, s, 0, w, lane);
+    state_store(s_out, s, w, lane);
   }
   __syncwarp();
-  put_rows<64>(ba, acc);                         // y leaves through this warp's own rows of a: no other warp reads them
+  put_rows(ba, acc);                         // y leaves through this warp's own rows of a: no other warp reads them
   __syncwarp();
   bf16* y = const_cast<bf16*>(at(Y, sp, sp.t0));
 #pragma unroll
@@ -384,9 +380,9 @@ __device__ __forceinline__ void scan(int len, const Run A, const Run B, const Ru
   cp_commit();
   decay_tables(pw, sc, lg, scale);
   float s[8][4];
-  state_load<64>(s, s_in, transposed, 0, w, lane);
+  state_load(s, s_in, transposed, w, lane);
   const uint32_t rows = lane_rows(lane), own = rows + w * 16 * PITCH, cols = lane_cols(lane);
-  put_rows<64>(tiles + 3 * TILE_B + own, s);
+  put_rows(tiles + 3 * TILE_B + own, s);
   const float* from_state = (rev ? pw : sc + 1) + 16 * w + g;            // weights of the rows' products with the state
   bf16* y = const_cast<bf16*>(Y.p) + (16 * w + (lane >> 3)) * Y.ts + (lane & 7) * 8;
   const uint32_t y_at = (16 * w + (lane >> 3)) * PITCH + (lane & 7) * 16;
@@ -452,8 +448,8 @@ __device__ __forceinline__ void scan(int len, const Run A, const Run B, const Ru
             mma(x[1], af[ks], b[2], b[3]);
           }
         }
-        if constexpr (TERMS == 3) state_mma<64, 3>(d, bt, cf, wt);
-        else state_mma<64, TERMS>(s, bt, cf, wt);
+        if constexpr (TERMS == 3) state_mma<TERMS>(d, bt, cf, wt);
+        else state_mma<TERMS>(s, bt, cf, wt);
         uint32_t pf[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -468,8 +464,8 @@ __device__ __forceinline__ void scan(int len, const Run A, const Run B, const Ru
           mma(acc[2 * np + 1], pf, cf[np][2], cf[np][3]);
         }
       } else {
-        if constexpr (TERMS == 3) state_mma<64, 3>(d, bt, cf, wt);
-        else state_mma<64, TERMS>(s, bt, cf, wt);
+        if constexpr (TERMS == 3) state_mma<TERMS>(d, bt, cf, wt);
+        else state_mma<TERMS>(s, bt, cf, wt);
       }
       bb += 16 * PITCH;
       bc += 16 * PITCH;
@@ -482,10 +478,10 @@ __device__ __forceinline__ void scan(int len, const Run A, const Run B, const Ru
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[j][e] = fmaf(ln, s[j][e], d[j][e]);
     }
-    put_rows<64>(other + 3 * TILE_B + own, s);
+    put_rows(other + 3 * TILE_B + own, s);
     // y leaves through this warp's own rows of a: no other warp reads them
     __syncwarp();
-    put_rows<64>(ba, acc);
+    put_rows(ba, acc);
     __syncwarp();
     const int left = n - 16 * w - (lane >> 3);   // rows 4 i of this warp with 4 i < left exist
 #pragma unroll
@@ -496,7 +492,7 @@ __device__ __forceinline__ void scan(int len, const Run A, const Run B, const Ru
     }
     y += C * Y.ts;
   }
-  if (s_out) state_store<64>(s_out, s, 0, w, lane);
+  if (s_out) state_store(s_out, s, w, lane);
 }
 
 // Entry states: from the workspace where segments were formed, else from the caller.
@@ -566,7 +562,7 @@ __device__ __forceinline__ void run_state(int len, const Run B, const Run Cc, bo
       for (int np = 0; np < 4; ++np) ldsm_t(cf[np], bc + np * 32);
       ldsm_t(bt, bt_at);
       const float wt[4] = {wj[0], wj[-1], wj[-8], wj[-9]};
-      state_mma<64, TERMS>(d, bt, cf, wt);
+      state_mma<TERMS>(d, bt, cf, wt);
       bt_at += 16 * PITCH;
       bc += 16 * PITCH;
       wj -= 16;
@@ -576,7 +572,7 @@ __device__ __forceinline__ void run_state(int len, const Run B, const Run Cc, bo
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[j][e] = fmaf(ln, s[j][e], d[j][e]);
   }
-  state_store<64>(out, s, 0, w, lane);
+  state_store(out, s, w, lane);
 }
 constexpr int SEG_SMEM = TAB + 6 * TILE_B;
 

@@ -160,6 +160,20 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         assert e.value.code in (ERR["SHAPE"], ERR["INVALID_ARG"])
 
 
+def test_binding_refuses_wrong_types_and_names():
+    """Tensors of another type would be read as what they are not."""
+    import torch
+    t = torch.zeros(2, 3, 2, 64, dtype=torch.bfloat16)
+    good = dict(q=t, k=t, v=t, o=t, log_decay=torch.zeros(2))
+    for change in (dict(log_decay=torch.zeros(2, dtype=torch.int32)), dict(log_decay=torch.zeros(1)), dict(lengths=torch.zeros(2)),
+                   dict(lengths=torch.zeros(2, dtype=torch.int64)), dict(state_in=torch.zeros(2, 2, 64, 64, dtype=torch.int32)),
+                   dict(state_out=torch.zeros(2, 64, 2, 64).transpose(1, 2)), dict(q=None), dict(q=t[0]), dict(mask=t)):
+        with pytest.raises(lp.LpError) as e:
+            lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, {**good, **change})
+        assert e.value.code in (ERR["SHAPE"], ERR["INVALID_ARG"])
+        assert "CUDA" not in str(e.value) and "device" not in str(e.value)
+
+
 # ---- the training step with dropout: the oracle's gradients against differences, and its refusals
 def test_oracle_gradients_with_dropout_match_differences():
     import lp_synth
