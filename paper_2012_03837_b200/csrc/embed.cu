@@ -13,13 +13,13 @@
 //             the rows.  The ids are small (32 KB for 8192 rows), so reading them n times costs less than the
 //             launches and grid-wide exchanges of a radix sort.
 //   sum     : the sorted rows are cut into stretches of P; a worker sums the tokens that start in its stretch, reading
-//             whole rows of dh.  A token with more than P rows is cut into pieces of P, one per worker, whose fp32
+//             whole rows of dh.  A token with more than 4 P rows is cut into pieces of 4 P, one per worker, whose fp32
 //             sums go to the workspace.  Further blocks of the launch write the zero rows and the position gradient.
-//   combine : adds the pieces of every such token in order (a launch of its own, only if more than P rows exist).
+//   combine : adds the pieces of every such token in order (a launch of its own, only if more than 4 P rows exist).
 // Measured: 8192 rows of 512 into 8192 tokens 14 us (sort 5, sums 6, pieces 2: launches that follow one another); 65536 rows
-// of 1024 into 32768 tokens of natural text 91 us: sort 19 with the position gradient's read of dh beside it 37, sums 46
-// (268 MB at 5.8 TB/s), pieces 6.  The floor of the latter, dh read once and both gradients written, is 41 us.  The lookup
-// of 8192 rows of 1024 with positions takes 5.2 us, the time of its bytes.
+// of 1024 into 32768 tokens of natural text 87 us: sort 16, the position gradient's read of dh 24, of which it hides
+// a third, sums 46 (268 MB at 5.8 TB/s), pieces 6.  The floor of the latter, dh read once and both gradients written, is 41
+// us.  The lookup of 8192 rows of 1024 with positions takes 5.1 us, the time of its bytes.
 #include <algorithm>
 #include <climits>
 
@@ -30,34 +30,39 @@ namespace lp {
 namespace {
 
 constexpr int SORT_WARPS = 32;
-constexpr int SORT_MAX_LOCAL = 1024;             // tokens of one sorting block: (32 + 2) * 1024 counters and the lists fit its shared memory
+constexpr int SORT_MAX_LOCAL = 1024;             // tokens of one sorting block (ten bits of a list entry): (32 + 2) * 1024 counters and the lists fit its shared memory
 constexpr int SORT_LIST = 512;                   // rows of this block that a warp remembers
-constexpr int SORT_BATCH = 8;                    // loads of ids in flight
+constexpr int SORT_IDS = 8;                       // ids of a lane at a time
 constexpr int SUM_THREADS = 128;
 constexpr int PIECES = 4;                        // rows of a piece of a long token, in stretches
 constexpr int ZERO_ROWS = 16;                    // table rows a zero-filling block looks at
+constexpr int POS_THREADS = 256;                 // of a block that sums positions beside the sort
 constexpr int POS_PIECE = 64;                    // rows one position worker sums
 constexpr uint32_t HEAVY = 0x80000000u;
 
-template <typename T, int VEC> struct Pack;      // VEC elements as loaded; get(i) converts
+template <typename T, int VEC> struct Pack;      // VEC elements as loaded (load_l2: past the SM's own cache); get(i) converts
 template <> struct Pack<float, 1> {
   float x;
   __device__ void load(const float* p) { x = *p; }
+  __device__ void load_l2(const float* p) { x = __ldcg(p); }
   __device__ float get(int) const { return x; }
 };
 template <> struct Pack<bf16, 1> {
   bf16 x;
   __device__ void load(const bf16* p) { x = *p; }
+  __device__ void load_l2(const bf16* p) { x = __ldcg(p); }
   __device__ float get(int) const { return to_f(x); }
 };
 template <> struct Pack<float, 4> {
   float x[4];
   __device__ void load(const float* p) { *(float4*)x = *(const float4*)p; }
+  __device__ void load_l2(const float* p) { *(float4*)x = __ldcg((const float4*)p); }
   __device__ float get(int i) const { return x[i]; }
 };
 template <> struct Pack<bf16, 8> {
   uint32_t x[4];
   __device__ void load(const bf16* p) { *(uint4*)x = *(const uint4*)p; }
+  __device__ void load_l2(const bf16* p) { *(uint4*)x = __ldcg((const uint4*)p); }
   __device__ float get(int i) const { return __uint_as_float(i & 1 ? x[i >> 1] & 0xffff0000u : x[i >> 1] << 16); }
 };
 template <typename T> __device__ __forceinline__ void store_vec(T* p, const float (&v)[1]) { *p = from_f<T>(v[0]); }
@@ -143,7 +148,7 @@ __device__ void pos_sums(const EmbedBwdProb& p, int lanes_log2, int split_log2, 
       for (long long k = k0; k < k1; k += U) {
         Pack<T, VEC> x[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) if (k + u < k1) x[u].load(dh + (size_t)((k + u) * step) * p.d);
+        for (int u = 0; u < U; ++u) if (k + u < k1) x[u].load_l2(dh + (size_t)((k + u) * step) * p.d);
 #pragma unroll
         for (int u = 0; u < U; ++u)
           if (k + u < k1) {
@@ -165,25 +170,32 @@ __device__ void pos_sums(const EmbedBwdProb& p, int lanes_log2, int split_log2, 
   }
 }
 
+// The position gradient beside the sort, whose blocks let this launch start once they know that all work before them is
+// complete.  It ends no earlier than the sort, so that what follows it finds both.
+template <typename T, int VEC>
+__global__ void __launch_bounds__(POS_THREADS) embed_pos_kernel(EmbedBwdProb p, int lanes_log2, int split_log2, int pos_pieces) {
+  __shared__ float buf[POS_THREADS * VEC];
+  pos_sums<T, VEC>(p, lanes_log2, split_log2, blockIdx.x, pos_pieces, buf);
+  cudaGridDependencySynchronize();
+}
+
 // Rows by token.  Block j owns the tokens t with t mod n = j (n a power of two), local index t div n.
 // sorted[p] = {row, token | HEAVY if the token has more than `piece` rows}; seg[t] = {first p, number of rows}.
-// First sweep: every warp counts its stretch's rows per token and lists those of this block; second sweep: over the list
-// (or over the stretch again, if the list overflowed).  The blocks behind the n sorting ones sum the position gradient.
-template <typename T, int VEC>
-__global__ void __launch_bounds__(SORT_WARPS * 32, 1) embed_sort_kernel(EmbedBwdProb p, int n_log2, int local, int piece, int* status, int lanes_log2,
-                                                                     int split_log2, int pos_pieces) {
+// First sweep: every warp counts its stretch's rows per token and lists those of this block, a lane taking eight ids at a
+// time and comparing their blocks as bytes (65536 rows: 13 thousand clocks; one id per lane at a time 15, and with the next
+// ones fetched ahead 17; the ids read once per cluster of four blocks, with lists passed through distributed shared memory,
+// gave 85 instead of 87 us for the whole gradient and 16 instead of 14 for 8192 rows).  Second sweep: over the list
+// (or over the stretch again, if the list overflowed).  let_next: the next launch may start beside this one.
+__global__ void __launch_bounds__(SORT_WARPS * 32, 1) embed_sort_kernel(EmbedBwdProb p, int n_log2, int local, int piece, int* status, bool let_next) {
   extern __shared__ int sm[];
   cudaGridDependencySynchronize();
-  if ((int)blockIdx.x >> n_log2) {
-    pos_sums<T, VEC>(p, lanes_log2, split_log2, (int)blockIdx.x - (1 << n_log2), pos_pieces, (float*)sm);
-    return;
-  }
+  if (let_next) cudaTriggerProgrammaticLaunchCompletion();
   const int pitch = local | 1;
   int* cnt = sm;                                 // [SORT_WARPS][pitch]
   int* start = cnt + SORT_WARPS * pitch;         // [local]
   int* total = start + local;                    // [local]
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, j = blockIdx.x, mask = (1 << n_log2) - 1;
-  int* list = total + local + w * SORT_LIST;     // [SORT_LIST] rows
+  uint32_t* list = (uint32_t*)(total + local) + w * SORT_LIST;           // [SORT_LIST] row in the stretch * 1024 + local index
   __shared__ int less_sum, carry_of[SORT_WARPS];
   for (int i = tid; i < SORT_WARPS * pitch; i += blockDim.x) cnt[i] = 0;
   if (tid == 0) {
@@ -197,33 +209,70 @@ __global__ void __launch_bounds__(SORT_WARPS * 32, 1) embed_sort_kernel(EmbedBwd
   int* mine = cnt + w * pitch;
   const unsigned below = (1u << lane) - 1;
   int less = 0, listed = 0;
-  bool bad = false;
-  auto take = [&](int id, int r, bool real) {
-    const int t = clamp_id(id, p.vocab), cls = real ? t & mask : INT_MAX;
-    bad |= real && id != t;
-    less += cls < j;
-    const unsigned hits = __ballot_sync(0xffffffffu, cls == j);
-    if (hits) {
-      if (cls == j) {
-        atomicAdd(&mine[t >> n_log2], 1);
-        const int at = listed + __popc(hits & below);
-        if (at < SORT_LIST) list[at] = r;
-      }
-      listed += __popc(hits);
+  uint32_t most = 0;                             // of all ids as unsigned numbers: at least vocab if one is out of range
+  const bool wide = ((uintptr_t)p.ids & 15) == 0;
+  const uint32_t jj = (uint32_t)j * 0x01010101u;
+  for (int rb = r0; rb < r1; rb += 32 * SORT_IDS) {                      // a lane looks at SORT_IDS consecutive ids
+    const int first = rb + lane * SORT_IDS;
+    const bool whole = rb + 32 * SORT_IDS <= r1;
+    int id[SORT_IDS];
+    if (whole && wide) {
+      *(int4*)id = *(const int4*)(p.ids + first);
+      *(int4*)(id + 4) = *(const int4*)(p.ids + first + 4);
+    } else {
+#pragma unroll
+      for (int u = 0; u < SORT_IDS; ++u) id[u] = first + u < r1 ? p.ids[first + u] : 0;
     }
-  };
-  int rb = r0;
-  for (; rb + 32 * SORT_BATCH <= r1; rb += 32 * SORT_BATCH) {
-    int id[SORT_BATCH];
+    uint32_t here = 0;
 #pragma unroll
-    for (int u = 0; u < SORT_BATCH; ++u) id[u] = p.ids[rb + 32 * u + lane];
+    for (int u = 0; u < SORT_IDS; ++u) here = max(here, (uint32_t)id[u]);
+    most = max(most, here);
+    if (__any_sync(0xffffffffu, here >= (uint32_t)p.vocab)) {
 #pragma unroll
-    for (int u = 0; u < SORT_BATCH; ++u) take(id[u], rb + 32 * u + lane, true);
+      for (int u = 0; u < SORT_IDS; ++u) id[u] = clamp_id(id[u], p.vocab);
+    }
+    uint32_t m = 0;                              // which of them are this block's
+    if (whole && n_log2 <= 7) {                  // blocks of four tokens as bytes of at most 127: compared all at once
+      uint32_t in[2], geq[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t c = __byte_perm(__byte_perm(id[4 * k], id[4 * k + 1], 0x0040), __byte_perm(id[4 * k + 2], id[4 * k + 3], 0x0040), 0x5410) &
+                           (uint32_t)mask * 0x01010101u;
+        geq[k] = ((c | 0x80808080u) - jj) & 0x80808080u;
+        in[k] = (0x80808080u - (c ^ jj)) & 0x80808080u;
+      }
+      less += SORT_IDS - __popc(geq[0] | geq[1] >> 1);
+      m = ((in[0] >> 7) * 0x10204080u) >> 28 | ((in[1] >> 7) * 0x10204080u) >> 28 << 4;    // bits 7, 15, 23, 31 side by side
+    } else {
+#pragma unroll
+      for (int u = 0; u < SORT_IDS; ++u) {
+        const int cls = first + u < r1 ? id[u] & mask : INT_MAX;
+        less += cls < j;
+        m |= (uint32_t)(cls == j) << u;
+      }
+    }
+    if (__any_sync(0xffffffffu, m)) {
+      const int n = __popc(m);
+      int at = listed;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {              // n <= 8 summed over the lanes, bit by bit
+        const unsigned v = __ballot_sync(0xffffffffu, n >> k & 1);
+        at += __popc(v & below) << k;
+        listed += __popc(v) << k;
+      }
+#pragma unroll
+      for (int u = 0; u < SORT_IDS; ++u)
+        if (m >> u & 1) {
+          const int lt = id[u] >> n_log2;
+          atomicAdd(&mine[lt], 1);
+          if (at < SORT_LIST) list[at] = (uint32_t)(first + u - r0) << 10 | (uint32_t)lt;
+          ++at;
+        }
+    }
   }
-  for (; rb < r1; rb += 32) take(rb + lane < r1 ? p.ids[rb + lane] : 0, rb + lane, rb + lane < r1);
   less = __reduce_add_sync(0xffffffffu, less);
   if (lane == 0 && less) atomicAdd(&less_sum, less);
-  if (bad && status && j == 0) atomicOr(status, ST_LABEL_RANGE);
+  if (most >= (uint32_t)p.vocab && status && j == 0) atomicOr(status, ST_LABEL_RANGE);
   __syncthreads();
   // per token: where each warp's rows begin; over the tokens: where each token's rows begin
   int carry = less_sum;
@@ -256,12 +305,20 @@ __global__ void __launch_bounds__(SORT_WARPS * 32, 1) embed_sort_kernel(EmbedBwd
     carry += all;
     __syncthreads();
   }
-  const bool fits = listed <= SORT_LIST;
+  const bool fits = listed <= SORT_LIST && stretch <= 1 << 22;
   const int steps = fits ? listed : r1 - r0;
   for (int b = 0; b < steps; b += 32) {
     const int i = b + lane;
-    const int r = i < steps ? (fits ? list[i] : r0 + i) : 0, t = i < steps ? clamp_id(p.ids[r], p.vocab) : 0;
-    const bool in = i < steps && (t & mask) == j;
+    int r = r0, t = 0;
+    bool in = i < steps;
+    if (in && fits) {
+      r += (int)(list[i] >> 10);
+      t = (int)(list[i] & 1023) << n_log2 | j;
+    } else if (in) {
+      r += i;
+      t = clamp_id(p.ids[r], p.vocab);
+      in = (t & mask) == j;
+    }
     if (__ballot_sync(0xffffffffu, in) == 0) continue;
     const int lt = in ? t >> n_log2 : ~lane;
     const unsigned peers = __match_any_sync(0xffffffffu, lt);
@@ -437,22 +494,27 @@ cudaError_t run_sort_and_sum(const EmbedBwdProb& p, int P, int chunks, int pos_p
   const int local = (int)(((long long)p.vocab + (1 << n_log2) - 1) >> n_log2);
   const size_t smem = ((size_t)SORT_WARPS * (local | 1) + 2 * (size_t)local + SORT_WARPS * SORT_LIST) * sizeof(int);
   static SmemLimit limit;
-  cudaError_t e = limit.raise((const void*)embed_sort_kernel<T, VEC>,
+  cudaError_t e = limit.raise((const void*)embed_sort_kernel,
                               (SORT_WARPS * (SORT_MAX_LOCAL | 1) + 2 * SORT_MAX_LOCAL + SORT_WARPS * SORT_LIST) * (int)sizeof(int));
   if (e != cudaSuccess) return e;
   // The position gradient reads dh a second time.  While dh stays in the L2 cache (126 MB) that is cheap, and it rides with
-  // the sums; a larger one is read under the sort, which leaves the memory idle.  ([8192, 512]: 15 against 20 us with
-  // the sort; [65536, 1024]: 104 against 93.)
+  // the sums; a larger one is read beside the sort, which leaves the memory idle: on the SMs that have no sorting block, and
+  // on the others as those end.  ([8192, 512]: 15 against 20 us with the sort; [65536, 1024]: 104 against 91 in the
+  // sort's own launch and 88 in one beside it; with few enough registers to share the SMs with it 93 to 99, since the sort
+  // then waits for its ids.)
   const long long pos_work = p.dpos ? (long long)p.T * pos_pieces : 0;
-  const bool early = (size_t)p.rows * p.d * sizeof(T) > ((size_t)64 << 20);
-  const int groups_log2 = 10 - ll;               // of a block of 1024 threads
-  int split = 0;                                 // groups per sum: until there is a block for every SM
-  while (split < groups_log2 && (pos_work << split >> groups_log2) < 148) ++split;
-  const long long pos_blocks = early ? ((pos_work << split) + (1 << groups_log2) - 1) >> groups_log2 : 0;
-  const long long pos_late = early ? 0 : (pos_work + per_block - 1) / per_block;
-  e = launch_after(embed_sort_kernel<T, VEC>, dim3((unsigned)((1 << n_log2) + pos_blocks)), SORT_WARPS * 32, smem, s, p, n_log2, local, PIECES * P, d_status, ll,
-                    split, pos_pieces);
+  const bool early = pos_work > 0 && (size_t)p.rows * p.d * sizeof(T) > ((size_t)64 << 20);
+  e = launch_after(embed_sort_kernel, dim3(1u << n_log2), SORT_WARPS * 32, smem, s, p, n_log2, local, PIECES * P, d_status, early);
   if (e != cudaSuccess) return e;
+  if (early) {
+    const int groups_log2 = 8 - ll;              // of a block
+    int split = 0;                               // groups per sum: until every SM has four blocks
+    while (split < groups_log2 && (pos_work << split >> groups_log2) < 4 * 148) ++split;
+    const long long blocks = ((pos_work << split) + (1 << groups_log2) - 1) >> groups_log2;
+    e = launch_after(embed_pos_kernel<T, VEC>, dim3((unsigned)blocks), POS_THREADS, 0, s, p, ll, split, pos_pieces);
+    if (e != cudaSuccess) return e;
+  }
+  const long long pos_late = early ? 0 : (pos_work + per_block - 1) / per_block;
   const int sum_blocks = (chunks + per_block - 1) / per_block;
   const long long zero_blocks = ((long long)p.vocab + ZERO_ROWS - 1) / ZERO_ROWS;
   const dim3 grid((unsigned)(sum_blocks + pos_late + zero_blocks), (unsigned)((vecs + (1 << ll) - 1) >> ll));

@@ -104,6 +104,41 @@ def test_embedding_ids_out_of_range_are_clamped_and_flagged():
     assert flag.item() == 0
 
 
+@pytest.mark.parametrize("rows,vocab,d,T,dt,kind,off", [
+    (70001, 1000, 512, 333, "bf16", "zipf", 0), (70001, 130, 512, 64, "bf16", "zipf", 1), (66000, 150000, 8, 0, "fp32", "uniform", 0),
+    (66000, 131072, 8, 5, "fp32", "zipf", 3), (33333, 6, 520, 1000, "fp32", "uniform", 0), (270000, 3, 16, 700, "bf16", "same", 0),
+])
+def test_embedding_gradient_of_many_rows(rows, vocab, d, T, dt, kind, off):
+    """Rows enough for whole batches of ids in every warp and for a gradient beyond the cache (its position sums then run
+    beside the sort); ids from an unaligned address, some of them out of range; equal bits on a second call."""
+    code, td, _ = DT[dt]
+    g = np.random.default_rng(rows + vocab)
+    ids = make_ids(g, rows, vocab, kind)
+    ids[g.integers(0, rows, 9)] = -5
+    ids[rows - 1] = vocab
+    t_ids = shifted((rows,), torch.int32, off, 0)
+    t_ids.copy_(cu(ids, torch.int32))
+    dout = torch.randn(rows, d, device="cuda").to(td)
+    ws = torch.full((lp.lp_embed_workspace_bytes(rows, vocab, d),), 255, dtype=torch.uint8, device="cuda")
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    runs = []
+    for _ in range(2):
+        dtab, dpos = torch.full((vocab, d), float("nan"), device="cuda"), torch.full((max(T, 1), d), float("nan"), device="cuda")
+        lp.lp_embed_backward(code, t_ids, dout, dtab, dpos if T else None, rows, vocab, d, T, 0.5, flag, ws, ws.numel())
+        runs.append((dtab, dpos))
+    assert flag.item() == 1
+    assert torch.equal(runs[0][0], runs[1][0]) and (not T or torch.equal(runs[0][1], runs[1][1]))
+    x, at = dout.double(), t_ids.long().clamp(0, vocab - 1)
+    count = torch.bincount(at, minlength=vocab)[:, None]
+    zeros = lambda n: torch.zeros(n, d, dtype=torch.float64, device="cuda")
+    want, mag = zeros(vocab).index_add_(0, at, x), zeros(vocab).index_add_(0, at, x.abs())
+    assert ((dtab.double() - 0.5 * want).abs() <= 0.5 * (count + 2) * U32 * mag).all()
+    if T:
+        at = torch.arange(rows, device="cuda") % T
+        want, mag = zeros(T).index_add_(0, at, x), zeros(T).index_add_(0, at, x.abs())
+        assert ((dpos.double() - want).abs() <= (rows / T + 2) * U32 * mag).all()
+
+
 # ------------------------------------------------------------------------------------------------ dropout
 @pytest.mark.parametrize("dt", ["fp32", "bf16"])
 @pytest.mark.parametrize("n,p,resid,off,offset", [
