@@ -25,6 +25,8 @@
 // used, with three blocks of four warps per SM; the rest are the waits of the chains ldmatrix, mma, scaling, mma.  Four
 // blocks (one buffer of tiles, 128 registers) were no faster, eight warps with half of the columns each slower (14.4
 // against 12.0 us on [32, 256, 8]).
+// The scans of dk and dv in one, for the state they share (five tiles, two blocks per SM, 240 registers): 50 against 52 us on
+// [16, 512, 16] and 168 against 177 on [64, 512, 16], but 45 against 40 on [12, 512, 16] and 71 against 51 on [3, 2048, 16].
 // On tcgen05 (chunks of 128, accumulators in tensor memory, TMA, eight row warps and two issuing ones, two blocks per
 // SM) the same scan was right and slower: 154 / 243 us on the two cases above.  Every chunk is a chain of four short
 // products with row work between them; a product of N = 64 and K = 128 took its issuing thread 2000 to 2600 clocks with
