@@ -490,6 +490,12 @@ int piece_rows(int rows, int d) {
 }
 // Pieces of a position's rows: only where the positions alone would not give every SM two workers.
 int pos_pieces_for(int rows, int T) { return T >= 296 ? 1 : (int)(((rows + T - 1) / T + POS_PIECE - 1) / POS_PIECE); }
+bool pos_beside_sort(const EmbedBwdProb& p, size_t elem) { return p.dpos && (size_t)p.rows * p.d * elem > ((size_t)64 << 20); }
+// What the last launch has to do at most: tokens of several pieces, positions of several pieces.
+struct Joins { int tokens, positions; };
+Joins joins_of(const EmbedBwdProb& p) {
+  return Joins{p.rows / (PIECES * piece_rows(p.rows, p.d) + 1), p.dpos && pos_pieces_for(p.rows, p.T) > 1 ? p.T : 0};
+}
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 template <typename T, int VEC>
@@ -510,7 +516,7 @@ cudaError_t run_sort_and_sum(const EmbedBwdProb& p, int P, int chunks, int pos_p
   // sort's own launch and 88 in one beside it; with few enough registers to share the SMs with it 93 to 99, since the sort
   // then waits for its ids.)
   const long long pos_work = p.dpos ? (long long)p.T * pos_pieces : 0;
-  const bool early = pos_work > 0 && (size_t)p.rows * p.d * sizeof(T) > ((size_t)64 << 20);
+  const bool early = pos_beside_sort(p, sizeof(T));
   e = launch_after(embed_sort_kernel, dim3(1u << n_log2), SORT_WARPS * 32, smem, s, p, n_log2, local, PIECES * P, d_status, early);
   if (e != cudaSuccess) return e;
   if (early) {
@@ -552,6 +558,11 @@ size_t embed_bwd_workspace(int rows, int vocab, int d) {
          up256(pos_rows * d * sizeof(float)) + 256 + up256(chunks * sizeof(int2));
 }
 
+int embed_bwd_launches(const EmbedBwdProb& p, bool is_bf16) {
+  const Joins joins = joins_of(p);
+  return 2 + (pos_beside_sort(p, is_bf16 ? 2 : 4) ? 1 : 0) + (joins.tokens + joins.positions > 0 ? 1 : 0);
+}
+
 cudaError_t launch_embed_bwd(EmbedBwdProb p, void* workspace, int* d_status, bool is_bf16, cudaStream_t s) {
   const int P = piece_rows(p.rows, p.d), chunks = (int)(((long long)p.rows + P - 1) / P), pos_pieces = p.dpos ? pos_pieces_for(p.rows, p.T) : 0;
   char* w = (char*)workspace;
@@ -568,10 +579,10 @@ cudaError_t launch_embed_bwd(EmbedBwdProb p, void* workspace, int* d_status, boo
   if (is_bf16) e = vec ? run_sort_and_sum<bf16, 8>(p, P, chunks, pos_pieces, d_status, s) : run_sort_and_sum<bf16, 1>(p, P, chunks, pos_pieces, d_status, s);
   else e = vec ? run_sort_and_sum<float, 4>(p, P, chunks, pos_pieces, d_status, s) : run_sort_and_sum<float, 1>(p, P, chunks, pos_pieces, d_status, s);
   if (e != cudaSuccess) return e;
-  const int most_long = p.rows / (PIECES * P + 1), positions = pos_pieces > 1 ? p.T : 0;
-  if (most_long + positions == 0) return cudaSuccess;
-  return launch_after(embed_combine_kernel, dim3((unsigned)std::min(most_long + positions, 148), (unsigned)((p.d + COMBINE_COLS - 1) / COMBINE_COLS)),
-                      COMBINE_WARPS * 32, 0, s, p, P, positions, pos_pieces);
+  const Joins joins = joins_of(p);
+  if (joins.tokens + joins.positions == 0) return cudaSuccess;
+  return launch_after(embed_combine_kernel, dim3((unsigned)std::min(joins.tokens + joins.positions, 148), (unsigned)((p.d + COMBINE_COLS - 1) / COMBINE_COLS)),
+                      COMBINE_WARPS * 32, 0, s, p, P, joins.positions, pos_pieces);
 }
 
 }  // namespace lp

@@ -162,6 +162,7 @@ struct EmbedBwdProb {
   int2* sorted; int2* seg; float* part; float* pos_part; int* n_long; int2* long_list;
 };
 size_t embed_bwd_workspace(int rows, int vocab, int d);
+int embed_bwd_launches(const EmbedBwdProb& p, bool is_bf16);
 cudaError_t launch_embed_bwd(EmbedBwdProb p, void* workspace, int* d_status, bool is_bf16, cudaStream_t s);
 
 // ---------------------------------------------------------------------------- dropout, linear attention

@@ -428,7 +428,7 @@ void build_lm(Handle& h) {
         if (!inner && it.c == &cb[0] && it.b == &cb[0].blocks[0]) {
           EmbedBwdProb e{(const int*)h.x_in, cb[0].G0, h.G("c0.tok"), h.G("c0.pos"), M, T, d, V, tok_scale, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
           if (drop_p > 0.f) emit_dropout(p, {DropItem{cb[0].G0, nullptr, cb[0].G0, 0}});
-          p.add(3, [e, emb_ws, bf](const RunCtx& c) { launch_embed_bwd(e, emb_ws, nullptr, bf, c.stream); }, KIND_EMBED, (double)M * d * es + 4.0 * V * d);
+          p.add(embed_bwd_launches(e, bf), [e, emb_ws, bf](const RunCtx& c) { launch_embed_bwd(e, emb_ws, nullptr, bf, c.stream); }, KIND_EMBED, (double)M * d * es + 4.0 * V * d);
         }
     }
     // ---- overlapping updates (Sec. 3, Fig. 2 c): chunk k's loss, whose gradient at the chunk input now sits in
