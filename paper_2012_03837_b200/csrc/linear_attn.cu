@@ -320,13 +320,15 @@ __global__ void __launch_bounds__(128) la_forward_short_kernel(LinAttnArgs p) {
   scan_short<3, false>(p, sp, p.q, p.k, p.v, p.o, p.state_in ? p.state_in + so : nullptr, false, p.state_out ? p.state_out + so : nullptr, smem);
 }
 
-// Three scans of every sequence and head: dq, dk, dv.
-__global__ void __launch_bounds__(128) la_backward_short_kernel(LinAttnArgs p) {
+// Scans of every sequence and head: dq, dk, dv (0, 1, 2), `scans` of them from `first` on.  dk's and dv's both begin with
+// dstate_out, each in a block of its own, and dv's ends with dstate_in: where that is the same memory, dv's scans have to
+// be a launch behind the other two (one_launch below).
+__global__ void __launch_bounds__(128) la_backward_short_kernel(LinAttnArgs p, int first, int scans) {
   extern __shared__ __align__(128) char smem[];
   cudaGridDependencySynchronize();
-  const int which = blockIdx.x % 3;
-  const Span sp = span_of(p, blockIdx.x / 3);
-  const size_t so = (size_t)(blockIdx.x / 3) * TILE;
+  const int which = first + blockIdx.x % scans, item = blockIdx.x / scans;
+  const Span sp = span_of(p, item);
+  const size_t so = (size_t)item * TILE;
   const float* r_in = p.dstate_out ? p.dstate_out + so : nullptr;
   if (which == 0) scan_short<1, false>(p, sp, p.dout, p.v, p.k, p.dq, p.state_in ? p.state_in + so : nullptr, true, nullptr, smem);
   else if (which == 1) scan_short<1, true>(p, sp, p.v, p.dout, p.q, p.dk, r_in, true, nullptr, smem);
@@ -515,12 +517,12 @@ __global__ void __launch_bounds__(128, TERMS == 3 ? 2 : 3) la_forward_kernel(Lin
   scan<TERMS>(sp.t1 - sp.t0, run_of(p.q, sp, false), run_of(p.k, sp, false), run_of(p.v, sp, false), run_of(p.o, sp, false), false, p.log_decay[sp.h],
               p.scale, in, false, p.seg_states || !p.state_out ? nullptr : p.state_out + so, smem);
 }
-// Three scans of every segment: dq, dk, dv.
+// Scans of every segment: dq, dk, dv, as in la_backward_short_kernel.
 template <int TERMS>
-__global__ void __launch_bounds__(128, TERMS == 3 ? 2 : 3) la_backward_kernel(LinAttnArgs p) {
+__global__ void __launch_bounds__(128, TERMS == 3 ? 2 : 3) la_backward_kernel(LinAttnArgs p, int first, int scans) {
   extern __shared__ __align__(128) char smem[];
   cudaGridDependencySynchronize();
-  const int which = blockIdx.x % 3, item = blockIdx.x / 3;
+  const int which = first + blockIdx.x % scans, item = blockIdx.x / scans;
   const Span sp = span_of(p, item);
   const size_t so = ((size_t)sp.b * p.H + sp.h) * TILE;
   const float* s_in = p.seg_states ? p.seg_states + (size_t)item * TILE : p.state_in ? p.state_in + so : nullptr;
@@ -698,10 +700,19 @@ cudaError_t launch_linattn_step(const LinAttnArgs& a, cudaStream_t s) {
 
 cudaError_t launch_linattn(LinAttnArgs a, bool backward, void* workspace, cudaStream_t s) {
   const int bh = a.B * a.H;
+  // The backward pass of `items` spans.  Without segments the gradient of the incoming state is written by dv's scans while dk's
+  // may still have to read the outgoing one: two launches where the caller gave one buffer for both (with segments the
+  // join has read and written it before, and the scans begin with the workspace).
+  auto run_backward = [&](void (*kernel)(LinAttnArgs, int, int), int items, size_t smem) {
+    const bool one_launch = a.n_seg > 1 || !a.dstate_in || a.dstate_in != a.dstate_out;
+    if (one_launch) return launch_after(kernel, dim3((unsigned)(3 * items)), 128, smem, s, a, 0, 3);
+    const cudaError_t e = launch_after(kernel, dim3((unsigned)(2 * items)), 128, smem, s, a, 0, 2);
+    return e != cudaSuccess ? e : launch_after(kernel, dim3((unsigned)items), 128, smem, s, a, 2, 1);
+  };
   if (a.T <= C) {
     a.n_seg = 1;
     a.seg_len = C;
-    return launch_after(backward ? la_backward_short_kernel : la_forward_short_kernel, dim3((unsigned)(backward ? 3 * bh : bh)), 128, SHORT_SMEM, s, a);
+    return backward ? run_backward(la_backward_short_kernel, bh, SHORT_SMEM) : launch_after(la_forward_short_kernel, dim3((unsigned)bh), 128, SHORT_SMEM, s, a);
   }
   const Layout l = choose_layout(bh, a.T, backward ? 3 : 1);
   a.n_seg = l.n_seg;
@@ -720,9 +731,15 @@ cudaError_t launch_linattn(LinAttnArgs a, bool backward, void* workspace, cudaSt
   }
   const bool three = leaves && a.n_seg == 1;     // otherwise the state that leaves comes from the segments
   static SmemLimit limit[4];
-  auto kernel = backward ? (three ? la_backward_kernel<3> : la_backward_kernel<2>) : three ? la_forward_kernel<3> : la_forward_kernel<2>;
-  e = limit[backward * 2 + three].raise((const void*)kernel, SCAN_SMEM);
-  return e != cudaSuccess ? e : launch_after(kernel, dim3((unsigned)((long long)bh * a.n_seg * (backward ? 3 : 1))), 128, (size_t)SCAN_SMEM, s, a);
+  SmemLimit& lim = limit[backward * 2 + three];
+  if (backward) {
+    auto kernel = three ? la_backward_kernel<3> : la_backward_kernel<2>;
+    e = lim.raise((const void*)kernel, SCAN_SMEM);
+    return e != cudaSuccess ? e : run_backward(kernel, bh * a.n_seg, SCAN_SMEM);
+  }
+  auto kernel = three ? la_forward_kernel<3> : la_forward_kernel<2>;
+  e = lim.raise((const void*)kernel, SCAN_SMEM);
+  return e != cudaSuccess ? e : launch_after(kernel, dim3((unsigned)(bh * a.n_seg)), 128, SCAN_SMEM, s, a);
 }
 
 }  // namespace lp

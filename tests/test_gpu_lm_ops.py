@@ -546,3 +546,31 @@ def test_linear_attention_does_not_depend_on_what_shared_memory_held():
                                         la_workspace(1, B, T, H))
             outs.append(g + [ds])
         assert all(torch.equal(x, y) and torch.isfinite(x).all() for x, y in zip(*outs))
+
+
+@pytest.mark.parametrize("T", [1, 9, 64, 70, 130, 512])
+def test_the_states_gradient_may_overwrite_the_one_it_came_from(T):
+    """dstate_in in dstate_out's buffer, for sequences that are not cut into segments: dk's scans still read the gradient of
+    the outgoing state, whatever dv's scans have written by then.  The same bits as from a buffer of its own, many times."""
+    B, H = 20, 16
+    t = la_inputs(B, T, H, 40 + T)
+    lens = np.array([T if b % 3 else (b * 7) % (T + 1) for b in range(B)], dtype=np.int32)
+    assert lp.lp_linear_attention_workspace_bytes(lp.LP_LINATTN_BACKWARD, B, T, H) == 0
+    base = dict(q=t["q"], k=t["k"], v=t["v"], dout=t["dout"], log_decay=t["log_decay"], scale=0.125, state_in=t["state_in"],
+                lengths=cu(lens, torch.int32))
+    grads = lambda: {n: torch.full((B, T, H, 64), 7.0, dtype=torch.bfloat16, device="cuda") for n in ("dq", "dk", "dv")}
+    want, s_want = grads(), torch.full((B, H, 64, 64), float("nan"), device="cuda")
+    lp.lp_linear_attention_bf16(lp.LP_LINATTN_BACKWARD, dict(base, dstate_out=t["dstate_out"], dstate_in=s_want, **want))
+    for _ in range(8):
+        got, s = grads(), t["dstate_out"].clone()
+        lp.lp_linear_attention_bf16(lp.LP_LINATTN_BACKWARD, dict(base, dstate_out=s, dstate_in=s, **got))
+        assert torch.equal(s, s_want)
+        for n in want:
+            assert torch.equal(got[n], want[n]), n
+    if T == 9:                                       # and the buffers of their own hold the formula's values
+        q, k, v, do = (np64(t[n]) for n in ("q", "k", "v", "dout"))
+        args = np64(t["log_decay"]), 0.125
+        refs = O.linear_attention_bwd(q, k, v, do, *args, np64(t["state_in"]), np64(t["dstate_out"]), lens)
+        mags = O.linear_attention_bwd(abs(q), abs(k), abs(v), abs(do), *args, abs(np64(t["state_in"])), abs(np64(t["dstate_out"])), lens)
+        for i, n in enumerate(("dq", "dk", "dv")):
+            check_tokens(n, got[n], refs[i], mags[i], lens, 7.0, True)
