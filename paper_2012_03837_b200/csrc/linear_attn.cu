@@ -40,11 +40,12 @@ namespace lp {
 namespace {
 
 // l^n for n >= 0, l = exp(lg), l^0 = 1 also for l = 0.  n lg is formed as a product and its rounding error, so that
-// the error of the result stays that of one expf.
+// the error of the result stays that of one expf.  A power of 0 takes no correction: of an n lg beyond fp32's range the
+// rounding error is infinite, of lg = -infinity it is no number.
 __device__ __forceinline__ float decay_pow(float lg, float n) {
   if (n == 0.f) return 1.f;
   const float x = n * lg, r = fmaf(n, lg, -x), e = expf(x);
-  return r == r ? fmaf(e, r, e) : e;             // lg = -infinity: no correction
+  return e > 0.f ? fmaf(e, r, e) : e;
 }
 
 // Tokens [t0, t1) of sequence (b, h) that a block covers.

@@ -574,3 +574,22 @@ def test_the_states_gradient_may_overwrite_the_one_it_came_from(T):
         mags = O.linear_attention_bwd(abs(q), abs(k), abs(v), abs(do), *args, abs(np64(t["state_in"])), abs(np64(t["dstate_out"])), lens)
         for i, n in enumerate(("dq", "dk", "dv")):
             check_tokens(n, got[n], refs[i], mags[i], lens, 7.0, True)
+
+
+@pytest.mark.parametrize("lg", [float(np.finfo(np.float32).min), -1e37, -2e36, -200.0])
+@pytest.mark.parametrize("B,T,H", [(2, 9, 2), (1, 64, 1), (3, 130, 2), (20, 1100, 6), (1, 2100, 1)])
+def test_decays_whose_powers_overflow_their_exponent(B, T, H, lg):
+    """exp of anything below -104 is 0 in fp32, so such a decay is one of minus infinity, bit for bit, also where a multiple of
+    it is no finite number any more; in one chunk, in several, in segments."""
+    t = la_inputs(B, T, H, 90 + T)
+    outs = []
+    for value in (lg, -np.inf):
+        o = {n: torch.zeros(B, T, H, 64, dtype=torch.bfloat16, device="cuda") for n in ("o", "dq", "dk", "dv")}
+        s, ds = torch.zeros(B, H, 64, 64, device="cuda"), torch.zeros(B, H, 64, 64, device="cuda")
+        base = dict(q=t["q"], k=t["k"], v=t["v"], scale=0.125, state_in=t["state_in"], log_decay=torch.full((H,), value, device="cuda"))
+        lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, dict(base, o=o["o"], state_out=s), la_workspace(0, B, T, H))
+        lp.lp_linear_attention_bf16(lp.LP_LINATTN_BACKWARD, dict(base, dout=t["dout"], dq=o["dq"], dk=o["dk"], dv=o["dv"],
+                                    dstate_out=t["dstate_out"], dstate_in=ds), la_workspace(1, B, T, H))
+        outs.append([*o.values(), s, ds])
+    for a, b in zip(*outs):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
