@@ -102,11 +102,16 @@ typedef struct {
      never stored: key dropout_seed, counter {i / 4 (low, high word), site, step} for element i of the [batch, seq_len,
      d_model] tensor; site 0 is the embedding, 1 + 2 n the attention branch and 2 + 2 n the feed-forward branch of the
      model's n-th block; step is the number of lp_step calls before this one (mod 2^32), which a checkpoint carries on.
-     lp_forward and lp_evaluate drop nothing.  Pieces of a chain on several GPUs take seeds of their own. */
+     lp_forward and lp_evaluate drop nothing. */
   float dropout;
   unsigned long long dropout_seed;
   /* LM: factor of the token embedding before the position is added (0: 1). */
   float embed_scale;
+  /* LM with dropout, pieces of a chain on several GPUs: blocks of the chain before this piece, added to n, and steps that
+     the chain had taken before this piece's first one, added to step (both 0 for a whole model).  With one seed for the chain
+     every block then draws masks of its own, the ones it would draw inside the whole model. */
+  int first_block;
+  int first_step;
 } lp_model_spec;
 
 /* Auxiliary head of every chunk (Sec. 3: same form as the global objective): softmax

@@ -152,7 +152,8 @@ class LocalUpdateOracle:
 
     def _drop(self, x, site):
         """x with the elements that this step drops at `site` set to 0 and the others divided by 1 - p; and the
-        factors, which the gradient is multiplied by.  Sites: 0 embedding, 1 + 2n and 2 + 2n the branches of block n."""
+        factors, which the gradient is multiplied by.  Sites: 0 embedding, 1 + 2n and 2 + 2n the branches of block n,
+        counted from the start of the chain that the model may be a piece of."""
         if self.drop_step is None:
             return x, None
         pr = float(np.float32(self.cfg["dropout"]))      # the specification holds it in 32 bits
@@ -175,7 +176,7 @@ class LocalUpdateOracle:
             qkv, cq = L.linear_fwd(a1.reshape(b * t, d), p[n + ".Wqkv"], p[n + ".bqkv"])
             o, ca = L.attention_fwd(qkv.reshape(b, t, 3 * d), self.cfg["n_heads"])
             r1, co = L.linear_fwd(o.reshape(b * t, d), p[n + ".Wo"], p[n + ".bo"])
-            site = 1 + 2 * int(n.split(".b")[1])
+            site = 1 + 2 * (self.cfg.get("first_block", 0) + int(n.split(".b")[1]))
             r1, f1 = self._drop(r1, site)
             h = h + r1.reshape(b, t, d)
             a2, cl2 = L.layernorm_fwd(h, p[n + ".ln2.g"], p[n + ".ln2.b"])
@@ -390,7 +391,7 @@ class LocalUpdateOracle:
         x = self._cast_input(x)
         losses = np.full(K, np.nan, dtype=np.float64)
         all_grads = [None] * K
-        self.drop_step = self.steps if self.cfg.get("dropout") else None
+        self.drop_step = self.cfg.get("first_step", 0) + self.steps if self.cfg.get("dropout") else None
         if self.overlap and schedule != "sync":
             raise ValueError("overlapping updates are defined for the synchronous schedule")
         if schedule == "sync":

@@ -43,7 +43,8 @@ class lp_model_spec(C.Structure):
                 ("stem_channels", C.c_int), ("stage_channels", C.POINTER(C.c_int)),
                 ("blocks_per_stage", C.c_int), ("gemm_backend", C.c_int), ("input_is_activation", C.c_int),
                 ("block_kind", C.c_int), ("stage_blocks", C.POINTER(C.c_int)), ("dropout", C.c_float),
-                ("dropout_seed", C.c_ulonglong), ("embed_scale", C.c_float)]
+                ("dropout_seed", C.c_ulonglong), ("embed_scale", C.c_float),
+                ("first_block", C.c_int), ("first_step", C.c_int)]
 
 
 class lp_head_spec(C.Structure):
@@ -155,6 +156,7 @@ def specs_from_config(cfg: dict, gemm_backend: int = 0):
         m.n_heads, m.d_ffn = cfg["n_heads"], cfg["d_ffn"]
         m.dropout, m.dropout_seed = cfg.get("dropout", 0.0), cfg.get("dropout_seed", 0)
         m.embed_scale = cfg.get("embed_scale", 0.0)
+        m.first_block, m.first_step = cfg.get("first_block", 0), cfg.get("first_step", 0)
         a = _ints(cfg["blocks_per_chunk"])
         keep.append(a)
         m.blocks_per_chunk = a

@@ -65,6 +65,7 @@ void validate(const lp_model_spec* m, int K, const lp_head_spec* hd, const lp_op
       if (hd->classes != m->vocab) throw ShapeError("LM head classes must equal vocab");
       if (!(m->dropout >= 0.f && m->dropout < 1.f)) throw std::invalid_argument("dropout must be in [0, 1)");
       if (!std::isfinite(m->embed_scale)) throw std::invalid_argument("embed_scale must be finite");
+      if (m->first_block < 0 || m->first_step < 0) throw std::invalid_argument("first_block and first_step must not be negative");
       for (int k = 0; k < K; ++k)
         if (m->blocks_per_chunk[k] < 1) throw ShapeError("every chunk needs at least one block");
       break;
@@ -213,7 +214,7 @@ lp_status run_step(Handle& h, int schedule, cudaStream_t s, const void* x = null
   RunCtx ctx{s, nullptr, h.profiling ? &h.prof : nullptr};
   const bool fused = step_is_fused(h);
   if (x && step_reads_in_place(h, schedule)) { ctx.x = x; ctx.y = y; }
-  ctx.step = (uint32_t)h.step_count;
+  ctx.step = (uint32_t)(h.spec.first_step + h.step_count);
   int launches = 0;
   std::vector<char> active;
   const bool any_idle = prepare_chunks(h, schedule, s, active);

@@ -17,7 +17,7 @@ namespace {
 
 struct BlockBufs {
   std::string name;
-  int index;                   // of the block in the model
+  unsigned index;              // of the block in the model, or in the chain that the model is a piece of
   const void* hin = nullptr;   // set per plan
   void *a1, *qkv, *o, *h1, *a2, *u, *g;
   void* hout_internal;         // output when this is not the chunk's last block
@@ -54,7 +54,7 @@ void build_lm(Handle& h) {
     for (int j = 0; j < h.per_chunk[k]; ++j, ++blk) {
       BlockBufs bb;
       bb.name = "c" + std::to_string(k) + ".b" + std::to_string(blk);
-      bb.index = blk;
+      bb.index = (unsigned)h.spec.first_block + (unsigned)blk;
       const std::string& n = bb.name;
       h.add_tensor(n + ".ln1.g", k, {d}, false);
       h.add_tensor(n + ".ln1.b", k, {d}, false);
@@ -140,7 +140,7 @@ void build_lm(Handle& h) {
 
   // Dropout of [M, d] tensors (training passes only): y = resid + dropped x, a launch per chunk.  The mask follows from
   // the site and the step's number alone, so the backward pass forms it again.
-  struct DropItem { const void* x; const void* resid; void* y; int site; };
+  struct DropItem { const void* x; const void* resid; void* y; uint32_t site; };
   const float drop_p = h.spec.dropout;
   const unsigned long long drop_seed = h.spec.dropout_seed;
   const float tok_scale = h.spec.embed_scale == 0.f ? 1.f : h.spec.embed_scale;
@@ -150,7 +150,7 @@ void build_lm(Handle& h) {
     double bytes = 0;
     for (auto& it : items) {
       args.push_back(DropoutArgs{it.x, it.resid, it.y, (long long)M * d, dropout_threshold((double)drop_p), (float)(1.0 / (1.0 - (double)drop_p)),
-                                 drop_seed, 0, nullptr, (uint32_t)it.site, 0});
+                                 drop_seed, 0, nullptr, it.site, 0});
       bytes += (it.resid ? 3.0 : 2.0) * md;
     }
     p.add((int)args.size(), [args, bf](const RunCtx& c) {

@@ -36,6 +36,10 @@ def stage_config(cfg: dict, r: int, count: int = 1) -> dict:
             c["d_in"] = cfg["chunks"][r - 1][-1]
     elif fam == "lm":
         c["blocks_per_chunk"] = list(cfg["blocks_per_chunk"][r:r + count])
+        # which masks dropout draws: the piece's first block in the chain, and its first step (chunk r's first
+        # minibatch reaches it at iteration r)
+        c["first_block"] = cfg.get("first_block", 0) + sum(cfg["blocks_per_chunk"][:r])
+        c["first_step"] = cfg.get("first_step", 0) + r
     else:
         c["stage_channels"] = list(cfg["stage_channels"][r:r + count])
         if isinstance(cfg["blocks_per_stage"], (list, tuple)):
