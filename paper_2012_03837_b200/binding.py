@@ -368,17 +368,52 @@ def lp_attention_bf16(form: int, qkv, o, lse, dout, dqkv, delta, batch: int, seq
                                         batch, seq_len, n_heads, stream))
 
 
-def _dev(t):
-    """Device address of a CUDA tensor or raw address; anything on the host is refused before a kernel can see it."""
+_kinds = None                                      # torch's types by what the operators below call them
+
+
+def _types():
+    """(element types by LP_* code, int32, float32, the 64-bit integers, bfloat16)"""
+    global _kinds
+    if _kinds is None:
+        import torch
+        _kinds = ({LP_FP32: torch.float32, LP_BF16: torch.bfloat16}, torch.int32, torch.float32, (torch.int64, torch.uint64),
+                  torch.bfloat16)
+    return _kinds
+
+
+def _buffer(what: str, t, kind, n: int):
+    """Device address of n elements: of a contiguous CUDA tensor of type `kind` that has as many, or a raw address as it
+    is.  A tensor of another type, a strided one or a short one would be read as what it is not; host memory is refused
+    before a kernel can see it."""
     if t is None:
         return None
     try:
-        if t.is_cuda:
-            return t.data_ptr()
+        cuda = t.is_cuda
     except AttributeError:
         if isinstance(t, int):
             return t
-    raise LpError(-1, "host memory was given where device memory is needed")
+        raise LpError(-1, f"{what}: host memory was given where device memory is needed") from None
+    if t.dtype is not kind or t.numel() < n or not t.is_contiguous():
+        raise LpError(-2, f"{what} must be contiguous {kind} of at least {n} elements, not {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
+    if not cuda:
+        raise LpError(-1, f"{what}: host memory was given where device memory is needed")
+    return t.data_ptr()
+
+
+def _workspace(what: str, t, nbytes: int):
+    """Device address of nbytes of scratch memory: a contiguous CUDA tensor of any type, or a raw address."""
+    if t is None or isinstance(t, int):
+        return t
+    try:
+        short = t.nbytes < nbytes or not t.is_contiguous()
+        cuda = t.is_cuda
+    except AttributeError:
+        cuda = short = False
+    if short:
+        raise LpError(-1, f"{what}: the workspace must be contiguous and hold {nbytes} bytes")
+    if not cuda:
+        raise LpError(-1, f"{what}: host memory was given where device memory is needed")
+    return t.data_ptr()
 
 
 _lib.lp_embed_forward.argtypes = [C.c_int] + [C.c_void_p] * 4 + [C.c_int] * 4 + [C.c_float, C.c_void_p, C.c_void_p]
@@ -390,10 +425,15 @@ _lib.lp_embed_workspace_bytes.restype = C.c_size_t
 
 def lp_embed_forward(dtype: int, ids, table, pos, out, rows: int, vocab: int, d: int, seq_len: int, scale: float = 1.0,
                      out_of_range=None, stream=None) -> None:
-    """out[r] = scale * table[ids[r]] + pos[r mod seq_len] (see lp.h).  Tensors may be CUDA tensors or raw device
-    pointers; pos and out_of_range may be None."""
-    _check(None, _lib.lp_embed_forward(dtype, _dev(ids), _dev(table), _dev(pos), _dev(out), rows, vocab, d, seq_len, scale,
-                                       _dev(out_of_range), stream))
+    """out[r] = scale * table[ids[r]] + pos[r mod seq_len] (see lp.h).  Contiguous CUDA tensors (ids int32, table, pos and
+    out of the type that `dtype` names) or raw device addresses; pos and out_of_range may be None."""
+    elem, i32, _, _, _ = _types()
+    e, f = elem.get(dtype), "lp_embed_forward: "
+    if e is None:
+        raise LpError(-1, f + "dtype")
+    _check(None, _lib.lp_embed_forward(dtype, _buffer(f + "ids", ids, i32, rows), _buffer(f + "table", table, e, vocab * d),
+                                       _buffer(f + "pos", pos, e, seq_len * d), _buffer(f + "out", out, e, rows * d), rows, vocab, d,
+                                       seq_len, scale, _buffer(f + "out_of_range", out_of_range, i32, 1), stream))
 
 
 def lp_embed_workspace_bytes(rows: int, vocab: int, d: int) -> int:
@@ -403,9 +443,15 @@ def lp_embed_workspace_bytes(rows: int, vocab: int, d: int) -> int:
 def lp_embed_backward(dtype: int, ids, dout, dtable, dpos, rows: int, vocab: int, d: int, seq_len: int, scale: float = 1.0,
                       out_of_range=None, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
     """Gradients of the token table (fp32 [vocab, d], written whole) and, if dpos is given, of the position table,
-    summed over the rows sorted by token (see lp.h)."""
-    _check(None, _lib.lp_embed_backward(dtype, _dev(ids), _dev(dout), _dev(dtable), _dev(dpos), rows, vocab, d, seq_len, scale,
-                                        _dev(out_of_range), _dev(workspace), workspace_bytes, stream))
+    summed over the rows sorted by token (see lp.h).  Tensors as in lp_embed_forward, dtable and dpos fp32."""
+    elem, i32, f32, _, _ = _types()
+    e, f = elem.get(dtype), "lp_embed_backward: "
+    if e is None:
+        raise LpError(-1, f + "dtype")
+    _check(None, _lib.lp_embed_backward(dtype, _buffer(f + "ids", ids, i32, rows), _buffer(f + "dout", dout, e, rows * d),
+                                        _buffer(f + "dtable", dtable, f32, vocab * d), _buffer(f + "dpos", dpos, f32, seq_len * d), rows,
+                                        vocab, d, seq_len, scale, _buffer(f + "out_of_range", out_of_range, i32, 1),
+                                        _workspace(f[:-2], workspace, workspace_bytes), workspace_bytes, stream))
 
 
 _lib.lp_dropout.argtypes = [C.c_int] + [C.c_void_p] * 3 + [C.c_longlong, C.c_double, C.c_ulonglong, C.c_ulonglong, C.c_void_p,
@@ -414,8 +460,15 @@ _lib.lp_dropout.argtypes = [C.c_int] + [C.c_void_p] * 3 + [C.c_longlong, C.c_dou
 
 def lp_dropout(dtype: int, x, resid, y, n: int, p: float, seed: int, offset: int = 0, offset_dev=None, stream=None) -> None:
     """y = resid + dropout(x), the mask drawn from Philox4x32-10 and never stored (see lp.h); the gradient of x is the
-    same call on dy with resid None.  y may be x or resid."""
-    _check(None, _lib.lp_dropout(dtype, _dev(x), _dev(resid), _dev(y), n, p, seed, offset, _dev(offset_dev), stream))
+    same call on dy with resid None.  y may be x or resid.  Contiguous CUDA tensors of the type that `dtype` names and at
+    least n elements (offset_dev: one 64-bit integer), or raw device addresses."""
+    elem, _, _, i64, _ = _types()
+    e, f = elem.get(dtype), "lp_dropout: "
+    if e is None:
+        raise LpError(-1, f + "dtype")
+    word = i64[1] if getattr(offset_dev, "dtype", None) is i64[1] else i64[0]
+    _check(None, _lib.lp_dropout(dtype, _buffer(f + "x", x, e, n), _buffer(f + "resid", resid, e, n), _buffer(f + "y", y, e, n), n, p,
+                                 seed, offset, _buffer(f + "offset_dev", offset_dev, word, 1), stream))
 
 
 LP_LINATTN_FORWARD, LP_LINATTN_BACKWARD, LP_LINATTN_STEP = 0, 1, 2
@@ -433,7 +486,6 @@ class lp_linattn_desc(C.Structure):
 
 _LINATTN_SLOTS = {n: 3 * i for i, n in enumerate(("q", "k", "v", "o", "dout", "dq", "dk", "dv"))}      # three values each
 _LINATTN_SLOTS |= {n: 24 + i for i, n in enumerate(("log_decay", "state_in", "state_out", "dstate_out", "dstate_in", "lengths"))}
-_linattn_types = None                              # torch's bfloat16, float32, int32 (torch is there once a tensor is)
 _linattn_layout = struct.Struct("=24q6Q3if")      # lp_linattn_desc, filled in one go
 assert _linattn_layout.size == C.sizeof(lp_linattn_desc)
 _LINATTN_PACK = _linattn_layout.pack
@@ -451,11 +503,7 @@ def lp_linear_attention_bf16(form: int, desc: dict, workspace=None, stream=None)
     tensors of lp_linattn_desc: q, k, v, o, dout, dq, dk, dv are bf16 CUDA tensors [batch, seq_len, n_heads, 64] (slices
     of larger ones are fine: strides are read off), the states fp32 [batch, n_heads, 64, 64], log_decay fp32 [n_heads],
     lengths int32 [batch]; `scale` a number (default 1).  Sizes come from q; the other tensors' shapes must agree."""
-    global _linattn_types
-    if _linattn_types is None:
-        import torch
-        _linattn_types = torch.bfloat16, torch.float32, torch.int32
-    bf16, f32, i32 = _linattn_types
+    _, i32, f32, _, bf16 = _types()
     q, scale = desc.get("q"), 1.0
     if q is None or q.dtype is not bf16 or q.ndim != 4:
         raise LpError(-2, "lp_linear_attention_bf16: q must be bf16 [batch, seq_len, n_heads, 64]")
@@ -480,13 +528,13 @@ def lp_linear_attention_bf16(form: int, desc: dict, workspace=None, stream=None)
                 raise LpError(-3, f"lp_linear_attention_bf16: the heads of {name} must lie 64 elements apart")
             v[at], v[at + 1], v[at + 2] = t.data_ptr(), sb, st
         else:
-            n, kind = (H, f32) if at == 24 else (B, i32) if at == 29 else (4096 * B * H, f32)
-            if t.dtype is not kind or t.numel() != n or not t.is_contiguous():
-                raise LpError(-2, f"lp_linear_attention_bf16: {name} has the wrong type or size or is not contiguous")
+            of, kind = ((H,), f32) if at == 24 else ((B,), i32) if at == 29 else ((B, H, 64, 64), f32)
+            if t.dtype is not kind or t.shape != of or not t.is_contiguous():
+                raise LpError(-2, f"lp_linear_attention_bf16: {name} must be contiguous {kind} {list(of)}")
             v[at] = t.data_ptr()
     nbytes = workspace.nbytes if workspace is not None else 0
-    code = _lib.lp_linear_attention_bf16(form, _LINATTN_PACK(*v, B, T, H, scale), _dev(workspace) if nbytes else None, nbytes,
-                                         stream)
+    code = _lib.lp_linear_attention_bf16(form, _LINATTN_PACK(*v, B, T, H, scale),
+                                         _workspace("lp_linear_attention_bf16", workspace, nbytes) if nbytes else None, nbytes, stream)
     if code:
         _check(None, code)
 

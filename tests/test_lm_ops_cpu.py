@@ -217,3 +217,81 @@ def test_create_refuses_bad_dropout():
         with pytest.raises(lp.LpError) as e:
             lp.lp_create(m, K, hd, op)
         assert lp.LP_ERR[e.value.code] == "INVALID_ARG", kw
+
+
+class OnDevice:
+    """What the binding looks at of a tensor on a GPU, here without one; its address is never read."""
+
+    def __init__(self, shape, dtype, stride=None):
+        import torch
+        t = torch.empty(shape, dtype=dtype, device="meta")
+        if stride is not None:
+            t = t.as_strided(shape, stride)
+        self.t, self.is_cuda, self.dtype, self.shape, self.nbytes, self.ndim = t, True, dtype, t.shape, t.nbytes, t.ndim
+
+    def __getattr__(self, name):                    # numel, stride, is_contiguous
+        return getattr(self.t, name)
+
+    def data_ptr(self):
+        return 256
+
+
+def refused(code, call, *args, says=""):
+    with pytest.raises(lp.LpError) as e:
+        call(*args)
+    assert e.value.code == ERR[code] and says in str(e.value), str(e.value)
+
+
+def test_binding_of_the_lookup_checks_types_and_sizes():
+    import torch
+    i32, i64, f32, b16 = torch.int32, torch.int64, torch.float32, torch.bfloat16
+    rows, vocab, d, T = 12, 7, 16, 4
+    X = OnDevice
+    good = dict(ids=X((3, 4), i32), table=X((vocab, d), b16), pos=X((T, d), b16), out=X((rows, d), b16), flag=X((1,), i32))
+    bad = dict(ids=[X((rows,), i64), X((rows - 1,), i32), X((rows,), i32, (2,)), X((rows,), torch.int16)],
+               table=[X((vocab, d), f32), X((vocab - 1, d), b16), X((vocab, d), b16, (2 * d, 1)), X((vocab, d), torch.float16)],
+               pos=[X((T, d), f32), X((T - 1, d), b16)], out=[X((rows, d), f32), X((rows, d - 1), b16), X((rows, d), b16, (1, rows))],
+               flag=[X((1,), i64), X((0,), i32)])
+    fwd = lambda ids, table, pos, out, flag: lp.lp_embed_forward(lp.LP_BF16, ids, table, pos, out, rows, vocab, d, T, 1.0, flag)
+    for name, cases in bad.items():
+        for t in cases:
+            refused("SHAPE", lambda: fwd(**{**good, name: t}), says="out_of_range" if name == "flag" else name)
+    refused("INVALID_ARG", lambda: lp.lp_embed_forward(7, *[good[n] for n in ("ids", "table", "pos", "out")], rows, vocab, d, T))
+    need = lp.lp_embed_workspace_bytes(rows, vocab, d)
+    good = dict(ids=X((rows,), i32), dout=X((rows, d), f32), dtable=X((vocab, d), f32), dpos=X((T, d), f32), ws=X((need,), torch.uint8))
+    bad = dict(ids=[X((rows,), i64)], dout=[X((rows, d), b16), X((rows - 1, d), f32), X((rows, d), f32, (0, 1))],
+               dtable=[X((vocab, d), b16), X((vocab - 1, d), f32)], dpos=[X((T, d), b16), X((T, d - 1), f32)])
+    bwd = lambda ids, dout, dtable, dpos, ws: lp.lp_embed_backward(lp.LP_FP32, ids, dout, dtable, dpos, rows, vocab, d, T, 1.0, None, ws, need)
+    for name, cases in bad.items():
+        for t in cases:
+            refused("SHAPE", lambda: bwd(**{**good, name: t}), says=name)
+    for ws in (X((need - 1,), torch.uint8), X((need,), torch.uint8, (2,)), X((need // 4 - 1,), f32), torch.zeros(need, dtype=torch.uint8),
+               np.zeros(need, dtype=np.uint8)):
+        refused("INVALID_ARG", lambda: bwd(**{**good, "ws": ws}))
+
+
+def test_binding_of_dropout_checks_types_and_sizes():
+    import torch
+    i64, f32, b16 = torch.int64, torch.float32, torch.bfloat16
+    n, X = 40, OnDevice
+    good = dict(x=X((5, 8), b16), resid=X((n,), b16), y=X((n + 3,), b16), word=X((1,), i64))
+    call = lambda x, resid, y, word: lp.lp_dropout(lp.LP_BF16, x, resid, y, n, 0.1, 1, 0, word)
+    bad = dict(x=[X((n,), f32), X((n - 1,), b16), X((5, 8), b16, (1, 5)), X((n,), b16, (2,))], resid=[X((n,), torch.float16)],
+               y=[X((n,), f32), X((n - 1,), b16)], word=[X((1,), torch.int32), X((1,), f32), X((0,), i64)])
+    for name, cases in bad.items():
+        for t in cases:
+            refused("SHAPE", lambda: call(**{**good, name: t}), says="offset_dev" if name == "word" else name)
+    refused("INVALID_ARG", lambda: lp.lp_dropout(5, good["x"], None, good["y"], n, 0.1, 1))
+    refused("INVALID_ARG", lambda: lp.lp_dropout(lp.LP_BF16, np.zeros(n, dtype=np.float32), None, good["y"], n, 0.1, 1), says="host")
+
+
+def test_binding_of_linear_attention_checks_the_shapes_of_states():
+    import torch
+    B, T, H = 2, 3, 4
+    X = OnDevice
+    t = X((B, T, H, 64), torch.bfloat16)
+    good = dict(q=t, k=t, v=t, o=t, log_decay=X((H,), torch.float32))
+    for change in (dict(state_in=X((H, B, 64, 64), torch.float32)), dict(state_out=X((B * H, 64, 64), torch.float32)),
+                   dict(log_decay=X((2, 2), torch.float32)), dict(lengths=X((1, B), torch.int32))):
+        refused("SHAPE", lambda: lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, {**good, **change}), says=list(change)[0])
+    refused("INVALID_ARG", lambda: lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, good, X((64,), torch.float32, (2,))), says="workspace")
