@@ -102,7 +102,7 @@ typedef struct {
      never stored: key dropout_seed, counter {i / 4 (low, high word), site, step} for element i of the [batch, seq_len,
      d_model] tensor; site 0 is the embedding, 1 + 2 n the attention branch and 2 + 2 n the feed-forward branch of the
      model's n-th block; step is the number of lp_step calls before this one (mod 2^32), which a checkpoint carries on.
-     lp_forward and lp_evaluate drop nothing. */
+     lp_forward and lp_evaluate drop nothing.  Other families refuse anything but 0 (INVALID_ARG). */
   float dropout;
   unsigned long long dropout_seed;
   /* LM: factor of the token embedding before the position is added (0: 1). */

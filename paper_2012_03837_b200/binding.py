@@ -139,6 +139,7 @@ def specs_from_config(cfg: dict, gemm_backend: int = 0):
     m.batch = cfg["batch"]
     m.gemm_backend = gemm_backend
     m.input_is_activation = 1 if cfg.get("input_is_activation") else 0
+    m.dropout = cfg.get("dropout", 0.0)             # of a family that has none it is refused by lp_create
     hd = lp_head_spec()
     if fam == "mlp":
         m.family = LP_FAMILY_MLP
@@ -154,7 +155,7 @@ def specs_from_config(cfg: dict, gemm_backend: int = 0):
         m.family = LP_FAMILY_LM
         m.vocab, m.seq_len, m.d_model = cfg["vocab"], cfg["seq_len"], cfg["d_model"]
         m.n_heads, m.d_ffn = cfg["n_heads"], cfg["d_ffn"]
-        m.dropout, m.dropout_seed = cfg.get("dropout", 0.0), cfg.get("dropout_seed", 0)
+        m.dropout_seed = cfg.get("dropout_seed", 0)
         m.embed_scale = cfg.get("embed_scale", 0.0)
         m.first_block, m.first_step = cfg.get("first_block", 0), cfg.get("first_step", 0)
         a = _ints(cfg["blocks_per_chunk"])

@@ -41,6 +41,7 @@ void validate(const lp_model_spec* m, int K, const lp_head_spec* hd, const lp_op
   if (m->dtype != LP_FP32 && m->dtype != LP_BF16) throw std::invalid_argument("dtype");
   if (o->kind != LP_OPT_SGDM && o->kind != LP_OPT_ADAM) throw std::invalid_argument("optimizer kind");
   if (hd->classes < 2) throw ShapeError("classes must be at least 2");
+  if (m->family != LP_FAMILY_LM && m->dropout != 0.f) throw std::invalid_argument("dropout is for the LM family");
   switch (m->family) {
     case LP_FAMILY_MLP: {
       if (hd->kind != LP_HEAD_LINEAR) throw std::invalid_argument("MLP takes LP_HEAD_LINEAR");

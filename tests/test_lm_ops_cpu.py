@@ -295,3 +295,10 @@ def test_binding_of_linear_attention_checks_the_shapes_of_states():
                    dict(log_decay=X((2, 2), torch.float32)), dict(lengths=X((1, B), torch.int32))):
         refused("SHAPE", lambda: lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, {**good, **change}), says=list(change)[0])
     refused("INVALID_ARG", lambda: lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, good, X((64,), torch.float32, (2,))), says="workspace")
+
+
+@pytest.mark.parametrize("workload", ["c1", "c4"])
+def test_families_without_dropout_refuse_it(workload):
+    import lp_synth
+    for p in (0.1, float("nan")):
+        refused("INVALID_ARG", lambda: lp.lp_create(*lp.specs_from_config(lp_synth.config(workload, dropout=p))), says="dropout")
