@@ -593,3 +593,117 @@ def test_decays_whose_powers_overflow_their_exponent(B, T, H, lg):
         outs.append([*o.values(), s, ds])
     for a, b in zip(*outs):
         assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
+# ------------------------------------------------------------------------------------------------ states handed out, fp32
+def two_terms(x):
+    """x as the sum of two bf16 numbers, which is how operands are split where no state leaves."""
+    hi = torch.tensor(x, dtype=torch.float32).to(torch.bfloat16).float()
+    return (hi + (torch.tensor(x, dtype=torch.float32) - hi).to(torch.bfloat16).float()).item()
+
+
+@pytest.mark.parametrize("B,T,H", [(1, 20, 1), (2, 70, 1), (10, 1100, 12), (1, 2100, 1)])
+def test_states_handed_out_are_exact_to_fp32(B, T, H):
+    """One chunk, several, many, segments.  The factors are chosen so that two bf16 terms would be off by 2^-17: an exact
+    16 * scale (all ones in 16 tokens, no decay: every partial sum has at most 22 bits), and one power of the decay, where
+    expf is off by 2 units in the last place at most (2^-22) and its correction by one rounding."""
+    scale = 1.0 + 2.0 ** -9 + 2.0 ** -17
+    assert abs(two_terms(scale) - scale) == 2.0 ** -17
+    tok = lambda: torch.zeros(B, T, H, 64, dtype=torch.bfloat16, device="cuda")
+    state = lambda: torch.full((B, H, 64, 64), float("nan"), device="cuda")
+    ones, s = tok(), state()
+    ones[:, 2:18] = 1
+    lp.lp_linear_attention_bf16(lp.LP_LINATTN_BACKWARD, dict(q=ones, k=ones, v=ones, dout=ones, dq=tok(), dk=tok(), dv=tok(),
+                                log_decay=torch.zeros(H, device="cuda"), scale=scale, dstate_in=s), la_workspace(1, B, T, H))
+    assert (s == 16 * scale).all()
+    lg = torch.tensor(np.log(0.5 * scale), dtype=torch.float32).item()
+    l = float(np.exp(np.float64(lg)))
+    assert abs(two_terms(l) - l) > 2.0 ** -18 * l
+    one, s = tok(), state()
+    one[:, T - 2] = 1
+    lp.lp_linear_attention_bf16(lp.LP_LINATTN_FORWARD, dict(q=one, k=one, v=one, o=tok(), log_decay=torch.full((H,), lg, device="cuda"),
+                                scale=1.0, state_out=s), la_workspace(0, B, T, H))
+    assert (np.abs(np64(s) - l) <= 2.0 ** -21 * l).all()
+
+
+# ------------------------------------------------------------------------------------------------ position sums beside the sort
+def test_position_sums_beside_the_sort_on_side_streams_and_in_graphs():
+    """More than 64 MiB of incoming gradient: the position sums start while the sort runs.  They come behind what wrote the
+    gradient and before what reads theirs, on two side streams at once and in replays of a graph, where another branch joins
+    in front of them."""
+    rows, vocab, d, T = 70001, 1000, 512, 333
+    g = np.random.default_rng(1)
+    ids = cu(make_ids(g, rows, vocab, "zipf"), torch.int32)
+    x = torch.randn(rows, d, device="cuda").to(torch.bfloat16)
+    n = rows * d
+
+    def call(b, s):                                  # writes b's gradient, sums it, takes the sums on
+        lp.lp_dropout(lp.LP_BF16, x, None, b["dh"], n, 0.3, 8, 0, b["word"], s)
+        lp.lp_embed_backward(lp.LP_BF16, ids, b["dh"], b["dtab"], b["dpos"], rows, vocab, d, T, 0.5, None, b["ws"], b["ws"].numel(), s)
+        lp.lp_dropout(lp.LP_FP32, b["dpos"], None, b["pos_out"], T * d, 0.0, 1, 0, None, s)
+        lp.lp_dropout(lp.LP_FP32, b["dtab"], None, b["tab_out"], vocab * d, 0.0, 1, 0, None, s)
+
+    def buffers():
+        f = lambda *shape: torch.full(shape, float("nan"), device="cuda")
+        return dict(dh=torch.full((rows, d), float("nan"), dtype=torch.bfloat16, device="cuda"), dtab=f(vocab, d), dpos=f(T, d), tab_out=f(vocab, d),
+                    pos_out=f(T, d), word=torch.zeros(1, dtype=torch.int64, device="cuda"),
+                    ws=torch.full((lp.lp_embed_workspace_bytes(rows, vocab, d),), 255, dtype=torch.uint8, device="cuda"))
+
+    def want(word):
+        b = buffers()
+        b["word"] += word
+        call(b, None)
+        torch.cuda.synchronize()
+        at = torch.arange(rows, device="cuda") % T
+        ref = torch.zeros(T, d, dtype=torch.float64, device="cuda").index_add_(0, at, b["dh"].double())
+        mag = torch.zeros(T, d, dtype=torch.float64, device="cuda").index_add_(0, at, b["dh"].double().abs())
+        assert ((b["pos_out"].double() - ref).abs() <= (rows / T + 2) * U32 * mag).all()
+        return b["pos_out"], b["tab_out"]
+
+    first, second = want(0), want(999)
+    assert not torch.equal(first[0], second[0])
+    streams, sets = [torch.cuda.Stream(), torch.cuda.Stream()], [buffers(), buffers()]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for s, b in zip(streams, sets):
+            call(b, s.cuda_stream)
+    torch.cuda.synchronize()
+    for b in sets:
+        assert torch.equal(b["pos_out"], first[0]) and torch.equal(b["tab_out"], first[1])
+    b, graph, other = sets[0], torch.cuda.CUDAGraph(), streams[1]
+    with torch.cuda.graph(graph, stream=streams[0]):
+        other.wait_stream(streams[0])
+        with torch.cuda.stream(other):
+            b["word"] += 999
+        streams[0].wait_stream(other)
+        call(b, streams[0].cuda_stream)
+    for k in ("dh", "dtab", "dpos", "pos_out", "tab_out"):
+        b[k].fill_(float("nan"))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(b["pos_out"], second[0]) and torch.equal(b["tab_out"], second[1])
+    b["word"].fill_(-999)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(b["pos_out"], first[0]) and torch.equal(b["tab_out"], first[1])
+
+
+def test_a_state_gradient_overwritten_in_a_replayed_graph():
+    B, T, H = 8, 70, 16
+    t = la_inputs(B, T, H, 77)
+    g = [torch.zeros(B, T, H, 64, dtype=torch.bfloat16, device="cuda") for _ in range(6)]
+    ds, inplace = torch.zeros(B, H, 64, 64, device="cuda"), t["dstate_out"].clone()
+    base = dict(q=t["q"], k=t["k"], v=t["v"], dout=t["dout"], log_decay=t["log_decay"], scale=0.125, state_in=t["state_in"])
+    lp.lp_linear_attention_bf16(lp.LP_LINATTN_BACKWARD, dict(base, dq=g[0], dk=g[1], dv=g[2], dstate_out=t["dstate_out"], dstate_in=ds))
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=stream):
+        lp.lp_linear_attention_bf16(lp.LP_LINATTN_BACKWARD, dict(base, dq=g[3], dk=g[4], dv=g[5], dstate_out=inplace, dstate_in=inplace), None,
+                                    stream.cuda_stream)
+    for _ in range(3):
+        inplace.copy_(t["dstate_out"])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(inplace, ds)
+        for a, b in zip(g[:3], g[3:]):
+            assert torch.equal(a, b)
