@@ -369,11 +369,11 @@ def lp_attention_bf16(form: int, qkv, o, lse, dout, dqkv, delta, batch: int, seq
                                         batch, seq_len, n_heads, stream))
 
 
-_kinds = None                                      # torch's types by what the operators below call them
+_kinds = None                                      # what _types returns
 
 
 def _types():
-    """(element types by LP_* code, int32, float32, the 64-bit integers, bfloat16)"""
+    """Element types by LP_* code, int32, float32, the 64-bit integers, bfloat16: torch's, which is there once a tensor is."""
     global _kinds
     if _kinds is None:
         import torch
@@ -382,7 +382,7 @@ def _types():
     return _kinds
 
 
-def _buffer(what: str, t, kind, n: int):
+def _buffer(t, kind, n: int, what: str):
     """Device address of n elements: of a contiguous CUDA tensor of type `kind` that has as many, or a raw address as it
     is.  A tensor of another type, a strided one or a short one would be read as what it is not; host memory is refused
     before a kernel can see it."""
@@ -390,31 +390,31 @@ def _buffer(what: str, t, kind, n: int):
         return None
     try:
         cuda = t.is_cuda
+        fits = t.dtype is kind and t.numel() >= n and t.is_contiguous()
+        if fits and cuda:
+            return t.data_ptr()
     except AttributeError:
         if isinstance(t, int):
             return t
-        raise LpError(-1, f"{what}: host memory was given where device memory is needed") from None
-    if t.dtype is not kind or t.numel() < n or not t.is_contiguous():
+        fits = True                                 # no tensor: memory of the host
+    if not fits:
         raise LpError(-2, f"{what} must be contiguous {kind} of at least {n} elements, not {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
-    if not cuda:
-        raise LpError(-1, f"{what}: host memory was given where device memory is needed")
-    return t.data_ptr()
+    raise LpError(-1, f"{what}: host memory was given where device memory is needed")
 
 
-def _workspace(what: str, t, nbytes: int):
+def _workspace(t, nbytes: int, what: str):
     """Device address of nbytes of scratch memory: a contiguous CUDA tensor of any type, or a raw address."""
     if t is None or isinstance(t, int):
         return t
     try:
-        short = t.nbytes < nbytes or not t.is_contiguous()
-        cuda = t.is_cuda
+        fits = t.nbytes >= nbytes and t.is_contiguous()
+        if fits and t.is_cuda:
+            return t.data_ptr()
     except AttributeError:
-        cuda = short = False
-    if short:
+        fits = True
+    if not fits:
         raise LpError(-1, f"{what}: the workspace must be contiguous and hold {nbytes} bytes")
-    if not cuda:
-        raise LpError(-1, f"{what}: host memory was given where device memory is needed")
-    return t.data_ptr()
+    raise LpError(-1, f"{what}: host memory was given where device memory is needed")
 
 
 _lib.lp_embed_forward.argtypes = [C.c_int] + [C.c_void_p] * 4 + [C.c_int] * 4 + [C.c_float, C.c_void_p, C.c_void_p]
@@ -428,13 +428,15 @@ def lp_embed_forward(dtype: int, ids, table, pos, out, rows: int, vocab: int, d:
                      out_of_range=None, stream=None) -> None:
     """out[r] = scale * table[ids[r]] + pos[r mod seq_len] (see lp.h).  Contiguous CUDA tensors (ids int32, table, pos and
     out of the type that `dtype` names) or raw device addresses; pos and out_of_range may be None."""
-    elem, i32, _, _, _ = _types()
-    e, f = elem.get(dtype), "lp_embed_forward: "
+    elem, i32, _, _, _ = _kinds or _types()
+    e = elem.get(dtype)
     if e is None:
-        raise LpError(-1, f + "dtype")
-    _check(None, _lib.lp_embed_forward(dtype, _buffer(f + "ids", ids, i32, rows), _buffer(f + "table", table, e, vocab * d),
-                                       _buffer(f + "pos", pos, e, seq_len * d), _buffer(f + "out", out, e, rows * d), rows, vocab, d,
-                                       seq_len, scale, _buffer(f + "out_of_range", out_of_range, i32, 1), stream))
+        raise LpError(-1, "lp_embed_forward: dtype")
+    _check(None, _lib.lp_embed_forward(dtype, _buffer(ids, i32, rows, "lp_embed_forward: ids"),
+                                       _buffer(table, e, vocab * d, "lp_embed_forward: table"),
+                                       _buffer(pos, e, seq_len * d, "lp_embed_forward: pos"),
+                                       _buffer(out, e, rows * d, "lp_embed_forward: out"), rows, vocab, d, seq_len, scale,
+                                       _buffer(out_of_range, i32, 1, "lp_embed_forward: out_of_range"), stream))
 
 
 def lp_embed_workspace_bytes(rows: int, vocab: int, d: int) -> int:
@@ -445,14 +447,16 @@ def lp_embed_backward(dtype: int, ids, dout, dtable, dpos, rows: int, vocab: int
                       out_of_range=None, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
     """Gradients of the token table (fp32 [vocab, d], written whole) and, if dpos is given, of the position table,
     summed over the rows sorted by token (see lp.h).  Tensors as in lp_embed_forward, dtable and dpos fp32."""
-    elem, i32, f32, _, _ = _types()
-    e, f = elem.get(dtype), "lp_embed_backward: "
+    elem, i32, f32, _, _ = _kinds or _types()
+    e = elem.get(dtype)
     if e is None:
-        raise LpError(-1, f + "dtype")
-    _check(None, _lib.lp_embed_backward(dtype, _buffer(f + "ids", ids, i32, rows), _buffer(f + "dout", dout, e, rows * d),
-                                        _buffer(f + "dtable", dtable, f32, vocab * d), _buffer(f + "dpos", dpos, f32, seq_len * d), rows,
-                                        vocab, d, seq_len, scale, _buffer(f + "out_of_range", out_of_range, i32, 1),
-                                        _workspace(f[:-2], workspace, workspace_bytes), workspace_bytes, stream))
+        raise LpError(-1, "lp_embed_backward: dtype")
+    _check(None, _lib.lp_embed_backward(dtype, _buffer(ids, i32, rows, "lp_embed_backward: ids"),
+                                        _buffer(dout, e, rows * d, "lp_embed_backward: dout"),
+                                        _buffer(dtable, f32, vocab * d, "lp_embed_backward: dtable"),
+                                        _buffer(dpos, f32, seq_len * d, "lp_embed_backward: dpos"), rows, vocab, d, seq_len, scale,
+                                        _buffer(out_of_range, i32, 1, "lp_embed_backward: out_of_range"),
+                                        _workspace(workspace, workspace_bytes, "lp_embed_backward"), workspace_bytes, stream))
 
 
 _lib.lp_dropout.argtypes = [C.c_int] + [C.c_void_p] * 3 + [C.c_longlong, C.c_double, C.c_ulonglong, C.c_ulonglong, C.c_void_p,
@@ -463,13 +467,15 @@ def lp_dropout(dtype: int, x, resid, y, n: int, p: float, seed: int, offset: int
     """y = resid + dropout(x), the mask drawn from Philox4x32-10 and never stored (see lp.h); the gradient of x is the
     same call on dy with resid None.  y may be x or resid.  Contiguous CUDA tensors of the type that `dtype` names and at
     least n elements (offset_dev: one 64-bit integer), or raw device addresses."""
-    elem, _, _, i64, _ = _types()
-    e, f = elem.get(dtype), "lp_dropout: "
+    elem, _, _, i64, _ = _kinds or _types()
+    e = elem.get(dtype)
     if e is None:
-        raise LpError(-1, f + "dtype")
-    word = i64[1] if getattr(offset_dev, "dtype", None) is i64[1] else i64[0]
-    _check(None, _lib.lp_dropout(dtype, _buffer(f + "x", x, e, n), _buffer(f + "resid", resid, e, n), _buffer(f + "y", y, e, n), n, p,
-                                 seed, offset, _buffer(f + "offset_dev", offset_dev, word, 1), stream))
+        raise LpError(-1, "lp_dropout: dtype")
+    if offset_dev is not None:
+        kind = i64[1] if getattr(offset_dev, "dtype", None) is i64[1] else i64[0]
+        offset_dev = _buffer(offset_dev, kind, 1, "lp_dropout: offset_dev")
+    _check(None, _lib.lp_dropout(dtype, _buffer(x, e, n, "lp_dropout: x"), _buffer(resid, e, n, "lp_dropout: resid"),
+                                 _buffer(y, e, n, "lp_dropout: y"), n, p, seed, offset, offset_dev, stream))
 
 
 LP_LINATTN_FORWARD, LP_LINATTN_BACKWARD, LP_LINATTN_STEP = 0, 1, 2
@@ -504,7 +510,7 @@ def lp_linear_attention_bf16(form: int, desc: dict, workspace=None, stream=None)
     tensors of lp_linattn_desc: q, k, v, o, dout, dq, dk, dv are bf16 CUDA tensors [batch, seq_len, n_heads, 64] (slices
     of larger ones are fine: strides are read off), the states fp32 [batch, n_heads, 64, 64], log_decay fp32 [n_heads],
     lengths int32 [batch]; `scale` a number (default 1).  Sizes come from q; the other tensors' shapes must agree."""
-    _, i32, f32, _, bf16 = _types()
+    _, i32, f32, _, bf16 = _kinds or _types()
     q, scale = desc.get("q"), 1.0
     if q is None or q.dtype is not bf16 or q.ndim != 4:
         raise LpError(-2, "lp_linear_attention_bf16: q must be bf16 [batch, seq_len, n_heads, 64]")
@@ -535,7 +541,7 @@ def lp_linear_attention_bf16(form: int, desc: dict, workspace=None, stream=None)
             v[at] = t.data_ptr()
     nbytes = workspace.nbytes if workspace is not None else 0
     code = _lib.lp_linear_attention_bf16(form, _LINATTN_PACK(*v, B, T, H, scale),
-                                         _workspace("lp_linear_attention_bf16", workspace, nbytes) if nbytes else None, nbytes, stream)
+                                         _workspace(workspace, nbytes, "lp_linear_attention_bf16") if nbytes else None, nbytes, stream)
     if code:
         _check(None, code)
 
