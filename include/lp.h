@@ -443,7 +443,7 @@ lp_status lp_dropout(int dtype, const void* x, const void* resid, void* y, long 
  *   FORWARD and BACKWARD form scores and state products on bf16 operands with fp32 accumulation; the operands of state_out
  *   and dstate_in are split into as many terms as they need, so those are as exact as sums in fp32.  A NaN or infinity in token t reaches the outputs from t
  *   on, and may reach earlier ones of the same 16 tokens.
- *   batch * n_heads <= 2^20.  workspace: lp_linear_attention_workspace_bytes (may be 0).
+ *   batch * n_heads <= 2^20, seq_len <= 2^30.  workspace: lp_linear_attention_workspace_bytes (may be 0).
  */
 enum { LP_LINATTN_FORWARD = 0, LP_LINATTN_BACKWARD = 1, LP_LINATTN_STEP = 2 };
 typedef struct { const void* p; long long batch_stride, token_stride; } lp_tokens;

@@ -860,7 +860,7 @@ lp_status lp_dropout(int dtype, const void* x, const void* resid, void* y, long 
 }
 
 size_t lp_linear_attention_workspace_bytes(int form, int batch, int seq_len, int n_heads) {
-  if (batch < 1 || seq_len < 1 || n_heads < 1 || (long long)batch * n_heads > (1 << 20)) return 0;
+  if (batch < 1 || seq_len < 1 || seq_len > (1 << 30) || n_heads < 1 || (long long)batch * n_heads > (1 << 20)) return 0;
   return form == LP_LINATTN_FORWARD || form == LP_LINATTN_BACKWARD ? linattn_workspace(form == LP_LINATTN_BACKWARD, batch, seq_len, n_heads) : 0;
 }
 
@@ -873,6 +873,7 @@ lp_status lp_linear_attention_bf16(int form, const lp_linattn_desc* d, void* wor
   if (back ? !d->dout.p || !d->dq.p || !d->dk.p || !d->dv.p : !d->o.p) return bad(LP_ERR_INVALID_ARG, "null pointer");
   if (d->batch < 1 || d->seq_len < 1 || d->n_heads < 1) return bad(LP_ERR_SHAPE, "sizes must be positive");
   if ((long long)d->batch * d->n_heads > (1 << 20)) return bad(LP_ERR_SHAPE, "batch * n_heads must be at most 2^20");
+  if (d->seq_len > (1 << 30)) return bad(LP_ERR_SHAPE, "seq_len must be at most 2^30");
   if (form == LP_LINATTN_STEP && d->seq_len != 1) return bad(LP_ERR_SHAPE, "the recurrent form takes one token");
   const lp_tokens* all[8] = {&d->q, &d->k, &d->v, &d->o, &d->dout, &d->dq, &d->dk, &d->dv};
   const bool used[8] = {true, true, true, !back, back, back, back, back};

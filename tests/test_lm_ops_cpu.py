@@ -302,3 +302,12 @@ def test_families_without_dropout_refuse_it(workload):
     import lp_synth
     for p in (0.1, float("nan")):
         refused("INVALID_ARG", lambda: lp.lp_create(*lp.specs_from_config(lp_synth.config(workload, dropout=p))), says="dropout")
+
+
+def test_linear_attention_refuses_lengths_whose_chunks_leave_32_bits():
+    """seq_len may be a capacity far above lengths; counted in chunks and segments it has to stay a positive int."""
+    for form in (lp.LP_LINATTN_FORWARD, lp.LP_LINATTN_BACKWARD):
+        for T in (2 ** 31 - 1, 2 ** 31 - 64, 2 ** 30 + 1):
+            assert lp.lp_linear_attention_workspace_bytes(form, 1, T, 1) == 0, T
+            assert linattn(form, ws=ONE, nbytes=1 << 40, batch=1, seq_len=T, lengths=0xb000) == ERR["SHAPE"], T
+        assert 0 < lp.lp_linear_attention_workspace_bytes(form, 1, 2 ** 30, 1) < 1 << 28
