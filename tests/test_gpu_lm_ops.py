@@ -707,3 +707,70 @@ def test_a_state_gradient_overwritten_in_a_replayed_graph():
         assert torch.equal(inplace, ds)
         for a, b in zip(g[:3], g[3:]):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("rows,vocab,d,T,dt,kind", [
+    (66001, 500, 513, 7, "bf16", "zipf"), (40003, 300, 421, 333, "fp32", "uniform"), (40003, 300, 421, 2, "fp32", "same"),
+    (4300001, 3, 8, 1, "bf16", "zipf"), (17000000, 40, 1, 100, "fp32", "uniform")])
+def test_position_sums_beside_the_sort_of_odd_and_narrow_widths(rows, vocab, d, T, dt, kind):
+    """Widths that take one element at a time, few lanes a row, a single position."""
+    code, td, _ = DT[dt]
+    ids = cu(make_ids(np.random.default_rng(rows), rows, vocab, kind), torch.int32)
+    dout = torch.randn(rows, d, device="cuda").to(td)
+    ws = torch.full((lp.lp_embed_workspace_bytes(rows, vocab, d),), 255, dtype=torch.uint8, device="cuda")
+    runs = []
+    for _ in range(2):
+        dtab, dpos = torch.full((vocab, d), float("nan"), device="cuda"), torch.full((T, d), float("nan"), device="cuda")
+        lp.lp_embed_backward(code, ids, dout, dtab, dpos, rows, vocab, d, T, 0.5, None, ws, ws.numel())
+        runs.append((dtab, dpos))
+    assert torch.equal(runs[0][0], runs[1][0]) and torch.equal(runs[0][1], runs[1][1])
+    x = dout.double()
+    for got, at, n, scale in ((dtab, ids.long(), vocab, 0.5), (dpos, torch.arange(rows, device="cuda") % T, T, 1.0)):
+        count = torch.bincount(at, minlength=n)[:, None]
+        want = torch.zeros(n, d, dtype=torch.float64, device="cuda").index_add_(0, at, x)
+        mag = torch.zeros(n, d, dtype=torch.float64, device="cuda").index_add_(0, at, x.abs())
+        assert ((got.double() - scale * want).abs() <= scale * (count + 2) * U32 * mag).all()
+
+
+FIRST_CALLS = """
+import sys
+sys.path.insert(0, sys.argv[1])
+import torch
+from paper_2012_03837_b200 import binding as lp
+B, T, H, V = 2, 2100, 2, 300
+rows, d = B * T, 64 * H
+bf = dict(dtype=torch.bfloat16, device="cuda")
+x, g, o = torch.randn(B, T, H, 64, **bf), [torch.zeros(B, T, H, 64, **bf) for _ in range(4)], torch.zeros(rows, d, **bf)
+ids, table, dtab = torch.randint(0, V, (rows,), device="cuda", dtype=torch.int32), torch.randn(V, d, **bf), torch.zeros(V, d, device="cuda")
+state, lg = torch.zeros(B, H, 64, 64, device="cuda"), torch.full((H,), -0.01, device="cuda")
+ws = [torch.empty(max(256, n), dtype=torch.uint8, device="cuda") for n in (
+    lp.lp_linear_attention_workspace_bytes(0, B, T, H), lp.lp_linear_attention_workspace_bytes(1, B, T, H), lp.lp_embed_workspace_bytes(rows, V, d))]
+
+def calls(s):
+    lp.lp_embed_forward(lp.LP_BF16, ids, table, None, o, rows, V, d, 0, 1.5, None, s)
+    lp.lp_linear_attention_bf16(0, dict(q=x, k=x, v=x, o=g[0], log_decay=lg, state_out=state), ws[0], s)
+    lp.lp_linear_attention_bf16(1, dict(q=x, k=x, v=x, dout=g[0], dq=g[1], dk=g[2], dv=g[3], log_decay=lg), ws[1], s)
+    lp.lp_dropout(lp.LP_BF16, g[1], o, o, rows * d, 0.1, 3, 0, None, s)
+    lp.lp_embed_backward(lp.LP_BF16, ids, o, dtab, None, rows, V, d, 0, 1.0, None, ws[2], ws[2].numel(), s)
+
+stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph, stream=stream):
+    calls(stream.cuda_stream)
+graph.replay()
+torch.cuda.synchronize()
+first = [t.clone() for t in g + [o, dtab, state]]
+calls(torch.cuda.current_stream().cuda_stream)
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(first, g + [o, dtab, state])) and dtab.abs().sum() > 0
+print("equal")
+"""
+
+
+def test_the_very_first_calls_may_be_captured():
+    """A process whose first calls of the operators are captured ones: kernels are loaded and limits raised meanwhile."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS, root], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "equal" in r.stdout, r.stdout + r.stderr
