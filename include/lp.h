@@ -382,8 +382,8 @@ lp_status lp_attention_bf16(int form, const void* qkv, void* o, float* lse, cons
  * Operators of language models, next to lp_attention_bf16: token embedding and its gradient, dropout, linear
  * attention.  They work on the caller's buffers alone and keep nothing between calls: scratch memory is a workspace the
  * caller owns (any content, 256-byte aligned, not shared by calls whose work may overlap on the GPU, a captured graph's
- * replays among them).  All pointers are device pointers of the current device; outputs must not overlap inputs except
- * where that is said.  The calls are asynchronous on `stream`, allocate nothing, do not synchronise and can be captured
+ * replays among them).  All pointers are device pointers of the current device; outputs must not overlap one another, nor
+ * inputs except where that is said.  The calls are asynchronous on `stream`, allocate nothing, do not synchronise and can be captured
  * into a CUDA graph.  Sums are in fp32 in a fixed order: equal calls give equal bits.  Errors of all of them:
  * INVALID_ARG (null or host pointer, unknown dtype or form, values out of range, workspace too small), SHAPE,
  * UNSUPPORTED (alignment, another device's memory), CUDA; message: lp_last_error(NULL).  A refused call launches nothing.
@@ -404,6 +404,7 @@ lp_status lp_embed_forward(int dtype, const int* ids, const void* table, const v
  * [seq_len, d] fp32, overwritten; dpos may be NULL.  The rows are sorted by token and every sum runs over its rows in
  * increasing r (in pieces of fixed length, added in order, for a token with many rows): no atomics on floats.
  * Ids out of range as in lp_embed_forward: their rows count for the clamped token.
+ * Made for vocabularies of up to 131072 tokens; from there on the sort takes time in proportion to rows * vocab.
  * rows <= 2^30, d <= 2^22 (lp_embed_forward too).  workspace: lp_embed_workspace_bytes(rows, vocab, d) (0: sizes not accepted).
  */
 size_t lp_embed_workspace_bytes(int rows, int vocab, int d);

@@ -8,9 +8,10 @@
 // A dropped element is selected away, not multiplied by zero: a NaN or an infinity there does not reach y.
 // Sums and products are in fp32 and rounded once, on storing.
 //
-// What bounds it: memory where three tensors pass (33.5 M bf16 with residual: 31 us, 6.5 TB/s, as fast as a copy), the
-// generator's instructions where two bf16 tensors do (30 us against 20 for the bytes: twenty wide products and twenty
-// three-way exclusive-ors per four elements, about 150 instructions per eight).  Sixteen random bits per element would
+// What bounds it: memory where three tensors pass (33.5 M bf16 with residual: 31 to 33 us in a replayed graph, 6.1 to 6.5 TB/s, 33
+// to 35 us as a call among others; fp32 60 us, 6.7 TB/s), the generator's instructions where two bf16 tensors do (30 to 33 us
+// against 20 for the bytes: twenty wide products and twenty three-way exclusive-ors per four elements, about 150 instructions
+// per eight; fp32 45 against 41).  Sixteen random bits per element would
 // halve that and tie p to multiples of 2^-16; a loop over blocks that fetches ahead was slower (35 to 41 us).
 #include <algorithm>
 

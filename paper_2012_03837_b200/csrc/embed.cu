@@ -18,8 +18,12 @@
 //   combine : adds the pieces of every such token in order (a launch of its own, only if more than 4 P rows exist).
 // Measured: 8192 rows of 512 into 8192 tokens 14 us (sort 5, sums 6, pieces 2: launches that follow one another); 65536 rows
 // of 1024 into 32768 tokens of natural text 87 us: sort 16, the position gradient's read of dh 24, of which it hides
-// a third, sums 46 (268 MB at 5.8 TB/s), pieces 6.  The floor of the latter, dh read once and both gradients written, is 41
-// us.  The lookup of 8192 rows of 1024 with positions takes 5.1 us, the time of its bytes.
+// a third, sums 46 (134 MB read and 134 written, of which 62 are still in the L2 cache when it ends: memory at 54 %), pieces
+// 6.  The floor of the latter, dh read once and both gradients written, is 41 us.  fp32: 16.5 and 136 us.  The lookup of 8192
+// rows of 1024 with positions takes 5.2 us with all of it in the L2 cache, as in a replayed graph, and 10.7 from memory.
+// More than 131072 tokens are sorted by more than 128 blocks, one on an SM at a time, which compare the ids one by one:
+// 65536 rows of 64 into 131072 tokens 28.8 us, 131073 39.0, 262144 51, 2^20 156 (floors 6.4, 6.4, 12, 42); rows of 512 80, 90,
+// 146, 535 (51, 51, 92, 338).  From there on the sort costs rows * vocab / 1024 reads of ids.
 #include <algorithm>
 #include <climits>
 
@@ -512,9 +516,11 @@ cudaError_t run_sort_and_sum(const EmbedBwdProb& p, int P, int chunks, int pos_p
   if (e != cudaSuccess) return e;
   // The position gradient reads dh a second time.  While dh stays in the L2 cache (126 MB) that is cheap, and it rides with
   // the sums; a larger one is read beside the sort, which leaves the memory idle: on the SMs that have no sorting block, and
-  // on the others as those end.  ([8192, 512]: 15 against 20 us with the sort; [65536, 1024]: 104 against 91 in the
-  // sort's own launch and 88 in one beside it; with few enough registers to share the SMs with it 93 to 99, since the sort
-  // then waits for its ids.)
+  // on the others as those end.  ([65536, 1024]: 91 us in the sort's own launch, 88 in one beside it; with few enough registers to
+  // share the SMs with it 93 to 99, since the sort then waits for its ids.)  With the sums / beside the sort, bf16, natural text:
+  // rows of 1024 into 32768 tokens, 512 positions, 8 MiB 43.2 / 43.8 us, 16 43.2 / 44.1, 32 49.5 / 50.5, 48 55.5 / 63, 64 65.1 / 68.8, 96
+  // 79.0 / 76.2, 128 93.1 / 88.6; rows of 512 into 8192, 256 positions, 8 MiB 18.5 / 22.2, 32 39.0 / 41.0, 64 51.4 / 55.4, 96 74.3 /
+  // 80.1, 128 94.2 / 98.3: beyond 64 MiB the wide rows gain, these lose 4 to 8 %.
   const long long pos_work = p.dpos ? (long long)p.T * pos_pieces : 0;
   const bool early = pos_beside_sort(p, sizeof(T));
   e = launch_after(embed_sort_kernel, dim3(1u << n_log2), SORT_WARPS * 32, smem, s, p, n_log2, local, PIECES * P, d_status, early);

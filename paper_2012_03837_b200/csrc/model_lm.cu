@@ -139,7 +139,9 @@ void build_lm(Handle& h) {
   };
 
   // Dropout of [M, d] tensors (training passes only): y = resid + dropped x, a launch per chunk.  The mask follows from
-  // the site and the step's number alone, so the backward pass forms it again.
+  // the site and the step's number alone, so the backward pass forms it again.  A dropped branch is rounded to the compute
+  // type once more than one that is not: its product is stored before it is dropped and joins the stream, which without
+  // dropout happens in fp32 in the product's epilogue.
   struct DropItem { const void* x; const void* resid; void* y; uint32_t site; };
   const float drop_p = h.spec.dropout;
   const unsigned long long drop_seed = h.spec.dropout_seed;
