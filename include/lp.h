@@ -463,6 +463,68 @@ size_t lp_linear_attention_workspace_bytes(int form, int batch, int seq_len, int
 lp_status lp_linear_attention_bf16(int form, const lp_linattn_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Operators that read a model's logits (lp_forward's, or any [rows, vocab] matrix): log probabilities of given tokens with
+ * entropy and top alternatives, their gradient, and distillation from a teacher's top logits.  What is said above of the
+ * operators holds for these too; they need no workspace.
+ *   dtype LP_FP32 or LP_BF16: type of logits and dlogits; element j of row r is p[r * ld + j], aligned to its element,
+ *   vocab <= ld <= 2^38 (rows 1: ignored), rows <= 2^27, vocab <= 2^18 (LP_LOGITS_VOCAB_MAX).  What lies between a row's
+ *   end and the next row is neither read nor written.  dlogits may be logits itself, with the same ld.
+ *   x: a row of logits; z = x / temperature, 2^-20 <= temperature <= 2^20; p = softmax(z); lse = log sum exp(z).  A logit
+ *   of -infinity is a masked token: probability 0, no part in the entropy, gradient 0.  A row of them alone: lse and log
+ *   probabilities are -infinity, entropy and gradients 0.  A row with a NaN or +infinity: NaN in lse, log probabilities,
+ *   entropy, loss and all of its gradient.
+ *   A token id below 0 says that there is none; one >= vocab is taken for none too and, if out_of_range is not NULL, bit 0
+ *   of that device int is set (never cleared).
+ */
+#define LP_LOGITS_VOCAB_MAX (1 << 18)
+#define LP_TOP_MAX 128
+
+/*
+ * lp_token_logprobs: any of (at least one)
+ *   logp[r]    = z[tokens[r]] - lse   (0 without a token; needs tokens, int32 [rows])
+ *   entropy[r] = - sum p log p        lse[r]
+ *   top_ids[r, i], top_logp[r, i]     the top_k <= LP_TOP_MAX, vocab tokens of the largest logits in descending order, equal
+ *                                     logits (-0 and 0 among them) by ascending id, NaN behind -infinity; int32 and fp32
+ *                                     [rows, top_k], contiguous, both or neither (top_k = 0)
+ * logp, entropy, lse: fp32 [rows].
+ */
+lp_status lp_token_logprobs(int dtype, const void* logits, long long ld, const int* tokens, float* logp, float* entropy,
+                            float* lse, int* top_ids, float* top_logp, int top_k, int rows, int vocab, float temperature,
+                            int* out_of_range, void* stream);
+
+/*
+ * lp_token_logprobs_backward: dlogits = the gradient of
+ *   sum_r dlogp[r] logp[r] + dentropy[r] entropy[r] + dlse[r] lse[r]
+ * with respect to the logits; each of dlogp (needs tokens), dentropy, dlse (fp32 [rows]) may be NULL, not all.  It needs
+ * nothing of the forward call but the logits.  A row whose factors are all 0 (dlogp of a row without a token counts as 0)
+ * gets zeros and its logits are not looked at.
+ */
+lp_status lp_token_logprobs_backward(int dtype, const void* logits, long long ld, const int* tokens, const float* dlogp,
+                                     const float* dentropy, const float* dlse, void* dlogits, long long ld_out, int rows,
+                                     int vocab, float temperature, int* out_of_range, void* stream);
+
+/*
+ * lp_distill: loss[r] = scale * KL(q || p), and its gradient dlogits = dloss[r] * scale * dKL / dlogits[r], q a teacher's
+ * distribution given by k <= LP_TOP_MAX entries (teacher_ids int32, teacher fp32, both [rows, k], contiguous).
+ *   LP_DISTILL_TOP:  teacher holds logits or log probabilities t; q = softmax(t / temperature) over the row's entries, 0
+ *                    elsewhere.
+ *   LP_DISTILL_REST: teacher holds log probabilities t over the whole vocabulary at the student's temperature (what
+ *                    lp_token_logprobs gives); q = exp(t), and what the entries lack of 1 is one more class, against the sum
+ *                    of the student's probabilities of all tokens not listed.  A rest of at most 2^-20 counts as none: it
+ *                    is the rounding of the entries.
+ *   An entry with an id below 0 is not there; one of -infinity has weight 0 (but is listed).  Entries of the same id each
+ *   count as they are; the token is listed once.  A row without any weight has loss 0 and gradient 0, and its logits are not looked at.
+ *   Where the student's probability of what has weight is 0, the loss is +infinity and the gradient is the formula's
+ *   (a rest that is empty takes no gradient).
+ *   loss (fp32 [rows]) and dlogits: either may be NULL, not both.  dloss: fp32 [rows], NULL for ones; a row of dloss 0 gets
+ *   zeros.  One pass gives both: the logits are read once.
+ */
+enum { LP_DISTILL_TOP = 0, LP_DISTILL_REST = 1 };
+lp_status lp_distill(int form, int dtype, const void* logits, long long ld, const int* teacher_ids, const float* teacher, int k,
+                     float* loss, const float* dloss, void* dlogits, long long ld_out, int rows, int vocab, float temperature,
+                     float scale, int* out_of_range, void* stream);
+
+/*
  * lp_gemm_bf16_static: lp_gemm_bf16 for callers that cannot allocate device memory.  (The paper
  * has no counterpart to this entry point; it exists for the library's users.)
  *

@@ -1,6 +1,7 @@
 """Plain NumPy forms, in 64 bits, of the operators that stand next to the transformer's layers: scaled embedding
-lookup and its gradients, dropout from a counter-based generator, linear attention with a decay per head.  Written
-from the formulas; no chunks, no sorting, no segments."""
+lookup and its gradients, dropout from a counter-based generator, linear attention with a decay per head, log
+probabilities of tokens with their gradient, distillation from a teacher's top logits.  Written from the formulas; no
+chunks, no sorting, no segments."""
 import numpy as np
 
 
@@ -83,3 +84,86 @@ def linear_attention_bwd(q, k, v, do, log_decay, scale, state=None, dstate=None,
             dv[b, t] = np.einsum("hkv,hk->hv", R[b], k[b, t])
             R[b] = l * R[b]
     return dq, dk, dv, R
+
+
+def log_softmax(x, temperature):
+    """Log probabilities of one row and its log-sum-exp; -infinity throughout where every logit is -infinity."""
+    z = np.asarray(x, dtype=np.float64) / temperature
+    m = z.max()
+    if m == -np.inf:
+        return np.full_like(z, -np.inf), -np.inf
+    if not m < np.inf:                              # NaN or +infinity in the row
+        return np.full_like(z, np.nan), np.nan
+    log_s = np.log(np.exp(z - m).sum())
+    return z - m - log_s, m + log_s                 # rows of huge values keep their digits
+
+
+def token_logprobs(x, tokens, temperature=1.0, top_k=0):
+    """logp, entropy, lse [rows], top ids and their log probabilities [rows, top_k]; token ids outside [0, vocab) are none."""
+    rows, n = x.shape
+    logp, ent, lses = np.zeros(rows), np.zeros(rows), np.zeros(rows)
+    ids, tops = np.zeros((rows, top_k), dtype=np.int64), np.zeros((rows, top_k))
+    for r in range(rows):
+        l, lses[r] = log_softmax(x[r], temperature)
+        p = np.exp(l)
+        ent[r] = -np.sum(p[p != 0] * l[p != 0])     # a NaN stays in
+        if tokens is not None and 0 <= tokens[r] < n:
+            logp[r] = l[tokens[r]]
+        order = sorted(range(n), key=lambda j: (bool(np.isnan(x[r, j])), 0.0 if np.isnan(x[r, j]) else -float(x[r, j]), j)) if top_k else []
+        ids[r] = order[:top_k]
+        tops[r] = l[ids[r]]
+    return logp, ent, lses, ids, tops
+
+
+def token_logprobs_bwd(x, tokens, dlogp=None, dentropy=None, dlse=None, temperature=1.0):
+    dx = np.zeros(x.shape)
+    for r in range(len(x)):
+        has = dlogp is not None and 0 <= tokens[r] < x.shape[1]
+        a, b, c = (dlogp[r] if has else 0.0), (0.0 if dentropy is None else dentropy[r]), (0.0 if dlse is None else dlse[r])
+        l, lse = log_softmax(x[r], temperature)
+        if (a == 0 and b == 0 and c == 0) or lse == -np.inf:
+            continue
+        p = np.exp(l)
+        pl = np.where(p == 0, 0.0, p * np.where(p == 0, 0.0, l))
+        dx[r] = (c - a) * p - b * (pl - p * pl.sum())
+        if has:
+            dx[r, tokens[r]] += a
+    return dx / temperature
+
+
+def distill(x, ids, teacher, rest, temperature=1.0, scale=1.0, dloss=None):
+    """loss [rows] = scale * KL(teacher || student) and its gradient with respect to the logits, times dloss."""
+    rows, n = x.shape
+    loss, dx = np.zeros(rows), np.zeros(x.shape)
+    for r in range(rows):
+        entries = [(int(i), float(t)) for i, t in zip(ids[r], teacher[r]) if 0 <= i < n]
+        t = np.array([e[1] for e in entries])
+        if not len(t) or (t == -np.inf).all():
+            continue
+        if rest:
+            q = np.exp(t)
+            qr = 1.0 - q.sum()
+            qr = qr if qr > 2.0 ** -20 else 0.0
+        else:
+            q = np.exp((t - t.max()) / temperature)
+            q, qr = q / q.sum(), 0.0
+        l, lse = log_softmax(x[r], temperature)
+        p = np.exp(l)
+        outside = np.ones(n, dtype=bool)
+        outside[[e[0] for e in entries]] = False
+        lo = l[outside]
+        log_rest = -np.inf if not len(lo) or lo.max() == -np.inf else lo.max() + np.log(np.exp(lo - lo.max()).sum())
+        kl = sum(qj * (np.log(qj) - l[i]) for (i, _), qj in zip(entries, q) if qj != 0)
+        if qr > 0:
+            kl += qr * (np.log(qr) - log_rest)
+        loss[r] = scale * kl
+        if lse == -np.inf:
+            continue
+        d = (q.sum() + qr) * p
+        for (i, _), qj in zip(entries, q):
+            d[i] -= qj
+        if qr > 0 and log_rest != -np.inf:
+            d[outside] -= qr * np.exp(lo - log_rest)
+        f = (1.0 if dloss is None else dloss[r]) * scale / temperature
+        dx[r] = d * f if f != 0 else 0.0
+    return loss, dx

@@ -66,7 +66,7 @@ EXPORTS = ["lp_create", "lp_step", "lp_step_host", "lp_forward", "lp_destroy", "
            "lp_state_size", "lp_save_state", "lp_load_state", "lp_last_step_launches", "lp_device_bytes",
            "lp_last_error", "lp_gemm_bf16", "lp_profile_enable", "lp_profile_read",
            "lp_attention_bf16", "lp_embed_forward", "lp_embed_backward", "lp_embed_workspace_bytes", "lp_dropout",
-           "lp_linear_attention_bf16", "lp_linear_attention_workspace_bytes", "lp_gemm_bf16_static", "lp_gemm_static_poll", "lp_gemm_static_last_error", "lp_conv3x3_bf16", "lp_conv2d_bf16", "lp_set_ramp", "lp_set_drain", "lp_set_fused_step", "lp_evaluate", "lp_set_overlap",
+           "lp_linear_attention_bf16", "lp_linear_attention_workspace_bytes", "lp_token_logprobs", "lp_token_logprobs_backward", "lp_distill", "lp_gemm_bf16_static", "lp_gemm_static_poll", "lp_gemm_static_last_error", "lp_conv3x3_bf16", "lp_conv2d_bf16", "lp_set_ramp", "lp_set_drain", "lp_set_fused_step", "lp_evaluate", "lp_set_overlap",
            "lp_cost_model", "lp_mlp_layer_flops", "lp_mlp_aux_flops", "lp_chunk_output_bytes", "lp_chunk_output"]
 LP_KIND_NAMES = ["other", "gemm_tc", "gemm_alu", "norm", "xent", "attn", "optim", "reduce", "embed", "conv_aux"]
 
@@ -544,6 +544,91 @@ def lp_linear_attention_bf16(form: int, desc: dict, workspace=None, stream=None)
                                          _workspace(workspace, nbytes, "lp_linear_attention_bf16") if nbytes else None, nbytes, stream)
     if code:
         _check(None, code)
+
+
+LP_LOGITS_VOCAB_MAX, LP_TOP_MAX = 1 << 18, 128
+LP_DISTILL_TOP, LP_DISTILL_REST = 0, 1
+_lib.lp_token_logprobs.argtypes = [C.c_int, C.c_void_p, C.c_longlong] + [C.c_void_p] * 6 + [C.c_int] * 3 + [C.c_float, C.c_void_p, C.c_void_p]
+_lib.lp_token_logprobs_backward.argtypes = [C.c_int, C.c_void_p, C.c_longlong] + [C.c_void_p] * 5 + [C.c_longlong, C.c_int, C.c_int, C.c_float,
+                                                                                                   C.c_void_p, C.c_void_p]
+_lib.lp_distill.argtypes = [C.c_int, C.c_int, C.c_void_p, C.c_longlong, C.c_void_p, C.c_void_p, C.c_int] + [C.c_void_p] * 3 + \
+    [C.c_longlong, C.c_int, C.c_int, C.c_float, C.c_float, C.c_void_p, C.c_void_p]
+
+
+def _logits(t, what: str, of=None):
+    """(LP_* code, device address, row stride, shape) of a CUDA matrix of logits: rows of any stride, their elements side
+    by side; `of`: the logits that a gradient has to match."""
+    code = _logits_codes.get(getattr(t, "dtype", None))
+    if code is None:
+        elem = (_kinds or _types())[0]
+        _logits_codes.update({kind: c for c, kind in elem.items()})
+        code = _logits_codes.get(getattr(t, "dtype", None))
+    if code is None or t.ndim != 2 or (of is not None and (t.dtype is not of.dtype or t.shape != of.shape)):
+        raise LpError(-2, f"{what} must be a fp32 or bf16 matrix" + (" like the logits" if of is not None else ""))
+    shape, (ld, step) = t.shape, t.stride()
+    if step != 1 and shape[1] > 1:
+        raise LpError(-3, f"{what}: the elements of a row must lie side by side")
+    if not t.is_cuda:
+        raise LpError(-1, f"{what}: host memory was given where device memory is needed")
+    return code, t.data_ptr(), ld, shape
+
+
+_logits_codes = {}
+
+
+def lp_token_logprobs(logits, tokens=None, logp=None, entropy=None, lse=None, top_ids=None, top_logp=None, temperature: float = 1.0,
+                      out_of_range=None, stream=None) -> None:
+    """Log probabilities of given tokens, entropy, log-sum-exp and the top alternatives of every row of `logits`, a CUDA
+    matrix [rows, vocab] in fp32 or bf16 whose rows may have a stride (see lp.h).  tokens int32 [rows]; logp, entropy, lse
+    fp32 [rows]; top_ids int32 and top_logp fp32 [rows, top_k]; outputs that are not wanted are None."""
+    code, x, ld, (rows, vocab) = _logits(logits, "lp_token_logprobs: logits")
+    _, i32, f32, _, _ = _kinds
+    k = 0
+    if top_ids is not None:
+        if top_ids.ndim != 2 or top_ids.shape[0] != rows:
+            raise LpError(-2, "lp_token_logprobs: top_ids must be [rows, top_k]")
+        k = top_ids.shape[1]
+    _check(None, _lib.lp_token_logprobs(code, x, ld, _buffer(tokens, i32, rows, "lp_token_logprobs: tokens"),
+                                        _buffer(logp, f32, rows, "lp_token_logprobs: logp"),
+                                        _buffer(entropy, f32, rows, "lp_token_logprobs: entropy"),
+                                        _buffer(lse, f32, rows, "lp_token_logprobs: lse"),
+                                        _buffer(top_ids, i32, rows * k, "lp_token_logprobs: top_ids"),
+                                        _buffer(top_logp, f32, rows * k, "lp_token_logprobs: top_logp"), k, rows, vocab, temperature,
+                                        _buffer(out_of_range, i32, 1, "lp_token_logprobs: out_of_range"), stream))
+
+
+def lp_token_logprobs_backward(logits, tokens=None, dlogp=None, dentropy=None, dlse=None, dlogits=None, temperature: float = 1.0,
+                               out_of_range=None, stream=None) -> None:
+    """dlogits = gradient of sum(dlogp * logp + dentropy * entropy + dlse * lse) with respect to the logits (see lp.h);
+    dlogits, of the logits' shape and type, may be the logits themselves.  Gradients that are None count as zeros."""
+    code, x, ld, (rows, vocab) = _logits(logits, "lp_token_logprobs_backward: logits")
+    _, dx, ld_out, _ = _logits(dlogits, "lp_token_logprobs_backward: dlogits", logits)
+    _, i32, f32, _, _ = _kinds
+    _check(None, _lib.lp_token_logprobs_backward(code, x, ld, _buffer(tokens, i32, rows, "lp_token_logprobs_backward: tokens"),
+                                                 _buffer(dlogp, f32, rows, "lp_token_logprobs_backward: dlogp"),
+                                                 _buffer(dentropy, f32, rows, "lp_token_logprobs_backward: dentropy"),
+                                                 _buffer(dlse, f32, rows, "lp_token_logprobs_backward: dlse"), dx, ld_out, rows, vocab,
+                                                 temperature, _buffer(out_of_range, i32, 1, "lp_token_logprobs_backward: out_of_range"),
+                                                 stream))
+
+
+def lp_distill(form: int, logits, teacher_ids, teacher, loss=None, dloss=None, dlogits=None, temperature: float = 1.0,
+               scale: float = 1.0, out_of_range=None, stream=None) -> None:
+    """loss[r] = scale * KL(teacher || student) of every row of the student's logits and, if dlogits is given, its gradient
+    times dloss[r] (None: ones), in one pass (see lp.h).  form: LP_DISTILL_TOP or LP_DISTILL_REST; teacher_ids int32 and
+    teacher fp32 [rows, k]; dlogits, of the logits' shape and type, may be the logits themselves."""
+    code, x, ld, (rows, vocab) = _logits(logits, "lp_distill: logits")
+    dx, ld_out = None, 0
+    if dlogits is not None:
+        _, dx, ld_out, _ = _logits(dlogits, "lp_distill: dlogits", logits)
+    _, i32, f32, _, _ = _kinds
+    if getattr(teacher_ids, "ndim", 0) != 2 or teacher_ids.shape[0] != rows:
+        raise LpError(-2, "lp_distill: teacher_ids must be [rows, k]")
+    k = teacher_ids.shape[1]
+    _check(None, _lib.lp_distill(form, code, x, ld, _buffer(teacher_ids, i32, rows * k, "lp_distill: teacher_ids"),
+                                 _buffer(teacher, f32, rows * k, "lp_distill: teacher"), k, _buffer(loss, f32, rows, "lp_distill: loss"),
+                                 _buffer(dloss, f32, rows, "lp_distill: dloss"), dx, ld_out, rows, vocab, temperature, scale,
+                                 _buffer(out_of_range, i32, 1, "lp_distill: out_of_range"), stream))
 
 
 _lib.lp_conv2d_bf16.argtypes = [C.c_int, C.c_void_p, C.c_void_p, C.c_void_p] + [C.c_int] * 7 + [C.c_void_p]

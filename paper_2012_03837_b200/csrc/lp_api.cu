@@ -1,6 +1,7 @@
 // C ABI of the local update step (include/lp.h): argument checks, handle life cycle, step
 // drivers, parameter access, checkpointing.  No exception leaves this file.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <initializer_list>
@@ -914,6 +915,86 @@ lp_status lp_linear_attention_bf16(int form, const lp_linattn_desc* d, void* wor
   // one token takes the recurrent kernel in either form: the chunked one would work on 63 empty rows
   const cudaError_t e = !back && d->seq_len == 1 ? launch_linattn_step(a, (cudaStream_t)stream) : launch_linattn(a, back, workspace, (cudaStream_t)stream);
   return launched(me, e);
+}
+
+// Checks that the operators on logits share; ld and ld_out of a single row are not looked at and set to vocab.
+static lp_status check_logits(const char* me, int dtype, const void* logits, long long& ld, const void* dlogits, long long& ld_out, int rows,
+                              int vocab, float temperature, const int* out_of_range) {
+  auto bad = [&](lp_status code, const char* why) { return fail(nullptr, code, std::string(me) + ": " + why); };
+  if (dtype != LP_FP32 && dtype != LP_BF16) return bad(LP_ERR_INVALID_ARG, "dtype");
+  if (!logits) return bad(LP_ERR_INVALID_ARG, "null pointer");
+  if (rows < 1 || rows > (1 << 27) || vocab < 1 || vocab > LP_LOGITS_VOCAB_MAX)
+    return bad(LP_ERR_SHAPE, "rows must be 1 to 2^27, vocab 1 to 2^18");
+  if (rows == 1) ld = ld_out = vocab;
+  if (ld < vocab || ld > 1LL << 38 || (dlogits && (ld_out < vocab || ld_out > 1LL << 38)))
+    return bad(LP_ERR_SHAPE, "rows must lie vocab to 2^38 elements apart");
+  if (!(temperature >= 0x1p-20f && temperature <= 0x1p20f)) return bad(LP_ERR_INVALID_ARG, "temperature must be 2^-20 to 2^20");
+  if (dlogits == logits && ld_out != ld) return bad(LP_ERR_INVALID_ARG, "a gradient in the logits' place has their row stride");
+  const size_t es = dtype == LP_BF16 ? 2 : 4;
+  if (!aligned_to(logits, es) || !aligned_to(dlogits, es) || !aligned_to(out_of_range, 4))
+    return bad(LP_ERR_UNSUPPORTED, "pointers must be aligned to their element");
+  return LP_OK;
+}
+
+lp_status lp_token_logprobs(int dtype, const void* logits, long long ld, const int* tokens, float* logp, float* entropy, float* lse,
+                            int* top_ids, float* top_logp, int top_k, int rows, int vocab, float temperature, int* out_of_range,
+                            void* stream) {
+  const char* me = "lp_token_logprobs";
+  auto bad = [&](lp_status code, const char* why) { return fail(nullptr, code, std::string(me) + ": " + why); };
+  long long unused = vocab;
+  lp_status st = check_logits(me, dtype, logits, ld, nullptr, unused, rows, vocab, temperature, out_of_range);
+  if (st != LP_OK) return st;
+  if (logp && !tokens) return bad(LP_ERR_INVALID_ARG, "logp needs tokens");
+  if (top_k < 0 || top_k > LP_TOP_MAX || top_k > vocab) return bad(LP_ERR_SHAPE, "top_k must be 0 to 128 and at most vocab");
+  if ((top_k > 0) != (top_ids != nullptr) || (top_k > 0) != (top_logp != nullptr))
+    return bad(LP_ERR_INVALID_ARG, "top_ids and top_logp go with a positive top_k");
+  if (!logp && !entropy && !lse && !top_k) return bad(LP_ERR_INVALID_ARG, "no output");
+  if (!aligned_to(tokens, 4) || !aligned_to(logp, 4) || !aligned_to(entropy, 4) || !aligned_to(lse, 4) || !aligned_to(top_ids, 4) ||
+      !aligned_to(top_logp, 4))
+    return bad(LP_ERR_UNSUPPORTED, "pointers must be aligned to their element");
+  st = check_memory(me, {logits, logp ? tokens : nullptr, logp, entropy, lse, top_ids, top_logp, out_of_range});
+  if (st != LP_OK) return st;
+  const LogprobsArgs a{{logits, ld, rows, vocab, temperature, out_of_range}, logp ? tokens : nullptr, logp, entropy, lse, top_logp, top_ids, top_k};
+  return launched(me, launch_logprobs(a, dtype == LP_BF16, (cudaStream_t)stream));
+}
+
+lp_status lp_token_logprobs_backward(int dtype, const void* logits, long long ld, const int* tokens, const float* dlogp,
+                                     const float* dentropy, const float* dlse, void* dlogits, long long ld_out, int rows, int vocab,
+                                     float temperature, int* out_of_range, void* stream) {
+  const char* me = "lp_token_logprobs_backward";
+  auto bad = [&](lp_status code, const char* why) { return fail(nullptr, code, std::string(me) + ": " + why); };
+  if (!dlogits) return bad(LP_ERR_INVALID_ARG, "null pointer");
+  lp_status st = check_logits(me, dtype, logits, ld, dlogits, ld_out, rows, vocab, temperature, out_of_range);
+  if (st != LP_OK) return st;
+  if (dlogp && !tokens) return bad(LP_ERR_INVALID_ARG, "dlogp needs tokens");
+  if (!dlogp && !dentropy && !dlse) return bad(LP_ERR_INVALID_ARG, "no incoming gradient");
+  if (!aligned_to(tokens, 4) || !aligned_to(dlogp, 4) || !aligned_to(dentropy, 4) || !aligned_to(dlse, 4))
+    return bad(LP_ERR_UNSUPPORTED, "pointers must be aligned to their element");
+  st = check_memory(me, {logits, dlogp ? tokens : nullptr, dlogp, dentropy, dlse, dlogits, out_of_range});
+  if (st != LP_OK) return st;
+  const LogprobsBwdArgs a{{logits, ld, rows, vocab, temperature, out_of_range}, dlogp ? tokens : nullptr, dlogp, dentropy, dlse, dlogits, ld_out};
+  return launched(me, launch_logprobs_bwd(a, dtype == LP_BF16, (cudaStream_t)stream));
+}
+
+lp_status lp_distill(int form, int dtype, const void* logits, long long ld, const int* teacher_ids, const float* teacher, int k,
+                     float* loss, const float* dloss, void* dlogits, long long ld_out, int rows, int vocab, float temperature, float scale,
+                     int* out_of_range, void* stream) {
+  const char* me = "lp_distill";
+  auto bad = [&](lp_status code, const char* why) { return fail(nullptr, code, std::string(me) + ": " + why); };
+  if (form != LP_DISTILL_TOP && form != LP_DISTILL_REST) return bad(LP_ERR_INVALID_ARG, "unknown form");
+  if (!teacher_ids || !teacher) return bad(LP_ERR_INVALID_ARG, "null pointer");
+  if (!loss && !dlogits) return bad(LP_ERR_INVALID_ARG, "no output");
+  lp_status st = check_logits(me, dtype, logits, ld, dlogits, ld_out, rows, vocab, temperature, out_of_range);
+  if (st != LP_OK) return st;
+  if (k < 1 || k > LP_TOP_MAX) return bad(LP_ERR_SHAPE, "k must be 1 to 128");
+  if (!(std::fabs(scale) <= FLT_MAX)) return bad(LP_ERR_INVALID_ARG, "scale must be finite");
+  if (!aligned_to(teacher_ids, 4) || !aligned_to(teacher, 4) || !aligned_to(loss, 4) || !aligned_to(dloss, 4))
+    return bad(LP_ERR_UNSUPPORTED, "pointers must be aligned to their element");
+  st = check_memory(me, {logits, teacher_ids, teacher, loss, dlogits ? dloss : nullptr, dlogits, out_of_range});
+  if (st != LP_OK) return st;
+  const DistillArgs a{{logits, ld, rows, vocab, temperature, out_of_range}, teacher_ids, teacher, k, form == LP_DISTILL_REST,
+                      loss, dlogits ? dloss : nullptr, dlogits, ld_out, scale};
+  return launched(me, launch_distill(a, dtype == LP_BF16, (cudaStream_t)stream));
 }
 
 lp_status lp_profile_enable(lp_handle hh, int on) {

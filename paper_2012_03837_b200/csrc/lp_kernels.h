@@ -187,6 +187,25 @@ size_t linattn_workspace(bool backward, int B, int T, int H);
 cudaError_t launch_linattn(LinAttnArgs a, bool backward, void* workspace, cudaStream_t s);
 cudaError_t launch_linattn_step(const LinAttnArgs& a, cudaStream_t s);
 
+// ---- operators that read logits (logits.cu)
+struct LogitsIn { const void* x; long long ld; int rows, vocab; float temperature; int* out_of_range; };
+struct LogprobsArgs {
+  LogitsIn in;
+  const int* tokens;
+  float *logp, *entropy, *lse, *top_logp;                  // each nullable
+  int* top_ids;
+  int top_k;
+};
+struct LogprobsBwdArgs { LogitsIn in; const int* tokens; const float *dlogp, *dentropy, *dlse; void* dx; long long ld_out; };
+struct DistillArgs {
+  LogitsIn in;
+  const int* ids; const float* teacher; int k; bool rest;
+  float* loss; const float* dloss; void* dx; long long ld_out; float scale;
+};
+cudaError_t launch_logprobs(const LogprobsArgs& a, bool is_bf16, cudaStream_t s);
+cudaError_t launch_logprobs_bwd(const LogprobsBwdArgs& a, bool is_bf16, cudaStream_t s);
+cudaError_t launch_distill(const DistillArgs& a, bool is_bf16, cudaStream_t s);
+
 struct AttnProb {     // causal attention over qkv [B*T, 3d], heads of 64
   const void* qkv; void* o; float* lse; const void* dout; void* dqkv; float* delta; int B, T, H;
 };
