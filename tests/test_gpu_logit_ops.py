@@ -46,6 +46,8 @@ def values(g, rows, vocab, kind):
         if rows > 1:
             x[1] = -np.inf
             x[1, vocab // 2] = 1.5                           # and one with a single token
+    elif kind == "lowmask":                                  # masked by the type's lowest value
+        x[g.random(x.shape) < 0.9] = -3.3895314e38
     elif kind == "peaked":
         x[np.arange(rows), g.integers(0, vocab, rows)] += 60.0
     elif kind == "ties":
@@ -116,7 +118,7 @@ SIZES = [  # rows, vocab, pad, offset, top_k
     (160, 515, 5, 7, 9), (2, 2049, 0, 0, 128), (1, 8192, 0, 0, 64), (6, 8200, 3, 5, 30), (300, 4096, 0, 0, 5), (2, 32768, 0, 0, 128),
     (3, 50021, 6, 1, 17), (330, 32771, 1, 0, 2), (1, 131071, 0, 1, 100), (2, 150001, 7, 2, 128), (1, 262144, 0, 0, 50), (149, 100003, 0, 0, 4),
 ]
-KINDS = ["normal", "masked", "peaked", "ties", "constant", "lowest", "highest", "far", "descending", "ascending"]
+KINDS = ["normal", "masked", "lowmask", "peaked", "ties", "constant", "lowest", "highest", "far", "descending", "ascending"]
 # every size with plain values, every kind of values at three sizes
 CASES = [(*s, "normal") for s in SIZES] + [(*s, k) for s in [(3, 700, 1, 1, 40), (4, 20011, 0, 0, 128), (2, 200000, 0, 3, 33)] for k in KINDS[1:]]
 
@@ -281,7 +283,7 @@ DISTILL = [(1, 1, 0, 0, 1), (2, 3, 0, 1, 5), (5, 7, 2, 0, 7), (9, 64, 0, 0, 128)
            (1, 8192, 0, 0, 64), (6, 8200, 3, 5, 30), (4, 32768, 0, 0, 128), (5, 50021, 6, 1, 17), (40, 32771, 1, 0, 5), (1, 131071, 0, 1, 100),
            (2, 150001, 7, 2, 128), (1, 262144, 0, 0, 50)]
 DISTILL_CASES = [(*s, "normal") for s in DISTILL] + [(*s, kind) for s in [(5, 700, 1, 1, 40), (4, 20011, 0, 0, 128), (4, 140000, 0, 3, 9)]
-                                                     for kind in ("masked", "peaked", "ties", "constant", "far")]
+                                                     for kind in ("masked", "lowmask", "peaked", "ties", "constant", "far")]
 
 
 @pytest.mark.parametrize("rest", [False, True])
