@@ -34,7 +34,8 @@ constexpr int TOP_MAX = 128;                  // LP_TOP_MAX
 constexpr float SMALLEST_REST = 0x1p-20f;
 constexpr float FAR = 1e23f;
 constexpr float LN2 = 0.693147180559945309f;
-constexpr int MAX_CLUSTER = 8, MAX_THREADS = 512, MAX_WARPS = MAX_THREADS / 32;
+constexpr int MAX_CLUSTER = 8;
+constexpr float SLACK = 8.f;                  // a sum's reference stays while no power of two exceeds 2^SLACK
 constexpr int CANDIDATES = 512;               // of the top alternatives
 
 // ---------------------------------------------------------------------------------------------- two floats at a time
@@ -71,6 +72,11 @@ __device__ __forceinline__ float ex2(float a) {
 __device__ __forceinline__ u64 ex22(u64 a) {
   const float2 v = unpack(a);
   return pack(ex2(v.x), ex2(v.y));
+}
+__device__ __forceinline__ float warp_most(float a) {     // of numbers
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(a));
+  return r;
 }
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
@@ -137,98 +143,124 @@ template <> struct Vec<float> {
 struct Geometry {
   float c, inv_t;                             // log2(e) / T, 1 / T
   float lo;                                   // logits below it have probability 0 in rows that are not far
-  int cluster;                                // blocks per row
+  float slack;                                // SLACK in units of a logit
+  int cluster, per, batches;                  // blocks per row, vectors of a block's piece, batches of 4 NT of them
 };
 
-// The block's piece of its row: vectors first .. first + count of the row's lattice of aligned 16 bytes, of which vector v
-// holds elements v N - shift .. v N - shift + N - 1.
-template <typename T>
+// A block's piece of a row.  Its vectors are those aligned 16 bytes that lie in the row as a whole, `first` .. `first` +
+// `count` of them here; element j of the row's ends, which no vector holds, belongs to one thread of the first block.
+// Thread t works on vectors t, t + NT, ..., four to a batch, and nobody else sees its copies of them.
+template <typename T, int NT>
 struct Piece {
+  static constexpr int N = Vec<T>::N;
   const T* x;                                 // the row
-  int n, shift, first, count, per;
-  uint4* buf;                                 // its vectors in shared memory, -infinity outside the row
-  __device__ __forceinline__ Piece(const T* row, int n_, int rank, int cluster, uint4* buf_) : x(row), n(n_), buf(buf_) {
-    shift = (int)(((uintptr_t)row & 15) / sizeof(T));
-    const int all = (n + shift + Vec<T>::N - 1) / Vec<T>::N;
-    per = (all + cluster - 1) / cluster;
-    first = min(all, rank * per);
-    count = min(all - first, per);
+  int head, first, count, edge;               // elements before the first vector; the thread's own element, or -1
+  __device__ __forceinline__ Piece(const LogitsIn& in, long long r, int rank, const Geometry& g) : x((const T*)in.x + r * in.ld) {
+    const int n = in.vocab, t = threadIdx.x;
+    head = min(n, (int)((16 - ((uintptr_t)x & 15)) / sizeof(T)) & (N - 1));
+    const int all = (n - head) / N, tail = head + all * N;
+    first = rank * g.per;
+    count = max(0, min(all - first, g.per));
+    edge = rank != 0 ? -1 : t < head ? t : t - head < n - tail ? tail + t - head : -1;
   }
-  __device__ __forceinline__ int element(int v) const { return (first + v) * Vec<T>::N - shift; }     // the first of vector v
-  __device__ __forceinline__ bool inside(int j) const { return j >= 0 && j + Vec<T>::N <= n; }
-  // Every thread fetches the vectors that it works on: v = threadIdx.x, + blockDim.x, ...
-  __device__ __forceinline__ void fetch() const {
-    for (int v = threadIdx.x; v < count; v += blockDim.x) {
-      const int j = element(v);
-      if (inside(j)) {
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(buf + v)), "l"(x + j) : "memory");
-      } else {
-        T* e = (T*)(buf + v);
+  __device__ __forceinline__ int element(int v) const { return head + (first + v) * N; }     // the first of vector v
+  __device__ __forceinline__ bool whole(int b) const { return (b + 1) * 4 * NT <= count; }
+  // Asks for batch b: its vectors u arrive at to[u * NT].  One group of copies, of nothing for b beyond the piece.
+  __device__ __forceinline__ void fetch(uint4* to, int b) const {
+    const int v = 4 * b * NT + threadIdx.x;
+    const uint32_t d = (uint32_t)__cvta_generic_to_shared(to);
+    const T* s = x + element(v);
+    if (whole(b)) {
 #pragma unroll
-        for (int i = 0; i < Vec<T>::N; ++i) e[i] = j + i >= 0 && j + i < n ? x[j + i] : from_f<T>(-INFINITY);
+      for (int u = 0; u < 4; ++u)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d + u * NT * 16), "l"(s + u * NT * N) : "memory");
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (v + u * NT < count) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d + u * NT * 16), "l"(s + u * NT * N) : "memory");
+    }
+    commit();
+  }
+  __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+  __device__ __forceinline__ void fetch_all(uint4* buf, const Geometry& g) const {
+    for (int b = 0; b < g.batches; ++b) fetch(buf + 4 * b * NT + threadIdx.x, b);
+  }
+  __device__ __forceinline__ float edge_value() const { return edge >= 0 ? to_f(x[edge]) : -INFINITY; }
+  __device__ __forceinline__ void load(uint4 (&a)[4], const uint4* from, int b) const {
+    if (whole(b)) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) a[u] = from[u * NT];
+    } else {
+      const int v = 4 * b * NT + threadIdx.x;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        a[u] = make_uint4(Vec<T>::NEG_INF, Vec<T>::NEG_INF, Vec<T>::NEG_INF, Vec<T>::NEG_INF);
+        if (v + u * NT < count) a[u] = from[u * NT];
       }
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
   }
-  __device__ __forceinline__ static void arrived() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-  // The vector's place in another matrix of rows, if it is aligned there.
   __device__ __forceinline__ void store(T* dst, int v, const uint4& r) const {
-    const int j = element(v);
-    if (inside(j) && ((uintptr_t)(dst + j) & 15) == 0) {
-      *(uint4*)(dst + j) = r;
+    T* d = dst + element(v);
+    if (((uintptr_t)d & 15) == 0) {
+      *(uint4*)d = r;
     } else {
-      const T* e = (const T*)&r;
 #pragma unroll
-      for (int i = 0; i < Vec<T>::N; ++i)
-        if (j + i >= 0 && j + i < n) dst[j + i] = e[i];
+      for (int i = 0; i < N; ++i) d[i] = from_f<T>(Vec<T>::get(r, i));
     }
   }
   __device__ __forceinline__ void zeros(T* dst) const {
-    for (int v = threadIdx.x; v < count; v += blockDim.x) store(dst, v, make_uint4(0, 0, 0, 0));
+    for (int v = threadIdx.x; v < count; v += NT) store(dst, v, make_uint4(0, 0, 0, 0));
+    if (edge >= 0) dst[edge] = from_f<T>(0.f);
   }
 };
 
-// ---------------------------------------------------------------------------------------------- sums of a row
-struct Sums { float m, s, w; };               // max x, sum 2^y, sum 2^y y against rho_of(m)
+// Waits until at most n of the thread's latest groups of copies are on their way (a smaller number waits for more).
+__device__ __forceinline__ void wait_groups(int n) {
+  if (n <= 0) asm volatile("cp.async.wait_group 0;" ::: "memory");
+  else if (n == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+  else if (n == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+  else asm volatile("cp.async.wait_group 3;" ::: "memory");
+}
 
+// ---------------------------------------------------------------------------------------------- sums of a row
 // The reference that a maximum gives; none below lo (masked tokens, of -infinity or the type's lowest value: their sum is
 // 0, unless the row has nothing else and is far).
 __device__ __forceinline__ float rho_of(float m, const Geometry& g) { return m < g.lo ? 0.f : __fmul_rn(m, g.c); }
 
-// Moves a sum from its reference to that of a larger maximum.
+struct Sums { float m, s, w; };               // max x, sum 2^y, sum 2^y y against rho_of(m)
+
+// A sum against the reference rho moved to that of a maximum m.
 template <bool W>
-__device__ __forceinline__ void move(Sums& a, float m, const Geometry& g) {
-  const float d = rho_of(a.m, g) - rho_of(m, g), f = a.m < g.lo ? 0.f : ex2(d);
-  if (W) a.w = f * fmaf(a.s, fmaxf(d, -1e30f), a.w);
-  a.s *= f;
-  a.m = m;
+__device__ __forceinline__ void move(float& s, float& w, float rho, float m, const Geometry& g) {
+  const float d = rho - rho_of(m, g), f = ex2(d);
+  if (W) w = f * fmaf(s, fmaxf(d, -1e30f), w);
+  s *= f;
 }
 
+// A thread's running sums.  The reference is the maximum of the first batch above lo, and is raised when a later one would
+// give a power above 2^SLACK; no batch but the first few of a row does.
 template <typename T, bool W>
-__device__ __forceinline__ Sums sweep(const Piece<T>& p, const Geometry& g) {
-  constexpr int P = Vec<T>::N / 2;
-  const u64 c2 = pack(g.c, g.c);
+struct Running {
   u64 s0 = 0, s1 = 0, w0 = 0, w1 = 0, nrho = 0;
-  float m = -INFINITY;
-  const int nt = blockDim.x;
-  for (int v = threadIdx.x; v < p.count; v += 4 * nt) {
-    uint4 a[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      a[u] = v + u * nt < p.count ? p.buf[v + u * nt] : make_uint4(Vec<T>::NEG_INF, Vec<T>::NEG_INF, Vec<T>::NEG_INF, Vec<T>::NEG_INF);
+  float m = -INFINITY, rho = 0.f, top;        // max x; what a logit may be without a new reference
+  __device__ __forceinline__ explicit Running(const Geometry& g) : top(g.lo) {}
+  __device__ __forceinline__ void raise(float to, const Geometry& g) {
+    const float r = rho_of(to, g), d = rho - r, f = ex2(fminf(d, 0.f));    // the first time the sums are 0, or NaN
+    const u64 f2 = pack(f, f), d2 = pack(d, d);
+    if (W) { w0 = mul2(f2, fma2(s0, d2, w0)); w1 = mul2(f2, fma2(s1, d2, w1)); }
+    s0 = mul2(s0, f2);
+    s1 = mul2(s1, f2);
+    rho = r;
+    nrho = pack(-r, -r);
+    top = to + g.slack;
+  }
+  // Adds a batch and returns its maximum.
+  __device__ __forceinline__ float add(uint4 (&a)[4], const Geometry& g) {
+    constexpr int P = Vec<T>::N / 2;
+    const u64 c2 = pack(g.c, g.c);
     const float bm = Vec<T>::max4(a);
-    if (bm > m) {
-      const float d = rho_of(m, g) - rho_of(bm, g), f = ex2(d);
-      if (m >= g.lo) {
-        const u64 f2 = pack(f, f), d2 = pack(d, d);
-        if (W) { w0 = mul2(f2, fma2(s0, d2, w0)); w1 = mul2(f2, fma2(s1, d2, w1)); }
-        s0 = mul2(s0, f2);
-        s1 = mul2(s1, f2);
-      }
-      m = bm;
-      const float r = -rho_of(m, g);
-      nrho = pack(r, r);
-    }
+    m = fmaxf(m, bm);
+    if (bm > top) raise(bm, g);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if (W) Vec<T>::clamp(a[u], g.lo);
@@ -241,29 +273,50 @@ __device__ __forceinline__ Sums sweep(const Piece<T>& p, const Geometry& g) {
         if (W) { w0 = fma2(e0, y0, w0); w1 = fma2(e1, y1, w1); }
       }
     }
+    return bm;
   }
-  const float2 s = unpack(add2(s0, s1)), w = unpack(add2(w0, w1));
-  return Sums{m, s.x + s.y, w.x + w.y};
-}
-
-// The same against the row's maximum, for far rows.
-template <typename T, bool W>
-__device__ __noinline__ Sums sweep_far(const Piece<T>& p, const Geometry& g, float m) {
-  Sums a{m, 0.f, 0.f};
-  for (int v = threadIdx.x; v < p.count; v += blockDim.x)
-    for (int i = 0; i < Vec<T>::N; ++i) {
-      const float x = Vec<T>::get(p.buf[v], i);
-      if (x == -INFINITY) continue;
-      const float y = (x - m) * g.c, e = ex2(y);
-      a.s += e;
-      if (W && e != 0.f) a.w = fmaf(e, y, a.w);
+  // The thread's own element of the row's ends, if it is there (not -infinity), and the sums against the warp's maximum.
+  __device__ __forceinline__ Sums end(float edge, const Geometry& g) {
+    m = fmaxf(m, edge);
+    if (edge > top) raise(edge, g);
+    const float2 sp = unpack(add2(s0, s1)), wp = unpack(add2(w0, w1));
+    float s = sp.x + sp.y, w = wp.x + wp.y;
+    if (edge != -INFINITY) {
+      const float y = fmaf(max_nan(edge, g.lo), g.c, -rho), e = ex2(y);
+      s += e;
+      if (W) w = fmaf(e, y, w);
     }
+    const float wm = warp_most(m);
+    if (top == g.lo) rho = rho_of(wm, g);                // nothing but masked tokens (or NaN)
+    move<W>(s, w, rho, wm, g);
+    return Sums{wm, s, w};
+  }
+};
+
+// The same against the row's maximum, for far rows, one element after the other, without the `k` tokens of `skip`.
+template <typename T, int NT, bool W>
+__device__ __noinline__ Sums sweep_far(const Piece<T, NT>& p, const Geometry& g, float m, float edge, const int* skip = nullptr, int k = 0) {
+  Sums a{m, 0.f, 0.f};
+  auto add = [&](float x) {
+    if (x == -INFINITY) return;
+    const float y = (x - m) * g.c, e = ex2(y);
+    a.s += e;
+    if (W && e != 0.f) a.w = fmaf(e, y, a.w);
+  };
+  for (int v = threadIdx.x; v < p.count; v += NT)
+    for (int i = 0; i < Vec<T>::N; ++i) {
+      const int j = p.element(v) + i;
+      bool out = false;
+      for (int l = 0; l < k; ++l) out = out || skip[l] == j;
+      if (!out) add(to_f(p.x[j]));
+    }
+  add(edge);
   return a;
 }
 
-struct Exchange {                             // what the warps of a row's blocks tell one another
-  float4 part[2][MAX_CLUSTER * MAX_WARPS];
-};
+// What the warps of a row's blocks tell one another; of two rows in turn.
+template <int NT>
+struct Exchange { float4 part[2][2][MAX_CLUSTER * NT / 32]; };
 
 template <bool CL>
 __device__ __forceinline__ void sync_row() {
@@ -275,34 +328,45 @@ __device__ __forceinline__ void sync_row() {
   }
 }
 
-// The row's sums, the same bits in every thread of its blocks.  FARROW: all parts have the row's maximum as their reference.
-template <bool W, bool CL, bool FARROW>
-__device__ __forceinline__ Sums join(Sums a, Exchange& ex, const Geometry& g, int rank) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  if (!FARROW) move<W>(a, warp_max(a.m), g);
+// The row's sums, the same bits in every thread of its blocks.  The parts of a warp have one reference, its maximum's, or in
+// a far row the row's.
+template <int NT, bool W, bool CL, bool FARROW>
+__device__ __forceinline__ Sums join(Sums a, float4* part, const Geometry& g, int rank) {
+  constexpr int WARPS = NT / 32;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   a.s = warp_sum(a.s);
   if (W) a.w = warp_sum(a.w);
-  float4* part = ex.part[FARROW ? 1 : 0];
   const float4 mine = make_float4(a.m, a.s, a.w, 0.f);
   if (CL) {
-    if (lane < g.cluster) cg::this_cluster().map_shared_rank(part, lane)[rank * warps + warp] = mine;
+    if (lane < g.cluster) cg::this_cluster().map_shared_rank(part, lane)[rank * WARPS + warp] = mine;
   } else if (lane == 0) {
     part[warp] = mine;
   }
   sync_row<CL>();
-  const int parts = CL ? g.cluster * warps : warps;
-  float m = a.m;
-  if (!FARROW) {
-    m = -INFINITY;
-    for (int i = lane; i < parts; i += 32) m = fmaxf(m, part[i].x);
-    m = warp_max(m);
+  Sums t{-INFINITY, 0.f, 0.f};
+  if (!CL) {
+    float4 q[WARPS];
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) {
+      q[i] = part[i];
+      t.m = fmaxf(t.m, q[i].x);
+    }
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) {
+      if (!FARROW) move<W>(q[i].y, q[i].z, rho_of(q[i].x, g), t.m, g);
+      t.s += q[i].y;
+      t.w += q[i].z;
+    }
+    return t;
   }
-  Sums t{m, 0.f, 0.f};
+  const int parts = g.cluster * WARPS;
+  for (int i = lane; i < parts; i += 32) t.m = fmaxf(t.m, part[i].x);
+  t.m = warp_most(t.m);
   for (int i = lane; i < parts; i += 32) {
-    Sums b{part[i].x, part[i].y, part[i].z};
-    if (!FARROW) move<W>(b, m, g);
-    t.s += b.s;
-    if (W) t.w += b.w;
+    float4 b = part[i];
+    if (!FARROW) move<W>(b.y, b.z, rho_of(b.x, g), t.m, g);
+    t.s += b.y;
+    t.w += b.z;
   }
   t.s = warp_sum(t.s);
   if (W) t.w = warp_sum(t.w);
@@ -320,15 +384,6 @@ struct Ref {
   // (x - m) / T, of a masked token's lowest value too
   __device__ __forceinline__ float nat(float x) const { return apart(x) ? (x - m) * inv_t : fmaf(x, c, -rho) * LN2; }
 };
-
-template <typename T, bool W, bool CL>
-__device__ __forceinline__ Sums row_sums(const Piece<T>& p, const Geometry& g, Exchange& ex, int rank, float& thread_max) {
-  const Sums own = sweep<T, W>(p, g);
-  thread_max = own.m;
-  Sums a = join<W, CL, false>(own, ex, g, rank);
-  if (Ref(a.m, g).far) a = join<W, CL, true>(sweep_far<T, W>(p, g, a.m), ex, g, rank);
-  return a;
-}
 
 extern __shared__ uint4 dynamic[];
 
@@ -364,73 +419,112 @@ __device__ __forceinline__ float value_of(uint32_t o) {
 }
 __device__ __forceinline__ u64 key_of(uint32_t order, int j) { return ((u64)order << 32) | (uint32_t)~j; }
 
+
+constexpr int ENTRIES = 8;                    // maxima that a thread leaves of its batches
+
+template <int NT>
 struct TopSpace {
   u64 list[CANDIDATES];
-  int count, base, warp_total[MAX_WARPS];
+  float maxima[ENTRIES][NT];                  // of `stride` batches each
+  uint32_t halves[2 * NT];                    // the order of every thread's maxima over vectors 0, 1 and 2, 3 of all batches
+  unsigned short hits[ENTRIES * NT];
+  uint32_t bound;
+  int count, found, warp_total[NT / 32];
   u64 sorted[MAX_CLUSTER][TOP_MAX];           // of the row's first block: what each block found
 };
 
-// Puts the keys of the block's k largest logits (all of them, if there are fewer) into ts.list and returns how many are
-// there: at least min(k, logits), at most CANDIDATES.
-//   bound: the k-th largest of the threads' maxima, or a little less: at least k logits reach it, and of logits in no
-//   particular order hardly more (k = 64 of 256 threads: 74).  Halving an interval of the order, one count per step.
-//   Where more than CANDIDATES reach it (many equal logits, or large ones side by side), the k-th largest value itself is
-//   found the same way among all logits, and the equal ones are taken in the order of their ids.
-template <typename T>
-__device__ int top_candidates(const Piece<T>& p, int k, float thread_max, TopSpace& ts) {
-  const int tid = threadIdx.x, nt = blockDim.x;
-  // bounds of the thread's largest logit: what counts as -infinity may be a NaN, which stands below
-  const uint32_t most = tid < p.count ? order_of(thread_max) : 0u, least = thread_max == -INFINITY ? 0u : most;
-  if (tid == 0) ts.count = 0;
-  uint32_t lo = 0, hi = 0xffffffffu;                     // at least k reach lo (0: all), fewer than k reach hi
-  while (hi - lo > 1) {
+// One warp: a bound that at least k of the values reach (0 if there are not as many), and not many more unless they are equal.
+template <int COUNT>
+__device__ __forceinline__ uint32_t bound_of(const uint32_t* values, int k) {
+  constexpr int P = COUNT / 32;
+  uint32_t v[P], lo = 0xffffffffu, hi = 0;
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    v[i] = values[32 * i + (threadIdx.x & 31)];
+    if (v[i]) { lo = min(lo, v[i]); ++n; }
+    hi = max(hi, v[i]);
+  }
+  if (__reduce_add_sync(0xffffffffu, n) < k) return 0;
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi) + 1;
+  while (hi - lo > 1) {                                  // at least k reach lo, fewer than k reach hi
     const uint32_t mid = lo + (hi - lo) / 2;
-    const int n = __syncthreads_count(least >= mid);
-    if (n >= k) {
+    n = 0;
+#pragma unroll
+    for (int i = 0; i < P; ++i) n += v[i] >= mid;
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (n < k) {
+      hi = mid;
+    } else {
       lo = mid;
       if (n <= k + k / 4) break;
-    } else {
-      hi = mid;
     }
   }
+  return lo;
+}
+
+// Puts the keys of the block's k largest logits (all of them, if there are fewer) into ts.list and returns how many are
+// there: at least min(k, logits), at most CANDIDATES.
+//   The k-th largest of the 2 NT maxima of the threads' halves, or a little less, is reached by at least k logits, and of
+//   logits in no particular order by hardly more (k = 64 of 256: 74).  Only batches whose maximum reaches it are read again.
+//   Where more than CANDIDATES logits reach it (many equal ones, or large ones side by side), the k-th largest value itself is
+//   found among all logits by halving, and the equal ones are taken in the order of their ids.
+template <typename T, int NT>
+__device__ int top_candidates(const Piece<T, NT>& p, float edge, int k, float thread_max, int stride, int entries, TopSpace<NT>& ts) {
+  constexpr int N = Vec<T>::N;
+  constexpr uint32_t NOTHING = 0x007fffffu;              // the order of -infinity
+  const int tid = threadIdx.x;
+  if (tid < 32) {
+    const uint32_t b = bound_of<2 * NT>(ts.halves, k);
+    if (tid == 0) { ts.bound = b; ts.count = 0; ts.found = 0; }
+  }
   __syncthreads();
+  uint32_t lo = ts.bound;
+  const float bound = lo <= NOTHING ? -INFINITY : value_of(lo);
   auto add = [&](uint32_t o, int j) {
     const int at = atomicAdd(&ts.count, 1);
     if (at < CANDIDATES) ts.list[at] = key_of(o, j);
   };
-  if (most >= lo) {
-    for (int v = tid; v < p.count; v += nt) {
-      const uint4 a = p.buf[v];
-      if (order_of(Vec<T>::max1(a)) < lo) continue;
-      const int j = p.element(v);
-      for (int i = 0; i < Vec<T>::N; ++i) {
-        const uint32_t o = order_of(Vec<T>::get(a, i));
-        if (o >= lo && j + i >= 0 && j + i < p.n) add(o, j + i);
-      }
+  auto vector = [&](int v) { return *(const uint4*)(p.x + p.element(v)); };
+  for (int e = 0; e < entries; ++e)
+    if (lo <= NOTHING || ts.maxima[e][tid] >= bound) ts.hits[atomicAdd(&ts.found, 1)] = (unsigned short)(e * NT + tid);
+  if (p.edge >= 0 && order_of(edge) >= lo) add(order_of(edge), p.edge);
+  __syncthreads();
+  const int per = 4 * stride, units = ts.found * per;
+  for (int i = tid; i < units; i += NT) {
+    const int h = ts.hits[i / per], at = i % per, v = ((h / NT * stride + at / 4) * 4 + at % 4) * NT + h % NT;
+    if (v >= p.count) continue;
+    const uint4 a = vector(v);
+    if (lo > NOTHING && !(Vec<T>::max1(a) >= bound)) continue;
+    for (int i = 0; i < N; ++i) {
+      const uint32_t o = order_of(Vec<T>::get(a, i));
+      if (o >= lo) add(o, p.element(v) + i);
     }
   }
   __syncthreads();
-  const int found = ts.count;
-  if (found <= CANDIDATES) return found;
+  if (ts.count <= CANDIDATES) return ts.count;
 
-  // exactly: the largest value that at least k logits reach
-  auto reaching = [&](uint32_t bound) {
+  // exactly: the largest value that at least k logits reach; most: the order of the thread's largest
+  const uint32_t most = max(order_of(thread_max), NOTHING);
+  auto reaching = [&](uint32_t b) {
     int n = 0;
-    if (most >= bound)
-      for (int v = tid; v < p.count; v += nt) {
-        const int j = p.element(v);
-        for (int i = 0; i < Vec<T>::N; ++i) n += j + i >= 0 && j + i < p.n && order_of(Vec<T>::get(p.buf[v], i)) >= bound;
+    if (most >= b) {
+      for (int v = tid; v < p.count; v += NT) {
+        const uint4 a = vector(v);
+        for (int i = 0; i < N; ++i) n += order_of(Vec<T>::get(a, i)) >= b;
       }
+      n += p.edge >= 0 && order_of(edge) >= b;
+    }
     n = __reduce_add_sync(0xffffffffu, n);
     __syncthreads();
-    if (tid == 0) ts.base = 0;
+    if ((tid & 31) == 0) ts.warp_total[tid >> 5] = n;
     __syncthreads();
-    if ((tid & 31) == 0) atomicAdd(&ts.base, n);
-    __syncthreads();
-    return ts.base;
+    n = 0;
+    for (int w = 0; w < NT / 32; ++w) n += ts.warp_total[w];
+    return n;
   };
-  hi = 0xffffffffu;
-  uint32_t probe = lo + 1;                               // often lo itself is the value
+  uint32_t hi = 0xffffffffu, probe = lo + 1;             // often lo itself is the value
   int above = 0;
   while (hi - lo > 1) {
     const int n = reaching(probe);
@@ -438,29 +532,35 @@ __device__ int top_candidates(const Piece<T>& p, int k, float thread_max, TopSpa
     else { hi = probe; above = n; }
     probe = lo + (hi - lo) / 2;
   }
+  if (tid == 0) ts.count = 0;
   __syncthreads();
-  if (tid == 0) { ts.count = 0; ts.base = 0; }
-  __syncthreads();
-  if (most > lo)
-    for (int v = tid; v < p.count; v += nt) {
-      const int j = p.element(v);
-      for (int i = 0; i < Vec<T>::N; ++i) {
-        const uint32_t o = order_of(Vec<T>::get(p.buf[v], i));
-        if (o > lo && j + i >= 0 && j + i < p.n) add(o, j + i);
+  if (most > lo) {
+    for (int v = tid; v < p.count; v += NT) {
+      const uint4 a = vector(v);
+      for (int i = 0; i < N; ++i) {
+        const uint32_t o = order_of(Vec<T>::get(a, i));
+        if (o > lo) add(o, p.element(v) + i);
       }
     }
-  int taken = above;                                     // ids ascend with v, and within a step with the thread
-  for (int v0 = 0; v0 < p.count && taken < k; v0 += nt) {
-    const int v = v0 + tid;
+    if (p.edge >= 0 && order_of(edge) > lo) add(order_of(edge), p.edge);
+  }
+  // ids ascend from the row's first elements over its vectors, step by step and within a step with the thread, to its last
+  int taken = above;
+  const int steps = (p.count + NT - 1) / NT;
+  for (int step = -1; step <= steps && taken < k; ++step) {
     unsigned same = 0;
-    int j = 0;
-    if (v < p.count) {
+    int j = p.edge;
+    const int v = step * NT + tid;
+    if (step < 0 || step == steps) {
+      if (p.edge >= 0 && (p.edge < p.head) == (step < 0) && order_of(edge) == lo) same = 1;
+    } else if (v < p.count) {
+      const uint4 a = vector(v);
       j = p.element(v);
-      for (int i = 0; i < Vec<T>::N; ++i)
-        if (j + i >= 0 && j + i < p.n && order_of(Vec<T>::get(p.buf[v], i)) == lo) same |= 1u << i;
+      for (int i = 0; i < N; ++i)
+        if (order_of(Vec<T>::get(a, i)) == lo) same |= 1u << i;
     }
-    int before = __popc(same);
-    const int own = before;
+    const int own = __popc(same);
+    int before = own;
     for (int o = 1; o < 32; o <<= 1) {
       const int y = __shfl_up_sync(0xffffffffu, before, o);
       if ((tid & 31) >= o) before += y;
@@ -470,7 +570,7 @@ __device__ int top_candidates(const Piece<T>& p, int k, float thread_max, TopSpa
     __syncthreads();
     int total = 0;
     before -= own;
-    for (int w = 0; w < nt >> 5; ++w) {
+    for (int w = 0; w < NT / 32; ++w) {
       if (w < tid >> 5) before += ts.warp_total[w];
       total += ts.warp_total[w];
     }
@@ -483,101 +583,169 @@ __device__ int top_candidates(const Piece<T>& p, int k, float thread_max, TopSpa
 }
 
 // ---------------------------------------------------------------------------------------------- kernels
-template <typename T, bool W, bool CL>
-__global__ void __launch_bounds__(MAX_THREADS) logprobs_kernel(const __grid_constant__ LogprobsArgs a, const __grid_constant__ Geometry g) {
-  __shared__ Exchange ex;
+// A block (a cluster) takes every groups-th row.
+struct Place {
+  int rank, groups;                           // of the block in its cluster; clusters
+  long long row;                              // the first
+  template <bool CL> static __device__ __forceinline__ Place of(const Geometry& g) {
+    return CL ? Place{(int)(blockIdx.x % g.cluster), (int)(gridDim.x / g.cluster), (long long)(blockIdx.x / g.cluster)}
+              : Place{0, (int)gridDim.x, (long long)blockIdx.x};
+  }
+};
+
+constexpr int STREAM = 128, SLOTS = 4;        // threads of a block that reads its rows once; batches that it has on their way
+
+// Batches pass through a ring of SLOTS, each thread's by itself: copies run ahead of the sums by SLOTS batches, over the end of
+// a row into the next ones, so that they go on while a row's sums are joined and handed out.
+template <typename T, bool W, bool CL, bool TOP>
+__global__ void __launch_bounds__(STREAM) logprobs_kernel(const __grid_constant__ LogprobsArgs a, const __grid_constant__ Geometry g) {
+  constexpr int NT = STREAM;
+  __shared__ Exchange<NT> ex;
   cudaGridDependencySynchronize();
   cluster_start<CL>();
-  const int rank = CL ? (int)(blockIdx.x % g.cluster) : 0, tid = threadIdx.x, nt = blockDim.x;
-  const long long r = CL ? blockIdx.x / g.cluster : blockIdx.x;
-  const T* x = (const T*)a.in.x + r * a.in.ld;
-  const Piece<T> p(x, a.in.vocab, rank, CL ? g.cluster : 1, dynamic);
-  p.fetch();
+  const Place me = Place::of<CL>(g);
+  const int rank = me.rank, tid = threadIdx.x, rows = a.in.rows;
   const bool speaks = rank == 0 && tid == 0;             // for the row
-  int t = -1;
-  float xt = 0.f;
-  if (speaks && a.tokens) {
-    t = token_of(a.tokens, r, p.n, a.in.out_of_range, true);
-    if (t >= 0) xt = to_f(x[t]);
-  }
-  p.arrived();
-  cluster_started<CL>();
-  float thread_max;
-  const Sums s = row_sums<T, W, CL>(p, g, ex, rank, thread_max);
-  const Ref ref(s.m, g);
-  const float logs = logf(s.s);
-  auto logp = [&](float v) { return s.s == 0.f ? -INFINITY : ref.nat(v) - logs; };
-  if (speaks) {
-    if (a.logp) a.logp[r] = t >= 0 ? logp(xt) : 0.f;
-    if (W && a.entropy) a.entropy[r] = s.s == 0.f ? 0.f : fmaf(-LN2, s.w / s.s, logs);
-    if (a.lse) a.lse[r] = s.s == 0.f ? -INFINITY : ref.far ? fmaf(s.m, g.inv_t, logs) : fmaf(ref.rho, LN2, logs);
-  }
-  if (a.top_k == 0) return;
-  const int k = a.top_k;
-  TopSpace& ts = *(TopSpace*)(dynamic + p.per);
-  auto put = [&](int at, u64 key) {
-    a.top_ids[r * k + at] = (int)~(uint32_t)key;
-    a.top_logp[r * k + at] = logp(value_of((uint32_t)(key >> 32)));
-  };
-  const int found = top_candidates(p, k, thread_max, ts);
-  u64* sorted = CL ? cg::this_cluster().map_shared_rank(&ts.sorted[rank][0], 0) : nullptr;
-  for (int i = tid; i < found; i += nt) {                // a candidate's place is the number of larger ones
-    const u64 key = ts.list[i];
-    int at = 0;
-    for (int j = 0; j < found; ++j) at += ts.list[j] > key;
-    if (at >= k) continue;
-    if (CL) sorted[at] = key;
-    else put(at, key);
-  }
-  if constexpr (CL) {
-    for (int i = found + tid; i < k; i += nt) sorted[i] = 0;   // fewer logits than k in this piece
-    sync_row<true>();
-    if (rank != 0) return;
-    for (int i = tid; i < g.cluster * k; i += nt) {        // the place among all: the larger ones of every block's list
-      const int q = i / k;
-      const u64 key = ts.sorted[q][i - q * k];
-      if (key == 0) continue;
-      int at = i - q * k;
-      for (int o = 0; o < g.cluster; ++o) {
-        if (o == q) continue;
-        int lo = 0, hi = k;
-        while (lo < hi) {
-          const int mid = (lo + hi) / 2;
-          if (ts.sorted[o][mid] > key) lo = mid + 1;
-          else hi = mid;
-        }
-        at += lo;
-      }
-      if (at < k) put(at, key);
+  Piece<T, NT> p(a.in, me.row, rank, g), ahead = p;
+  long long ahead_row = me.row;
+  int ahead_batch = 0, slot = 0;
+  auto fetch = [&]() {
+    if (ahead_row >= rows) return p.commit();
+    ahead.fetch(dynamic + slot * 4 * NT + tid, ahead_batch);
+    if (++ahead_batch == g.batches) {
+      ahead_batch = 0;
+      ahead_row += me.groups;
+      if (ahead_row < rows) ahead = Piece<T, NT>(a.in, ahead_row, rank, g);
     }
+  };
+  for (; slot < SLOTS; ++slot) fetch();
+  slot = 0;
+  float edge = p.edge_value();
+  int t = speaks && a.tokens ? token_of(a.tokens, me.row, a.in.vocab, a.in.out_of_range, true) : -1;
+  float xt = t >= 0 ? to_f(p.x[t]) : 0.f;
+  cluster_started<CL>();
+  TopSpace<NT>& ts = *(TopSpace<NT>*)(dynamic + SLOTS * 4 * NT);
+  const int stride = TOP ? (g.batches + ENTRIES - 1) / ENTRIES : 1;
+  int turn = 0;
+  for (long long r = me.row; r < rows; r += me.groups, turn ^= 1) {
+    const bool has_next = r + me.groups < rows;
+    const Piece<T, NT> next(a.in, has_next ? r + me.groups : r, rank, g);
+    const float next_edge = next.edge_value();
+    const int next_t = speaks && a.tokens && has_next ? token_of(a.tokens, r + me.groups, a.in.vocab, a.in.out_of_range, true) : -1;
+    Running<T, W> run(g);
+    float h0 = -INFINITY, h1 = -INFINITY, em = -INFINITY;
+    int entry = 0, in_entry = 0;
+    for (int b = 0; b < g.batches; ++b) {
+      wait_groups(SLOTS - 1);
+      uint4 v[4];
+      p.load(v, dynamic + slot * 4 * NT + tid, b);
+      if (TOP) {
+        h0 = fmaxf(h0, fmaxf(Vec<T>::max1(v[0]), Vec<T>::max1(v[1])));
+        h1 = fmaxf(h1, fmaxf(Vec<T>::max1(v[2]), Vec<T>::max1(v[3])));
+      }
+      const float bm = run.add(v, g);
+      if (TOP) {
+        em = fmaxf(em, bm);
+        if (++in_entry == stride || b + 1 == g.batches) {
+          ts.maxima[entry++][tid] = em;
+          em = -INFINITY;
+          in_entry = 0;
+        }
+      }
+      fetch();
+      slot = slot + 1 == SLOTS ? 0 : slot + 1;
+    }
+    if (TOP) {
+      h1 = fmaxf(h1, edge);
+      ts.halves[tid] = h0 == -INFINITY ? 0u : order_of(h0);          // what counts as -infinity may be a NaN, which stands below
+      ts.halves[NT + tid] = h1 == -INFINITY ? 0u : order_of(h1);
+    }
+    Sums s = join<NT, W, CL, false>(run.end(edge, g), ex.part[turn][0], g, rank);
+    const Ref ref(s.m, g);
+    if (ref.far) s = join<NT, W, CL, true>(sweep_far<T, NT, W>(p, g, s.m, edge), ex.part[turn][1], g, rank);
+    const float logs = logf(s.s);
+    auto logp = [&](float v) { return s.s == 0.f ? -INFINITY : ref.nat(v) - logs; };
+    const float next_xt = next_t >= 0 ? to_f(next.x[next_t]) : 0.f;
+    if (speaks) {
+      if (a.logp) a.logp[r] = t >= 0 ? logp(xt) : 0.f;
+      if (W && a.entropy) a.entropy[r] = s.s == 0.f ? 0.f : fmaf(-LN2, s.w / s.s, logs);
+      if (a.lse) a.lse[r] = s.s == 0.f ? -INFINITY : ref.far ? fmaf(s.m, g.inv_t, logs) : fmaf(ref.rho, LN2, logs);
+    }
+    if constexpr (TOP) {
+      const int k = a.top_k;
+      auto put = [&](int at, u64 key) {
+        a.top_ids[r * k + at] = (int)~(uint32_t)key;
+        a.top_logp[r * k + at] = logp(value_of((uint32_t)(key >> 32)));
+      };
+      const int found = top_candidates<T, NT>(p, edge, k, run.m, stride, entry, ts);
+      u64* sorted = CL ? cg::this_cluster().map_shared_rank(&ts.sorted[rank][0], 0) : nullptr;
+      for (int i = tid; i < found; i += NT) {            // a candidate's place is the number of larger ones
+        const u64 key = ts.list[i];
+        int at = 0;
+#pragma unroll 8
+        for (int j = 0; j < found; ++j) at += ts.list[j] > key;
+        if (at >= k) continue;
+        if (CL) sorted[at] = key;
+        else put(at, key);
+      }
+      if constexpr (CL) {
+        for (int i = found + tid; i < k; i += NT) sorted[i] = 0;   // fewer logits than k in this piece
+        sync_row<true>();
+        if (rank == 0)
+          for (int i = tid; i < g.cluster * k; i += NT) {          // the place among all: the larger ones of every block's list
+            const int q = i / k;
+            const u64 key = ts.sorted[q][i - q * k];
+            if (key == 0) continue;
+            int at = i - q * k;
+            for (int o = 0; o < g.cluster; ++o) {
+              if (o == q) continue;
+              int lo = 0, hi = k;
+              while (lo < hi) {
+                const int mid = (lo + hi) / 2;
+                if (ts.sorted[o][mid] > key) lo = mid + 1;
+                else hi = mid;
+              }
+              at += lo;
+            }
+            if (at < k) put(at, key);
+          }
+      }
+      // the lists are used again behind the barrier of the next row's sums
+    }
+    p = next;
+    edge = next_edge;
+    t = next_t;
+    xt = next_xt;
   }
+  wait_groups(0);
 }
 
-// The row's second pass: dst = 2^y (k0 + k1 y), a token's own term added.
-template <typename T, bool W>
-__device__ __forceinline__ void gradient(const Piece<T>& p, const Geometry& g, const Ref& ref, float k0, float k1, int t, float at_t, T* dst) {
+// The row's second pass: dst = 2^y (k0 + k1 y), a token's own term added; the next row takes the place.
+template <typename T, int NT, bool W>
+__device__ __forceinline__ void gradient(const Piece<T, NT>& p, uint4* buf, float edge, const Geometry& g, const Ref& ref, float k0, float k1,
+                                         int t, float at_t, T* dst, const Piece<T, NT>& next, bool fetch_next) {
   constexpr int N = Vec<T>::N;
+  auto one = [&](float x, int j) {
+    const float y = ref.y(W && !ref.far ? max_nan(x, g.lo) : x), e = ex2(y);
+    return (e == 0.f && k0 == k0 ? 0.f : W ? e * fmaf(k1, y, k0) : e * k0) + (j == t ? at_t : 0.f);
+  };
+  if (p.edge >= 0) dst[p.edge] = from_f<T>(one(edge, p.edge));
   if (ref.far) {
-    for (int v = threadIdx.x; v < p.count; v += blockDim.x) {
+    for (int v = threadIdx.x; v < p.count; v += NT) {
       uint4 o;
       const int j = p.element(v);
-      float d[N];
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float y = ref.y(Vec<T>::get(p.buf[v], i)), e = ex2(y);
-        d[i] = e == 0.f && k0 == k0 ? 0.f : W ? e * fmaf(k1, y, k0) : e * k0;
-        if (j + i == t) d[i] += at_t;
-      }
-#pragma unroll
-      for (int i = 0; i < N / 2; ++i) Vec<T>::set_pair(o, i, pack(d[2 * i], d[2 * i + 1]));
+      for (int i = 0; i < N / 2; ++i)
+        Vec<T>::set_pair(o, i, pack(one(Vec<T>::get(buf[v], 2 * i), j + 2 * i), one(Vec<T>::get(buf[v], 2 * i + 1), j + 2 * i + 1)));
       p.store(dst, v, o);
     }
+    if (fetch_next) next.fetch_all(buf, g);
     return;
   }
   const u64 c2 = pack(g.c, g.c), nrho = pack(-ref.rho, -ref.rho), k02 = pack(k0, k0), k12 = pack(k1, k1);
-#pragma unroll 2
-  for (int v = threadIdx.x; v < p.count; v += blockDim.x) {
-    uint4 a = p.buf[v], o;
+  const bool aligned = ((uintptr_t)(dst + p.head) & 15) == 0;
+  auto one_vector = [&](uint4 a, int v) {
+    uint4 o;
     if (W) Vec<T>::clamp(a, g.lo);
     u64 d[N / 2];
 #pragma unroll
@@ -593,213 +761,319 @@ __device__ __forceinline__ void gradient(const Piece<T>& p, const Geometry& g, c
     }
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) Vec<T>::set_pair(o, i, d[i]);
-    p.store(dst, v, o);
+    return o;
+  };
+  for (int b = 0; b < g.batches; ++b) {
+    const int v0 = 4 * b * NT + threadIdx.x;
+    if (p.whole(b) && aligned) {
+      uint4* d = (uint4*)(dst + p.element(v0));
+#pragma unroll
+      for (int u = 0; u < 4; ++u) d[u * NT] = one_vector(buf[v0 + u * NT], v0 + u * NT);
+    } else {
+      for (int v = v0; v < min(v0 + 4 * NT, p.count); v += NT) p.store(dst, v, one_vector(buf[v], v));
+    }
+    if (fetch_next) next.fetch(buf + v0, b);
   }
 }
 
+// The sums of a row whose batches all have their place: they stay, or as they are read make room for those of the next row.
+template <typename T, int NT, bool W, bool REFILL>
+__device__ __forceinline__ Sums sweep(const Piece<T, NT>& p, uint4* buf, float edge, const Geometry& g, const Piece<T, NT>& next, bool has_next) {
+  Running<T, W> run(g);
+  for (int b = 0; b < g.batches; ++b) {
+    wait_groups(REFILL ? g.batches - 1 : g.batches - 1 - b);
+    uint4 v[4];
+    p.load(v, buf + 4 * b * NT + threadIdx.x, b);
+    run.add(v, g);
+    if (REFILL) {
+      if (has_next) next.fetch(buf + 4 * b * NT + threadIdx.x, b);
+      else p.commit();
+    }
+  }
+  return run.end(edge, g);
+}
+
+constexpr int STAY = 256;                     // threads of a block whose rows stay for a second pass
+
 template <typename T, bool W, bool CL>
-__global__ void __launch_bounds__(MAX_THREADS) logprobs_bwd_kernel(const __grid_constant__ LogprobsBwdArgs a, const __grid_constant__ Geometry g) {
-  __shared__ Exchange ex;
+__global__ void __launch_bounds__(STAY, 3) logprobs_bwd_kernel(const __grid_constant__ LogprobsBwdArgs a, const __grid_constant__ Geometry g) {
+  constexpr int NT = STAY;
+  __shared__ Exchange<NT> ex;
   cudaGridDependencySynchronize();
   cluster_start<CL>();
-  const int rank = CL ? (int)(blockIdx.x % g.cluster) : 0;
-  const long long r = CL ? blockIdx.x / g.cluster : blockIdx.x;
-  const Piece<T> p((const T*)a.in.x + r * a.in.ld, a.in.vocab, rank, CL ? g.cluster : 1, dynamic);
-  T* dx = (T*)a.dx + r * a.ld_out;
-  const int t = a.dlogp ? token_of(a.tokens, r, p.n, a.in.out_of_range, rank == 0 && threadIdx.x == 0) : -1;
-  const float ga = t >= 0 ? a.dlogp[r] : 0.f, gb = W ? a.dentropy[r] : 0.f, gl = a.dlse ? a.dlse[r] : 0.f;
-  if (ga == 0.f && gb == 0.f && gl == 0.f) {
-    p.zeros(dx);
-    cluster_started<CL>();
-    return;
-  }
-  p.fetch();
-  p.arrived();
+  const Place me = Place::of<CL>(g);
+  const int rank = me.rank, rows = a.in.rows;
+  uint4* buf = dynamic;
+  struct In {                                 // what comes into a row
+    int t;
+    float ga, gb, gl;
+    __device__ __forceinline__ bool any() const { return !(ga == 0.f && gb == 0.f && gl == 0.f); }
+  };
+  auto incoming = [&](long long r) {
+    In i{-1, 0.f, W ? a.dentropy[r] : 0.f, a.dlse ? a.dlse[r] : 0.f};
+    if (a.dlogp) {
+      i.t = token_of(a.tokens, r, a.in.vocab, a.in.out_of_range, rank == 0 && threadIdx.x == 0);
+      i.ga = i.t >= 0 ? a.dlogp[r] : 0.f;
+    }
+    return i;
+  };
+  Piece<T, NT> p(a.in, me.row, rank, g);
+  In in = incoming(me.row);
+  if (in.any()) p.fetch_all(buf, g);
+  float edge = p.edge_value();
   cluster_started<CL>();
-  float thread_max;
-  const Sums s = row_sums<T, W, CL>(p, g, ex, rank, thread_max);
-  if (s.s == 0.f) {                                      // no token
-    p.zeros(dx);
-    return;
+  int turn = 0;
+  for (long long r = me.row; r < rows; r += me.groups, turn ^= 1) {
+    const long long rn = r + me.groups < rows ? r + me.groups : r;
+    const Piece<T, NT> next(a.in, rn, rank, g);
+    const In next_in = incoming(rn);
+    const float next_edge = next.edge_value();
+    T* dx = (T*)a.dx + r * a.ld_out;
+    if (in.any()) {
+      Sums s = join<NT, W, CL, false>(sweep<T, NT, W, false>(p, buf, edge, g, next, false), ex.part[turn][0], g, rank);
+      const Ref ref(s.m, g);
+      if (ref.far) s = join<NT, W, CL, true>(sweep_far<T, NT, W>(p, g, s.m, edge), ex.part[turn][1], g, rank);
+      const bool more = rn != r && next_in.any();
+      if (s.s == 0.f) {                                  // no token
+        p.zeros(dx);
+        if (more) next.fetch_all(buf, g);
+      } else {
+        const float k = g.inv_t / s.s;
+        gradient<T, NT, W>(p, buf, edge, g, ref, W ? (in.gl - in.ga + in.gb * (LN2 * (s.w / s.s))) * k : (in.gl - in.ga) * k, -in.gb * LN2 * k, in.t,
+                       in.ga * g.inv_t, dx, next, more);
+      }
+    } else {
+      p.zeros(dx);
+      if (rn != r && next_in.any()) next.fetch_all(buf, g);
+    }
+    p = next;
+    in = next_in;
+    edge = next_edge;
   }
-  const Ref ref(s.m, g);
-  const float k = g.inv_t / s.s;
-  gradient<T, W>(p, g, ref, W ? (gl - ga + gb * (LN2 * (s.w / s.s))) * k : (gl - ga) * k, -gb * LN2 * k, t, ga * g.inv_t, dx);
+  wait_groups(0);
 }
 
 __device__ __forceinline__ void sync_teacher() { asm volatile("bar.sync 1, 128;" ::: "memory"); }   // the first four warps
 
 template <typename T, bool CL>
-__global__ void __launch_bounds__(MAX_THREADS) distill_kernel(const __grid_constant__ DistillArgs a, const __grid_constant__ Geometry g) {
-  __shared__ Exchange ex;
+__global__ void __launch_bounds__(STAY, 3) distill_kernel(const __grid_constant__ DistillArgs a, const __grid_constant__ Geometry g) {
+  struct Shared {                             // of two rows in turn
+    float most_student, student[4], has[4];
+    double mass[4];
+  };
+  constexpr int NT = STAY;
+  __shared__ Exchange<NT> ex;
+  __shared__ Shared shared[2];
   __shared__ __align__(16) int id[TOP_MAX];
-  __shared__ float weight[TOP_MAX];
-  __shared__ float red[4][4];
-  __shared__ double red_mass[4];
-  __shared__ int any_weight;
+  __shared__ float weight[TOP_MAX], red[4][2];
   cudaGridDependencySynchronize();
   cluster_start<CL>();
-  const int rank = CL ? (int)(blockIdx.x % g.cluster) : 0, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, k = a.k;
-  const long long r = CL ? blockIdx.x / g.cluster : blockIdx.x;
-  const T* x = (const T*)a.in.x + r * a.in.ld;
-  const Piece<T> p(x, a.in.vocab, rank, CL ? g.cluster : 1, dynamic);
-  T* dx = a.dx ? (T*)a.dx + r * a.ld_out : nullptr;
-  p.fetch();
-  const float dl = a.dloss ? a.dloss[r] : 1.f;
-
-  // The teacher's row and what the student gives its tokens, an entry per thread of four warps, while the logits arrive.
-  float q = 0.f, lq = 0.f, xi = -INFINITY;
-  int i = -1, twins = 0;
-  bool first = false;
-  if (warp < 4) {
-    float t = -INFINITY;
+  const Place me = Place::of<CL>(g);
+  const int rank = me.rank, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, k = a.k, rows = a.in.rows;
+  uint4* buf = dynamic;
+  struct Entry { int i; float t, x; };        // the thread's entry of the teacher's row: token, value; the student's logit
+  auto entry = [&](long long r) {
+    Entry e{-1, -INFINITY, -INFINITY};
     if (tid < k) {
-      i = token_of(a.ids, r * k + tid, p.n, a.in.out_of_range, rank == 0);
-      if (i >= 0) { t = a.teacher[r * k + tid]; xi = to_f(x[i]); }
+      e.i = token_of(a.ids, r * k + tid, a.in.vocab, a.in.out_of_range, rank == 0);
+      e.t = a.teacher[r * k + tid];
     }
-    id[tid] = i;
-    const float wt = warp_max(t), wx = warp_max(xi);
-    const bool some = __any_sync(0xffffffffu, !(t == -INFINITY));
-    if (lane == 0) { red[warp][0] = wt; red[warp][1] = wx; red[warp][2] = some ? 1.f : 0.f; }
-    sync_teacher();
-    float mt = -INFINITY, ml = -INFINITY, has = 0.f;
-    for (int w = 0; w < 4; ++w) {
-      mt = fmaxf(mt, red[w][0]);
-      ml = fmaxf(ml, red[w][1]);
-      has += red[w][2];
-    }
-    const double e = t == -INFINITY ? 0.0 : a.rest ? exp((double)t) : (double)expf((t - mt) * g.inv_t);
-    first = i >= 0;
-    for (int j = 0; j < k; j += 4) {
-      const int4 o = *(const int4*)&id[j];
-      const int same = (o.x == i) + (o.y == i) + (o.z == i) + (o.w == i);
-      twins += same;                                     // entries of the same token; the first one stands for it
-      if (same && (o.x == i ? j : o.y == i ? j + 1 : o.z == i ? j + 2 : j + 3) < tid) first = false;
-    }
-    const Ref rl(ml, g);
-    const float el = first && xi != -INFINITY ? ex2(rl.y(xi)) : 0.f;
-    double mass = e;
-    for (int o = 16; o > 0; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
-    const float sl = warp_sum(el);
-    sync_teacher();                                      // red is read
-    if (lane == 0) { red_mass[warp] = mass; red[warp][3] = sl; red[warp][1] = ml; }
-    if (tid == 0) any_weight = has != 0.f;
-    sync_teacher();
-    mass = red_mass[0] + red_mass[1] + red_mass[2] + red_mass[3];
-    q = a.rest ? (float)e : (float)(e / mass);
-    lq = a.rest ? t : (t - mt) * g.inv_t - logf((float)mass);
-    weight[tid] = q;
-  }
-  p.arrived();
+    return e;
+  };
+  Piece<T, NT> p(a.in, me.row, rank, g);
+  p.fetch_all(buf, g);
+  float edge = p.edge_value();
+  Entry en = entry(me.row);
+  if (en.i >= 0) en.x = to_f(p.x[en.i]);
+  else en.t = -INFINITY;
   cluster_started<CL>();
-  __syncthreads();
-  if (!any_weight) {
-    if (rank == 0 && tid == 0 && a.loss) a.loss[r] = 0.f;
-    if (dx) p.zeros(dx);
-    return;
-  }
-  const int spot = i + p.shift - p.first * Vec<T>::N;    // the token's place in the piece, if it is there
-  const bool here = i >= 0 && spot >= 0 && spot < p.count * Vec<T>::N;
-  if (here) ((T*)p.buf)[spot] = from_f<T>(-INFINITY);    // what stays are the tokens not listed
-  __syncthreads();
-  float unused;
-  const Sums rest = row_sums<T, false, CL>(p, g, ex, rank, unused);
-  const double mass = red_mass[0] + red_mass[1] + red_mass[2] + red_mass[3];
-  const float qr = a.rest && 1.0 - mass > SMALLEST_REST ? (float)(1.0 - mass) : 0.f;
-  const float Q = a.rest ? (float)(qr > 0.f ? 1.0 : mass) : (float)(mass / mass);
-  const float ml = red[0][1], R = rest.s, m = fmaxf(rest.m, ml);
-  const Ref ref(m, g), rr(rest.m, g), rl(ml, g);
-  const bool far = ref.far || rr.far;
-  auto factor = [&](const Ref& o) { return o.m == -INFINITY ? 0.f : ex2(ref.far ? (o.m - m) * g.c : o.rho - ref.rho); };
-  const float f = factor(rr), S = R * f + (red[0][3] + red[1][3] + red[2][3] + red[3][3]) * factor(rl), logs = logf(S);
-  if (a.loss && rank == 0 && warp < 4) {
-    float l = i >= 0 && !(q == 0.f) ? q * (lq - (S == 0.f ? -INFINITY : ref.nat(xi) - logs)) : 0.f;
-    l = warp_sum(l);
-    if (lane == 0) red[warp][2] = l;
-    sync_teacher();
-    if (tid == 0) {
-      l = red[0][2] + red[1][2] + red[2][2] + red[3][2];
-      if (qr > 0.f) l += qr * (logf(qr) - (R == 0.f ? -INFINITY : (far ? (rest.m - m) * g.inv_t : (rr.rho - ref.rho) * LN2) + logf(R) - logs));
-      a.loss[r] = a.scale * l;
+  int turn = 0;
+  for (long long r = me.row; r < rows; r += me.groups, turn ^= 1) {
+    const bool has_next = r + me.groups < rows;
+    const long long rn = has_next ? r + me.groups : r;
+    const Piece<T, NT> next(a.in, rn, rank, g);
+    const float next_edge = next.edge_value();
+    Entry next_en = entry(rn);
+    const float dl = a.dloss ? a.dloss[r] : 1.f;
+    Shared& sh = shared[turn];
+
+    // The teacher's row and what the student gives its tokens, an entry per thread of four warps.
+    float q = 0.f, lq = 0.f;
+    const float xi = en.x;
+    const int i = en.i;
+    int twins = 0;                                       // entries of the same token; the first one stands for it
+    bool first = i >= 0;
+    if (warp < 4) {
+      const float t = en.t;
+      sync_teacher();                                    // the row before has been read
+      id[tid] = i;
+      const float wt = warp_max(t), wx = warp_max(xi);
+      const bool some = __any_sync(0xffffffffu, !(t == -INFINITY));
+      if (lane == 0) { red[warp][0] = wt; red[warp][1] = wx; sh.has[warp] = some ? 1.f : 0.f; }
+      sync_teacher();
+      const float mt = fmaxf(fmaxf(red[0][0], red[1][0]), fmaxf(red[2][0], red[3][0]));
+      const float ml = fmaxf(fmaxf(red[0][1], red[1][1]), fmaxf(red[2][1], red[3][1]));
+      const double e = t == -INFINITY ? 0.0 : a.rest ? exp((double)t) : (double)expf((t - mt) * g.inv_t);
+      for (int j = 0; j < k; j += 4) {
+        const int4 o = *(const int4*)&id[j];
+        const int same = (o.x == i) + (o.y == i) + (o.z == i) + (o.w == i);
+        twins += same;
+        if (same && (o.x == i ? j : o.y == i ? j + 1 : o.z == i ? j + 2 : j + 3) < tid) first = false;
+      }
+      const float el = first && xi != -INFINITY ? ex2(Ref(ml, g).y(xi)) : 0.f;
+      double mass = e;
+      for (int o = 16; o > 0; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
+      const float sl = warp_sum(el);
+      if (lane == 0) { sh.mass[warp] = mass; sh.student[warp] = sl; }
+      if (tid == 0) sh.most_student = ml;
+      sync_teacher();
+      mass = sh.mass[0] + sh.mass[1] + sh.mass[2] + sh.mass[3];
+      q = a.rest ? (float)e : (float)(e / mass);
+      lq = a.rest ? t : (t - mt) * g.inv_t - logf((float)mass);
+      weight[tid] = q;
     }
-  }
-  if (!dx) return;
-  if (dl == 0.f) {
-    p.zeros(dx);
-    return;
-  }
-  const float w = dl * a.scale * g.inv_t;
-  const float kappa = S != S ? S : R == 0.f ? 0.f : (Q * f / S - (qr > 0.f ? qr / R : 0.f)) * w;
-  gradient<T, false>(p, g, rr, kappa, 0.f, -1, 0.f, dx);
-  __syncthreads();
-  if (first && here) {
-    float qi = q;
-    if (twins > 1) {
-      qi = 0.f;
-      for (int j = 0; j < k; ++j) qi += id[j] == i ? weight[j] : 0.f;
+    const int spot = i - p.head - p.first * Vec<T>::N;   // the token's place in the piece, if it is there
+    if (a.rest) {                                        // what stays are the tokens not listed
+      wait_groups(0);
+      __syncthreads();
+      if (i >= 0 && spot >= 0 && spot < p.count * Vec<T>::N) ((T*)buf)[spot] = from_f<T>(-INFINITY);
+      if (p.edge >= 0)
+        for (int j = 0; j < k; ++j)
+          if (id[j] == p.edge) edge = -INFINITY;
+      __syncthreads();
     }
-    const float pi = (xi == -INFINITY ? 0.f : ex2(ref.y(xi))) / S;
-    dx[i] = from_f<T>(S == 0.f ? 0.f : (Q * pi - qi) * w);
+    // Without a rest the sums are those of all tokens.
+    Sums o;
+    if (a.dx) o = join<NT, false, CL, false>(sweep<T, NT, false, false>(p, buf, edge, g, next, false), ex.part[turn][0], g, rank);
+    else o = join<NT, false, CL, false>(sweep<T, NT, false, true>(p, buf, edge, g, next, has_next), ex.part[turn][0], g, rank);
+    const Ref ro(o.m, g);
+    if (ro.far) o = join<NT, false, CL, true>(sweep_far<T, NT, false>(p, g, o.m, edge, id, a.rest ? k : 0), ex.part[turn][1], g, rank);
+    if (next_en.i >= 0) next_en.x = to_f(next.x[next_en.i]);
+    else next_en.t = -INFINITY;
+
+    const bool any = sh.has[0] + sh.has[1] + sh.has[2] + sh.has[3] != 0.f;
+    const double mass = sh.mass[0] + sh.mass[1] + sh.mass[2] + sh.mass[3];
+    const float qr = a.rest && 1.0 - mass > SMALLEST_REST ? (float)(1.0 - mass) : 0.f, R = o.s;
+    const float Q = a.rest ? (float)(qr > 0.f ? 1.0 : mass) : (float)(mass / mass);
+    const float m = a.rest ? fmaxf(o.m, sh.most_student) : o.m;
+    const Ref ref(m, g);
+    float f = 1.f, S = R;                                // of the sums o, against the row's maximum
+    if (a.rest) {
+      auto factor = [&](const Ref& b) { return b.m == -INFINITY ? 0.f : ex2(ref.far ? (b.m - m) * g.c : b.rho - ref.rho); };
+      f = factor(ro);
+      S = R * f + (sh.student[0] + sh.student[1] + sh.student[2] + sh.student[3]) * factor(Ref(sh.most_student, g));
+    }
+    if (a.loss && rank == 0 && warp < 4) {
+      const float logs = logf(S);
+      float l = i >= 0 && !(q == 0.f) ? q * (lq - (S == 0.f ? -INFINITY : ref.nat(xi) - logs)) : 0.f;
+      l = warp_sum(l);
+      sync_teacher();                                    // red has been read
+      if (lane == 0) red[warp][0] = l;
+      sync_teacher();
+      if (tid == 0) {
+        l = red[0][0] + red[1][0] + red[2][0] + red[3][0];
+        if (qr > 0.f)
+          l += qr * (logf(qr) - (R == 0.f ? -INFINITY : (ref.far || ro.far ? (o.m - m) * g.inv_t : (ro.rho - ref.rho) * LN2) + logf(R) - logs));
+        a.loss[r] = any ? a.scale * l : 0.f;
+      }
+    }
+    if (a.dx) {
+      T* dx = (T*)a.dx + r * a.ld_out;
+      if (!any || dl == 0.f) {
+        p.zeros(dx);
+        if (has_next) next.fetch_all(buf, g);
+      } else {
+        const float w = dl * a.scale * g.inv_t;
+        const float kappa = S != S ? S : R == 0.f ? 0.f : (Q * f / S - (qr > 0.f ? qr / R : 0.f)) * w;
+        gradient<T, NT, false>(p, buf, edge, g, ro, kappa, 0.f, -1, 0.f, dx, next, has_next);
+        __syncthreads();
+        const bool here = spot >= 0 && spot < p.count * Vec<T>::N, outside = i < p.head || i >= a.in.vocab - (a.in.vocab - p.head) % Vec<T>::N;
+        if (first && (here || (rank == 0 && outside))) {
+          float qi = q;
+          if (twins > 1) {
+            qi = 0.f;
+            for (int j = 0; j < k; ++j) qi += id[j] == i ? weight[j] : 0.f;
+          }
+          const float pi = (xi == -INFINITY ? 0.f : ex2(ref.y(xi))) / S;
+          dx[i] = from_f<T>(S == 0.f ? 0.f : (Q * pi - qi) * w);
+        }
+      }
+    }
+    p = next;
+    edge = next_edge;
+    en = next_en;
   }
+  wait_groups(0);
 }
 
 // ---------------------------------------------------------------------------------------------- launches
-constexpr int PIECE = 4160;                   // vectors of a block's piece that let three blocks stay on an SM
+constexpr int PIECE = 4160;                   // vectors of a staying piece that let three blocks share an SM
+constexpr int STATIC = 6 * 1024 + 512;        // shared memory beside it, at most
 
 struct Plan {
   Geometry g;
   dim3 grid;
-  int threads, per;                           // vectors of the longest piece
+  int threads;
+  size_t smem;
 };
-Plan plan_rows(const LogitsIn& in, int elem_bytes, int min_threads) {
+// Blocks of `threads`; stay: rows stay in shared memory as a whole, otherwise it takes `smem` bytes.
+Plan plan_rows(const LogitsIn& in, int elem_bytes, int threads, bool stay, size_t smem, size_t smem_cluster) {
   Plan p{};
-  const int N = 16 / elem_bytes, all = (in.vocab + 2 * N - 2) / N;      // a row may begin inside its first vector
-  int c = std::min(MAX_CLUSTER, (all + PIECE - 1) / PIECE);
+  const int N = 16 / elem_bytes, all = std::max(1, in.vocab / N);
+  int c = stay ? std::min(MAX_CLUSTER, (all + PIECE - 1) / PIECE) : 1;
   while (2 * c <= MAX_CLUSTER && (long long)in.rows * c < 2 * 148 && all / (2 * c) >= 256) c *= 2;
-  p.per = (all + c - 1) / c;
-  p.threads = p.per > PIECE ? 512 : std::max(min_threads, std::min(256, (p.per + 31) / 32 * 32));
-  p.grid = dim3((unsigned)((long long)in.rows * c));
+  const int per = (all + c - 1) / c;
+  p.threads = threads;
+  p.smem = (stay ? (size_t)per * 16 : smem) + (c > 1 ? smem_cluster : 0);
+  const int blocks = std::min({32, 65536 / (80 * threads), (int)(228 * 1024 / (p.smem + STATIC + 1024))});
+  p.grid = dim3((unsigned)(std::min<long long>(in.rows, std::max(1, 148 * blocks / c)) * c));
   const double cc = 1.4426950408889634 / (double)in.temperature;
-  p.g = Geometry{(float)cc, (float)(1.0 / (double)in.temperature), (float)(-1e30 * std::min(1.0, 1.0 / cc)), c};
+  p.g = Geometry{(float)cc, (float)(1.0 / (double)in.temperature), (float)(-1e30 * std::min(1.0, 1.0 / cc)), (float)(SLACK / cc), c, per,
+                 (per + 4 * threads - 1) / (4 * threads)};
   return p;
 }
 
 template <typename... KArgs, typename A>
-cudaError_t run(void (*kernel)(KArgs...), SmemLimit& limit, const Plan& p, size_t extra, cudaStream_t s, const A& a) {
+cudaError_t run(void (*kernel)(KArgs...), SmemLimit& limit, const Plan& p, cudaStream_t s, const A& a) {
   const cudaError_t e = limit.raise((const void*)kernel, 160 * 1024);
   if (e != cudaSuccess) return e;
-  return launch_cluster_after(kernel, p.g.cluster, p.grid, p.threads, (size_t)p.per * 16 + extra, s, a, p.g);
+  return launch_cluster_after(kernel, p.g.cluster, p.grid, p.threads, p.smem, s, a, p.g);
 }
 
-template <typename T, bool W, bool CL>
+template <typename T, bool W, bool CL, bool TOP>
 cudaError_t run_logprobs(const LogprobsArgs& a, const Plan& p, cudaStream_t s) {
   static SmemLimit limit;
-  return run(logprobs_kernel<T, W, CL>, limit, p, a.top_k == 0 ? 0 : CL ? sizeof(TopSpace) : offsetof(TopSpace, sorted), s, a);
+  return run(logprobs_kernel<T, W, CL, TOP>, limit, p, s, a);
+}
+template <typename T, bool W>
+cudaError_t run_logprobs(const LogprobsArgs& a, const Plan& p, cudaStream_t s) {
+  if (a.top_k > 0) return p.g.cluster > 1 ? run_logprobs<T, W, true, true>(a, p, s) : run_logprobs<T, W, false, true>(a, p, s);
+  return p.g.cluster > 1 ? run_logprobs<T, W, true, false>(a, p, s) : run_logprobs<T, W, false, false>(a, p, s);
 }
 template <typename T, bool W, bool CL>
 cudaError_t run_bwd(const LogprobsBwdArgs& a, const Plan& p, cudaStream_t s) {
   static SmemLimit limit;
-  return run(logprobs_bwd_kernel<T, W, CL>, limit, p, 0, s, a);
+  return run(logprobs_bwd_kernel<T, W, CL>, limit, p, s, a);
 }
 template <typename T, bool CL>
 cudaError_t run_distill(const DistillArgs& a, const Plan& p, cudaStream_t s) {
   static SmemLimit limit;
-  return run(distill_kernel<T, CL>, limit, p, 0, s, a);
+  return run(distill_kernel<T, CL>, limit, p, s, a);
 }
 
 }  // namespace
 
 cudaError_t launch_logprobs(const LogprobsArgs& a, bool is_bf16, cudaStream_t s) {
-  const Plan p = plan_rows(a.in, is_bf16 ? 2 : 4, 64);
-  const bool w = a.entropy != nullptr, cl = p.g.cluster > 1;
-  if (is_bf16) return w ? (cl ? run_logprobs<bf16, true, true>(a, p, s) : run_logprobs<bf16, true, false>(a, p, s))
-                        : (cl ? run_logprobs<bf16, false, true>(a, p, s) : run_logprobs<bf16, false, false>(a, p, s));
-  return w ? (cl ? run_logprobs<float, true, true>(a, p, s) : run_logprobs<float, true, false>(a, p, s))
-           : (cl ? run_logprobs<float, false, true>(a, p, s) : run_logprobs<float, false, false>(a, p, s));
+  typedef TopSpace<STREAM> Top;
+  const size_t ring = SLOTS * 4 * STREAM * 16;
+  const Plan p = a.top_k > 0 ? plan_rows(a.in, is_bf16 ? 2 : 4, STREAM, false, ring + offsetof(Top, sorted), sizeof(Top) - offsetof(Top, sorted))
+                             : plan_rows(a.in, is_bf16 ? 2 : 4, STREAM, false, ring, 0);
+  if (is_bf16) return a.entropy ? run_logprobs<bf16, true>(a, p, s) : run_logprobs<bf16, false>(a, p, s);
+  return a.entropy ? run_logprobs<float, true>(a, p, s) : run_logprobs<float, false>(a, p, s);
 }
 
 cudaError_t launch_logprobs_bwd(const LogprobsBwdArgs& a, bool is_bf16, cudaStream_t s) {
-  const Plan p = plan_rows(a.in, is_bf16 ? 2 : 4, 64);
+  const Plan p = plan_rows(a.in, is_bf16 ? 2 : 4, STAY, true, 0, 0);
   const bool w = a.dentropy != nullptr, cl = p.g.cluster > 1;
   if (is_bf16) return w ? (cl ? run_bwd<bf16, true, true>(a, p, s) : run_bwd<bf16, true, false>(a, p, s))
                         : (cl ? run_bwd<bf16, false, true>(a, p, s) : run_bwd<bf16, false, false>(a, p, s));
@@ -808,7 +1082,7 @@ cudaError_t launch_logprobs_bwd(const LogprobsBwdArgs& a, bool is_bf16, cudaStre
 }
 
 cudaError_t launch_distill(const DistillArgs& a, bool is_bf16, cudaStream_t s) {
-  const Plan p = plan_rows(a.in, is_bf16 ? 2 : 4, TOP_MAX);
+  const Plan p = plan_rows(a.in, is_bf16 ? 2 : 4, STAY, true, 0, 0);
   if (is_bf16) return p.g.cluster > 1 ? run_distill<bf16, true>(a, p, s) : run_distill<bf16, false>(a, p, s);
   return p.g.cluster > 1 ? run_distill<float, true>(a, p, s) : run_distill<float, false>(a, p, s);
 }
