@@ -85,57 +85,61 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 }
 
 // ---------------------------------------------------------------------------------------------- vectors of 16 bytes
+struct Quad { uint32_t w[4]; };
+__device__ __forceinline__ Quad quad(const uint4& v) { return Quad{{v.x, v.y, v.z, v.w}}; }
+__device__ __forceinline__ uint4 four(const Quad& q) { return make_uint4(q.w[0], q.w[1], q.w[2], q.w[3]); }
+template <typename T> __device__ __forceinline__ Quad nothing();          // -infinity throughout
+template <> __device__ __forceinline__ Quad nothing<bf16>() { return Quad{{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u}}; }
+template <> __device__ __forceinline__ Quad nothing<float>() { return Quad{{0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u}}; }
 template <typename T> struct Vec;
 template <> struct Vec<bf16> {
   static constexpr int N = 8;
-  static constexpr uint32_t NEG_INF = 0xFF80FF80u;
-  static __device__ __forceinline__ u64 pair(const uint4& v, int i) {
-    const uint32_t w = (&v.x)[i];
+  static __device__ __forceinline__ u64 pair(const Quad& v, int i) {
+    const uint32_t w = v.w[i];
     return pack(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
   }
   static __device__ __forceinline__ __nv_bfloat162 b2(uint32_t w) { return *(__nv_bfloat162*)&w; }
   static __device__ __forceinline__ uint32_t u2(__nv_bfloat162 w) { return *(uint32_t*)&w; }
   // the largest element; a NaN only if there is nothing else
-  static __device__ __forceinline__ float max1(const uint4& v) {
-    const __nv_bfloat162 m = __hmax2(__hmax2(b2(v.x), b2(v.y)), __hmax2(b2(v.z), b2(v.w)));
+  static __device__ __forceinline__ float max1(const Quad& v) {
+    const __nv_bfloat162 m = __hmax2(__hmax2(b2(v.w[0]), b2(v.w[1])), __hmax2(b2(v.w[2]), b2(v.w[3])));
     return __bfloat162float(__hmax(__low2bfloat16(m), __high2bfloat16(m)));
   }
-  static __device__ __forceinline__ float max4(const uint4* v) {
-    __nv_bfloat162 m = b2(v[0].x);
+  static __device__ __forceinline__ float max4(const Quad* v) {
+    __nv_bfloat162 m = b2(v[0].w[0]);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) m = __hmax2(m, __hmax2(__hmax2(b2(v[u].x), b2(v[u].y)), __hmax2(b2(v[u].z), b2(v[u].w))));
+    for (int u = 0; u < 4; ++u) m = __hmax2(m, __hmax2(__hmax2(b2(v[u].w[0]), b2(v[u].w[1])), __hmax2(b2(v[u].w[2]), b2(v[u].w[3]))));
     return __bfloat162float(__hmax(__low2bfloat16(m), __high2bfloat16(m)));
   }
-  static __device__ __forceinline__ void clamp(uint4& v, float lo) {
+  static __device__ __forceinline__ void clamp(Quad& v, float lo) {
     const __nv_bfloat162 l = __float2bfloat162_rn(lo);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) (&v.x)[i] = u2(__hmax2_nan(b2((&v.x)[i]), l));
+    for (int i = 0; i < 4; ++i) v.w[i] = u2(__hmax2_nan(b2(v.w[i]), l));
   }
-  static __device__ __forceinline__ float get(const uint4& v, int i) {
-    const uint32_t w = (&v.x)[i >> 1];
+  static __device__ __forceinline__ float get(const Quad& v, int i) {
+    const uint32_t w = v.w[i >> 1];
     return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
   }
-  static __device__ __forceinline__ void set_pair(uint4& v, int i, u64 p) {
+  static __device__ __forceinline__ void set_pair(Quad& v, int i, u64 p) {
     const float2 f = unpack(p);
-    (&v.x)[i] = u2(__floats2bfloat162_rn(f.x, f.y));
+    v.w[i] = u2(__floats2bfloat162_rn(f.x, f.y));
   }
 };
 template <> struct Vec<float> {
   static constexpr int N = 4;
-  static constexpr uint32_t NEG_INF = 0xFF800000u;
-  static __device__ __forceinline__ float at(const uint4& v, int i) { return __uint_as_float((&v.x)[i]); }
-  static __device__ __forceinline__ u64 pair(const uint4& v, int i) { return pack(at(v, 2 * i), at(v, 2 * i + 1)); }
-  static __device__ __forceinline__ float max1(const uint4& v) { return fmaxf(fmaxf(at(v, 0), at(v, 1)), fmaxf(at(v, 2), at(v, 3))); }
-  static __device__ __forceinline__ float max4(const uint4* v) { return fmaxf(fmaxf(max1(v[0]), max1(v[1])), fmaxf(max1(v[2]), max1(v[3]))); }
-  static __device__ __forceinline__ void clamp(uint4& v, float lo) {
+  static __device__ __forceinline__ float at(const Quad& v, int i) { return __uint_as_float(v.w[i]); }
+  static __device__ __forceinline__ u64 pair(const Quad& v, int i) { return pack(at(v, 2 * i), at(v, 2 * i + 1)); }
+  static __device__ __forceinline__ float max1(const Quad& v) { return fmaxf(fmaxf(at(v, 0), at(v, 1)), fmaxf(at(v, 2), at(v, 3))); }
+  static __device__ __forceinline__ float max4(const Quad* v) { return fmaxf(fmaxf(max1(v[0]), max1(v[1])), fmaxf(max1(v[2]), max1(v[3]))); }
+  static __device__ __forceinline__ void clamp(Quad& v, float lo) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) (&v.x)[i] = __float_as_uint(max_nan(at(v, i), lo));
+    for (int i = 0; i < 4; ++i) v.w[i] = __float_as_uint(max_nan(at(v, i), lo));
   }
-  static __device__ __forceinline__ float get(const uint4& v, int i) { return at(v, i); }
-  static __device__ __forceinline__ void set_pair(uint4& v, int i, u64 p) {
+  static __device__ __forceinline__ float get(const Quad& v, int i) { return at(v, i); }
+  static __device__ __forceinline__ void set_pair(Quad& v, int i, u64 p) {
     const float2 f = unpack(p);
-    (&v.x)[2 * i] = __float_as_uint(f.x);
-    (&v.x)[2 * i + 1] = __float_as_uint(f.y);
+    v.w[2 * i] = __float_as_uint(f.x);
+    v.w[2 * i + 1] = __float_as_uint(f.y);
   }
 };
 
@@ -186,30 +190,30 @@ struct Piece {
     for (int b = 0; b < g.batches; ++b) fetch(buf + 4 * b * NT + threadIdx.x, b);
   }
   __device__ __forceinline__ float edge_value() const { return edge >= 0 ? to_f(x[edge]) : -INFINITY; }
-  __device__ __forceinline__ void load(uint4 (&a)[4], const uint4* from, int b) const {
+  __device__ __forceinline__ void load(Quad (&a)[4], const uint4* from, int b) const {
     if (whole(b)) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) a[u] = from[u * NT];
+      for (int u = 0; u < 4; ++u) a[u] = quad(from[u * NT]);
     } else {
       const int v = 4 * b * NT + threadIdx.x;
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        a[u] = make_uint4(Vec<T>::NEG_INF, Vec<T>::NEG_INF, Vec<T>::NEG_INF, Vec<T>::NEG_INF);
-        if (v + u * NT < count) a[u] = from[u * NT];
+        a[u] = nothing<T>();
+        if (v + u * NT < count) a[u] = quad(from[u * NT]);
       }
     }
   }
-  __device__ __forceinline__ void store(T* dst, int v, const uint4& r) const {
+  __device__ __forceinline__ void store(T* dst, int v, const Quad& r) const {
     T* d = dst + element(v);
     if (((uintptr_t)d & 15) == 0) {
-      *(uint4*)d = r;
+      *(uint4*)d = four(r);
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) d[i] = from_f<T>(Vec<T>::get(r, i));
     }
   }
   __device__ __forceinline__ void zeros(T* dst) const {
-    for (int v = threadIdx.x; v < count; v += NT) store(dst, v, make_uint4(0, 0, 0, 0));
+    for (int v = threadIdx.x; v < count; v += NT) store(dst, v, Quad{{0, 0, 0, 0}});
     if (edge >= 0) dst[edge] = from_f<T>(0.f);
   }
 };
@@ -255,7 +259,7 @@ struct Running {
     top = to + g.slack;
   }
   // Adds a batch and returns its maximum.
-  __device__ __forceinline__ float add(uint4 (&a)[4], const Geometry& g) {
+  __device__ __forceinline__ float add(Quad (&a)[4], const Geometry& g) {
     constexpr int P = Vec<T>::N / 2;
     const u64 c2 = pack(g.c, g.c);
     const float bm = Vec<T>::max4(a);
@@ -295,7 +299,7 @@ struct Running {
 
 // The same against the row's maximum, for far rows, one element after the other, without the `k` tokens of `skip`.
 template <typename T, int NT, bool W>
-__device__ __noinline__ Sums sweep_far(const Piece<T, NT>& p, const Geometry& g, float m, float edge, const int* skip = nullptr, int k = 0) {
+__device__ __noinline__ Sums sweep_far(const Piece<T, NT> p, const Geometry g, float m, float edge, const int* skip = nullptr, int k = 0) {
   Sums a{m, 0.f, 0.f};
   auto add = [&](float x) {
     if (x == -INFINITY) return;
@@ -318,48 +322,55 @@ __device__ __noinline__ Sums sweep_far(const Piece<T, NT>& p, const Geometry& g,
 template <int NT>
 struct Exchange { float4 part[2][2][MAX_CLUSTER * NT / 32]; };
 
+// All warps of the block, wherever in the code each of them is.
+__device__ __forceinline__ void sync_block() {
+  __syncwarp();
+  asm volatile("bar.sync 0;" ::: "memory");
+}
+
 template <bool CL>
 __device__ __forceinline__ void sync_row() {
   if (CL) {
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   } else {
-    __syncthreads();
+    sync_block();
   }
 }
 
-// The row's sums, the same bits in every thread of its blocks.  The parts of a warp have one reference, its maximum's, or in
-// a far row the row's.
-template <int NT, bool W, bool CL, bool FARROW>
-__device__ __forceinline__ Sums join(Sums a, float4* part, const Geometry& g, int rank) {
-  constexpr int WARPS = NT / 32;
+// Joins the warps' sums: every warp leaves its part with all blocks of the row, and behind sync_row takes the whole, the same
+// bits in every thread.  The parts of a warp have one reference, its maximum's, or in a far row the row's.
+template <int NT, bool W, bool CL>
+__device__ __forceinline__ void leave_part(Sums a, float4* part, const Geometry& g, int rank) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   a.s = warp_sum(a.s);
   if (W) a.w = warp_sum(a.w);
   const float4 mine = make_float4(a.m, a.s, a.w, 0.f);
   if (CL) {
-    if (lane < g.cluster) cg::this_cluster().map_shared_rank(part, lane)[rank * WARPS + warp] = mine;
+    if (lane < g.cluster) cg::this_cluster().map_shared_rank(part, lane)[rank * (NT / 32) + warp] = mine;
   } else if (lane == 0) {
     part[warp] = mine;
   }
-  sync_row<CL>();
+}
+template <int NT, bool W, bool CL, bool FARROW>
+__device__ __forceinline__ Sums take_parts(const float4* part, const Geometry& g) {
+  const int lane = threadIdx.x & 31, parts = CL ? g.cluster * (NT / 32) : NT / 32;
   Sums t{-INFINITY, 0.f, 0.f};
-  if (!CL) {
-    float4 q[WARPS];
+  if constexpr (!CL && NT <= 128) {                      // few parts: each thread by itself
+    float4 q[NT / 32];
 #pragma unroll
-    for (int i = 0; i < WARPS; ++i) {
+    for (int i = 0; i < NT / 32; ++i) {
       q[i] = part[i];
       t.m = fmaxf(t.m, q[i].x);
     }
 #pragma unroll
-    for (int i = 0; i < WARPS; ++i) {
+    for (int i = 0; i < NT / 32; ++i) {
       if (!FARROW) move<W>(q[i].y, q[i].z, rho_of(q[i].x, g), t.m, g);
       t.s += q[i].y;
       t.w += q[i].z;
     }
     return t;
-  }
-  const int parts = g.cluster * WARPS;
+  } else {
   for (int i = lane; i < parts; i += 32) t.m = fmaxf(t.m, part[i].x);
   t.m = warp_most(t.m);
   for (int i = lane; i < parts; i += 32) {
@@ -368,9 +379,25 @@ __device__ __forceinline__ Sums join(Sums a, float4* part, const Geometry& g, in
     t.s += b.y;
     t.w += b.z;
   }
-  t.s = warp_sum(t.s);
-  if (W) t.w = warp_sum(t.w);
+  if (CL || NT > 256) {
+    t.s = warp_sum(t.s);
+    if (W) t.w = warp_sum(t.w);
+  } else {                                               // eight lanes hold them
+    for (int o = 4; o > 0; o >>= 1) {
+      t.s += __shfl_xor_sync(0xffffffffu, t.s, o);
+      if (W) t.w += __shfl_xor_sync(0xffffffffu, t.w, o);
+    }
+    t.s = __shfl_sync(0xffffffffu, t.s, 0);
+    if (W) t.w = __shfl_sync(0xffffffffu, t.w, 0);
+  }
   return t;
+  }
+}
+template <int NT, bool W, bool CL, bool FARROW>
+__device__ __forceinline__ Sums join(Sums a, float4* part, const Geometry& g, int rank) {
+  leave_part<NT, W, CL>(a, part, g, rank);
+  sync_row<CL>();
+  return take_parts<NT, W, CL, FARROW>(part, g);
 }
 
 // A row's reference.
@@ -486,7 +513,7 @@ __device__ int top_candidates(const Piece<T, NT>& p, float edge, int k, float th
     const int at = atomicAdd(&ts.count, 1);
     if (at < CANDIDATES) ts.list[at] = key_of(o, j);
   };
-  auto vector = [&](int v) { return *(const uint4*)(p.x + p.element(v)); };
+  auto vector = [&](int v) { return quad(*(const uint4*)(p.x + p.element(v))); };
   for (int e = 0; e < entries; ++e)
     if (lo <= NOTHING || ts.maxima[e][tid] >= bound) ts.hits[atomicAdd(&ts.found, 1)] = (unsigned short)(e * NT + tid);
   if (p.edge >= 0 && order_of(edge) >= lo) add(order_of(edge), p.edge);
@@ -495,7 +522,7 @@ __device__ int top_candidates(const Piece<T, NT>& p, float edge, int k, float th
   for (int i = tid; i < units; i += NT) {
     const int h = ts.hits[i / per], at = i % per, v = ((h / NT * stride + at / 4) * 4 + at % 4) * NT + h % NT;
     if (v >= p.count) continue;
-    const uint4 a = vector(v);
+    const Quad a = vector(v);
     if (lo > NOTHING && !(Vec<T>::max1(a) >= bound)) continue;
     for (int i = 0; i < N; ++i) {
       const uint32_t o = order_of(Vec<T>::get(a, i));
@@ -511,7 +538,7 @@ __device__ int top_candidates(const Piece<T, NT>& p, float edge, int k, float th
     int n = 0;
     if (most >= b) {
       for (int v = tid; v < p.count; v += NT) {
-        const uint4 a = vector(v);
+        const Quad a = vector(v);
         for (int i = 0; i < N; ++i) n += order_of(Vec<T>::get(a, i)) >= b;
       }
       n += p.edge >= 0 && order_of(edge) >= b;
@@ -536,7 +563,7 @@ __device__ int top_candidates(const Piece<T, NT>& p, float edge, int k, float th
   __syncthreads();
   if (most > lo) {
     for (int v = tid; v < p.count; v += NT) {
-      const uint4 a = vector(v);
+      const Quad a = vector(v);
       for (int i = 0; i < N; ++i) {
         const uint32_t o = order_of(Vec<T>::get(a, i));
         if (o > lo) add(o, p.element(v) + i);
@@ -554,7 +581,7 @@ __device__ int top_candidates(const Piece<T, NT>& p, float edge, int k, float th
     if (step < 0 || step == steps) {
       if (p.edge >= 0 && (p.edge < p.head) == (step < 0) && order_of(edge) == lo) same = 1;
     } else if (v < p.count) {
-      const uint4 a = vector(v);
+      const Quad a = vector(v);
       j = p.element(v);
       for (int i = 0; i < N; ++i)
         if (order_of(Vec<T>::get(a, i)) == lo) same |= 1u << i;
@@ -637,7 +664,7 @@ __global__ void __launch_bounds__(STREAM) logprobs_kernel(const __grid_constant_
     int entry = 0, in_entry = 0;
     for (int b = 0; b < g.batches; ++b) {
       wait_groups(SLOTS - 1);
-      uint4 v[4];
+      Quad v[4];
       p.load(v, dynamic + slot * 4 * NT + tid, b);
       if (TOP) {
         h0 = fmaxf(h0, fmaxf(Vec<T>::max1(v[0]), Vec<T>::max1(v[1])));
@@ -732,11 +759,12 @@ __device__ __forceinline__ void gradient(const Piece<T, NT>& p, uint4* buf, floa
   if (p.edge >= 0) dst[p.edge] = from_f<T>(one(edge, p.edge));
   if (ref.far) {
     for (int v = threadIdx.x; v < p.count; v += NT) {
-      uint4 o;
+      const Quad x = quad(buf[v]);
+      Quad o;
       const int j = p.element(v);
 #pragma unroll
       for (int i = 0; i < N / 2; ++i)
-        Vec<T>::set_pair(o, i, pack(one(Vec<T>::get(buf[v], 2 * i), j + 2 * i), one(Vec<T>::get(buf[v], 2 * i + 1), j + 2 * i + 1)));
+        Vec<T>::set_pair(o, i, pack(one(Vec<T>::get(x, 2 * i), j + 2 * i), one(Vec<T>::get(x, 2 * i + 1), j + 2 * i + 1)));
       p.store(dst, v, o);
     }
     if (fetch_next) next.fetch_all(buf, g);
@@ -744,20 +772,18 @@ __device__ __forceinline__ void gradient(const Piece<T, NT>& p, uint4* buf, floa
   }
   const u64 c2 = pack(g.c, g.c), nrho = pack(-ref.rho, -ref.rho), k02 = pack(k0, k0), k12 = pack(k1, k1);
   const bool aligned = ((uintptr_t)(dst + p.head) & 15) == 0;
-  auto one_vector = [&](uint4 a, int v) {
-    uint4 o;
+  // the token's element, written again by the thread that writes its vector
+  const int spot = t - p.head - p.first * N;
+  const bool mine = t >= 0 && spot >= 0 && spot < p.count * N && spot / N % NT == threadIdx.x;
+  const float at = mine ? one(to_f(((const T*)buf)[spot]), t) : 0.f;
+  auto one_vector = [&](Quad a) {
+    Quad o;
     if (W) Vec<T>::clamp(a, g.lo);
     u64 d[N / 2];
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) {
       const u64 y = fma2(Vec<T>::pair(a, i), c2, nrho), e = ex22(y);
       d[i] = mul2(e, W ? fma2(k12, y, k02) : k02);
-    }
-    const unsigned off = (unsigned)(t - p.element(v));
-    if (t >= 0 && off < N) {
-#pragma unroll
-      for (int i = 0; i < N / 2; ++i)
-        if (off >> 1 == i) d[i] = add2(d[i], off & 1 ? pack(0.f, at_t) : pack(at_t, 0.f));
     }
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) Vec<T>::set_pair(o, i, d[i]);
@@ -768,12 +794,13 @@ __device__ __forceinline__ void gradient(const Piece<T, NT>& p, uint4* buf, floa
     if (p.whole(b) && aligned) {
       uint4* d = (uint4*)(dst + p.element(v0));
 #pragma unroll
-      for (int u = 0; u < 4; ++u) d[u * NT] = one_vector(buf[v0 + u * NT], v0 + u * NT);
+      for (int u = 0; u < 4; ++u) d[u * NT] = four(one_vector(quad(buf[v0 + u * NT])));
     } else {
-      for (int v = v0; v < min(v0 + 4 * NT, p.count); v += NT) p.store(dst, v, one_vector(buf[v], v));
+      for (int v = v0; v < min(v0 + 4 * NT, p.count); v += NT) p.store(dst, v, one_vector(quad(buf[v])));
     }
     if (fetch_next) next.fetch(buf + v0, b);
   }
+  if (mine) dst[t] = from_f<T>(at);
 }
 
 // The sums of a row whose batches all have their place: they stay, or as they are read make room for those of the next row.
@@ -782,7 +809,7 @@ __device__ __forceinline__ Sums sweep(const Piece<T, NT>& p, uint4* buf, float e
   Running<T, W> run(g);
   for (int b = 0; b < g.batches; ++b) {
     wait_groups(REFILL ? g.batches - 1 : g.batches - 1 - b);
-    uint4 v[4];
+    Quad v[4];
     p.load(v, buf + 4 * b * NT + threadIdx.x, b);
     run.add(v, g);
     if (REFILL) {
@@ -853,157 +880,249 @@ __global__ void __launch_bounds__(STAY, 3) logprobs_bwd_kernel(const __grid_cons
   wait_groups(0);
 }
 
-__device__ __forceinline__ void sync_teacher() { asm volatile("bar.sync 1, 128;" ::: "memory"); }   // the first four warps
+// Distillation: warps that sweep over the logits, as above, and one for the teacher's row.  Four entries per lane; while the
+// others sum a row it prepares the next one, and behind their sums it forms the loss and writes the listed tokens' gradient.
+constexpr int PER_LANE = TOP_MAX / 32;
+
+struct Lesson {                               // what the sums of a row are weighed with
+  alignas(16) int id[TOP_MAX];                // tokens listed, -1: none; read four at a time
+  float most, student;                        // largest logit of the listed tokens; their sum against it
+  float Q, qr;                                // teacher's weight in all, and of what is not listed
+  int any;                                    // there is weight
+};
+static_assert(offsetof(Lesson, id) % 16 == 0 && sizeof(Lesson) % 16 == 0, "four ids at a time");
+
+// A row's sums weighed: S against the row's maximum, f the factor of the sums o to it, kappa of the gradient.
+struct Weighed {
+  Ref ro, ref;
+  float f, S;
+  __device__ __forceinline__ Weighed(const Sums& o, const Lesson& l, bool rest, const Geometry& g)
+      : ro(o.m, g), ref(rest ? fmaxf(o.m, l.most) : o.m, g), f(1.f), S(o.s) {
+    if (!rest) return;                                   // the sums are those of all tokens
+    f = factor(ro);
+    S = o.s * f + l.student * factor(Ref(l.most, g));
+  }
+  __device__ __forceinline__ float factor(const Ref& b) const {
+    return b.m == -INFINITY ? 0.f : ex2(ref.far ? (b.m - ref.m) * b.c : b.rho - ref.rho);
+  }
+};
 
 template <typename T, bool CL>
-__global__ void __launch_bounds__(STAY, 3) distill_kernel(const __grid_constant__ DistillArgs a, const __grid_constant__ Geometry g) {
-  struct Shared {                             // of two rows in turn
-    float most_student, student[4], has[4];
-    double mass[4];
-  };
-  constexpr int NT = STAY;
+__global__ void __launch_bounds__(STAY + 32, 3) distill_kernel(const __grid_constant__ DistillArgs a, const __grid_constant__ Geometry g) {
+  constexpr int NT = STAY, N = Vec<T>::N;
   __shared__ Exchange<NT> ex;
-  __shared__ Shared shared[2];
-  __shared__ __align__(16) int id[TOP_MAX];
-  __shared__ float weight[TOP_MAX], red[4][2];
+  __shared__ Lesson lessons[2];               // of two rows in turn
+  __shared__ float edges[2 * N];
   cudaGridDependencySynchronize();
   cluster_start<CL>();
   const Place me = Place::of<CL>(g);
-  const int rank = me.rank, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, k = a.k, rows = a.in.rows;
+  const int rank = me.rank, lane = threadIdx.x & 31, rows = a.in.rows;
   uint4* buf = dynamic;
-  struct Entry { int i; float t, x; };        // the thread's entry of the teacher's row: token, value; the student's logit
-  auto entry = [&](long long r) {
-    Entry e{-1, -INFINITY, -INFINITY};
-    if (tid < k) {
-      e.i = token_of(a.ids, r * k + tid, a.in.vocab, a.in.out_of_range, rank == 0);
-      e.t = a.teacher[r * k + tid];
-    }
-    return e;
-  };
   Piece<T, NT> p(a.in, me.row, rank, g);
-  p.fetch_all(buf, g);
-  float edge = p.edge_value();
-  Entry en = entry(me.row);
-  if (en.i >= 0) en.x = to_f(p.x[en.i]);
-  else en.t = -INFINITY;
-  cluster_started<CL>();
   int turn = 0;
-  for (long long r = me.row; r < rows; r += me.groups, turn ^= 1) {
-    const bool has_next = r + me.groups < rows;
-    const long long rn = has_next ? r + me.groups : r;
-    const Piece<T, NT> next(a.in, rn, rank, g);
-    const float next_edge = next.edge_value();
-    Entry next_en = entry(rn);
-    const float dl = a.dloss ? a.dloss[r] : 1.f;
-    Shared& sh = shared[turn];
 
-    // The teacher's row and what the student gives its tokens, an entry per thread of four warps.
-    float q = 0.f, lq = 0.f;
-    const float xi = en.x;
-    const int i = en.i;
-    int twins = 0;                                       // entries of the same token; the first one stands for it
-    bool first = i >= 0;
-    if (warp < 4) {
-      const float t = en.t;
-      sync_teacher();                                    // the row before has been read
-      id[tid] = i;
-      const float wt = warp_max(t), wx = warp_max(xi);
-      const bool some = __any_sync(0xffffffffu, !(t == -INFINITY));
-      if (lane == 0) { red[warp][0] = wt; red[warp][1] = wx; sh.has[warp] = some ? 1.f : 0.f; }
-      sync_teacher();
-      const float mt = fmaxf(fmaxf(red[0][0], red[1][0]), fmaxf(red[2][0], red[3][0]));
-      const float ml = fmaxf(fmaxf(red[0][1], red[1][1]), fmaxf(red[2][1], red[3][1]));
-      const double e = t == -INFINITY ? 0.0 : a.rest ? exp((double)t) : (double)expf((t - mt) * g.inv_t);
-      for (int j = 0; j < k; j += 4) {
-        const int4 o = *(const int4*)&id[j];
-        const int same = (o.x == i) + (o.y == i) + (o.z == i) + (o.w == i);
-        twins += same;
-        if (same && (o.x == i ? j : o.y == i ? j + 1 : o.z == i ? j + 2 : j + 3) < tid) first = false;
+  if (threadIdx.x < NT) {
+    p.fetch_all(buf, g);
+    float edge = p.edge_value();
+    cluster_started<CL>();
+    for (long long r = me.row; r < rows; r += me.groups, turn ^= 1) {
+      const bool has_next = r + me.groups < rows;
+      const Piece<T, NT> next(a.in, has_next ? r + me.groups : r, rank, g);
+      const float next_edge = next.edge_value(), dl = a.dloss ? a.dloss[r] : 1.f;
+      if (a.rest) {                                      // the listed tokens leave the row
+        wait_groups(0);
+        if (p.edge >= 0) edges[threadIdx.x] = edge;
+        sync_block();
+        sync_block();
+        if (p.edge >= 0) edge = edges[threadIdx.x];
       }
-      const float el = first && xi != -INFINITY ? ex2(Ref(ml, g).y(xi)) : 0.f;
-      double mass = e;
-      for (int o = 16; o > 0; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
-      const float sl = warp_sum(el);
-      if (lane == 0) { sh.mass[warp] = mass; sh.student[warp] = sl; }
-      if (tid == 0) sh.most_student = ml;
-      sync_teacher();
-      mass = sh.mass[0] + sh.mass[1] + sh.mass[2] + sh.mass[3];
-      q = a.rest ? (float)e : (float)(e / mass);
-      lq = a.rest ? t : (t - mt) * g.inv_t - logf((float)mass);
-      weight[tid] = q;
+      leave_part<NT, false, CL>(a.dx ? sweep<T, NT, false, false>(p, buf, edge, g, next, false) : sweep<T, NT, false, true>(p, buf, edge, g, next, has_next),
+                                ex.part[turn][0], g, rank);
+      sync_row<CL>();
+      Sums o = take_parts<NT, false, CL, false>(ex.part[turn][0], g);
+      const Lesson& l = lessons[turn];
+      if (Ref(o.m, g).far) o = join<NT, false, CL, true>(sweep_far<T, NT, false>(p, g, o.m, edge, l.id, a.rest ? a.k : 0), ex.part[turn][1], g, rank);
+      if (a.dx) {
+        T* dx = (T*)a.dx + r * a.ld_out;
+        if (!l.any || dl == 0.f) {
+          p.zeros(dx);
+          if (has_next) next.fetch_all(buf, g);
+        } else {
+          const Weighed s(o, l, a.rest, g);
+          const float kappa = s.S != s.S ? s.S : o.s == 0.f ? 0.f : (l.Q * s.f / s.S - (l.qr > 0.f ? l.qr / o.s : 0.f)) * (dl * a.scale * g.inv_t);
+          gradient<T, NT, false>(p, buf, edge, g, s.ro, kappa, 0.f, -1, 0.f, dx, next, has_next);
+        }
+        sync_block();                                 // the listed tokens' gradient goes over it
+      }
+      p = next;
+      edge = next_edge;
     }
-    const int spot = i - p.head - p.first * Vec<T>::N;   // the token's place in the piece, if it is there
-    if (a.rest) {                                        // what stays are the tokens not listed
-      wait_groups(0);
-      __syncthreads();
-      if (i >= 0 && spot >= 0 && spot < p.count * Vec<T>::N) ((T*)buf)[spot] = from_f<T>(-INFINITY);
-      if (p.edge >= 0)
-        for (int j = 0; j < k; ++j)
-          if (id[j] == p.edge) edge = -INFINITY;
-      __syncthreads();
-    }
-    // Without a rest the sums are those of all tokens.
-    Sums o;
-    if (a.dx) o = join<NT, false, CL, false>(sweep<T, NT, false, false>(p, buf, edge, g, next, false), ex.part[turn][0], g, rank);
-    else o = join<NT, false, CL, false>(sweep<T, NT, false, true>(p, buf, edge, g, next, has_next), ex.part[turn][0], g, rank);
-    const Ref ro(o.m, g);
-    if (ro.far) o = join<NT, false, CL, true>(sweep_far<T, NT, false>(p, g, o.m, edge, id, a.rest ? k : 0), ex.part[turn][1], g, rank);
-    if (next_en.i >= 0) next_en.x = to_f(next.x[next_en.i]);
-    else next_en.t = -INFINITY;
+    wait_groups(0);
+    return;
+  }
 
-    const bool any = sh.has[0] + sh.has[1] + sh.has[2] + sh.has[3] != 0.f;
-    const double mass = sh.mass[0] + sh.mass[1] + sh.mass[2] + sh.mass[3];
-    const float qr = a.rest && 1.0 - mass > SMALLEST_REST ? (float)(1.0 - mass) : 0.f, R = o.s;
-    const float Q = a.rest ? (float)(qr > 0.f ? 1.0 : mass) : (float)(mass / mass);
-    const float m = a.rest ? fmaxf(o.m, sh.most_student) : o.m;
-    const Ref ref(m, g);
-    float f = 1.f, S = R;                                // of the sums o, against the row's maximum
+  struct Entries { int id[PER_LANE]; float t[PER_LANE], x[PER_LANE]; };       // token, teacher's value, student's logit
+  struct Weights { float q[PER_LANE], lq[PER_LANE]; bool first[PER_LANE], twins; };
+  auto read = [&](long long r, Entries& e) {
+#pragma unroll
+    for (int i = 0; i < PER_LANE; ++i) {
+      const int j = lane + 32 * i;
+      e.id[i] = -1;
+      e.t[i] = -INFINITY;
+      if (j < a.k && r < rows) {
+        e.id[i] = a.ids[r * a.k + j];
+        e.t[i] = a.teacher[r * a.k + j];
+      }
+    }
+  };
+  auto look = [&](const T* x, Entries& e) {              // up the student's logits
+#pragma unroll
+    for (int i = 0; i < PER_LANE; ++i) {
+      if (e.id[i] >= a.in.vocab && a.in.out_of_range) atomicOr(a.in.out_of_range, 1);
+      if (e.id[i] < 0 || e.id[i] >= a.in.vocab) { e.id[i] = -1; e.t[i] = -INFINITY; }
+      e.x[i] = e.id[i] >= 0 ? to_f(x[e.id[i]]) : -INFINITY;
+    }
+  };
+  auto prepare = [&](const Entries& e, Weights& w, Lesson& l) {
+    float mt = -INFINITY, most = -INFINITY;
+    bool some = false;
+#pragma unroll
+    for (int i = 0; i < PER_LANE; ++i) {
+      l.id[lane + 32 * i] = e.id[i];
+      mt = fmaxf(mt, e.t[i]);
+      most = fmaxf(most, e.x[i]);
+      some = some || !(e.t[i] == -INFINITY);
+    }
+    __syncwarp();
+    mt = warp_most(mt);
+    double mass = 0.0, v[PER_LANE];
+    int count[PER_LANE];
+#pragma unroll
+    for (int i = 0; i < PER_LANE; ++i) {
+      count[i] = 0;
+      v[i] = e.t[i] == -INFINITY ? 0.0 : a.rest ? exp((double)e.t[i]) : (double)expf((e.t[i] - mt) * g.inv_t);
+      mass += v[i];
+    }
+    for (int o = 16; o > 0; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
+    const float scale = a.rest ? 1.f : (float)(1.0 / mass), shift = a.rest ? 0.f : fmaf(mt, g.inv_t, logf((float)mass));
+    for (int j = 0; j < a.k; j += 4) {
+      const int4 o = *(const int4*)&l.id[j];
+#pragma unroll
+      for (int i = 0; i < PER_LANE; ++i) count[i] += (o.x == e.id[i]) + (o.y == e.id[i]) + (o.z == e.id[i]) + (o.w == e.id[i]);
+    }
+    bool twins = false;
+#pragma unroll
+    for (int i = 0; i < PER_LANE; ++i) {
+      w.q[i] = (float)v[i] * scale;
+      w.lq[i] = a.rest ? e.t[i] : fmaf(e.t[i], g.inv_t, -shift);
+      w.first[i] = e.id[i] >= 0;
+      twins = twins || (e.id[i] >= 0 && count[i] > 1);
+    }
+    w.twins = __any_sync(0xffffffffu, twins);            // entries of one token: the first stands for it
+    if (w.twins)
+      for (int j = 0; j < a.k; ++j)
+#pragma unroll
+        for (int i = 0; i < PER_LANE; ++i) w.first[i] = w.first[i] && !(j < lane + 32 * i && l.id[j] == e.id[i]);
+    float student = 0.f;
     if (a.rest) {
-      auto factor = [&](const Ref& b) { return b.m == -INFINITY ? 0.f : ex2(ref.far ? (b.m - m) * g.c : b.rho - ref.rho); };
-      f = factor(ro);
-      S = R * f + (sh.student[0] + sh.student[1] + sh.student[2] + sh.student[3]) * factor(Ref(sh.most_student, g));
+      most = warp_most(most);
+      const Ref rl(most, g);
+#pragma unroll
+      for (int i = 0; i < PER_LANE; ++i) student += w.first[i] && e.x[i] != -INFINITY ? ex2(rl.y(e.x[i])) : 0.f;
+      student = warp_sum(student);
     }
-    if (a.loss && rank == 0 && warp < 4) {
-      const float logs = logf(S);
-      float l = i >= 0 && !(q == 0.f) ? q * (lq - (S == 0.f ? -INFINITY : ref.nat(xi) - logs)) : 0.f;
-      l = warp_sum(l);
-      sync_teacher();                                    // red has been read
-      if (lane == 0) red[warp][0] = l;
-      sync_teacher();
-      if (tid == 0) {
-        l = red[0][0] + red[1][0] + red[2][0] + red[3][0];
-        if (qr > 0.f)
-          l += qr * (logf(qr) - (R == 0.f ? -INFINITY : (ref.far || ro.far ? (o.m - m) * g.inv_t : (ro.rho - ref.rho) * LN2) + logf(R) - logs));
-        a.loss[r] = any ? a.scale * l : 0.f;
+    some = __any_sync(0xffffffffu, some);
+    if (lane == 0) {
+      l.most = most;
+      l.student = student;
+      l.qr = a.rest && 1.0 - mass > SMALLEST_REST ? (float)(1.0 - mass) : 0.f;
+      l.Q = a.rest ? (float)(l.qr > 0.f ? 1.0 : mass) : (float)(mass / mass);
+      l.any = some;
+    }
+    __syncwarp();
+  };
+
+  Entries now, later;
+  Weights w, next_w;
+  read(me.row, now);
+  look(p.x, now);
+  read(me.row + me.groups, later);
+  prepare(now, w, lessons[0]);
+  cluster_started<CL>();
+  for (long long r = me.row; r < rows; r += me.groups, turn ^= 1) {
+    const Lesson& l = lessons[turn];
+    auto place = [&](int id) { return id - p.head - p.first * N; };           // in the piece
+    const bool has_next = r + me.groups < rows;
+    const Piece<T, NT> next(a.in, has_next ? r + me.groups : r, rank, g);
+    const int beyond = a.in.vocab - (a.in.vocab - p.head) % N;                // elements from here on are in no vector
+    if (a.rest) {
+      sync_block();
+#pragma unroll
+      for (int i = 0; i < PER_LANE; ++i) {
+        const int id = now.id[i], at = place(id);
+        if (id < 0) continue;
+        if (at >= 0 && at < p.count * N) ((T*)buf)[at] = from_f<T>(-INFINITY);
+        else if (rank == 0 && id < p.head) edges[id] = -INFINITY;
+        else if (rank == 0 && id >= beyond) edges[p.head + id - beyond] = -INFINITY;
       }
+      sync_block();
+    }
+    Entries coming;
+    if (has_next) {
+      look(next.x, later);
+      read(r + 2 * me.groups, coming);
+      prepare(later, next_w, lessons[turn ^ 1]);
+    }
+    const float dl = a.dloss ? a.dloss[r] : 1.f;
+    sync_row<CL>();
+    Sums o = take_parts<NT, false, CL, false>(ex.part[turn][0], g);
+    if (Ref(o.m, g).far) {
+      sync_row<CL>();
+      o = take_parts<NT, false, CL, true>(ex.part[turn][1], g);
+    }
+    const Weighed s(o, l, a.rest, g);
+    if (a.loss && rank == 0) {
+      const float logs = logf(s.S);
+      float loss = 0.f;
+#pragma unroll
+      for (int i = 0; i < PER_LANE; ++i)
+        if (now.id[i] >= 0 && !(w.q[i] == 0.f)) loss += w.q[i] * (w.lq[i] - (s.S == 0.f ? -INFINITY : s.ref.nat(now.x[i]) - logs));
+      loss = warp_sum(loss);
+      if (l.qr > 0.f) {
+        const float lr = s.ref.far || s.ro.far ? (o.m - s.ref.m) * g.inv_t : (s.ro.rho - s.ref.rho) * LN2;
+        loss += l.qr * (logf(l.qr) - (o.s == 0.f ? -INFINITY : lr + logf(o.s) - logs));
+      }
+      if (lane == 0) a.loss[r] = l.any ? a.scale * loss : 0.f;
     }
     if (a.dx) {
-      T* dx = (T*)a.dx + r * a.ld_out;
-      if (!any || dl == 0.f) {
-        p.zeros(dx);
-        if (has_next) next.fetch_all(buf, g);
-      } else {
-        const float w = dl * a.scale * g.inv_t;
-        const float kappa = S != S ? S : R == 0.f ? 0.f : (Q * f / S - (qr > 0.f ? qr / R : 0.f)) * w;
-        gradient<T, NT, false>(p, buf, edge, g, ro, kappa, 0.f, -1, 0.f, dx, next, has_next);
-        __syncthreads();
-        const bool here = spot >= 0 && spot < p.count * Vec<T>::N, outside = i < p.head || i >= a.in.vocab - (a.in.vocab - p.head) % Vec<T>::N;
-        if (first && (here || (rank == 0 && outside))) {
-          float qi = q;
-          if (twins > 1) {
-            qi = 0.f;
-            for (int j = 0; j < k; ++j) qi += id[j] == i ? weight[j] : 0.f;
+      sync_block();
+      if (l.any && dl != 0.f) {
+        T* dx = (T*)a.dx + r * a.ld_out;
+        const float f = dl * a.scale * g.inv_t;
+#pragma unroll
+        for (int i = 0; i < PER_LANE; ++i) {
+          const int id = now.id[i], at = place(id);
+          float q = w.q[i];
+          if (w.twins) {                                 // the sum over the entries of the token
+            q = 0.f;
+            for (int b = 0; b < PER_LANE; ++b)
+              for (int j = 0; j < 32; ++j) {
+                const float other = __shfl_sync(0xffffffffu, w.q[b], j);
+                if (32 * b + j < a.k && l.id[32 * b + j] == id) q += other;
+              }
           }
-          const float pi = (xi == -INFINITY ? 0.f : ex2(ref.y(xi))) / S;
-          dx[i] = from_f<T>(S == 0.f ? 0.f : (Q * pi - qi) * w);
+          const bool here = (at >= 0 && at < p.count * N) || (rank == 0 && (id < p.head || id >= beyond));
+          if (!w.first[i] || !here) continue;
+          const float pi = (now.x[i] == -INFINITY ? 0.f : ex2(s.ref.y(now.x[i]))) / s.S;
+          dx[id] = from_f<T>(s.S == 0.f ? 0.f : (l.Q * pi - q) * f);
         }
       }
     }
     p = next;
-    edge = next_edge;
-    en = next_en;
+    now = later;
+    later = coming;
+    w = next_w;
   }
-  wait_groups(0);
 }
 
 // ---------------------------------------------------------------------------------------------- launches
@@ -1017,15 +1136,15 @@ struct Plan {
   size_t smem;
 };
 // Blocks of `threads`; stay: rows stay in shared memory as a whole, otherwise it takes `smem` bytes.
-Plan plan_rows(const LogitsIn& in, int elem_bytes, int threads, bool stay, size_t smem, size_t smem_cluster) {
+Plan plan_rows(const LogitsIn& in, int elem_bytes, int threads, bool stay, size_t smem, size_t smem_cluster, int more_threads = 0) {
   Plan p{};
   const int N = 16 / elem_bytes, all = std::max(1, in.vocab / N);
   int c = stay ? std::min(MAX_CLUSTER, (all + PIECE - 1) / PIECE) : 1;
   while (2 * c <= MAX_CLUSTER && (long long)in.rows * c < 2 * 148 && all / (2 * c) >= 256) c *= 2;
   const int per = (all + c - 1) / c;
-  p.threads = threads;
+  p.threads = threads + more_threads;
   p.smem = (stay ? (size_t)per * 16 : smem) + (c > 1 ? smem_cluster : 0);
-  const int blocks = std::min({32, 65536 / (80 * threads), (int)(228 * 1024 / (p.smem + STATIC + 1024))});
+  const int blocks = std::min({32, 65536 / (72 * p.threads), (int)(228 * 1024 / (p.smem + STATIC + 1024))});
   p.grid = dim3((unsigned)(std::min<long long>(in.rows, std::max(1, 148 * blocks / c)) * c));
   const double cc = 1.4426950408889634 / (double)in.temperature;
   p.g = Geometry{(float)cc, (float)(1.0 / (double)in.temperature), (float)(-1e30 * std::min(1.0, 1.0 / cc)), (float)(SLACK / cc), c, per,
@@ -1082,7 +1201,7 @@ cudaError_t launch_logprobs_bwd(const LogprobsBwdArgs& a, bool is_bf16, cudaStre
 }
 
 cudaError_t launch_distill(const DistillArgs& a, bool is_bf16, cudaStream_t s) {
-  const Plan p = plan_rows(a.in, is_bf16 ? 2 : 4, STAY, true, 0, 0);
+  const Plan p = plan_rows(a.in, is_bf16 ? 2 : 4, STAY, true, 0, 0, 32);
   if (is_bf16) return p.g.cluster > 1 ? run_distill<bf16, true>(a, p, s) : run_distill<bf16, false>(a, p, s);
   return p.g.cluster > 1 ? run_distill<float, true>(a, p, s) : run_distill<float, false>(a, p, s);
 }
