@@ -624,9 +624,8 @@ constexpr int STREAM = 128, SLOTS = 4;        // threads of a block that reads i
 
 // Batches pass through a ring of SLOTS, each thread's by itself: copies run ahead of the sums by SLOTS batches, over the end of
 // a row into the next ones, so that they go on while a row's sums are joined and handed out.
-template <typename T, bool W, bool CL, bool TOP>
-__global__ void __launch_bounds__(STREAM) logprobs_kernel(const __grid_constant__ LogprobsArgs a, const __grid_constant__ Geometry g) {
-  constexpr int NT = STREAM;
+template <typename T, int NT, bool W, bool CL, bool TOP>
+__global__ void __launch_bounds__(NT) logprobs_kernel(const __grid_constant__ LogprobsArgs a, const __grid_constant__ Geometry g) {
   __shared__ Exchange<NT> ex;
   cudaGridDependencySynchronize();
   cluster_start<CL>();
@@ -820,11 +819,11 @@ __device__ __forceinline__ Sums sweep(const Piece<T, NT>& p, uint4* buf, float e
   return run.end(edge, g);
 }
 
-constexpr int STAY = 256;                     // threads of a block whose rows stay for a second pass
+// Threads that sweep over a row; FEW where rows are short and many.
+constexpr int STAY = 256, FEW = 32;
 
-template <typename T, bool W, bool CL>
-__global__ void __launch_bounds__(STAY, 3) logprobs_bwd_kernel(const __grid_constant__ LogprobsBwdArgs a, const __grid_constant__ Geometry g) {
-  constexpr int NT = STAY;
+template <typename T, int NT, bool W, bool CL>
+__global__ void __launch_bounds__(NT, NT == 256 ? 3 : 1) logprobs_bwd_kernel(const __grid_constant__ LogprobsBwdArgs a, const __grid_constant__ Geometry g) {
   __shared__ Exchange<NT> ex;
   cudaGridDependencySynchronize();
   cluster_start<CL>();
@@ -882,7 +881,7 @@ __global__ void __launch_bounds__(STAY, 3) logprobs_bwd_kernel(const __grid_cons
 
 // Distillation: warps that sweep over the logits, as above, and one for the teacher's row.  Four entries per lane; while the
 // others sum a row it prepares the next one, and behind their sums it forms the loss and writes the listed tokens' gradient.
-constexpr int PER_LANE = TOP_MAX / 32;
+constexpr int PER_LANE = TOP_MAX / 32, CLAIMS = 512;
 
 struct Lesson {                               // what the sums of a row are weighed with
   alignas(16) int id[TOP_MAX];                // tokens listed, -1: none; read four at a time
@@ -907,12 +906,49 @@ struct Weighed {
   }
 };
 
-template <typename T, bool CL>
-__global__ void __launch_bounds__(STAY + 32, 3) distill_kernel(const __grid_constant__ DistillArgs a, const __grid_constant__ Geometry g) {
-  constexpr int NT = STAY, N = Vec<T>::N;
+// Where the two meet; whoever has nothing to wait for arrives and goes on.
+enum { LANDED = 1, PATCHED, LESSON, SUMMED, WRITTEN };
+template <int NT>
+__device__ __forceinline__ void arrive(int what) {
+  __syncwarp();
+  asm volatile("bar.arrive %0, %1;" ::"r"(what), "n"(NT + 32) : "memory");
+}
+template <int NT>
+__device__ __forceinline__ void await(int what) {
+  __syncwarp();
+  asm volatile("bar.sync %0, %1;" ::"r"(what), "n"(NT + 32) : "memory");
+}
+// The sums of a row: the sweeping warps leave them when the row's lesson is there; the teacher's warp hands it over and goes
+// on, and takes the sums up later.
+template <int NT, bool CL>
+__device__ __forceinline__ void hand_over() {
+  __syncwarp();
+  if (CL) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  else arrive<NT>(LESSON);
+}
+template <int NT, bool CL>
+__device__ __forceinline__ void take_up() {
+  __syncwarp();
+  if (CL) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  else await<NT>(SUMMED);
+}
+template <int NT, bool CL>
+__device__ __forceinline__ void summed() {
+  if (CL) {
+    sync_row<true>();
+  } else {
+    await<NT>(LESSON);
+    arrive<NT>(SUMMED);
+  }
+}
+
+template <typename T, int NT, bool CL>
+__global__ void __launch_bounds__(NT + 32, NT == 256 ? 3 : 1) distill_kernel(const __grid_constant__ DistillArgs a, const __grid_constant__ Geometry g) {
+  constexpr int N = Vec<T>::N;
   __shared__ Exchange<NT> ex;
   __shared__ Lesson lessons[2];               // of two rows in turn
   __shared__ float edges[2 * N];
+  __shared__ int claims[CLAIMS];              // the teacher's warp's
   cudaGridDependencySynchronize();
   cluster_start<CL>();
   const Place me = Place::of<CL>(g);
@@ -932,13 +968,13 @@ __global__ void __launch_bounds__(STAY + 32, 3) distill_kernel(const __grid_cons
       if (a.rest) {                                      // the listed tokens leave the row
         wait_groups(0);
         if (p.edge >= 0) edges[threadIdx.x] = edge;
-        sync_block();
-        sync_block();
+        arrive<NT>(LANDED);
+        await<NT>(PATCHED);
         if (p.edge >= 0) edge = edges[threadIdx.x];
       }
       leave_part<NT, false, CL>(a.dx ? sweep<T, NT, false, false>(p, buf, edge, g, next, false) : sweep<T, NT, false, true>(p, buf, edge, g, next, has_next),
                                 ex.part[turn][0], g, rank);
-      sync_row<CL>();
+      summed<NT, CL>();
       Sums o = take_parts<NT, false, CL, false>(ex.part[turn][0], g);
       const Lesson& l = lessons[turn];
       if (Ref(o.m, g).far) o = join<NT, false, CL, true>(sweep_far<T, NT, false>(p, g, o.m, edge, l.id, a.rest ? a.k : 0), ex.part[turn][1], g, rank);
@@ -952,7 +988,7 @@ __global__ void __launch_bounds__(STAY + 32, 3) distill_kernel(const __grid_cons
           const float kappa = s.S != s.S ? s.S : o.s == 0.f ? 0.f : (l.Q * s.f / s.S - (l.qr > 0.f ? l.qr / o.s : 0.f)) * (dl * a.scale * g.inv_t);
           gradient<T, NT, false>(p, buf, edge, g, s.ro, kappa, 0.f, -1, 0.f, dx, next, has_next);
         }
-        sync_block();                                 // the listed tokens' gradient goes over it
+        arrive<NT>(WRITTEN);                             // the listed tokens' gradient goes over it
       }
       p = next;
       edge = next_edge;
@@ -962,13 +998,15 @@ __global__ void __launch_bounds__(STAY + 32, 3) distill_kernel(const __grid_cons
   }
 
   struct Entries { int id[PER_LANE]; float t[PER_LANE], x[PER_LANE]; };       // token, teacher's value, student's logit
-  struct Weights { float q[PER_LANE], lq[PER_LANE]; bool first[PER_LANE], twins; };
+  struct Weights { float q[PER_LANE], lq[PER_LANE]; unsigned first; bool twins; };
+  const int used = (a.k + 31) / 32;                      // entries per lane
   auto read = [&](long long r, Entries& e) {
 #pragma unroll
     for (int i = 0; i < PER_LANE; ++i) {
       const int j = lane + 32 * i;
       e.id[i] = -1;
       e.t[i] = -INFINITY;
+      e.x[i] = -INFINITY;
       if (j < a.k && r < rows) {
         e.id[i] = a.ids[r * a.k + j];
         e.t[i] = a.teacher[r * a.k + j];
@@ -978,9 +1016,10 @@ __global__ void __launch_bounds__(STAY + 32, 3) distill_kernel(const __grid_cons
   auto look = [&](const T* x, Entries& e) {              // up the student's logits
 #pragma unroll
     for (int i = 0; i < PER_LANE; ++i) {
+      if (i >= used) break;
       if (e.id[i] >= a.in.vocab && a.in.out_of_range) atomicOr(a.in.out_of_range, 1);
       if (e.id[i] < 0 || e.id[i] >= a.in.vocab) { e.id[i] = -1; e.t[i] = -INFINITY; }
-      e.x[i] = e.id[i] >= 0 ? to_f(x[e.id[i]]) : -INFINITY;
+      if (e.id[i] >= 0) e.x[i] = to_f(x[e.id[i]]);
     }
   };
   auto prepare = [&](const Entries& e, Weights& w, Lesson& l) {
@@ -988,47 +1027,58 @@ __global__ void __launch_bounds__(STAY + 32, 3) distill_kernel(const __grid_cons
     bool some = false;
 #pragma unroll
     for (int i = 0; i < PER_LANE; ++i) {
+      if (i >= used) break;
       l.id[lane + 32 * i] = e.id[i];
       mt = fmaxf(mt, e.t[i]);
       most = fmaxf(most, e.x[i]);
       some = some || !(e.t[i] == -INFINITY);
     }
-    __syncwarp();
-    mt = warp_most(mt);
-    double mass = 0.0, v[PER_LANE];
-    int count[PER_LANE];
+    mt = a.rest ? 0.f : warp_most(mt);
+    const float by = a.rest ? 1.f : g.inv_t;
+    double mass = 0.0;                                   // of which the rest is what lacks of 1
+    w.twins = false;
+    w.first = 0;
+    int claim[PER_LANE];
 #pragma unroll
     for (int i = 0; i < PER_LANE; ++i) {
-      count[i] = 0;
-      v[i] = e.t[i] == -INFINITY ? 0.0 : a.rest ? exp((double)e.t[i]) : (double)expf((e.t[i] - mt) * g.inv_t);
-      mass += v[i];
+      claim[i] = -1;
+      w.q[i] = 0.f;
+      if (i >= used) continue;
+      w.q[i] = e.t[i] == -INFINITY ? 0.f : expf((e.t[i] - mt) * by);
+      mass += (double)w.q[i];
+      if (e.id[i] < 0) continue;
+      // Does a token stand in two entries?  Each claims a place by its id.
+      unsigned at = (unsigned)e.id[i] * 2654435761u >> 23;
+      int had;
+      while ((had = atomicCAS(&claims[at], 0, e.id[i] + 1)) != 0 && had != e.id[i] + 1) at = (at + 1) % CLAIMS;
+      if (had == 0) claim[i] = (int)at;
+      else w.twins = true;
+      w.first |= 1u << i;
     }
     for (int o = 16; o > 0; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
-    const float scale = a.rest ? 1.f : (float)(1.0 / mass), shift = a.rest ? 0.f : fmaf(mt, g.inv_t, logf((float)mass));
-    for (int j = 0; j < a.k; j += 4) {
-      const int4 o = *(const int4*)&l.id[j];
-#pragma unroll
-      for (int i = 0; i < PER_LANE; ++i) count[i] += (o.x == e.id[i]) + (o.y == e.id[i]) + (o.z == e.id[i]) + (o.w == e.id[i]);
-    }
-    bool twins = false;
+    const float scale = a.rest ? 1.f : 1.f / (float)mass, shift = a.rest ? 0.f : logf((float)mass);
 #pragma unroll
     for (int i = 0; i < PER_LANE; ++i) {
-      w.q[i] = (float)v[i] * scale;
-      w.lq[i] = a.rest ? e.t[i] : fmaf(e.t[i], g.inv_t, -shift);
-      w.first[i] = e.id[i] >= 0;
-      twins = twins || (e.id[i] >= 0 && count[i] > 1);
+      if (i >= used) break;
+      if (claim[i] >= 0) claims[claim[i]] = 0;
+      w.q[i] *= scale;
+      w.lq[i] = fmaf(e.t[i] - mt, by, -shift);
     }
-    w.twins = __any_sync(0xffffffffu, twins);            // entries of one token: the first stands for it
+    w.twins = __any_sync(0xffffffffu, w.twins);          // then the first entry stands for the token
     if (w.twins)
       for (int j = 0; j < a.k; ++j)
 #pragma unroll
-        for (int i = 0; i < PER_LANE; ++i) w.first[i] = w.first[i] && !(j < lane + 32 * i && l.id[j] == e.id[i]);
+        for (int i = 0; i < PER_LANE; ++i)
+          if (j < lane + 32 * i && l.id[j] == e.id[i]) w.first &= ~(1u << i);
     float student = 0.f;
     if (a.rest) {
       most = warp_most(most);
       const Ref rl(most, g);
 #pragma unroll
-      for (int i = 0; i < PER_LANE; ++i) student += w.first[i] && e.x[i] != -INFINITY ? ex2(rl.y(e.x[i])) : 0.f;
+      for (int i = 0; i < PER_LANE; ++i) {
+        if (i >= used) break;
+        student += (w.first >> i & 1) && e.x[i] != -INFINITY ? ex2(rl.y(e.x[i])) : 0.f;
+      }
       student = warp_sum(student);
     }
     some = __any_sync(0xffffffffu, some);
@@ -1036,57 +1086,68 @@ __global__ void __launch_bounds__(STAY + 32, 3) distill_kernel(const __grid_cons
       l.most = most;
       l.student = student;
       l.qr = a.rest && 1.0 - mass > SMALLEST_REST ? (float)(1.0 - mass) : 0.f;
-      l.Q = a.rest ? (float)(l.qr > 0.f ? 1.0 : mass) : (float)(mass / mass);
+      l.Q = a.rest ? (l.qr > 0.f ? 1.f : (float)mass) : mass == mass ? 1.f : (float)mass;
       l.any = some;
     }
     __syncwarp();
   };
+  auto beyond = [&](const Piece<T, NT>& p) { return a.in.vocab - (a.in.vocab - p.head) % N; };   // from here on in no vector
+  auto patch = [&](const Piece<T, NT>& p, const Entries& e) {
+    await<NT>(LANDED);
+    const int end = beyond(p);
+#pragma unroll
+    for (int i = 0; i < PER_LANE; ++i) {
+      const int id = e.id[i], at = id - p.head - p.first * N;
+      if (i >= used) break;
+      if (id < 0) continue;
+      if (at >= 0 && at < p.count * N) ((T*)buf)[at] = from_f<T>(-INFINITY);
+      else if (rank == 0 && id < p.head) edges[id] = -INFINITY;
+      else if (rank == 0 && id >= end) edges[p.head + id - end] = -INFINITY;
+    }
+    arrive<NT>(PATCHED);
+  };
 
   Entries now, later;
-  Weights w, next_w;
+  Weights w;
+  for (int i = lane; i < CLAIMS; i += 32) claims[i] = 0;
+#pragma unroll
+  for (int i = 0; i < PER_LANE; ++i) lessons[0].id[lane + 32 * i] = lessons[1].id[lane + 32 * i] = -1;
+  __syncwarp();
   read(me.row, now);
   look(p.x, now);
   read(me.row + me.groups, later);
   prepare(now, w, lessons[0]);
   cluster_started<CL>();
+  if (a.rest) patch(p, now);
   for (long long r = me.row; r < rows; r += me.groups, turn ^= 1) {
     const Lesson& l = lessons[turn];
-    auto place = [&](int id) { return id - p.head - p.first * N; };           // in the piece
     const bool has_next = r + me.groups < rows;
     const Piece<T, NT> next(a.in, has_next ? r + me.groups : r, rank, g);
-    const int beyond = a.in.vocab - (a.in.vocab - p.head) % N;                // elements from here on are in no vector
-    if (a.rest) {
-      sync_block();
-#pragma unroll
-      for (int i = 0; i < PER_LANE; ++i) {
-        const int id = now.id[i], at = place(id);
-        if (id < 0) continue;
-        if (at >= 0 && at < p.count * N) ((T*)buf)[at] = from_f<T>(-INFINITY);
-        else if (rank == 0 && id < p.head) edges[id] = -INFINITY;
-        else if (rank == 0 && id >= beyond) edges[p.head + id - beyond] = -INFINITY;
-      }
-      sync_block();
-    }
+    const float dl = a.dloss ? a.dloss[r] : 1.f;
     Entries coming;
-    if (has_next) {
+    Weights next_w;
+    hand_over<NT, CL>();
+    if (has_next) {                                      // while the others sum the row
       look(next.x, later);
       read(r + 2 * me.groups, coming);
       prepare(later, next_w, lessons[turn ^ 1]);
     }
-    const float dl = a.dloss ? a.dloss[r] : 1.f;
-    sync_row<CL>();
+    take_up<NT, CL>();
     Sums o = take_parts<NT, false, CL, false>(ex.part[turn][0], g);
     if (Ref(o.m, g).far) {
       sync_row<CL>();
       o = take_parts<NT, false, CL, true>(ex.part[turn][1], g);
     }
+    if (!a.dx && a.rest && has_next) patch(next, later);
     const Weighed s(o, l, a.rest, g);
     if (a.loss && rank == 0) {
       const float logs = logf(s.S);
       float loss = 0.f;
 #pragma unroll
-      for (int i = 0; i < PER_LANE; ++i)
+      for (int i = 0; i < PER_LANE; ++i) {
+        if (i >= used) break;
         if (now.id[i] >= 0 && !(w.q[i] == 0.f)) loss += w.q[i] * (w.lq[i] - (s.S == 0.f ? -INFINITY : s.ref.nat(now.x[i]) - logs));
+      }
       loss = warp_sum(loss);
       if (l.qr > 0.f) {
         const float lr = s.ref.far || s.ro.far ? (o.m - s.ref.m) * g.inv_t : (s.ro.rho - s.ref.rho) * LN2;
@@ -1095,26 +1156,30 @@ __global__ void __launch_bounds__(STAY + 32, 3) distill_kernel(const __grid_cons
       if (lane == 0) a.loss[r] = l.any ? a.scale * loss : 0.f;
     }
     if (a.dx) {
-      sync_block();
+      await<NT>(WRITTEN);
+      if (a.rest && has_next) patch(next, later);
       if (l.any && dl != 0.f) {
         T* dx = (T*)a.dx + r * a.ld_out;
-        const float f = dl * a.scale * g.inv_t;
+        const float f = dl * a.scale * g.inv_t, share = l.Q / s.S;
+        const int end = beyond(p);
 #pragma unroll
         for (int i = 0; i < PER_LANE; ++i) {
-          const int id = now.id[i], at = place(id);
+          if (i >= used) break;
+          const int id = now.id[i], at = id - p.head - p.first * N;
           float q = w.q[i];
           if (w.twins) {                                 // the sum over the entries of the token
             q = 0.f;
+#pragma unroll
             for (int b = 0; b < PER_LANE; ++b)
               for (int j = 0; j < 32; ++j) {
                 const float other = __shfl_sync(0xffffffffu, w.q[b], j);
                 if (32 * b + j < a.k && l.id[32 * b + j] == id) q += other;
               }
           }
-          const bool here = (at >= 0 && at < p.count * N) || (rank == 0 && (id < p.head || id >= beyond));
-          if (!w.first[i] || !here) continue;
-          const float pi = (now.x[i] == -INFINITY ? 0.f : ex2(s.ref.y(now.x[i]))) / s.S;
-          dx[id] = from_f<T>(s.S == 0.f ? 0.f : (l.Q * pi - q) * f);
+          const bool here = (at >= 0 && at < p.count * N) || (rank == 0 && (id < p.head || id >= end));
+          if (!(w.first >> i & 1) || !here) continue;
+          const float e = now.x[i] == -INFINITY ? 0.f : ex2(s.ref.y(now.x[i]));
+          dx[id] = from_f<T>(s.S == 0.f ? 0.f : fmaf(e, share, -q) * f);
         }
       }
     }
@@ -1127,7 +1192,6 @@ __global__ void __launch_bounds__(STAY + 32, 3) distill_kernel(const __grid_cons
 
 // ---------------------------------------------------------------------------------------------- launches
 constexpr int PIECE = 4160;                   // vectors of a staying piece that let three blocks share an SM
-constexpr int STATIC = 6 * 1024 + 512;        // shared memory beside it, at most
 
 struct Plan {
   Geometry g;
@@ -1140,17 +1204,21 @@ Plan plan_rows(const LogitsIn& in, int elem_bytes, int threads, bool stay, size_
   Plan p{};
   const int N = 16 / elem_bytes, all = std::max(1, in.vocab / N);
   int c = stay ? std::min(MAX_CLUSTER, (all + PIECE - 1) / PIECE) : 1;
-  while (2 * c <= MAX_CLUSTER && (long long)in.rows * c < 2 * 148 && all / (2 * c) >= 256) c *= 2;
+  while (threads > FEW && 2 * c <= MAX_CLUSTER && (long long)in.rows * c < 2 * 148 && all / (2 * c) >= 256) c *= 2;
   const int per = (all + c - 1) / c;
   p.threads = threads + more_threads;
   p.smem = (stay ? (size_t)per * 16 : smem) + (c > 1 ? smem_cluster : 0);
-  const int blocks = std::min({32, 65536 / (72 * p.threads), (int)(228 * 1024 / (p.smem + STATIC + 1024))});
+  const size_t fixed = threads == FEW ? 3840 : 7424;       // shared memory of a kernel beside that, at most
+  const int blocks = std::min({32, 65536 / (std::max(threads >= STAY ? 72 : 80, 1) * p.threads), (int)(228 * 1024 / (p.smem + fixed + 1024))});
   p.grid = dim3((unsigned)(std::min<long long>(in.rows, std::max(1, 148 * blocks / c)) * c));
   const double cc = 1.4426950408889634 / (double)in.temperature;
   p.g = Geometry{(float)cc, (float)(1.0 / (double)in.temperature), (float)(-1e30 * std::min(1.0, 1.0 / cc)), (float)(SLACK / cc), c, per,
                  (per + 4 * threads - 1) / (4 * threads)};
   return p;
 }
+
+// Rows of at most 16 KB, enough of them to give every warp of the device one.
+bool short_rows(const LogitsIn& in, size_t elem_bytes) { return in.vocab * elem_bytes <= 16384 && in.rows >= 148 * 8; }
 
 template <typename... KArgs, typename A>
 cudaError_t run(void (*kernel)(KArgs...), SmemLimit& limit, const Plan& p, cudaStream_t s, const A& a) {
@@ -1159,51 +1227,64 @@ cudaError_t run(void (*kernel)(KArgs...), SmemLimit& limit, const Plan& p, cudaS
   return launch_cluster_after(kernel, p.g.cluster, p.grid, p.threads, p.smem, s, a, p.g);
 }
 
-template <typename T, bool W, bool CL, bool TOP>
+template <typename T, int NT, bool W, bool CL, bool TOP>
 cudaError_t run_logprobs(const LogprobsArgs& a, const Plan& p, cudaStream_t s) {
   static SmemLimit limit;
-  return run(logprobs_kernel<T, W, CL, TOP>, limit, p, s, a);
+  return run(logprobs_kernel<T, NT, W, CL, TOP>, limit, p, s, a);
+}
+template <typename T, int NT, bool W, bool TOP>
+cudaError_t run_logprobs(const LogprobsArgs& a, cudaStream_t s) {
+  typedef TopSpace<NT> Top;
+  const size_t ring = SLOTS * 4 * NT * 16;
+  const Plan p = TOP ? plan_rows(a.in, sizeof(T), NT, false, ring + offsetof(Top, sorted), sizeof(Top) - offsetof(Top, sorted))
+                     : plan_rows(a.in, sizeof(T), NT, false, ring, 0);
+  if constexpr (NT == STREAM)
+    if (p.g.cluster > 1) return run_logprobs<T, NT, W, true, TOP>(a, p, s);
+  return run_logprobs<T, NT, W, false, TOP>(a, p, s);
 }
 template <typename T, bool W>
-cudaError_t run_logprobs(const LogprobsArgs& a, const Plan& p, cudaStream_t s) {
-  if (a.top_k > 0) return p.g.cluster > 1 ? run_logprobs<T, W, true, true>(a, p, s) : run_logprobs<T, W, false, true>(a, p, s);
-  return p.g.cluster > 1 ? run_logprobs<T, W, true, false>(a, p, s) : run_logprobs<T, W, false, false>(a, p, s);
+cudaError_t run_logprobs(const LogprobsArgs& a, cudaStream_t s) {
+  if (short_rows(a.in, sizeof(T)) && a.top_k <= FEW) return a.top_k > 0 ? run_logprobs<T, FEW, W, true>(a, s) : run_logprobs<T, FEW, W, false>(a, s);
+  return a.top_k > 0 ? run_logprobs<T, STREAM, W, true>(a, s) : run_logprobs<T, STREAM, W, false>(a, s);
 }
-template <typename T, bool W, bool CL>
+template <typename T, int NT, bool W, bool CL>
 cudaError_t run_bwd(const LogprobsBwdArgs& a, const Plan& p, cudaStream_t s) {
   static SmemLimit limit;
-  return run(logprobs_bwd_kernel<T, W, CL>, limit, p, s, a);
+  return run(logprobs_bwd_kernel<T, NT, W, CL>, limit, p, s, a);
 }
-template <typename T, bool CL>
+template <typename T, bool W>
+cudaError_t run_bwd(const LogprobsBwdArgs& a, cudaStream_t s) {
+  if (short_rows(a.in, sizeof(T))) return run_bwd<T, FEW, W, false>(a, plan_rows(a.in, sizeof(T), FEW, true, 0, 0), s);
+  const Plan p = plan_rows(a.in, sizeof(T), STAY, true, 0, 0);
+  return p.g.cluster > 1 ? run_bwd<T, STAY, W, true>(a, p, s) : run_bwd<T, STAY, W, false>(a, p, s);
+}
+
+template <typename T, int NT, bool CL>
 cudaError_t run_distill(const DistillArgs& a, const Plan& p, cudaStream_t s) {
   static SmemLimit limit;
-  return run(distill_kernel<T, CL>, limit, p, s, a);
+  return run(distill_kernel<T, NT, CL>, limit, p, s, a);
+}
+template <typename T>
+cudaError_t run_distill(const DistillArgs& a, cudaStream_t s) {
+  if (short_rows(a.in, sizeof(T))) return run_distill<T, FEW, false>(a, plan_rows(a.in, sizeof(T), FEW, true, 0, 0, 32), s);
+  const Plan p = plan_rows(a.in, sizeof(T), STAY, true, 0, 0, 32);
+  return p.g.cluster > 1 ? run_distill<T, STAY, true>(a, p, s) : run_distill<T, STAY, false>(a, p, s);
 }
 
 }  // namespace
 
 cudaError_t launch_logprobs(const LogprobsArgs& a, bool is_bf16, cudaStream_t s) {
-  typedef TopSpace<STREAM> Top;
-  const size_t ring = SLOTS * 4 * STREAM * 16;
-  const Plan p = a.top_k > 0 ? plan_rows(a.in, is_bf16 ? 2 : 4, STREAM, false, ring + offsetof(Top, sorted), sizeof(Top) - offsetof(Top, sorted))
-                             : plan_rows(a.in, is_bf16 ? 2 : 4, STREAM, false, ring, 0);
-  if (is_bf16) return a.entropy ? run_logprobs<bf16, true>(a, p, s) : run_logprobs<bf16, false>(a, p, s);
-  return a.entropy ? run_logprobs<float, true>(a, p, s) : run_logprobs<float, false>(a, p, s);
+  if (is_bf16) return a.entropy ? run_logprobs<bf16, true>(a, s) : run_logprobs<bf16, false>(a, s);
+  return a.entropy ? run_logprobs<float, true>(a, s) : run_logprobs<float, false>(a, s);
 }
 
 cudaError_t launch_logprobs_bwd(const LogprobsBwdArgs& a, bool is_bf16, cudaStream_t s) {
-  const Plan p = plan_rows(a.in, is_bf16 ? 2 : 4, STAY, true, 0, 0);
-  const bool w = a.dentropy != nullptr, cl = p.g.cluster > 1;
-  if (is_bf16) return w ? (cl ? run_bwd<bf16, true, true>(a, p, s) : run_bwd<bf16, true, false>(a, p, s))
-                        : (cl ? run_bwd<bf16, false, true>(a, p, s) : run_bwd<bf16, false, false>(a, p, s));
-  return w ? (cl ? run_bwd<float, true, true>(a, p, s) : run_bwd<float, true, false>(a, p, s))
-           : (cl ? run_bwd<float, false, true>(a, p, s) : run_bwd<float, false, false>(a, p, s));
+  if (is_bf16) return a.dentropy ? run_bwd<bf16, true>(a, s) : run_bwd<bf16, false>(a, s);
+  return a.dentropy ? run_bwd<float, true>(a, s) : run_bwd<float, false>(a, s);
 }
 
 cudaError_t launch_distill(const DistillArgs& a, bool is_bf16, cudaStream_t s) {
-  const Plan p = plan_rows(a.in, is_bf16 ? 2 : 4, STAY, true, 0, 0, 32);
-  if (is_bf16) return p.g.cluster > 1 ? run_distill<bf16, true>(a, p, s) : run_distill<bf16, false>(a, p, s);
-  return p.g.cluster > 1 ? run_distill<float, true>(a, p, s) : run_distill<float, false>(a, p, s);
+  return is_bf16 ? run_distill<bf16>(a, s) : run_distill<float>(a, s);
 }
 
 }  // namespace lp
