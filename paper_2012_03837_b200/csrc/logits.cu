@@ -17,6 +17,7 @@
 // a gradient or the top alternatives take.  Long rows, and rows too few for the device, are cut over a cluster of up to
 // eight blocks, which exchange their sums through distributed shared memory.
 #include <algorithm>
+#include <atomic>
 #include <cstddef>
 
 #include <cooperative_groups.h>
@@ -1195,42 +1196,84 @@ constexpr int PIECE = 4160;                   // vectors of a staying piece that
 
 struct Plan {
   Geometry g;
-  dim3 grid;
-  int threads;
+  int rows, threads;
   size_t smem;
 };
-// Blocks of `threads`; stay: rows stay in shared memory as a whole, otherwise it takes `smem` bytes.
+// Blocks of `threads` (and more_threads); stay: rows stay in shared memory as a whole, otherwise it takes `smem` bytes.
 Plan plan_rows(const LogitsIn& in, int elem_bytes, int threads, bool stay, size_t smem, size_t smem_cluster, int more_threads = 0) {
   Plan p{};
   const int N = 16 / elem_bytes, all = std::max(1, in.vocab / N);
   int c = stay ? std::min(MAX_CLUSTER, (all + PIECE - 1) / PIECE) : 1;
   while (threads > FEW && 2 * c <= MAX_CLUSTER && (long long)in.rows * c < 2 * 148 && all / (2 * c) >= 256) c *= 2;
   const int per = (all + c - 1) / c;
+  p.rows = in.rows;
   p.threads = threads + more_threads;
   p.smem = (stay ? (size_t)per * 16 : smem) + (c > 1 ? smem_cluster : 0);
-  const size_t fixed = threads == FEW ? 3840 : 7424;       // shared memory of a kernel beside that, at most
-  const int blocks = std::min({32, 65536 / (std::max(threads >= STAY ? 72 : 80, 1) * p.threads), (int)(228 * 1024 / (p.smem + fixed + 1024))});
-  p.grid = dim3((unsigned)(std::min<long long>(in.rows, std::max(1, 148 * blocks / c)) * c));
   const double cc = 1.4426950408889634 / (double)in.temperature;
   p.g = Geometry{(float)cc, (float)(1.0 / (double)in.temperature), (float)(-1e30 * std::min(1.0, 1.0 / cc)), (float)(SLACK / cc), c, per,
                  (per + 4 * threads - 1) / (4 * threads)};
   return p;
 }
 
+// What a kernel needs to know of the device, asked for once: the limit of its shared memory, and how many clusters run at
+// a time (blocks beyond would start on their rows when the others are through), for the last size of each cluster.
+struct Residency {
+  SmemLimit limit;
+  std::atomic<unsigned long long> seen[MAX_CLUSTER + 1];
+  template <typename... KArgs>
+  cudaError_t of(void (*kernel)(KArgs...), const Plan& p, int* clusters) {
+    cudaError_t e = limit.raise((const void*)kernel, 160 * 1024);
+    if (e != cudaSuccess) return e;
+    int dev = 0;
+    if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
+    const unsigned long long key = ((unsigned long long)(dev + 1) << 40 | p.smem << 16) & ~0xffffull;
+    const unsigned long long had = seen[p.g.cluster].load(std::memory_order_relaxed);
+    if ((had & ~0xffffull) == key) {
+      *clusters = (int)(had & 0xffff);
+      return cudaSuccess;
+    }
+    int n = 0;
+    if (p.g.cluster > 1) {
+      cudaLaunchConfig_t cfg{};
+      cudaLaunchAttribute at{};
+      at.id = cudaLaunchAttributeClusterDimension;
+      at.val.clusterDim.x = (unsigned)p.g.cluster;
+      at.val.clusterDim.y = at.val.clusterDim.z = 1;
+      cfg.gridDim = dim3((unsigned)p.g.cluster);
+      cfg.blockDim = dim3((unsigned)p.threads);
+      cfg.dynamicSmemBytes = p.smem;
+      cfg.attrs = &at;
+      cfg.numAttrs = 1;
+      if ((e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg)) != cudaSuccess) return e;
+    } else {
+      int sms = 0;
+      if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, p.threads, p.smem)) != cudaSuccess) return e;
+      if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
+      n *= sms;
+    }
+    n = std::min(std::max(n, 1), 0xffff);
+    seen[p.g.cluster].store(key | (unsigned)n, std::memory_order_relaxed);
+    *clusters = n;
+    return cudaSuccess;
+  }
+};
+
 // Rows of at most 16 KB, enough of them to give every warp of the device one.
 bool short_rows(const LogitsIn& in, size_t elem_bytes) { return in.vocab * elem_bytes <= 16384 && in.rows >= 148 * 8; }
 
 template <typename... KArgs, typename A>
-cudaError_t run(void (*kernel)(KArgs...), SmemLimit& limit, const Plan& p, cudaStream_t s, const A& a) {
-  const cudaError_t e = limit.raise((const void*)kernel, 160 * 1024);
+cudaError_t run(void (*kernel)(KArgs...), Residency& residency, const Plan& p, cudaStream_t s, const A& a) {
+  int clusters = 0;
+  const cudaError_t e = residency.of(kernel, p, &clusters);
   if (e != cudaSuccess) return e;
-  return launch_cluster_after(kernel, p.g.cluster, p.grid, p.threads, p.smem, s, a, p.g);
+  const dim3 grid((unsigned)(std::min(p.rows, clusters) * p.g.cluster));
+  return launch_cluster_after(kernel, p.g.cluster, grid, p.threads, p.smem, s, a, p.g);
 }
 
 template <typename T, int NT, bool W, bool CL, bool TOP>
 cudaError_t run_logprobs(const LogprobsArgs& a, const Plan& p, cudaStream_t s) {
-  static SmemLimit limit;
-  return run(logprobs_kernel<T, NT, W, CL, TOP>, limit, p, s, a);
+  static Residency residency;
+  return run(logprobs_kernel<T, NT, W, CL, TOP>, residency, p, s, a);
 }
 template <typename T, int NT, bool W, bool TOP>
 cudaError_t run_logprobs(const LogprobsArgs& a, cudaStream_t s) {
@@ -1249,8 +1292,8 @@ cudaError_t run_logprobs(const LogprobsArgs& a, cudaStream_t s) {
 }
 template <typename T, int NT, bool W, bool CL>
 cudaError_t run_bwd(const LogprobsBwdArgs& a, const Plan& p, cudaStream_t s) {
-  static SmemLimit limit;
-  return run(logprobs_bwd_kernel<T, NT, W, CL>, limit, p, s, a);
+  static Residency residency;
+  return run(logprobs_bwd_kernel<T, NT, W, CL>, residency, p, s, a);
 }
 template <typename T, bool W>
 cudaError_t run_bwd(const LogprobsBwdArgs& a, cudaStream_t s) {
@@ -1261,8 +1304,8 @@ cudaError_t run_bwd(const LogprobsBwdArgs& a, cudaStream_t s) {
 
 template <typename T, int NT, bool CL>
 cudaError_t run_distill(const DistillArgs& a, const Plan& p, cudaStream_t s) {
-  static SmemLimit limit;
-  return run(distill_kernel<T, NT, CL>, limit, p, s, a);
+  static Residency residency;
+  return run(distill_kernel<T, NT, CL>, residency, p, s, a);
 }
 template <typename T>
 cudaError_t run_distill(const DistillArgs& a, cudaStream_t s) {
