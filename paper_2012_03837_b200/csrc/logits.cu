@@ -37,7 +37,8 @@ constexpr float FAR = 1e23f;
 constexpr float LN2 = 0.693147180559945309f;
 constexpr int MAX_CLUSTER = 8;
 constexpr float SLACK = 8.f;                  // a sum's reference stays while no power of two exceeds 2^SLACK
-constexpr int CANDIDATES = 512;               // of the top alternatives
+constexpr int BATCH = 8;                      // vectors that a thread takes at a time
+constexpr int CANDIDATES = 256;               // of the top alternatives
 
 // ---------------------------------------------------------------------------------------------- two floats at a time
 __device__ __forceinline__ u64 pack(float a, float b) {
@@ -101,17 +102,12 @@ template <> struct Vec<bf16> {
   }
   static __device__ __forceinline__ __nv_bfloat162 b2(uint32_t w) { return *(__nv_bfloat162*)&w; }
   static __device__ __forceinline__ uint32_t u2(__nv_bfloat162 w) { return *(uint32_t*)&w; }
-  // the largest element; a NaN only if there is nothing else
-  static __device__ __forceinline__ float max1(const Quad& v) {
-    const __nv_bfloat162 m = __hmax2(__hmax2(b2(v.w[0]), b2(v.w[1])), __hmax2(b2(v.w[2]), b2(v.w[3])));
-    return __bfloat162float(__hmax(__low2bfloat16(m), __high2bfloat16(m)));
-  }
-  static __device__ __forceinline__ float max4(const Quad* v) {
-    __nv_bfloat162 m = b2(v[0].w[0]);
-#pragma unroll
-    for (int u = 0; u < 4; ++u) m = __hmax2(m, __hmax2(__hmax2(b2(v[u].w[0]), b2(v[u].w[1])), __hmax2(b2(v[u].w[2]), b2(v[u].w[3]))));
-    return __bfloat162float(__hmax(__low2bfloat16(m), __high2bfloat16(m)));
-  }
+  // the largest element; a NaN only if there is nothing else.  First in two halves.
+  typedef __nv_bfloat162 Most;
+  static __device__ __forceinline__ Most lowest() { return b2(0xFF80FF80u); }
+  static __device__ __forceinline__ Most most(const Quad& v) { return __hmax2(__hmax2(b2(v.w[0]), b2(v.w[1])), __hmax2(b2(v.w[2]), b2(v.w[3]))); }
+  static __device__ __forceinline__ Most more(Most a, Most b) { return __hmax2(a, b); }
+  static __device__ __forceinline__ float value(Most m) { return __bfloat162float(__hmax(__low2bfloat16(m), __high2bfloat16(m))); }
   static __device__ __forceinline__ void clamp(Quad& v, float lo) {
     const __nv_bfloat162 l = __float2bfloat162_rn(lo);
 #pragma unroll
@@ -130,8 +126,11 @@ template <> struct Vec<float> {
   static constexpr int N = 4;
   static __device__ __forceinline__ float at(const Quad& v, int i) { return __uint_as_float(v.w[i]); }
   static __device__ __forceinline__ u64 pair(const Quad& v, int i) { return pack(at(v, 2 * i), at(v, 2 * i + 1)); }
-  static __device__ __forceinline__ float max1(const Quad& v) { return fmaxf(fmaxf(at(v, 0), at(v, 1)), fmaxf(at(v, 2), at(v, 3))); }
-  static __device__ __forceinline__ float max4(const Quad* v) { return fmaxf(fmaxf(max1(v[0]), max1(v[1])), fmaxf(max1(v[2]), max1(v[3]))); }
+  typedef float Most;
+  static __device__ __forceinline__ Most lowest() { return -INFINITY; }
+  static __device__ __forceinline__ Most most(const Quad& v) { return fmaxf(fmaxf(at(v, 0), at(v, 1)), fmaxf(at(v, 2), at(v, 3))); }
+  static __device__ __forceinline__ Most more(Most a, Most b) { return fmaxf(a, b); }
+  static __device__ __forceinline__ float value(Most m) { return m; }
   static __device__ __forceinline__ void clamp(Quad& v, float lo) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v.w[i] = __float_as_uint(max_nan(at(v, i), lo));
@@ -149,12 +148,13 @@ struct Geometry {
   float c, inv_t;                             // log2(e) / T, 1 / T
   float lo;                                   // logits below it have probability 0 in rows that are not far
   float slack;                                // SLACK in units of a logit
-  int cluster, per, batches;                  // blocks per row, vectors of a block's piece, batches of 4 NT of them
+  int cluster, per, batches;                  // blocks per row, vectors of a block's piece, batches of BATCH NT of them
+  int shift;                                  // log2 of the fours of vectors of which a thread leaves one maximum
 };
 
 // A block's piece of a row.  Its vectors are those aligned 16 bytes that lie in the row as a whole, `first` .. `first` +
 // `count` of them here; element j of the row's ends, which no vector holds, belongs to one thread of the first block.
-// Thread t works on vectors t, t + NT, ..., four to a batch, and nobody else sees its copies of them.
+// Thread t works on vectors t, t + NT, ..., eight to a batch, and nobody else sees its copies of them.
 template <typename T, int NT>
 struct Piece {
   static constexpr int N = Vec<T>::N;
@@ -169,41 +169,28 @@ struct Piece {
     edge = rank != 0 ? -1 : t < head ? t : t - head < n - tail ? tail + t - head : -1;
   }
   __device__ __forceinline__ int element(int v) const { return head + (first + v) * N; }     // the first of vector v
-  __device__ __forceinline__ bool whole(int b) const { return (b + 1) * 4 * NT <= count; }
+  __device__ __forceinline__ bool whole(int b) const { return (b + 1) * BATCH * NT <= count; }
   // Asks for batch b: its vectors u arrive at to[u * NT].  One group of copies, of nothing for b beyond the piece.
   __device__ __forceinline__ void fetch(uint4* to, int b) const {
-    const int v = 4 * b * NT + threadIdx.x;
+    const int v = BATCH * b * NT + threadIdx.x;
     const uint32_t d = (uint32_t)__cvta_generic_to_shared(to);
     const T* s = x + element(v);
     if (whole(b)) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < BATCH; ++u)
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d + u * NT * 16), "l"(s + u * NT * N) : "memory");
     } else {
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < BATCH; ++u)
         if (v + u * NT < count) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d + u * NT * 16), "l"(s + u * NT * N) : "memory");
     }
     commit();
   }
   __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
   __device__ __forceinline__ void fetch_all(uint4* buf, const Geometry& g) const {
-    for (int b = 0; b < g.batches; ++b) fetch(buf + 4 * b * NT + threadIdx.x, b);
+    for (int b = 0; b < g.batches; ++b) fetch(buf + BATCH * b * NT + threadIdx.x, b);
   }
   __device__ __forceinline__ float edge_value() const { return edge >= 0 ? to_f(x[edge]) : -INFINITY; }
-  __device__ __forceinline__ void load(Quad (&a)[4], const uint4* from, int b) const {
-    if (whole(b)) {
-#pragma unroll
-      for (int u = 0; u < 4; ++u) a[u] = quad(from[u * NT]);
-    } else {
-      const int v = 4 * b * NT + threadIdx.x;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        a[u] = nothing<T>();
-        if (v + u * NT < count) a[u] = quad(from[u * NT]);
-      }
-    }
-  }
   __device__ __forceinline__ void store(T* dst, int v, const Quad& r) const {
     T* d = dst + element(v);
     if (((uintptr_t)d & 15) == 0) {
@@ -259,15 +246,14 @@ struct Running {
     nrho = pack(-r, -r);
     top = to + g.slack;
   }
-  // Adds a batch and returns its maximum.
-  __device__ __forceinline__ float add(Quad (&a)[4], const Geometry& g) {
+  template <int M>
+  __device__ __forceinline__ void add(Quad (&a)[M], float bm, const Geometry& g) {
     constexpr int P = Vec<T>::N / 2;
     const u64 c2 = pack(g.c, g.c);
-    const float bm = Vec<T>::max4(a);
     m = fmaxf(m, bm);
     if (bm > top) raise(bm, g);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < M; ++u) {
       if (W) Vec<T>::clamp(a[u], g.lo);
 #pragma unroll
       for (int i = 0; i < P; i += 2) {
@@ -278,7 +264,36 @@ struct Running {
         if (W) { w0 = fma2(e0, y0, w0); w1 = fma2(e1, y1, w1); }
       }
     }
-    return bm;
+  }
+  // Adds batch b, which has arrived; leaf(group, maximum of even vectors, of odd ones) hears of every four vectors.
+  template <int NT, typename Leaf>
+  __device__ __forceinline__ void batch(const Piece<T, NT>& p, const uint4* from, int b, const Geometry& g, Leaf leaf) {
+    typedef Vec<T> V;
+    if (p.whole(b)) {
+      Quad a[BATCH];
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) a[u] = quad(from[u * NT]);
+      typename V::Most e[2], o[2];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        e[q] = V::more(V::most(a[4 * q]), V::most(a[4 * q + 2]));
+        o[q] = V::more(V::most(a[4 * q + 1]), V::most(a[4 * q + 3]));
+        leaf(2 * b + q, e[q], o[q]);
+      }
+      add<BATCH>(a, V::value(V::more(V::more(e[0], o[0]), V::more(e[1], o[1]))), g);
+    } else {
+      const int first = threadIdx.x & ~31;               // of the warp: what no lane has is left out
+#pragma unroll 1
+      for (int u = 0; u < BATCH; ++u) {
+        const int v = (BATCH * b + u) * NT;
+        if (v + first >= p.count) break;
+        Quad a[1] = {nothing<T>()};
+        if (v + (int)threadIdx.x < p.count) a[0] = quad(from[u * NT]);
+        const typename V::Most m = V::most(a[0]);
+        leaf(2 * b + u / 4, u & 1 ? V::lowest() : m, u & 1 ? m : V::lowest());
+        add<1>(a, V::value(m), g);
+      }
+    }
   }
   // The thread's own element of the row's ends, if it is there (not -infinity), and the sums against the warp's maximum.
   __device__ __forceinline__ Sums end(float edge, const Geometry& g) {
@@ -320,8 +335,8 @@ __device__ __noinline__ Sums sweep_far(const Piece<T, NT> p, const Geometry g, f
 }
 
 // What the warps of a row's blocks tell one another; of two rows in turn.
-template <int NT>
-struct Exchange { float4 part[2][2][MAX_CLUSTER * NT / 32]; };
+template <int NT, bool CL>
+struct Exchange { float4 part[2][2][(CL ? MAX_CLUSTER : 1) * NT / 32]; };
 
 // All warps of the block, wherever in the code each of them is.
 __device__ __forceinline__ void sync_block() {
@@ -452,12 +467,13 @@ constexpr int ENTRIES = 8;                    // maxima that a thread leaves of 
 
 template <int NT>
 struct TopSpace {
-  u64 list[CANDIDATES];
-  float maxima[ENTRIES][NT];                  // of `stride` batches each
-  uint32_t halves[2 * NT];                    // the order of every thread's maxima over vectors 0, 1 and 2, 3 of all batches
+  alignas(16) u64 list[CANDIDATES];           // read two at a time
+  float maxima[ENTRIES][NT];                  // of 2^shift fours of vectors each
+  uint32_t halves[2 * NT];                    // the order of every thread's maxima over its even and odd vectors
   unsigned short hits[ENTRIES * NT];
+  int queue[CANDIDATES];                      // vectors to look at
   uint32_t bound;
-  int count, found, warp_total[NT / 32];
+  int count, found, queued;
   u64 sorted[MAX_CLUSTER][TOP_MAX];           // of the row's first block: what each block found
 };
 
@@ -486,128 +502,134 @@ __device__ __forceinline__ uint32_t bound_of(const uint32_t* values, int k) {
       hi = mid;
     } else {
       lo = mid;
-      if (n <= k + k / 4) break;
+      if (n <= k + k / 8) break;
     }
   }
   return lo;
 }
 
-// Puts the keys of the block's k largest logits (all of them, if there are fewer) into ts.list and returns how many are
+// Puts the keys of the piece's k largest logits (all of them, if there are fewer) into ts.list and returns how many are
 // there: at least min(k, logits), at most CANDIDATES.
-//   The k-th largest of the 2 NT maxima of the threads' halves, or a little less, is reached by at least k logits, and of
-//   logits in no particular order by hardly more (k = 64 of 256: 74).  Only batches whose maximum reaches it are read again.
-//   Where more than CANDIDATES logits reach it (many equal ones, or large ones side by side), the k-th largest value itself is
-//   found among all logits by halving, and the equal ones are taken in the order of their ids.
+//   The k-th largest of the 2 NT maxima of the threads' even and odd vectors, or a little less, is reached by at least k
+//   logits, and of logits in no particular order by hardly more (k = 64 of 256: 74).  Only vectors under a maximum that
+//   reaches it are read again, and only elements of those that do are compared.
+//   Where more than CANDIDATES logits reach it (many equal ones, or large ones side by side), the bound is raised by halving
+//   until they fit, or until it is the k-th largest value itself, of which those with the lowest ids are taken.
 template <typename T, int NT>
-__device__ int top_candidates(const Piece<T, NT>& p, float edge, int k, float thread_max, int stride, int entries, TopSpace<NT>& ts) {
-  constexpr int N = Vec<T>::N;
-  constexpr uint32_t NOTHING = 0x007fffffu;              // the order of -infinity
-  const int tid = threadIdx.x;
-  if (tid < 32) {
-    const uint32_t b = bound_of<2 * NT>(ts.halves, k);
-    if (tid == 0) { ts.bound = b; ts.count = 0; ts.found = 0; }
-  }
-  __syncthreads();
-  uint32_t lo = ts.bound;
-  const float bound = lo <= NOTHING ? -INFINITY : value_of(lo);
-  auto add = [&](uint32_t o, int j) {
-    const int at = atomicAdd(&ts.count, 1);
-    if (at < CANDIDATES) ts.list[at] = key_of(o, j);
-  };
+__device__ int top_candidates(const Piece<T, NT>& p, float edge, int k, int shift, TopSpace<NT>& ts) {
+  constexpr int N = Vec<T>::N, AT_ONCE = 3;
+  constexpr uint32_t NOTHING = 0x007fffffu;              // the order of -infinity; maxima of it may hide a NaN, which stands below
+  const int t = threadIdx.x, per = 4 << shift, entries = (p.count + per * NT - 1) / (per * NT);
   auto vector = [&](int v) { return quad(*(const uint4*)(p.x + p.element(v))); };
-  for (int e = 0; e < entries; ++e)
-    if (lo <= NOTHING || ts.maxima[e][tid] >= bound) ts.hits[atomicAdd(&ts.found, 1)] = (unsigned short)(e * NT + tid);
-  if (p.edge >= 0 && order_of(edge) >= lo) add(order_of(edge), p.edge);
-  __syncthreads();
-  const int per = 4 * stride, units = ts.found * per;
-  for (int i = tid; i < units; i += NT) {
-    const int h = ts.hits[i / per], at = i % per, v = ((h / NT * stride + at / 4) * 4 + at % 4) * NT + h % NT;
-    if (v >= p.count) continue;
-    const Quad a = vector(v);
-    if (lo > NOTHING && !(Vec<T>::max1(a) >= bound)) continue;
-    for (int i = 0; i < N; ++i) {
-      const uint32_t o = order_of(Vec<T>::get(a, i));
-      if (o >= lo) add(o, p.element(v) + i);
-    }
-  }
-  __syncthreads();
-  if (ts.count <= CANDIDATES) return ts.count;
-
-  // exactly: the largest value that at least k logits reach; most: the order of the thread's largest
-  const uint32_t most = max(order_of(thread_max), NOTHING);
-  auto reaching = [&](uint32_t b) {
-    int n = 0;
-    if (most >= b) {
-      for (int v = tid; v < p.count; v += NT) {
-        const Quad a = vector(v);
-        for (int i = 0; i < N; ++i) n += order_of(Vec<T>::get(a, i)) >= b;
+  // The logits that reach b go to the list; returns how many there are, or some number above CANDIDATES if there are more.
+  auto collect = [&](uint32_t b) {
+    sync_block();
+    if (t == 0) ts.count = ts.found = ts.queued = 0;
+    sync_block();
+    const float bound = b <= NOTHING ? -INFINITY : value_of(b);
+    auto add = [&](float x, int j) {
+      const uint32_t o = order_of(x);
+      if (o < b) return;
+      const int at = atomicAdd(&ts.count, 1);
+      if (at < CANDIDATES) ts.list[at] = key_of(o, j);
+    };
+    for (int e = 0; e < entries; ++e)
+      if (e * per * NT + t < p.count && (b <= NOTHING || ts.maxima[e][t] >= bound))
+        ts.hits[atomicAdd(&ts.found, 1)] = (unsigned short)(e * NT + t);
+    if (p.edge >= 0) add(edge, p.edge);
+    sync_block();
+    const int units = ts.found * per;
+    for (int i0 = t; i0 < units; i0 += AT_ONCE * NT) {
+      Quad a[AT_ONCE];
+      int v[AT_ONCE];
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const int i = i0 + u * NT, h = i < units ? ts.hits[i >> (shift + 2)] : 0;
+        v[u] = i < units ? ((h / NT << (shift + 2)) + (i & (per - 1))) * NT + h % NT : p.count;
+        a[u] = v[u] < p.count ? vector(v[u]) : nothing<T>();
       }
-      n += p.edge >= 0 && order_of(edge) >= b;
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u)
+        if (v[u] < p.count && (b == 0 || Vec<T>::value(Vec<T>::most(a[u])) >= bound)) {
+          const int at = atomicAdd(&ts.queued, 1);
+          if (at < CANDIDATES) ts.queue[at] = v[u];
+        }
     }
-    n = __reduce_add_sync(0xffffffffu, n);
-    __syncthreads();
-    if ((tid & 31) == 0) ts.warp_total[tid >> 5] = n;
-    __syncthreads();
-    n = 0;
-    for (int w = 0; w < NT / 32; ++w) n += ts.warp_total[w];
-    return n;
+    sync_block();
+    if (ts.queued > CANDIDATES) return ts.queued;        // each has a logit that reaches it
+    for (int i = t; i < ts.queued * N; i += NT) {
+      const int j = p.element(ts.queue[i / N]) + i % N;
+      add(to_f(p.x[j]), j);
+    }
+    sync_block();
+    return ts.count;
   };
+  if (t < 32) {
+    const uint32_t b = bound_of<2 * NT>(ts.halves, k);
+    if (t == 0) ts.bound = b;
+  }
+  sync_block();
+  uint32_t lo = ts.bound;
+  int n = collect(lo);
+  if (n <= CANDIDATES) return n;
   uint32_t hi = 0xffffffffu, probe = lo + 1;             // often lo itself is the value
-  int above = 0;
   while (hi - lo > 1) {
-    const int n = reaching(probe);
-    if (n >= k) lo = probe;
-    else { hi = probe; above = n; }
+    n = collect(probe);
+    if (n < k) hi = probe;
+    else if (n <= CANDIDATES) return n;
+    else lo = probe;
     probe = lo + (hi - lo) / 2;
   }
-  if (tid == 0) ts.count = 0;
-  __syncthreads();
-  if (most > lo) {
-    for (int v = tid; v < p.count; v += NT) {
-      const Quad a = vector(v);
-      for (int i = 0; i < N; ++i) {
-        const uint32_t o = order_of(Vec<T>::get(a, i));
-        if (o > lo) add(o, p.element(v) + i);
+  n = collect(hi);                                       // fewer than k; the rest are equal to lo, their ids ascending
+  if (t < 32) {                                          // one warp, from the row's first elements over its vectors to its last
+    auto take = [&](unsigned same, int j) {              // bit i: element j + i is equal
+      int before = __popc(same);
+      const int own = before;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, before, o);
+        if (t >= o) before += y;
       }
+      const int total = __shfl_sync(0xffffffffu, before, 31);
+      for (int at = n + before - own; same && at < k; ++at) {
+        const int i = __ffs(same) - 1;
+        ts.list[at] = key_of(lo, j + i);
+        same &= same - 1;
+      }
+      n += total;
+    };
+    const bool equal = p.edge >= 0 && order_of(edge) == lo;
+    take(equal && p.edge < p.head, p.edge);
+    for (int v0 = 0; v0 < p.count && n < k; v0 += 32) {
+      const int v = v0 + t;
+      unsigned same = 0;
+      if (v < p.count) {
+        const Quad a = vector(v);
+#pragma unroll
+        for (int l = 0; l < N; ++l) same |= (unsigned)(order_of(Vec<T>::get(a, l)) == lo) << l;
+      }
+      take(same, p.element(v));
     }
-    if (p.edge >= 0 && order_of(edge) > lo) add(order_of(edge), p.edge);
+    if (n < k) take(equal && p.edge >= p.head, p.edge);
+    if (t == 0) ts.bound = (uint32_t)min(n, k);
   }
-  // ids ascend from the row's first elements over its vectors, step by step and within a step with the thread, to its last
-  int taken = above;
-  const int steps = (p.count + NT - 1) / NT;
-  for (int step = -1; step <= steps && taken < k; ++step) {
-    unsigned same = 0;
-    int j = p.edge;
-    const int v = step * NT + tid;
-    if (step < 0 || step == steps) {
-      if (p.edge >= 0 && (p.edge < p.head) == (step < 0) && order_of(edge) == lo) same = 1;
-    } else if (v < p.count) {
-      const Quad a = vector(v);
-      j = p.element(v);
-      for (int i = 0; i < N; ++i)
-        if (order_of(Vec<T>::get(a, i)) == lo) same |= 1u << i;
+  sync_block();
+  return (int)ts.bound;
+}
+
+// A candidate's place is the number of larger ones.
+template <int NT, typename Put>
+__device__ __forceinline__ void rank_candidates(const u64* list, int found, int k, Put put) {
+  for (int i = threadIdx.x; i < found; i += NT) {
+    const u64 key = list[i];
+    int at = 0;
+#pragma unroll 4
+    for (int j = 0; j < found / 2; ++j) {
+      const ulonglong2 two = ((const ulonglong2*)list)[j];
+      at += (two.x > key) + (two.y > key);
     }
-    const int own = __popc(same);
-    int before = own;
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, before, o);
-      if ((tid & 31) >= o) before += y;
-    }
-    __syncthreads();
-    if ((tid & 31) == 31) ts.warp_total[tid >> 5] = before;
-    __syncthreads();
-    int total = 0;
-    before -= own;
-    for (int w = 0; w < NT / 32; ++w) {
-      if (w < tid >> 5) before += ts.warp_total[w];
-      total += ts.warp_total[w];
-    }
-    for (int i = 0, at = taken + before; same && at < k; ++i)
-      if (same >> i & 1) { add(lo, j + i); ++at; same &= ~(1u << i); }
-    taken += total;
+    if (found & 1) at += list[found - 1] > key;
+    if (at < k) put(at, key);
   }
-  __syncthreads();
-  return min(ts.count, CANDIDATES);
 }
 
 // ---------------------------------------------------------------------------------------------- kernels
@@ -621,13 +643,36 @@ struct Place {
   }
 };
 
-constexpr int STREAM = 128, SLOTS = 4;        // threads of a block that reads its rows once; batches that it has on their way
+// What a thread leaves of a row for the search of its top alternatives.
+template <typename T, int NT>
+struct Leaves {
+  typedef Vec<T> V;
+  typename V::Most even = V::lowest(), odd = V::lowest(), m = V::lowest();
+  __device__ __forceinline__ void group(TopSpace<NT>& ts, int q, typename V::Most e, typename V::Most o, int shift) {
+    if (m_of != q >> shift) {
+      m = V::lowest();
+      m_of = q >> shift;
+    }
+    even = V::more(even, e);
+    odd = V::more(odd, o);
+    m = V::more(m, V::more(e, o));
+    ts.maxima[q >> shift][threadIdx.x] = V::value(m);
+  }
+  int m_of = -1;                              // the entry that m belongs to
+  __device__ __forceinline__ void end(TopSpace<NT>& ts, float edge) {
+    const float a = V::value(even), b = fmaxf(V::value(odd), edge);
+    ts.halves[threadIdx.x] = a > -INFINITY ? order_of(a) : 0u;         // what counts as -infinity may be a NaN, which stands below
+    ts.halves[NT + threadIdx.x] = b > -INFINITY ? order_of(b) : 0u;
+  }
+};
+
+constexpr int STREAM = 128, SLOTS = 2;        // threads of a block that reads its rows once; batches that it has on their way
 
 // Batches pass through a ring of SLOTS, each thread's by itself: copies run ahead of the sums by SLOTS batches, over the end of
 // a row into the next ones, so that they go on while a row's sums are joined and handed out.
 template <typename T, int NT, bool W, bool CL, bool TOP>
 __global__ void __launch_bounds__(NT) logprobs_kernel(const __grid_constant__ LogprobsArgs a, const __grid_constant__ Geometry g) {
-  __shared__ Exchange<NT> ex;
+  __shared__ Exchange<NT, CL> ex;
   cudaGridDependencySynchronize();
   cluster_start<CL>();
   const Place me = Place::of<CL>(g);
@@ -638,7 +683,7 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(const __grid_constant__ Lo
   int ahead_batch = 0, slot = 0;
   auto fetch = [&]() {
     if (ahead_row >= rows) return p.commit();
-    ahead.fetch(dynamic + slot * 4 * NT + tid, ahead_batch);
+    ahead.fetch(dynamic + slot * BATCH * NT + tid, ahead_batch);
     if (++ahead_batch == g.batches) {
       ahead_batch = 0;
       ahead_row += me.groups;
@@ -647,12 +692,12 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(const __grid_constant__ Lo
   };
   for (; slot < SLOTS; ++slot) fetch();
   slot = 0;
+  static_assert(SLOTS == 2, "slots take turns");
   float edge = p.edge_value();
   int t = speaks && a.tokens ? token_of(a.tokens, me.row, a.in.vocab, a.in.out_of_range, true) : -1;
   float xt = t >= 0 ? to_f(p.x[t]) : 0.f;
   cluster_started<CL>();
-  TopSpace<NT>& ts = *(TopSpace<NT>*)(dynamic + SLOTS * 4 * NT);
-  const int stride = TOP ? (g.batches + ENTRIES - 1) / ENTRIES : 1;
+  TopSpace<NT>& ts = *(TopSpace<NT>*)(dynamic + SLOTS * BATCH * NT);
   int turn = 0;
   for (long long r = me.row; r < rows; r += me.groups, turn ^= 1) {
     const bool has_next = r + me.groups < rows;
@@ -660,33 +705,16 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(const __grid_constant__ Lo
     const float next_edge = next.edge_value();
     const int next_t = speaks && a.tokens && has_next ? token_of(a.tokens, r + me.groups, a.in.vocab, a.in.out_of_range, true) : -1;
     Running<T, W> run(g);
-    float h0 = -INFINITY, h1 = -INFINITY, em = -INFINITY;
-    int entry = 0, in_entry = 0;
+    Leaves<T, NT> leaves;
     for (int b = 0; b < g.batches; ++b) {
       wait_groups(SLOTS - 1);
-      Quad v[4];
-      p.load(v, dynamic + slot * 4 * NT + tid, b);
-      if (TOP) {
-        h0 = fmaxf(h0, fmaxf(Vec<T>::max1(v[0]), Vec<T>::max1(v[1])));
-        h1 = fmaxf(h1, fmaxf(Vec<T>::max1(v[2]), Vec<T>::max1(v[3])));
-      }
-      const float bm = run.add(v, g);
-      if (TOP) {
-        em = fmaxf(em, bm);
-        if (++in_entry == stride || b + 1 == g.batches) {
-          ts.maxima[entry++][tid] = em;
-          em = -INFINITY;
-          in_entry = 0;
-        }
-      }
+      run.batch(p, dynamic + slot * BATCH * NT + tid, b, g, [&](int q, typename Vec<T>::Most e, typename Vec<T>::Most o) {
+        if (TOP) leaves.group(ts, q, e, o, g.shift);
+      });
       fetch();
-      slot = slot + 1 == SLOTS ? 0 : slot + 1;
+      slot ^= 1;
     }
-    if (TOP) {
-      h1 = fmaxf(h1, edge);
-      ts.halves[tid] = h0 == -INFINITY ? 0u : order_of(h0);          // what counts as -infinity may be a NaN, which stands below
-      ts.halves[NT + tid] = h1 == -INFINITY ? 0u : order_of(h1);
-    }
+    if (TOP) leaves.end(ts, edge);
     Sums s = join<NT, W, CL, false>(run.end(edge, g), ex.part[turn][0], g, rank);
     const Ref ref(s.m, g);
     if (ref.far) s = join<NT, W, CL, true>(sweep_far<T, NT, W>(p, g, s.m, edge), ex.part[turn][1], g, rank);
@@ -704,17 +732,12 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(const __grid_constant__ Lo
         a.top_ids[r * k + at] = (int)~(uint32_t)key;
         a.top_logp[r * k + at] = logp(value_of((uint32_t)(key >> 32)));
       };
-      const int found = top_candidates<T, NT>(p, edge, k, run.m, stride, entry, ts);
+      const int found = top_candidates<T, NT>(p, edge, k, g.shift, ts);
       u64* sorted = CL ? cg::this_cluster().map_shared_rank(&ts.sorted[rank][0], 0) : nullptr;
-      for (int i = tid; i < found; i += NT) {            // a candidate's place is the number of larger ones
-        const u64 key = ts.list[i];
-        int at = 0;
-#pragma unroll 8
-        for (int j = 0; j < found; ++j) at += ts.list[j] > key;
-        if (at >= k) continue;
+      rank_candidates<NT>(ts.list, found, k, [&](int at, u64 key) {
         if (CL) sorted[at] = key;
         else put(at, key);
-      }
+      });
       if constexpr (CL) {
         for (int i = found + tid; i < k; i += NT) sorted[i] = 0;   // fewer logits than k in this piece
         sync_row<true>();
@@ -790,13 +813,13 @@ __device__ __forceinline__ void gradient(const Piece<T, NT>& p, uint4* buf, floa
     return o;
   };
   for (int b = 0; b < g.batches; ++b) {
-    const int v0 = 4 * b * NT + threadIdx.x;
+    const int v0 = BATCH * b * NT + threadIdx.x;
     if (p.whole(b) && aligned) {
       uint4* d = (uint4*)(dst + p.element(v0));
 #pragma unroll
-      for (int u = 0; u < 4; ++u) d[u * NT] = four(one_vector(quad(buf[v0 + u * NT])));
+      for (int u = 0; u < BATCH; ++u) d[u * NT] = four(one_vector(quad(buf[v0 + u * NT])));
     } else {
-      for (int v = v0; v < min(v0 + 4 * NT, p.count); v += NT) p.store(dst, v, one_vector(quad(buf[v])));
+      for (int v = v0; v < min(v0 + BATCH * NT, p.count); v += NT) p.store(dst, v, one_vector(quad(buf[v])));
     }
     if (fetch_next) next.fetch(buf + v0, b);
   }
@@ -809,11 +832,9 @@ __device__ __forceinline__ Sums sweep(const Piece<T, NT>& p, uint4* buf, float e
   Running<T, W> run(g);
   for (int b = 0; b < g.batches; ++b) {
     wait_groups(REFILL ? g.batches - 1 : g.batches - 1 - b);
-    Quad v[4];
-    p.load(v, buf + 4 * b * NT + threadIdx.x, b);
-    run.add(v, g);
+    run.batch(p, buf + BATCH * b * NT + threadIdx.x, b, g, [](int, typename Vec<T>::Most, typename Vec<T>::Most) {});
     if (REFILL) {
-      if (has_next) next.fetch(buf + 4 * b * NT + threadIdx.x, b);
+      if (has_next) next.fetch(buf + BATCH * b * NT + threadIdx.x, b);
       else p.commit();
     }
   }
@@ -821,11 +842,11 @@ __device__ __forceinline__ Sums sweep(const Piece<T, NT>& p, uint4* buf, float e
 }
 
 // Threads that sweep over a row; FEW where rows are short and many.
-constexpr int STAY = 256, FEW = 32;
+constexpr int STAY = 128, FEW = 32;
 
 template <typename T, int NT, bool W, bool CL>
-__global__ void __launch_bounds__(NT, NT == 256 ? 3 : 1) logprobs_bwd_kernel(const __grid_constant__ LogprobsBwdArgs a, const __grid_constant__ Geometry g) {
-  __shared__ Exchange<NT> ex;
+__global__ void __launch_bounds__(NT, NT == STAY ? 4 : 1) logprobs_bwd_kernel(const __grid_constant__ LogprobsBwdArgs a, const __grid_constant__ Geometry g) {
+  __shared__ Exchange<NT, CL> ex;
   cudaGridDependencySynchronize();
   cluster_start<CL>();
   const Place me = Place::of<CL>(g);
@@ -944,9 +965,9 @@ __device__ __forceinline__ void summed() {
 }
 
 template <typename T, int NT, bool CL>
-__global__ void __launch_bounds__(NT + 32, NT == 256 ? 3 : 1) distill_kernel(const __grid_constant__ DistillArgs a, const __grid_constant__ Geometry g) {
+__global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(const __grid_constant__ DistillArgs a, const __grid_constant__ Geometry g) {
   constexpr int N = Vec<T>::N;
-  __shared__ Exchange<NT> ex;
+  __shared__ Exchange<NT, CL> ex;
   __shared__ Lesson lessons[2];               // of two rows in turn
   __shared__ float edges[2 * N];
   __shared__ int claims[CLAIMS];              // the teacher's warp's
@@ -1211,7 +1232,8 @@ Plan plan_rows(const LogitsIn& in, int elem_bytes, int threads, bool stay, size_
   p.smem = (stay ? (size_t)per * 16 : smem) + (c > 1 ? smem_cluster : 0);
   const double cc = 1.4426950408889634 / (double)in.temperature;
   p.g = Geometry{(float)cc, (float)(1.0 / (double)in.temperature), (float)(-1e30 * std::min(1.0, 1.0 / cc)), (float)(SLACK / cc), c, per,
-                 (per + 4 * threads - 1) / (4 * threads)};
+                 (per + BATCH * threads - 1) / (BATCH * threads), 0};
+  while (BATCH / 4 * p.g.batches > ENTRIES << p.g.shift) ++p.g.shift;
   return p;
 }
 
@@ -1278,9 +1300,8 @@ cudaError_t run_logprobs(const LogprobsArgs& a, const Plan& p, cudaStream_t s) {
 template <typename T, int NT, bool W, bool TOP>
 cudaError_t run_logprobs(const LogprobsArgs& a, cudaStream_t s) {
   typedef TopSpace<NT> Top;
-  const size_t ring = SLOTS * 4 * NT * 16;
-  const Plan p = TOP ? plan_rows(a.in, sizeof(T), NT, false, ring + offsetof(Top, sorted), sizeof(Top) - offsetof(Top, sorted))
-                     : plan_rows(a.in, sizeof(T), NT, false, ring, 0);
+  const size_t ring = SLOTS * BATCH * NT * 16, desk = offsetof(Top, sorted);
+  const Plan p = TOP ? plan_rows(a.in, sizeof(T), NT, false, ring + desk, sizeof(Top) - desk) : plan_rows(a.in, sizeof(T), NT, false, ring, 0);
   if constexpr (NT == STREAM)
     if (p.g.cluster > 1) return run_logprobs<T, NT, W, true, TOP>(a, p, s);
   return run_logprobs<T, NT, W, false, TOP>(a, p, s);
