@@ -18,6 +18,7 @@
 // eight blocks, which exchange their sums through distributed shared memory.
 #include <algorithm>
 #include <atomic>
+#include <cfloat>
 #include <cstddef>
 
 #include <cooperative_groups.h>
@@ -37,7 +38,6 @@ constexpr float FAR = 1e23f;
 constexpr float LN2 = 0.693147180559945309f;
 constexpr int MAX_CLUSTER = 8;
 constexpr float SLACK = 8.f;                  // a sum's reference stays while no power of two exceeds 2^SLACK
-constexpr int BATCH = 8;                      // vectors that a thread takes at a time
 constexpr int CANDIDATES = 256;               // of the top alternatives
 
 // ---------------------------------------------------------------------------------------------- two floats at a time
@@ -144,18 +144,24 @@ template <> struct Vec<float> {
 };
 
 // ---------------------------------------------------------------------------------------------- a row's pieces
+// Threads that sweep over a row that passes by, or stays in shared memory for a second pass; FEW where rows are short and many.
+constexpr int STREAM = 128, STAY = 128, FEW = 32;
+// Vectors that a thread takes at a time: fewer steps with eight (scoring 8192 rows of 32768 in bf16 84.5 us against 89.6), more blocks
+// on an SM and less left over in short rows with four (the same with 64 alternatives 157 against 167, 16384 rows of 512 30 against 36).
+__host__ __device__ constexpr int batch_of(int threads, bool top) { return threads == FEW || top ? 4 : 8; }
+
 struct Geometry {
   float c, inv_t;                             // log2(e) / T, 1 / T
   float lo;                                   // logits below it have probability 0 in rows that are not far
   float slack;                                // SLACK in units of a logit
-  int cluster, per, batches;                  // blocks per row, vectors of a block's piece, batches of BATCH NT of them
+  int cluster, per, batches;                  // blocks per row, vectors of a block's piece, batches of them
   int shift;                                  // log2 of the fours of vectors of which a thread leaves one maximum
 };
 
 // A block's piece of a row.  Its vectors are those aligned 16 bytes that lie in the row as a whole, `first` .. `first` +
 // `count` of them here; element j of the row's ends, which no vector holds, belongs to one thread of the first block.
-// Thread t works on vectors t, t + NT, ..., eight to a batch, and nobody else sees its copies of them.
-template <typename T, int NT>
+// Thread t works on vectors t, t + NT, ..., B to a batch, and nobody else sees its copies of them.
+template <typename T, int NT, int B>
 struct Piece {
   static constexpr int N = Vec<T>::N;
   const T* x;                                 // the row
@@ -169,26 +175,26 @@ struct Piece {
     edge = rank != 0 ? -1 : t < head ? t : t - head < n - tail ? tail + t - head : -1;
   }
   __device__ __forceinline__ int element(int v) const { return head + (first + v) * N; }     // the first of vector v
-  __device__ __forceinline__ bool whole(int b) const { return (b + 1) * BATCH * NT <= count; }
+  __device__ __forceinline__ bool whole(int b) const { return (b + 1) * B * NT <= count; }
   // Asks for batch b: its vectors u arrive at to[u * NT].  One group of copies, of nothing for b beyond the piece.
   __device__ __forceinline__ void fetch(uint4* to, int b) const {
-    const int v = BATCH * b * NT + threadIdx.x;
+    const int v = B * b * NT + threadIdx.x;
     const uint32_t d = (uint32_t)__cvta_generic_to_shared(to);
     const T* s = x + element(v);
     if (whole(b)) {
 #pragma unroll
-      for (int u = 0; u < BATCH; ++u)
+      for (int u = 0; u < B; ++u)
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d + u * NT * 16), "l"(s + u * NT * N) : "memory");
     } else {
 #pragma unroll
-      for (int u = 0; u < BATCH; ++u)
+      for (int u = 0; u < B; ++u)
         if (v + u * NT < count) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d + u * NT * 16), "l"(s + u * NT * N) : "memory");
     }
     commit();
   }
   __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
   __device__ __forceinline__ void fetch_all(uint4* buf, const Geometry& g) const {
-    for (int b = 0; b < g.batches; ++b) fetch(buf + BATCH * b * NT + threadIdx.x, b);
+    for (int b = 0; b < g.batches; ++b) fetch(buf + B * b * NT + threadIdx.x, b);
   }
   __device__ __forceinline__ float edge_value() const { return edge >= 0 ? to_f(x[edge]) : -INFINITY; }
   __device__ __forceinline__ void store(T* dst, int v, const Quad& r) const {
@@ -265,33 +271,43 @@ struct Running {
       }
     }
   }
-  // Adds batch b, which has arrived; leaf(group, maximum of even vectors, of odd ones) hears of every four vectors.
-  template <int NT, typename Leaf>
-  __device__ __forceinline__ void batch(const Piece<T, NT>& p, const uint4* from, int b, const Geometry& g, Leaf leaf) {
+  // Adds batch b, which has arrived; leaf(four, maximum of its even vectors, of the odd ones) hears of every four vectors.
+  // The reference goes by fours whatever the batch, so that kernels of other batches give the same bits.
+  template <int NT, int B, typename Leaf>
+  __device__ __forceinline__ void batch(const Piece<T, NT, B>& p, const uint4* from, int b, const Geometry& g, Leaf leaf) {
     typedef Vec<T> V;
+    auto four = [&](Quad (&a)[4], int q) {
+      const typename V::Most e = V::more(V::most(a[0]), V::most(a[2])), o = V::more(V::most(a[1]), V::most(a[3]));
+      leaf(q, e, o);
+      add<4>(a, V::value(V::more(e, o)), g);
+    };
     if (p.whole(b)) {
-      Quad a[BATCH];
+      Quad a[B / 4][4];
 #pragma unroll
-      for (int u = 0; u < BATCH; ++u) a[u] = quad(from[u * NT]);
-      typename V::Most e[2], o[2];
+      for (int u = 0; u < B; ++u) a[u / 4][u % 4] = quad(from[u * NT]);
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        e[q] = V::more(V::most(a[4 * q]), V::most(a[4 * q + 2]));
-        o[q] = V::more(V::most(a[4 * q + 1]), V::most(a[4 * q + 3]));
-        leaf(2 * b + q, e[q], o[q]);
-      }
-      add<BATCH>(a, V::value(V::more(V::more(e[0], o[0]), V::more(e[1], o[1]))), g);
+      for (int q = 0; q < B / 4; ++q) four(a[q], B / 4 * b + q);
     } else {
       const int first = threadIdx.x & ~31;               // of the warp: what no lane has is left out
 #pragma unroll 1
-      for (int u = 0; u < BATCH; ++u) {
-        const int v = (BATCH * b + u) * NT;
-        if (v + first >= p.count) break;
-        Quad a[1] = {nothing<T>()};
-        if (v + (int)threadIdx.x < p.count) a[0] = quad(from[u * NT]);
-        const typename V::Most m = V::most(a[0]);
-        leaf(2 * b + u / 4, u & 1 ? V::lowest() : m, u & 1 ? m : V::lowest());
-        add<1>(a, V::value(m), g);
+      for (int q = B / 4 * b; q < B / 4 * (b + 1); ++q, from += 4 * NT) {
+        if (4 * (q + 1) * NT <= p.count) {
+          Quad a[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) a[u] = quad(from[u * NT]);
+          four(a, q);
+          continue;
+        }
+#pragma unroll 1
+        for (int u = 0; u < 4; ++u) {
+          const int v = (4 * q + u) * NT;
+          if (v + first >= p.count) return;
+          Quad a[1] = {nothing<T>()};
+          if (v + (int)threadIdx.x < p.count) a[0] = quad(from[u * NT]);
+          const typename V::Most m = V::most(a[0]);
+          leaf(q, u & 1 ? V::lowest() : m, u & 1 ? m : V::lowest());
+          add<1>(a, V::value(m), g);
+        }
       }
     }
   }
@@ -314,8 +330,8 @@ struct Running {
 };
 
 // The same against the row's maximum, for far rows, one element after the other, without the `k` tokens of `skip`.
-template <typename T, int NT, bool W>
-__device__ __noinline__ Sums sweep_far(const Piece<T, NT> p, const Geometry g, float m, float edge, const int* skip = nullptr, int k = 0) {
+template <typename T, int NT, int B, bool W>
+__device__ __noinline__ Sums sweep_far(const Piece<T, NT, B> p, const Geometry g, float m, float edge, const int* skip = nullptr, int k = 0) {
   Sums a{m, 0.f, 0.f};
   auto add = [&](float x) {
     if (x == -INFINITY) return;
@@ -424,8 +440,9 @@ struct Ref {
                                                               far(m_ != -INFINITY && !(fabsf(m_) * g.c <= FAR)) {}
   __device__ __forceinline__ bool apart(float x) const { return far || fabsf(x) * c > FAR; }
   __device__ __forceinline__ float y(float x) const { return far ? (x - m) * c : fmaf(x, c, -rho); }
-  // (x - m) / T, of a masked token's lowest value too
+  // (x - m) / T, of a masked token's lowest value too, and v above it
   __device__ __forceinline__ float nat(float x) const { return apart(x) ? (x - m) * inv_t : fmaf(x, c, -rho) * LN2; }
+  __device__ __forceinline__ float above(float v, float x) const { return apart(x) ? v - (x - m) * inv_t : fmaf(-fmaf(x, c, -rho), LN2, v); }
 };
 
 extern __shared__ uint4 dynamic[];
@@ -440,6 +457,13 @@ __device__ __forceinline__ void cluster_started() {
     __syncwarp();
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
   }
+}
+
+// log v to about 3e-8 whatever its size: the exponent's part in 64 bits.
+__device__ __forceinline__ double log_wide(float v) {
+  if (!(v >= FLT_MIN && v <= FLT_MAX)) return (double)logf(v);
+  const int bits = __float_as_int(v) - 0x3f400000, e = bits >> 23;       // v = 2^e f, f from 0.75 to 1.5
+  return (double)e * 0.693147180559945309417 + (double)logf(__int_as_float((bits & 0x7fffff) + 0x3f400000));
 }
 
 // A token id, or -1 where there is none.
@@ -515,8 +539,8 @@ __device__ __forceinline__ uint32_t bound_of(const uint32_t* values, int k) {
 //   reaches it are read again, and only elements of those that do are compared.
 //   Where more than CANDIDATES logits reach it (many equal ones, or large ones side by side), the bound is raised by halving
 //   until they fit, or until it is the k-th largest value itself, of which those with the lowest ids are taken.
-template <typename T, int NT>
-__device__ int top_candidates(const Piece<T, NT>& p, float edge, int k, int shift, TopSpace<NT>& ts) {
+template <typename T, int NT, int B>
+__device__ int top_candidates(const Piece<T, NT, B>& p, float edge, int k, int shift, TopSpace<NT>& ts) {
   constexpr int N = Vec<T>::N, AT_ONCE = 3;
   constexpr uint32_t NOTHING = 0x007fffffu;              // the order of -infinity; maxima of it may hide a NaN, which stands below
   const int t = threadIdx.x, per = 4 << shift, entries = (p.count + per * NT - 1) / (per * NT);
@@ -666,28 +690,29 @@ struct Leaves {
   }
 };
 
-constexpr int STREAM = 128, SLOTS = 2;        // threads of a block that reads its rows once; batches that it has on their way
+constexpr int SLOTS = 2;        // threads of a block that reads its rows once; batches that it has on their way
 
 // Batches pass through a ring of SLOTS, each thread's by itself: copies run ahead of the sums by SLOTS batches, over the end of
 // a row into the next ones, so that they go on while a row's sums are joined and handed out.
 template <typename T, int NT, bool W, bool CL, bool TOP>
 __global__ void __launch_bounds__(NT) logprobs_kernel(const __grid_constant__ LogprobsArgs a, const __grid_constant__ Geometry g) {
+  constexpr int B = batch_of(NT, TOP);
   __shared__ Exchange<NT, CL> ex;
   cudaGridDependencySynchronize();
   cluster_start<CL>();
   const Place me = Place::of<CL>(g);
   const int rank = me.rank, tid = threadIdx.x, rows = a.in.rows;
   const bool speaks = rank == 0 && tid == 0;             // for the row
-  Piece<T, NT> p(a.in, me.row, rank, g), ahead = p;
+  Piece<T, NT, B> p(a.in, me.row, rank, g), ahead = p;
   long long ahead_row = me.row;
   int ahead_batch = 0, slot = 0;
   auto fetch = [&]() {
     if (ahead_row >= rows) return p.commit();
-    ahead.fetch(dynamic + slot * BATCH * NT + tid, ahead_batch);
+    ahead.fetch(dynamic + slot * B * NT + tid, ahead_batch);
     if (++ahead_batch == g.batches) {
       ahead_batch = 0;
       ahead_row += me.groups;
-      if (ahead_row < rows) ahead = Piece<T, NT>(a.in, ahead_row, rank, g);
+      if (ahead_row < rows) ahead = Piece<T, NT, B>(a.in, ahead_row, rank, g);
     }
   };
   for (; slot < SLOTS; ++slot) fetch();
@@ -697,18 +722,18 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(const __grid_constant__ Lo
   int t = speaks && a.tokens ? token_of(a.tokens, me.row, a.in.vocab, a.in.out_of_range, true) : -1;
   float xt = t >= 0 ? to_f(p.x[t]) : 0.f;
   cluster_started<CL>();
-  TopSpace<NT>& ts = *(TopSpace<NT>*)(dynamic + SLOTS * BATCH * NT);
+  TopSpace<NT>& ts = *(TopSpace<NT>*)(dynamic + SLOTS * B * NT);
   int turn = 0;
   for (long long r = me.row; r < rows; r += me.groups, turn ^= 1) {
     const bool has_next = r + me.groups < rows;
-    const Piece<T, NT> next(a.in, has_next ? r + me.groups : r, rank, g);
+    const Piece<T, NT, B> next(a.in, has_next ? r + me.groups : r, rank, g);
     const float next_edge = next.edge_value();
     const int next_t = speaks && a.tokens && has_next ? token_of(a.tokens, r + me.groups, a.in.vocab, a.in.out_of_range, true) : -1;
     Running<T, W> run(g);
     Leaves<T, NT> leaves;
     for (int b = 0; b < g.batches; ++b) {
       wait_groups(SLOTS - 1);
-      run.batch(p, dynamic + slot * BATCH * NT + tid, b, g, [&](int q, typename Vec<T>::Most e, typename Vec<T>::Most o) {
+      run.batch(p, dynamic + slot * B * NT + tid, b, g, [&](int q, typename Vec<T>::Most e, typename Vec<T>::Most o) {
         if (TOP) leaves.group(ts, q, e, o, g.shift);
       });
       fetch();
@@ -717,7 +742,7 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(const __grid_constant__ Lo
     if (TOP) leaves.end(ts, edge);
     Sums s = join<NT, W, CL, false>(run.end(edge, g), ex.part[turn][0], g, rank);
     const Ref ref(s.m, g);
-    if (ref.far) s = join<NT, W, CL, true>(sweep_far<T, NT, W>(p, g, s.m, edge), ex.part[turn][1], g, rank);
+    if (ref.far) s = join<NT, W, CL, true>(sweep_far<T, NT, B, W>(p, g, s.m, edge), ex.part[turn][1], g, rank);
     const float logs = logf(s.s);
     auto logp = [&](float v) { return s.s == 0.f ? -INFINITY : ref.nat(v) - logs; };
     const float next_xt = next_t >= 0 ? to_f(next.x[next_t]) : 0.f;
@@ -732,7 +757,7 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(const __grid_constant__ Lo
         a.top_ids[r * k + at] = (int)~(uint32_t)key;
         a.top_logp[r * k + at] = logp(value_of((uint32_t)(key >> 32)));
       };
-      const int found = top_candidates<T, NT>(p, edge, k, g.shift, ts);
+      const int found = top_candidates<T, NT, B>(p, edge, k, g.shift, ts);
       u64* sorted = CL ? cg::this_cluster().map_shared_rank(&ts.sorted[rank][0], 0) : nullptr;
       rank_candidates<NT>(ts.list, found, k, [&](int at, u64 key) {
         if (CL) sorted[at] = key;
@@ -771,9 +796,9 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(const __grid_constant__ Lo
 }
 
 // The row's second pass: dst = 2^y (k0 + k1 y), a token's own term added; the next row takes the place.
-template <typename T, int NT, bool W>
-__device__ __forceinline__ void gradient(const Piece<T, NT>& p, uint4* buf, float edge, const Geometry& g, const Ref& ref, float k0, float k1,
-                                         int t, float at_t, T* dst, const Piece<T, NT>& next, bool fetch_next) {
+template <typename T, int NT, int B, bool W>
+__device__ __forceinline__ void gradient(const Piece<T, NT, B>& p, uint4* buf, float edge, const Geometry& g, const Ref& ref, float k0, float k1,
+                                         int t, float at_t, T* dst, const Piece<T, NT, B>& next, bool fetch_next) {
   constexpr int N = Vec<T>::N;
   auto one = [&](float x, int j) {
     const float y = ref.y(W && !ref.far ? max_nan(x, g.lo) : x), e = ex2(y);
@@ -813,13 +838,13 @@ __device__ __forceinline__ void gradient(const Piece<T, NT>& p, uint4* buf, floa
     return o;
   };
   for (int b = 0; b < g.batches; ++b) {
-    const int v0 = BATCH * b * NT + threadIdx.x;
+    const int v0 = B * b * NT + threadIdx.x;
     if (p.whole(b) && aligned) {
       uint4* d = (uint4*)(dst + p.element(v0));
 #pragma unroll
-      for (int u = 0; u < BATCH; ++u) d[u * NT] = four(one_vector(quad(buf[v0 + u * NT])));
+      for (int u = 0; u < B; ++u) d[u * NT] = four(one_vector(quad(buf[v0 + u * NT])));
     } else {
-      for (int v = v0; v < min(v0 + BATCH * NT, p.count); v += NT) p.store(dst, v, one_vector(quad(buf[v])));
+      for (int v = v0; v < min(v0 + B * NT, p.count); v += NT) p.store(dst, v, one_vector(quad(buf[v])));
     }
     if (fetch_next) next.fetch(buf + v0, b);
   }
@@ -827,25 +852,24 @@ __device__ __forceinline__ void gradient(const Piece<T, NT>& p, uint4* buf, floa
 }
 
 // The sums of a row whose batches all have their place: they stay, or as they are read make room for those of the next row.
-template <typename T, int NT, bool W, bool REFILL>
-__device__ __forceinline__ Sums sweep(const Piece<T, NT>& p, uint4* buf, float edge, const Geometry& g, const Piece<T, NT>& next, bool has_next) {
+template <typename T, int NT, int B, bool W, bool REFILL>
+__device__ __forceinline__ Sums sweep(const Piece<T, NT, B>& p, uint4* buf, float edge, const Geometry& g, const Piece<T, NT, B>& next, bool has_next) {
   Running<T, W> run(g);
   for (int b = 0; b < g.batches; ++b) {
     wait_groups(REFILL ? g.batches - 1 : g.batches - 1 - b);
-    run.batch(p, buf + BATCH * b * NT + threadIdx.x, b, g, [](int, typename Vec<T>::Most, typename Vec<T>::Most) {});
+    run.batch(p, buf + B * b * NT + threadIdx.x, b, g, [](int, typename Vec<T>::Most, typename Vec<T>::Most) {});
     if (REFILL) {
-      if (has_next) next.fetch(buf + BATCH * b * NT + threadIdx.x, b);
+      if (has_next) next.fetch(buf + B * b * NT + threadIdx.x, b);
       else p.commit();
     }
   }
   return run.end(edge, g);
 }
 
-// Threads that sweep over a row; FEW where rows are short and many.
-constexpr int STAY = 128, FEW = 32;
 
 template <typename T, int NT, bool W, bool CL>
 __global__ void __launch_bounds__(NT, NT == STAY ? 4 : 1) logprobs_bwd_kernel(const __grid_constant__ LogprobsBwdArgs a, const __grid_constant__ Geometry g) {
+  constexpr int B = batch_of(NT, false);
   __shared__ Exchange<NT, CL> ex;
   cudaGridDependencySynchronize();
   cluster_start<CL>();
@@ -865,7 +889,7 @@ __global__ void __launch_bounds__(NT, NT == STAY ? 4 : 1) logprobs_bwd_kernel(co
     }
     return i;
   };
-  Piece<T, NT> p(a.in, me.row, rank, g);
+  Piece<T, NT, B> p(a.in, me.row, rank, g);
   In in = incoming(me.row);
   if (in.any()) p.fetch_all(buf, g);
   float edge = p.edge_value();
@@ -873,21 +897,21 @@ __global__ void __launch_bounds__(NT, NT == STAY ? 4 : 1) logprobs_bwd_kernel(co
   int turn = 0;
   for (long long r = me.row; r < rows; r += me.groups, turn ^= 1) {
     const long long rn = r + me.groups < rows ? r + me.groups : r;
-    const Piece<T, NT> next(a.in, rn, rank, g);
+    const Piece<T, NT, B> next(a.in, rn, rank, g);
     const In next_in = incoming(rn);
     const float next_edge = next.edge_value();
     T* dx = (T*)a.dx + r * a.ld_out;
     if (in.any()) {
-      Sums s = join<NT, W, CL, false>(sweep<T, NT, W, false>(p, buf, edge, g, next, false), ex.part[turn][0], g, rank);
+      Sums s = join<NT, W, CL, false>(sweep<T, NT, B, W, false>(p, buf, edge, g, next, false), ex.part[turn][0], g, rank);
       const Ref ref(s.m, g);
-      if (ref.far) s = join<NT, W, CL, true>(sweep_far<T, NT, W>(p, g, s.m, edge), ex.part[turn][1], g, rank);
+      if (ref.far) s = join<NT, W, CL, true>(sweep_far<T, NT, B, W>(p, g, s.m, edge), ex.part[turn][1], g, rank);
       const bool more = rn != r && next_in.any();
       if (s.s == 0.f) {                                  // no token
         p.zeros(dx);
         if (more) next.fetch_all(buf, g);
       } else {
         const float k = g.inv_t / s.s;
-        gradient<T, NT, W>(p, buf, edge, g, ref, W ? (in.gl - in.ga + in.gb * (LN2 * (s.w / s.s))) * k : (in.gl - in.ga) * k, -in.gb * LN2 * k, in.t,
+        gradient<T, NT, B, W>(p, buf, edge, g, ref, W ? (in.gl - in.ga + in.gb * (LN2 * (s.w / s.s))) * k : (in.gl - in.ga) * k, -in.gb * LN2 * k, in.t,
                        in.ga * g.inv_t, dx, next, more);
       }
     } else {
@@ -966,7 +990,7 @@ __device__ __forceinline__ void summed() {
 
 template <typename T, int NT, bool CL>
 __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(const __grid_constant__ DistillArgs a, const __grid_constant__ Geometry g) {
-  constexpr int N = Vec<T>::N;
+  constexpr int N = Vec<T>::N, B = batch_of(NT, false);
   __shared__ Exchange<NT, CL> ex;
   __shared__ Lesson lessons[2];               // of two rows in turn
   __shared__ float edges[2 * N];
@@ -976,7 +1000,7 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
   const Place me = Place::of<CL>(g);
   const int rank = me.rank, lane = threadIdx.x & 31, rows = a.in.rows;
   uint4* buf = dynamic;
-  Piece<T, NT> p(a.in, me.row, rank, g);
+  Piece<T, NT, B> p(a.in, me.row, rank, g);
   int turn = 0;
 
   if (threadIdx.x < NT) {
@@ -985,7 +1009,7 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
     cluster_started<CL>();
     for (long long r = me.row; r < rows; r += me.groups, turn ^= 1) {
       const bool has_next = r + me.groups < rows;
-      const Piece<T, NT> next(a.in, has_next ? r + me.groups : r, rank, g);
+      const Piece<T, NT, B> next(a.in, has_next ? r + me.groups : r, rank, g);
       const float next_edge = next.edge_value(), dl = a.dloss ? a.dloss[r] : 1.f;
       if (a.rest) {                                      // the listed tokens leave the row
         wait_groups(0);
@@ -994,12 +1018,12 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
         await<NT>(PATCHED);
         if (p.edge >= 0) edge = edges[threadIdx.x];
       }
-      leave_part<NT, false, CL>(a.dx ? sweep<T, NT, false, false>(p, buf, edge, g, next, false) : sweep<T, NT, false, true>(p, buf, edge, g, next, has_next),
+      leave_part<NT, false, CL>(a.dx ? sweep<T, NT, B, false, false>(p, buf, edge, g, next, false) : sweep<T, NT, B, false, true>(p, buf, edge, g, next, has_next),
                                 ex.part[turn][0], g, rank);
       summed<NT, CL>();
       Sums o = take_parts<NT, false, CL, false>(ex.part[turn][0], g);
       const Lesson& l = lessons[turn];
-      if (Ref(o.m, g).far) o = join<NT, false, CL, true>(sweep_far<T, NT, false>(p, g, o.m, edge, l.id, a.rest ? a.k : 0), ex.part[turn][1], g, rank);
+      if (Ref(o.m, g).far) o = join<NT, false, CL, true>(sweep_far<T, NT, B, false>(p, g, o.m, edge, l.id, a.rest ? a.k : 0), ex.part[turn][1], g, rank);
       if (a.dx) {
         T* dx = (T*)a.dx + r * a.ld_out;
         if (!l.any || dl == 0.f) {
@@ -1008,7 +1032,7 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
         } else {
           const Weighed s(o, l, a.rest, g);
           const float kappa = s.S != s.S ? s.S : o.s == 0.f ? 0.f : (l.Q * s.f / s.S - (l.qr > 0.f ? l.qr / o.s : 0.f)) * (dl * a.scale * g.inv_t);
-          gradient<T, NT, false>(p, buf, edge, g, s.ro, kappa, 0.f, -1, 0.f, dx, next, has_next);
+          gradient<T, NT, B, false>(p, buf, edge, g, s.ro, kappa, 0.f, -1, 0.f, dx, next, has_next);
         }
         arrive<NT>(WRITTEN);                             // the listed tokens' gradient goes over it
       }
@@ -1020,7 +1044,7 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
   }
 
   struct Entries { int id[PER_LANE]; float t[PER_LANE], x[PER_LANE]; };       // token, teacher's value, student's logit
-  struct Weights { float q[PER_LANE], lq[PER_LANE]; unsigned first; bool twins; };
+  struct Weights { float q[PER_LANE], lq[PER_LANE]; double all, shift; unsigned first; bool twins; };   // log q = lq - shift, all: sum q
   const int used = (a.k + 31) / 32;                      // entries per lane
   auto read = [&](long long r, Entries& e) {
 #pragma unroll
@@ -1078,13 +1102,15 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
       w.first |= 1u << i;
     }
     for (int o = 16; o > 0; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
-    const float scale = a.rest ? 1.f : 1.f / (float)mass, shift = a.rest ? 0.f : logf((float)mass);
+    const float scale = a.rest ? 1.f : 1.f / (float)mass;
+    w.all = a.rest ? mass : mass == mass ? 1.0 : mass;
+    w.shift = a.rest || !a.loss ? 0.0 : log_wide((float)mass);
 #pragma unroll
     for (int i = 0; i < PER_LANE; ++i) {
       if (i >= used) break;
       if (claim[i] >= 0) claims[claim[i]] = 0;
       w.q[i] *= scale;
-      w.lq[i] = fmaf(e.t[i] - mt, by, -shift);
+      w.lq[i] = (e.t[i] - mt) * by;
     }
     w.twins = __any_sync(0xffffffffu, w.twins);          // then the first entry stands for the token
     if (w.twins)
@@ -1113,8 +1139,8 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
     }
     __syncwarp();
   };
-  auto beyond = [&](const Piece<T, NT>& p) { return a.in.vocab - (a.in.vocab - p.head) % N; };   // from here on in no vector
-  auto patch = [&](const Piece<T, NT>& p, const Entries& e) {
+  auto beyond = [&](const Piece<T, NT, B>& p) { return a.in.vocab - (a.in.vocab - p.head) % N; };   // from here on in no vector
+  auto patch = [&](const Piece<T, NT, B>& p, const Entries& e) {
     await<NT>(LANDED);
     const int end = beyond(p);
 #pragma unroll
@@ -1144,7 +1170,7 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
   for (long long r = me.row; r < rows; r += me.groups, turn ^= 1) {
     const Lesson& l = lessons[turn];
     const bool has_next = r + me.groups < rows;
-    const Piece<T, NT> next(a.in, has_next ? r + me.groups : r, rank, g);
+    const Piece<T, NT, B> next(a.in, has_next ? r + me.groups : r, rank, g);
     const float dl = a.dloss ? a.dloss[r] : 1.f;
     Entries coming;
     Weights next_w;
@@ -1163,19 +1189,21 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
     if (!a.dx && a.rest && has_next) patch(next, later);
     const Weighed s(o, l, a.rest, g);
     if (a.loss && rank == 0) {
-      const float logs = logf(s.S);
-      float loss = 0.f;
+      // sum q ((lq - y ln 2) + (log S - shift)): what the logarithms are large in they share with one another
+      float part = 0.f;
 #pragma unroll
       for (int i = 0; i < PER_LANE; ++i) {
         if (i >= used) break;
-        if (now.id[i] >= 0 && !(w.q[i] == 0.f)) loss += w.q[i] * (w.lq[i] - (s.S == 0.f ? -INFINITY : s.ref.nat(now.x[i]) - logs));
+        if (now.id[i] >= 0 && !(w.q[i] == 0.f)) part += w.q[i] * s.ref.above(w.lq[i], now.x[i]);
       }
-      loss = warp_sum(loss);
-      if (l.qr > 0.f) {
+      part = warp_sum(part);
+      const double logs = log_wide(s.S);
+      double loss = s.S == 0.f ? (double)INFINITY : (double)part + w.all * (logs - w.shift);
+      if (l.qr > 0.f && s.S != 0.f) {
         const float lr = s.ref.far || s.ro.far ? (o.m - s.ref.m) * g.inv_t : (s.ro.rho - s.ref.rho) * LN2;
-        loss += l.qr * (logf(l.qr) - (o.s == 0.f ? -INFINITY : lr + logf(o.s) - logs));
+        loss += (double)l.qr * ((log_wide(l.qr) - log_wide(o.s)) - ((double)lr - logs));
       }
-      if (lane == 0) a.loss[r] = l.any ? a.scale * loss : 0.f;
+      if (lane == 0) a.loss[r] = l.any ? (float)((double)a.scale * loss) : 0.f;
     }
     if (a.dx) {
       await<NT>(WRITTEN);
@@ -1221,7 +1249,7 @@ struct Plan {
   size_t smem;
 };
 // Blocks of `threads` (and more_threads); stay: rows stay in shared memory as a whole, otherwise it takes `smem` bytes.
-Plan plan_rows(const LogitsIn& in, int elem_bytes, int threads, bool stay, size_t smem, size_t smem_cluster, int more_threads = 0) {
+Plan plan_rows(const LogitsIn& in, int elem_bytes, int threads, int batch, bool stay, size_t smem, size_t smem_cluster, int more_threads = 0) {
   Plan p{};
   const int N = 16 / elem_bytes, all = std::max(1, in.vocab / N);
   int c = stay ? std::min(MAX_CLUSTER, (all + PIECE - 1) / PIECE) : 1;
@@ -1232,8 +1260,8 @@ Plan plan_rows(const LogitsIn& in, int elem_bytes, int threads, bool stay, size_
   p.smem = (stay ? (size_t)per * 16 : smem) + (c > 1 ? smem_cluster : 0);
   const double cc = 1.4426950408889634 / (double)in.temperature;
   p.g = Geometry{(float)cc, (float)(1.0 / (double)in.temperature), (float)(-1e30 * std::min(1.0, 1.0 / cc)), (float)(SLACK / cc), c, per,
-                 (per + BATCH * threads - 1) / (BATCH * threads), 0};
-  while (BATCH / 4 * p.g.batches > ENTRIES << p.g.shift) ++p.g.shift;
+                 (per + batch * threads - 1) / (batch * threads), 0};
+  while (batch / 4 * p.g.batches > ENTRIES << p.g.shift) ++p.g.shift;
   return p;
 }
 
@@ -1300,8 +1328,9 @@ cudaError_t run_logprobs(const LogprobsArgs& a, const Plan& p, cudaStream_t s) {
 template <typename T, int NT, bool W, bool TOP>
 cudaError_t run_logprobs(const LogprobsArgs& a, cudaStream_t s) {
   typedef TopSpace<NT> Top;
-  const size_t ring = SLOTS * BATCH * NT * 16, desk = offsetof(Top, sorted);
-  const Plan p = TOP ? plan_rows(a.in, sizeof(T), NT, false, ring + desk, sizeof(Top) - desk) : plan_rows(a.in, sizeof(T), NT, false, ring, 0);
+  constexpr int B = batch_of(NT, TOP);
+  const size_t ring = SLOTS * B * NT * 16, desk = offsetof(Top, sorted);
+  const Plan p = TOP ? plan_rows(a.in, sizeof(T), NT, B, false, ring + desk, sizeof(Top) - desk) : plan_rows(a.in, sizeof(T), NT, B, false, ring, 0);
   if constexpr (NT == STREAM)
     if (p.g.cluster > 1) return run_logprobs<T, NT, W, true, TOP>(a, p, s);
   return run_logprobs<T, NT, W, false, TOP>(a, p, s);
@@ -1318,8 +1347,8 @@ cudaError_t run_bwd(const LogprobsBwdArgs& a, const Plan& p, cudaStream_t s) {
 }
 template <typename T, bool W>
 cudaError_t run_bwd(const LogprobsBwdArgs& a, cudaStream_t s) {
-  if (short_rows(a.in, sizeof(T))) return run_bwd<T, FEW, W, false>(a, plan_rows(a.in, sizeof(T), FEW, true, 0, 0), s);
-  const Plan p = plan_rows(a.in, sizeof(T), STAY, true, 0, 0);
+  if (short_rows(a.in, sizeof(T))) return run_bwd<T, FEW, W, false>(a, plan_rows(a.in, sizeof(T), FEW, batch_of(FEW, false), true, 0, 0), s);
+  const Plan p = plan_rows(a.in, sizeof(T), STAY, batch_of(STAY, false), true, 0, 0);
   return p.g.cluster > 1 ? run_bwd<T, STAY, W, true>(a, p, s) : run_bwd<T, STAY, W, false>(a, p, s);
 }
 
@@ -1330,8 +1359,8 @@ cudaError_t run_distill(const DistillArgs& a, const Plan& p, cudaStream_t s) {
 }
 template <typename T>
 cudaError_t run_distill(const DistillArgs& a, cudaStream_t s) {
-  if (short_rows(a.in, sizeof(T))) return run_distill<T, FEW, false>(a, plan_rows(a.in, sizeof(T), FEW, true, 0, 0, 32), s);
-  const Plan p = plan_rows(a.in, sizeof(T), STAY, true, 0, 0, 32);
+  if (short_rows(a.in, sizeof(T))) return run_distill<T, FEW, false>(a, plan_rows(a.in, sizeof(T), FEW, batch_of(FEW, false), true, 0, 0, 32), s);
+  const Plan p = plan_rows(a.in, sizeof(T), STAY, batch_of(STAY, false), true, 0, 0, 32);
   return p.g.cluster > 1 ? run_distill<T, STAY, true>(a, p, s) : run_distill<T, STAY, false>(a, p, s);
 }
 
