@@ -1249,11 +1249,17 @@ struct Plan {
   size_t smem;
 };
 // Blocks of `threads` (and more_threads); stay: rows stay in shared memory as a whole, otherwise it takes `smem` bytes.
-Plan plan_rows(const LogitsIn& in, int elem_bytes, int threads, int batch, bool stay, size_t smem, size_t smem_cluster, int more_threads = 0) {
+Plan plan_rows(const LogitsIn& in, int elem_bytes, int threads, int batch, bool stay, bool top, size_t smem, size_t smem_cluster, int more_threads = 0) {
   Plan p{};
   const int N = 16 / elem_bytes, all = std::max(1, in.vocab / N);
   int c = stay ? std::min(MAX_CLUSTER, (all + PIECE - 1) / PIECE) : 1;
-  while (threads > FEW && 2 * c <= MAX_CLUSTER && (long long)in.rows * c < 2 * 148 && all / (2 * c) >= 256) c *= 2;
+  // More blocks for rows too few for the device, where a piece is still worth the exchange: four to an SM of pieces of 64 KB,
+  // one to an SM of 16 KB where no alternatives have to be joined.
+  auto split = [&](int blocks, int vectors) {
+    while (threads > FEW && 2 * c <= MAX_CLUSTER && (long long)in.rows * c < blocks && all / (2 * c) >= vectors) c *= 2;
+  };
+  split(4 * 148, 4096);
+  if (!top) split(148, 1024);
   const int per = (all + c - 1) / c;
   p.rows = in.rows;
   p.threads = threads + more_threads;
@@ -1308,8 +1314,8 @@ struct Residency {
   }
 };
 
-// Rows of at most 16 KB, enough of them to give every warp of the device one.
-bool short_rows(const LogitsIn& in, size_t elem_bytes) { return in.vocab * elem_bytes <= 16384 && in.rows >= 148 * 8; }
+// Rows of at most `limit` bytes, enough of them to give every warp of the device one.
+bool short_rows(const LogitsIn& in, size_t elem_bytes, size_t limit) { return in.vocab * elem_bytes <= limit && in.rows >= 148 * 8; }
 
 template <typename... KArgs, typename A>
 cudaError_t run(void (*kernel)(KArgs...), Residency& residency, const Plan& p, cudaStream_t s, const A& a) {
@@ -1330,14 +1336,14 @@ cudaError_t run_logprobs(const LogprobsArgs& a, cudaStream_t s) {
   typedef TopSpace<NT> Top;
   constexpr int B = batch_of(NT, TOP);
   const size_t ring = SLOTS * B * NT * 16, desk = offsetof(Top, sorted);
-  const Plan p = TOP ? plan_rows(a.in, sizeof(T), NT, B, false, ring + desk, sizeof(Top) - desk) : plan_rows(a.in, sizeof(T), NT, B, false, ring, 0);
+  const Plan p = TOP ? plan_rows(a.in, sizeof(T), NT, B, false, true, ring + desk, sizeof(Top) - desk) : plan_rows(a.in, sizeof(T), NT, B, false, false, ring, 0);
   if constexpr (NT == STREAM)
     if (p.g.cluster > 1) return run_logprobs<T, NT, W, true, TOP>(a, p, s);
   return run_logprobs<T, NT, W, false, TOP>(a, p, s);
 }
 template <typename T, bool W>
 cudaError_t run_logprobs(const LogprobsArgs& a, cudaStream_t s) {
-  if (short_rows(a.in, sizeof(T)) && a.top_k <= FEW) return a.top_k > 0 ? run_logprobs<T, FEW, W, true>(a, s) : run_logprobs<T, FEW, W, false>(a, s);
+  if (short_rows(a.in, sizeof(T), 16384) && a.top_k <= FEW) return a.top_k > 0 ? run_logprobs<T, FEW, W, true>(a, s) : run_logprobs<T, FEW, W, false>(a, s);
   return a.top_k > 0 ? run_logprobs<T, STREAM, W, true>(a, s) : run_logprobs<T, STREAM, W, false>(a, s);
 }
 template <typename T, int NT, bool W, bool CL>
@@ -1347,8 +1353,8 @@ cudaError_t run_bwd(const LogprobsBwdArgs& a, const Plan& p, cudaStream_t s) {
 }
 template <typename T, bool W>
 cudaError_t run_bwd(const LogprobsBwdArgs& a, cudaStream_t s) {
-  if (short_rows(a.in, sizeof(T))) return run_bwd<T, FEW, W, false>(a, plan_rows(a.in, sizeof(T), FEW, batch_of(FEW, false), true, 0, 0), s);
-  const Plan p = plan_rows(a.in, sizeof(T), STAY, batch_of(STAY, false), true, 0, 0);
+  if (short_rows(a.in, sizeof(T), 16384)) return run_bwd<T, FEW, W, false>(a, plan_rows(a.in, sizeof(T), FEW, batch_of(FEW, false), true, false, 0, 0), s);
+  const Plan p = plan_rows(a.in, sizeof(T), STAY, batch_of(STAY, false), true, false, 0, 0);
   return p.g.cluster > 1 ? run_bwd<T, STAY, W, true>(a, p, s) : run_bwd<T, STAY, W, false>(a, p, s);
 }
 
@@ -1359,8 +1365,8 @@ cudaError_t run_distill(const DistillArgs& a, const Plan& p, cudaStream_t s) {
 }
 template <typename T>
 cudaError_t run_distill(const DistillArgs& a, cudaStream_t s) {
-  if (short_rows(a.in, sizeof(T))) return run_distill<T, FEW, false>(a, plan_rows(a.in, sizeof(T), FEW, batch_of(FEW, false), true, 0, 0, 32), s);
-  const Plan p = plan_rows(a.in, sizeof(T), STAY, batch_of(STAY, false), true, 0, 0, 32);
+  if (short_rows(a.in, sizeof(T), 8192)) return run_distill<T, FEW, false>(a, plan_rows(a.in, sizeof(T), FEW, batch_of(FEW, false), true, false, 0, 0, 32), s);
+  const Plan p = plan_rows(a.in, sizeof(T), STAY, batch_of(STAY, false), true, false, 0, 0, 32);
   return p.g.cluster > 1 ? run_distill<T, STAY, true>(a, p, s) : run_distill<T, STAY, false>(a, p, s);
 }
 
