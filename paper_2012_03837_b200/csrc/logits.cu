@@ -948,7 +948,8 @@ struct Weighed {
     S = o.s * f + l.student * factor(Ref(l.most, g));
   }
   __device__ __forceinline__ float factor(const Ref& b) const {
-    return b.m == -INFINITY ? 0.f : ex2(ref.far ? (b.m - ref.m) * b.c : b.rho - ref.rho);
+    // a far maximum below one that is not is a masked token's
+    return b.m == -INFINITY || (b.far && !ref.far) ? 0.f : ex2(ref.far ? (b.m - ref.m) * b.c : b.rho - ref.rho);
   }
 };
 

@@ -159,14 +159,22 @@ def test_log_probabilities(rows, vocab, pad, off, k, kind, dt):
     order = np.argsort(-x, axis=1, kind="stable")[:, :k]
     assert np.array_equal(o["top_ids"].cpu().numpy(), order)
     close(np64(o["top_logp"]), np.take_along_axis(E["l"], order, 1), np.take_along_axis(E["e_l"], order, 1), "top_logp of all rows")
-    # each output alone, and again, gives the same bits
-    for name, v in o.items():
-        if name.startswith("top"):
-            again = dict(top_ids=torch.zeros_like(o["top_ids"]), top_logp=torch.zeros_like(o["top_logp"]))
-        else:
-            again = {name: torch.zeros_like(v)}
-        lp.lp_token_logprobs(t, cu(tok, torch.int32) if name == "logp" else None, temperature=T, **again)
-        assert torch.equal(again[name], v), name
+    # again, and each output alone, the same bits; a row is cut otherwise where alternatives are asked for, and its sums round otherwise
+    t_tok = cu(tok, torch.int32)
+    again = {n: torch.zeros_like(v) for n, v in o.items()}
+    lp.lp_token_logprobs(t, t_tok, temperature=T, **again)
+    assert all(torch.equal(v, o[n]) for n, v in again.items())
+    tops = {n: torch.zeros_like(v) for n, v in o.items() if n.startswith("top")}
+    lp.lp_token_logprobs(t, temperature=T, **tops)
+    assert all(torch.equal(v, o[n]) for n, v in tops.items())
+    rest = {n: torch.zeros_like(v) for n, v in o.items() if n not in tops}
+    lp.lp_token_logprobs(t, t_tok, temperature=T, **rest)
+    close(np64(rest["lse"])[some], lse, E["e_lse"][some, 0], "lse without alternatives")
+    close(np64(rest["entropy"])[some], ent, E["e_h"][some, 0], "entropy without alternatives")
+    for name, v in rest.items():
+        alone = {name: torch.zeros_like(v)}
+        lp.lp_token_logprobs(t, t_tok if name == "logp" else None, temperature=T, **alone)
+        assert torch.equal(alone[name], v), name
 
 
 @pytest.mark.parametrize("dt", ["fp32", "bf16"])
@@ -322,6 +330,145 @@ def test_distillation(rows, vocab, pad, off, k, kind, dt, rest):
     y = put(x, td, pad, off)
     lp.lp_distill(form, y, *args[2:], loss=alone, dloss=cu(dl), dlogits=y, temperature=T, scale=scale)
     assert torch.equal(y, dx) and torch.equal(alone, loss) and torch.isnan(between(y)).all()
+
+
+MANY = [(5000, 50, 0, 1), (3001, 1000, 1, 3), (2500, 4099, 0, 0), (1500, 9000, 7, 0), (1300, 33001, 0, 1), (640, 70003, 1, 0), (300, 140001, 0, 0)]
+
+
+def many_rows(rows, vocab, pad, off, dt, seed):
+    """Rows enough that every block takes several, of all kinds in turn."""
+    g = np.random.default_rng(seed)
+    kinds = ["normal", "masked", "peaked", "ties", "lowest", "normal", "constant", "lowmask", "descending", "highest"]
+    t = matrix(rows, vocab, DT[dt][0], pad, off)
+    for i, k in enumerate(kinds):
+        if len(range(i, rows, len(kinds))):
+            t[i::len(kinds)] = cu(values(g, len(range(i, rows, len(kinds))), vocab, k).astype(np.float32)).to(t.dtype)
+    return g, t
+
+
+def many_reference(t, T):
+    """log p, p and the bound of a probability's relative error, in 64 bits on the GPU; rows without any token: p = 0."""
+    x = t.double()
+    m = x.max(1, keepdim=True).values
+    y = torch.where(m > -INF, (x - m) / T, -INF)
+    s = y.exp().sum(1, keepdim=True)
+    l = torch.where(m > -INF, y - s.log(), -INF)
+    far = torch.where(l.exp() > 0, -y, 0.0)
+    rel = (t.shape[1] / 256 + 64) * U + 2 * EXP + 8 * U + 3 * U * (far + (l.exp() * far).sum(1, keepdim=True)) + 2 * U * s.log().clamp(min=0)
+    return l, l.exp(), rel
+
+
+def same(got, want, tol, what):
+    fin = torch.isfinite(want) & torch.isfinite(want.float())
+    assert torch.equal(torch.where(fin, 0.0, got.double()), torch.where(fin, 0.0, want.float().double())), what
+    gap = torch.where(fin, (got.double() - want).abs() - tol, -1.0)
+    assert (gap <= 0).all(), (what, gap.max(), (gap > 0).nonzero()[:5])
+
+
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,vocab,pad,off", MANY)
+def test_many_rows(rows, vocab, pad, off, dt):
+    g, t = many_rows(rows, vocab, pad, off, dt, rows)
+    us, T = DT[dt][1], 1.25
+    l, p, rel = many_reference(t, T)
+    tok = cu(g.integers(-1, vocab, rows), torch.int32)
+    has, at = tok >= 0, tok.long().clamp(min=0)[:, None]
+    f = lambda *s: torch.full(s, 7.0, device="cuda")
+    for k in (0, 1, min(40, vocab)):
+        o = dict(logp=f(rows), entropy=f(rows), lse=f(rows))
+        if k:
+            o.update(top_ids=torch.zeros(rows, k, dtype=torch.int32, device="cuda"), top_logp=f(rows, k))
+        lp.lp_token_logprobs(t, tok, temperature=T, **o)
+        lz = torch.where(torch.isfinite(l), l, 0.0)
+        plain = torch.where(p > 0, l, 0.0)
+        # a log probability: that of log S, the difference's, the difference itself rounded three times
+        e_l = rel + 4 * U * lz.abs()
+        same(o["logp"], torch.where(has, l.gather(1, at)[:, 0], 0.0), e_l.gather(1, at)[:, 0], "logp")
+        H = -(p * plain).sum(1)
+        same(o["entropy"], H, (p * (rel * (1 + plain.abs()) + 8 * U * plain.abs())).sum(1) * 2 + 2 * U * H, "entropy")
+        if k:
+            order = torch.sort(t.float(), dim=1, descending=True, stable=True).indices[:, :k]
+            assert torch.equal(o["top_ids"].long(), order)
+            same(o["top_logp"], l.gather(1, order), e_l.gather(1, order), "top_logp")
+    for which in ("a", "ab"):
+        a, b = cu(g.standard_normal(rows)), cu(g.standard_normal(rows)) * 0.5
+        a[3::7], b[3::7] = 0.0, 0.0                               # rows of zeros among the others
+        a0 = torch.where(has, a, 0.0).double()[:, None]
+        b0 = b.double()[:, None] if "b" in which else torch.zeros_like(a0)
+        pl = p * plain
+        want = -a0 * p - b0 * (pl - p * pl.sum(1, keepdim=True))
+        want.scatter_add_(1, at, a0)
+        size = a0.abs() + b0.abs() * (plain.abs() - pl.sum(1, keepdim=True))
+        tol = p * (2 * rel * size + b0.abs() * 2 * rel) + TINY * (1 + size)
+        tol.scatter_add_(1, at, 16 * U * a0.abs())
+        want, tol = want / T, tol / T
+        want[~(p > 0).any(1)] = 0.0                               # no token at all
+        dx = matrix(rows, vocab, t.dtype, pad, off, 5.0)
+        lp.lp_token_logprobs_backward(t, tok, dlogp=a, dentropy=b if "b" in which else None, dlogits=dx, temperature=T)
+        same(dx, want, tol + us * want.abs() * (1 + us), which)
+        assert (between(dx) == 5.0).all()
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,vocab,pad,off", MANY)
+def test_distillation_of_many_rows(rows, vocab, pad, off, dt, rest):
+    g, t = many_rows(rows, vocab, pad, off, dt, rows + 1)
+    us, T, k = DT[dt][1], 1.25, 20
+    l, p, rel = many_reference(t, T)
+    # the teacher's entries: among the student's best, a token often twice, some missing
+    ids = torch.sort(t.float(), dim=1, descending=True, stable=True).indices[:, :15]
+    ids = torch.cat([ids, cu(g.integers(0, vocab, (rows, k - 15)), torch.int64)], 1)
+    q = cu(g.random((rows, k))) + 0.01
+    te = (q / q.sum(1, keepdim=True) * 0.8).log()
+    ids[cu(g.random((rows, k))) < 0.1] = -1
+    ids[5::11] = -1                                               # rows without entries
+    dl = cu(g.standard_normal(rows))
+    dl[2::9] = 0.0
+    there = ids >= 0
+    at = ids.clamp(min=0)
+    v = torch.where(there, te.double(), -INF)
+    any_ = there.any(1, keepdim=True)
+    if rest:
+        q = v.exp()
+        qr = 1 - q.sum(1, keepdim=True)
+        qr = torch.where(any_ & (qr > 2.0 ** -20), qr, 0.0)
+    else:
+        q = torch.softmax(v / T, 1).nan_to_num(0.0)
+        qr = torch.zeros(rows, 1, dtype=torch.float64, device="cuda")
+    q = torch.where(any_, q, 0.0)
+    inside = torch.zeros(rows, vocab + 1, dtype=torch.bool, device="cuda").scatter_(1, torch.where(there, ids, vocab), True)[:, :-1]
+    out = torch.where(inside, -INF, l)
+    lr = torch.logsumexp(out, 1, keepdim=True)
+    lj = l.gather(1, at)
+    zl = lambda a: torch.where(torch.isfinite(a), a, 0.0)
+    want = torch.where(q > 0, q * (q.clamp(min=1e-300).log() - lj), 0.0).sum(1) + torch.where(qr > 0, qr * (qr.clamp(min=1e-300).log() - lr), 0.0)[:, 0]
+    e_q = (k + 8) * U + 2 * EXP
+    e_j = rel.gather(1, at) + 8 * U * zl(lj).abs() + 8 * U * 12 + e_q * 2
+    e_rest = (rel * p).sum(1, keepdim=True) + 6 * U * zl(lr).abs() + (vocab / 256 + 64) * U + 40 * U + 4 * EXP     # of log of the rest's sum, against its own maximum
+    tol = (q * (e_j + e_q * (12 + zl(lj).abs()))).sum(1) + (qr * e_rest + e_q * (zl(lr).abs() + 12) * (qr > 0))[:, 0]
+    loss, dx = torch.full((rows,), 9.0, device="cuda"), matrix(rows, vocab, t.dtype, pad, off, 5.0)
+    form = lp.LP_DISTILL_REST if rest else lp.LP_DISTILL_TOP
+    args = (form, t, ids.to(torch.int32), te.float())
+    lp.lp_distill(*args, loss=loss, dloss=dl, dlogits=dx, temperature=T, scale=2.0)
+    same(loss, 2 * want, 2 * tol, "loss")
+    Q = q.sum(1, keepdim=True) + qr
+    w = torch.softmax(out, 1).nan_to_num(0.0)                     # against the rest's own maximum: it may be the type's lowest value
+    grad = Q * p - qr * w
+    grad.scatter_add_(1, at, -torch.where(there, q, 0.0))
+    # the rest's share is formed against the rest's own maximum: as many roundings of its own
+    y = torch.where(w > 0, -(l - l.masked_fill(inside, -INF).max(1, keepdim=True).values), 0.0).nan_to_num(0.0, posinf=0.0, neginf=0.0).abs()
+    tolg = Q * p * (rel + e_rest + e_q) + (w * qr) * (rel + e_rest + 3 * U * y) + w * e_q * (qr > 0) + TINY * (Q + qr)
+    tolg.scatter_add_(1, at, torch.where(there, q * (e_q + 3 * U * 12), 0.0))
+    f = (dl.double() * 2.0 / T)[:, None]
+    grad = torch.where((p > 0).any(1, keepdim=True), grad, 0.0) * f
+    same(dx, grad, tolg * f.abs() + us * grad.abs() * (1 + us), "gradient")
+    assert (between(dx) == 5.0).all()
+    alone = torch.zeros(rows, device="cuda")
+    lp.lp_distill(*args, loss=alone, temperature=T, scale=2.0)
+    assert torch.equal(alone, loss)
+    lp.lp_distill(form, t, *args[2:], dloss=dl, dlogits=t, temperature=T, scale=2.0)       # in the logits' place
+    assert torch.equal(t, dx)
 
 
 @pytest.mark.parametrize("dt", ["fp32", "bf16"])
