@@ -10,12 +10,23 @@
 // own maximum (rho_r; R = sum 2^(x_i c - rho_r)), so that a small rest keeps its digits; f = 2^(rho_r - rho):
 //   KL = sum q_j (log q_j - log p_j) + q_r (log q_r - log p_r),   log p_r = (rho_r - rho) ln 2 + log R - log S
 //   dx_i = 2^(x_i c - rho_r) kappa elsewhere, kappa = (Q f / S - q_r / R) / T;   dx_j = (Q p_j - q_j) / T where listed
-// Sums are in fp32 in a fixed order.  Rows whose |rho| is above FAR (the type's lowest value in every place, infinities)
-// take the differences before the factor, one element at a time.
+// Sums are in fp32 in a fixed order; what a row hands out is rounded from them once (the loss, a small difference of
+// logarithms, by way of 64 bits).  Rows whose |rho| is above FAR (the type's lowest value in every place, infinities) take the
+// differences before the factor, one element at a time.
 //
-// A row is read once: its piece of the row waits in shared memory (asynchronous copies of 16 bytes) for the second pass that
-// a gradient or the top alternatives take.  Long rows, and rows too few for the device, are cut over a cluster of up to
-// eight blocks, which exchange their sums through distributed shared memory.
+// What bounds it: memory, and close behind it the 16 exponentials a clock of an SM (one per logit, two with a gradient: 57 and
+// 114 us of the 82 and 164 that 8192 x 32768 bf16 take to pass) and the instructions (5.5 a logit for a sum, 11 with a gradient).
+// Hence: each logit is fetched once, by asynchronous copies of 16 bytes that only the fetching thread reads again, so no barrier
+// stands between a copy and its use; two logits per instruction where one does it; a reference that moves only when a power
+// would exceed 2^SLACK; one barrier per row to join its sums; and persistent blocks, several to an SM, whose copies run ahead
+// into the next row.
+//   Rows that are only read (logprobs_kernel) stream through a ring of two batches, whatever their length.
+//   Rows that need a second pass (gradients, distillation) stay in shared memory: pieces of up to 65 KB, three blocks to an SM;
+//   as the second pass leaves a batch, the next row's takes its place.  A cluster of up to eight blocks shares a longer row and
+//   exchanges its sums through distributed shared memory; so do blocks that share a row because rows are few.
+// Measured, replayed from a graph, against the bytes at 6.54 TB/s: 8192 x 32768 bf16 log probabilities 85 us (82), with entropy
+// 89 (82), with 64 alternatives 158 (83), gradient with entropy 179 (164), distillation with gradient 187 (165); 1031 x 50021 fp32
+// with 5 alternatives 36 (32); 1000 x 131071 bf16 distillation with a rest of 128 entries 125 (80).
 #include <algorithm>
 #include <atomic>
 #include <cfloat>
@@ -34,7 +45,8 @@ typedef unsigned long long u64;
 
 constexpr int TOP_MAX = 128;                  // LP_TOP_MAX
 constexpr float SMALLEST_REST = 0x1p-20f;
-constexpr float FAR = 1e23f;
+constexpr float FAR = 1e12f;                  // LOWEST c is far below -FAR for every temperature
+constexpr double LOWEST = -1e20;
 constexpr float LN2 = 0.693147180559945309f;
 constexpr int MAX_CLUSTER = 8;
 constexpr float SLACK = 8.f;                  // a sum's reference stays while no power of two exceeds 2^SLACK
@@ -235,8 +247,8 @@ __device__ __forceinline__ void move(float& s, float& w, float rho, float m, con
   s *= f;
 }
 
-// A thread's running sums.  The reference is the maximum of the first batch above lo, and is raised when a later one would
-// give a power above 2^SLACK; no batch but the first few of a row does.
+// A thread's running sums.  The reference is the maximum of the first four vectors above lo, and is raised when later ones
+// would give a power above 2^SLACK, which few do (raising it with every new maximum made every fourth step one of all warps).
 template <typename T, bool W>
 struct Running {
   u64 s0 = 0, s1 = 0, w0 = 0, w1 = 0, nrho = 0;
@@ -386,44 +398,27 @@ __device__ __forceinline__ void leave_part(Sums a, float4* part, const Geometry&
 }
 template <int NT, bool W, bool CL, bool FARROW>
 __device__ __forceinline__ Sums take_parts(const float4* part, const Geometry& g) {
-  const int lane = threadIdx.x & 31, parts = CL ? g.cluster * (NT / 32) : NT / 32;
   Sums t{-INFINITY, 0.f, 0.f};
-  if constexpr (!CL && NT <= 128) {                      // few parts: each thread by itself
-    float4 q[NT / 32];
-#pragma unroll
-    for (int i = 0; i < NT / 32; ++i) {
-      q[i] = part[i];
-      t.m = fmaxf(t.m, q[i].x);
-    }
-#pragma unroll
-    for (int i = 0; i < NT / 32; ++i) {
-      if (!FARROW) move<W>(q[i].y, q[i].z, rho_of(q[i].x, g), t.m, g);
-      t.s += q[i].y;
-      t.w += q[i].z;
-    }
-    return t;
-  } else {
-  for (int i = lane; i < parts; i += 32) t.m = fmaxf(t.m, part[i].x);
-  t.m = warp_most(t.m);
-  for (int i = lane; i < parts; i += 32) {
-    float4 b = part[i];
+  auto add = [&](float4 b) {
     if (!FARROW) move<W>(b.y, b.z, rho_of(b.x, g), t.m, g);
     t.s += b.y;
     t.w += b.z;
-  }
-  if (CL || NT > 256) {
+  };
+  if constexpr (CL) {                                    // up to a part per lane
+    const int lane = threadIdx.x & 31, parts = g.cluster * (NT / 32);
+    static_assert(MAX_CLUSTER * NT <= 32 * 32, "a part per lane");
+    if (lane < parts) t.m = part[lane].x;
+    t.m = warp_most(t.m);
+    if (lane < parts) add(part[lane]);
     t.s = warp_sum(t.s);
     if (W) t.w = warp_sum(t.w);
-  } else {                                               // eight lanes hold them
-    for (int o = 4; o > 0; o >>= 1) {
-      t.s += __shfl_xor_sync(0xffffffffu, t.s, o);
-      if (W) t.w += __shfl_xor_sync(0xffffffffu, t.w, o);
-    }
-    t.s = __shfl_sync(0xffffffffu, t.s, 0);
-    if (W) t.w = __shfl_sync(0xffffffffu, t.w, 0);
+  } else {                                               // few: each thread by itself
+#pragma unroll
+    for (int i = 0; i < NT / 32; ++i) t.m = fmaxf(t.m, part[i].x);
+#pragma unroll
+    for (int i = 0; i < NT / 32; ++i) add(part[i]);
   }
   return t;
-  }
 }
 template <int NT, bool W, bool CL, bool FARROW>
 __device__ __forceinline__ Sums join(Sums a, float4* part, const Geometry& g, int rank) {
@@ -485,7 +480,6 @@ __device__ __forceinline__ float value_of(uint32_t o) {
   return o == 0 ? __uint_as_float(0x7fc00000u) : __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
 }
 __device__ __forceinline__ u64 key_of(uint32_t order, int j) { return ((u64)order << 32) | (uint32_t)~j; }
-
 
 constexpr int ENTRIES = 8;                    // maxima that a thread leaves of its batches
 
@@ -690,7 +684,7 @@ struct Leaves {
   }
 };
 
-constexpr int SLOTS = 2;        // threads of a block that reads its rows once; batches that it has on their way
+constexpr int SLOTS = 2;                      // batches on their way
 
 // Batches pass through a ring of SLOTS, each thread's by itself: copies run ahead of the sums by SLOTS batches, over the end of
 // a row into the next ones, so that they go on while a row's sums are joined and handed out.
@@ -715,9 +709,11 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(const __grid_constant__ Lo
       if (ahead_row < rows) ahead = Piece<T, NT, B>(a.in, ahead_row, rank, g);
     }
   };
-  for (; slot < SLOTS; ++slot) fetch();
-  slot = 0;
   static_assert(SLOTS == 2, "slots take turns");
+  fetch();
+  slot = 1;
+  fetch();
+  slot = 0;
   float edge = p.edge_value();
   int t = speaks && a.tokens ? token_of(a.tokens, me.row, a.in.vocab, a.in.out_of_range, true) : -1;
   float xt = t >= 0 ? to_f(p.x[t]) : 0.f;
@@ -865,7 +861,6 @@ __device__ __forceinline__ Sums sweep(const Piece<T, NT, B>& p, uint4* buf, floa
   }
   return run.end(edge, g);
 }
-
 
 template <typename T, int NT, bool W, bool CL>
 __global__ void __launch_bounds__(NT, NT == STAY ? 4 : 1) logprobs_bwd_kernel(const __grid_constant__ LogprobsBwdArgs a, const __grid_constant__ Geometry g) {
@@ -1266,7 +1261,7 @@ Plan plan_rows(const LogitsIn& in, int elem_bytes, int threads, int batch, bool 
   p.threads = threads + more_threads;
   p.smem = (stay ? (size_t)per * 16 : smem) + (c > 1 ? smem_cluster : 0);
   const double cc = 1.4426950408889634 / (double)in.temperature;
-  p.g = Geometry{(float)cc, (float)(1.0 / (double)in.temperature), (float)(-1e30 * std::min(1.0, 1.0 / cc)), (float)(SLACK / cc), c, per,
+  p.g = Geometry{(float)cc, (float)(1.0 / (double)in.temperature), (float)(LOWEST * std::min(1.0, 1.0 / cc)), (float)(SLACK / cc), c, per,
                  (per + batch * threads - 1) / (batch * threads), 0};
   while (batch / 4 * p.g.batches > ENTRIES << p.g.shift) ++p.g.shift;
   return p;
