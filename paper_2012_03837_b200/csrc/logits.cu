@@ -25,8 +25,8 @@
 //   as the second pass leaves a batch, the next row's takes its place.  A cluster of up to eight blocks shares a longer row and
 //   exchanges its sums through distributed shared memory; so do blocks that share a row because rows are few.
 // Measured, replayed from a graph, against the bytes at 6.54 TB/s: 8192 x 32768 bf16 log probabilities 85 us (82), with entropy
-// 89 (82), with 64 alternatives 158 (83), gradient with entropy 179 (164), distillation with gradient 187 (165); 1031 x 50021 fp32
-// with 5 alternatives 36 (32); 1000 x 131071 bf16 distillation with a rest of 128 entries 125 (80).
+// 89 (82), with 64 alternatives 158 (83), gradient with entropy 179 (164), distillation with gradient 190 (165), with a rest 208;
+// 1031 x 50021 fp32 with 5 alternatives 36 (32); 1000 x 131071 bf16 distillation from 128 entries and a rest 125 (80).
 #include <algorithm>
 #include <atomic>
 #include <cfloat>
@@ -461,6 +461,13 @@ __device__ __forceinline__ double log_wide(float v) {
   return (double)e * 0.693147180559945309417 + (double)logf(__int_as_float((bits & 0x7fffff) + 0x3f400000));
 }
 
+// exp v to about 3e-8 of itself (expf: 1e-7, and a teacher's rest is what 1 lacks of many): 2^n (1 + (e^r - 1)), the 1 in 64 bits.
+__device__ __forceinline__ double exp_wide(float v) {
+  if (!(fabsf(v) < 80.f)) return (double)expf(v);
+  const float n = rintf(v * 1.44269504f), r = fmaf(n, -1.42860677e-6f, fmaf(n, -0.693145752f, v));     // ln 2 in two parts
+  return (1.0 + (double)expm1f(r)) * (double)__int_as_float(((int)n + 127) << 23);
+}
+
 // A token id, or -1 where there is none.
 __device__ __forceinline__ int token_of(const int* tokens, long long i, int n, int* out_of_range, bool report) {
   const int t = tokens[i];
@@ -508,6 +515,21 @@ __device__ __forceinline__ uint32_t bound_of(const uint32_t* values, int k) {
     hi = max(hi, v[i]);
   }
   if (__reduce_add_sync(0xffffffffu, n) < k) return 0;
+  if (k * P <= 16) {                                     // few: one after the other
+    for (n = 0; n < k;) {
+      hi = 0;
+#pragma unroll
+      for (int i = 0; i < P; ++i) hi = max(hi, v[i]);
+      hi = __reduce_max_sync(0xffffffffu, hi);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const bool is = v[i] == hi;
+        n += __popc(__ballot_sync(0xffffffffu, is));
+        if (is) v[i] = 0;
+      }
+    }
+    return hi;
+  }
   lo = __reduce_min_sync(0xffffffffu, lo);
   hi = __reduce_max_sync(0xffffffffu, hi) + 1;
   while (hi - lo > 1) {                                  // at least k reach lo, fewer than k reach hi
@@ -1086,8 +1108,9 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
       claim[i] = -1;
       w.q[i] = 0.f;
       if (i >= used) continue;
-      w.q[i] = e.t[i] == -INFINITY ? 0.f : expf((e.t[i] - mt) * by);
-      mass += (double)w.q[i];
+      const double v = e.t[i] == -INFINITY ? 0.0 : a.rest ? exp_wide(e.t[i]) : (double)expf((e.t[i] - mt) * by);
+      w.q[i] = (float)v;
+      mass += v;
       if (e.id[i] < 0) continue;
       // Does a token stand in two entries?  Each claims a place by its id.
       unsigned at = (unsigned)e.id[i] * 2654435761u >> 23;
@@ -1193,12 +1216,23 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
         if (now.id[i] >= 0 && !(w.q[i] == 0.f)) part += w.q[i] * s.ref.above(w.lq[i], now.x[i]);
       }
       part = warp_sum(part);
-      const double logs = log_wide(s.S);
-      double loss = s.S == 0.f ? (double)INFINITY : (double)part + w.all * (logs - w.shift);
-      if (l.qr > 0.f && s.S != 0.f) {
-        const float lr = s.ref.far || s.ro.far ? (o.m - s.ref.m) * g.inv_t : (s.ro.rho - s.ref.rho) * LN2;
-        loss += (double)l.qr * ((log_wide(l.qr) - log_wide(o.s)) - ((double)lr - logs));
+      const double LN2D = 0.693147180559945309417;
+      double logs = log_wide(s.S), logr = 0.0;           // log S, log p_r
+      if (a.rest) {
+        const Ref rl(l.most, g);
+        if (s.ref.far || s.ro.far || rl.far || o.s == 0.f || l.student == 0.f) {
+          logr = o.s == 0.f ? -(double)INFINITY : (s.ref.far || s.ro.far ? (double)((o.m - s.ref.m) * g.inv_t) : ((double)s.ro.rho - (double)s.ref.rho) * LN2D) + log_wide(o.s) - logs;
+        } else {
+          // both from one ratio of the listed to the others, whose rounding they then share: it enters the loss by p_r - q_r only
+          const double apart = (double)rl.rho - (double)s.ro.rho;
+          const float u = l.student / o.s * ex2((float)apart), v = o.s / l.student * ex2((float)-apart);
+          const double lr = log_wide(o.s) + ((double)s.ro.rho - (double)s.ref.rho) * LN2D;
+          logs = u <= 1.f ? lr + (double)log1pf(u) : log_wide(l.student) + ((double)rl.rho - (double)s.ref.rho) * LN2D + (double)log1pf(v);
+          logr = u <= 1.f ? -(double)log1pf(u) : lr - logs;
+        }
       }
+      double loss = s.S == 0.f ? (double)INFINITY : (double)part + w.all * (logs - w.shift);
+      if (l.qr > 0.f && s.S != 0.f) loss += (double)l.qr * (log_wide(l.qr) - logr);
       if (lane == 0) a.loss[r] = l.any ? (float)((double)a.scale * loss) : 0.f;
     }
     if (a.dx) {
