@@ -332,7 +332,7 @@ def test_distillation(rows, vocab, pad, off, k, kind, dt, rest):
     assert torch.equal(y, dx) and torch.equal(alone, loss) and torch.isnan(between(y)).all()
 
 
-MANY = [(5000, 50, 0, 1), (3001, 1000, 1, 3), (2500, 4099, 0, 0), (1500, 9000, 7, 0), (1300, 33001, 0, 1), (640, 70003, 1, 0), (300, 140001, 0, 0)]
+MANY = [(1400, 1, 0, 0), (2000, 3, 0, 1), (1300, 17, 2, 0), (5000, 50, 0, 1), (3001, 1000, 1, 3), (2500, 4099, 0, 0), (1500, 9000, 7, 0), (1300, 33001, 0, 1), (640, 70003, 1, 0), (300, 140001, 0, 0)]
 
 
 def many_rows(rows, vocab, pad, off, dt, seed):
@@ -418,7 +418,7 @@ def test_distillation_of_many_rows(rows, vocab, pad, off, dt, rest):
     l, p, rel = many_reference(t, T)
     # the teacher's entries: among the student's best, a token often twice, some missing
     ids = torch.sort(t.float(), dim=1, descending=True, stable=True).indices[:, :15]
-    ids = torch.cat([ids, cu(g.integers(0, vocab, (rows, k - 15)), torch.int64)], 1)
+    ids = torch.cat([ids, cu(g.integers(0, vocab, (rows, k - ids.shape[1])), torch.int64)], 1)
     q = cu(g.random((rows, k))) + 0.01
     te = (q / q.sum(1, keepdim=True) * 0.8).log()
     ids[cu(g.random((rows, k))) < 0.1] = -1
@@ -543,6 +543,65 @@ def test_impossible_tokens_and_an_impossible_rest(dt):
         close(np64(loss), want, 1e-5 * np.abs(np.where(np.isfinite(want), want, 0.0)) + 1e-5)
         close(np64(dx), w_dx, 2e-5 + DT[dt][1] * np.abs(w_dx) * 1.01)
         assert (np64(dx)[3] == 0).all()
+
+
+@pytest.mark.parametrize("T", [2.0 ** -20, 2.0 ** -8, 2.0 ** 8, 2.0 ** 20])
+@pytest.mark.parametrize("rows,vocab,dt", [(5, 3001, "fp32"), (3, 40000, "bf16")])
+def test_extreme_temperatures(rows, vocab, dt, T):
+    g, t, x = make(rows, vocab, 1, 0, "normal", dt, 7)
+    k = 9
+    tok = x.argmax(1).astype(np.int32)
+    tok[0] = 5
+    E = errors(x, T, vocab)
+    f = lambda *s: torch.zeros(*s, device="cuda")
+    o = dict(logp=f(rows), entropy=f(rows), lse=f(rows), top_ids=torch.zeros(rows, k, dtype=torch.int32, device="cuda"), top_logp=f(rows, k))
+    lp.lp_token_logprobs(t, cu(tok, torch.int32), temperature=T, **o)
+    logp, ent, lse, ids, tops = O.token_logprobs(x, tok, T, k)
+    close(np64(o["logp"]), logp, np.take_along_axis(E["e_l"], tok[:, None], 1)[:, 0], "logp")
+    close(np64(o["entropy"]), ent, E["e_h"][:, 0], "entropy")
+    close(np64(o["lse"]), lse, E["e_lse"][:, 0], "lse")
+    assert np.array_equal(o["top_ids"].cpu().numpy(), ids)
+    close(np64(o["top_logp"]), tops, np.take_along_axis(E["e_l"], ids, 1), "top_logp")
+    one = np.ones(rows, dtype=np.float32)
+    dx = torch.zeros_like(t)
+    lp.lp_token_logprobs_backward(t, cu(tok, torch.int32), dlogp=cu(one), dlogits=dx, temperature=T)
+    want = O.token_logprobs_bwd(x, tok, one, None, None, T)
+    close(np64(dx) * T, want * T, E["p"] * (E["rel"] + 8 * U) + DT[dt][1] * np.abs(want * T) * 1.01 + 16 * U * (np.arange(vocab) == tok[:, None]) + TINY, "gradient")
+    te = tops.astype(np.float32)
+    for rest in (False, True):
+        use = te if rest else te * np.float32(T)
+        w_loss, w_dx = O.distill(x, ids, use.astype(np.float64), rest, T)
+        loss = f(rows)
+        lp.lp_distill(int(rest), t, cu(ids.astype(np.int32), torch.int32), cu(use), loss=loss, dlogits=dx, temperature=T)
+        # te, use: each rounded once to fp32
+        tl, tg = distill_bounds(x, E, ids, use, rest, T, 1.0, None)
+        close(np64(loss), w_loss, tl + 1e-6, "loss")
+        close(np64(dx) * T, w_dx * T, tg * T + DT[dt][1] * np.abs(w_dx * T) * 1.01 + 1e-6, "gradient of the loss")
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("vocab", [90, 5003, 70000])
+def test_one_token_in_every_entry(vocab, rest):
+    """128 entries of a single token, and of two in turn, beside rows of other sizes of the same."""
+    g = np.random.default_rng(vocab)
+    rows, k = 4, 128
+    t = put(values(g, rows, vocab, "normal"), torch.float32)
+    x = np64(t)
+    ids = np.full((rows, k), vocab - 1, dtype=np.int32)
+    ids[1, ::2] = 0
+    ids[2] = np.arange(k) % 7
+    te = np.log(g.random((rows, k)) / k * 0.9).astype(np.float32)
+    want, w_dx = O.distill(x, ids, te.astype(np.float64), rest, 1.0)
+    E = errors(x, 1.0, vocab)
+    tl, tg = distill_bounds(x, E, ids, te, rest, 1.0, 1.0, None)
+    runs = []
+    for _ in range(3):
+        loss, dx = torch.zeros(rows, device="cuda"), torch.zeros_like(t)
+        lp.lp_distill(int(rest), t, cu(ids, torch.int32), cu(te), loss=loss, dlogits=dx)
+        runs.append((loss, dx))
+    close(np64(loss), want, tl, "loss")
+    close(np64(dx), w_dx, tg + U * np.abs(w_dx) * (1 + U), "gradient")
+    assert all(torch.equal(a, loss) and torch.equal(b, dx) for a, b in runs)
 
 
 def test_strides_beyond_two_to_the_31_elements():
