@@ -473,6 +473,8 @@ lp_status lp_linear_attention_bf16(int form, const lp_linattn_desc* desc, void* 
  *   of -infinity is a masked token: probability 0, no part in the entropy, gradient 0.  A row of them alone: lse and log
  *   probabilities are -infinity, entropy and gradients 0.  A row with a NaN or +infinity: NaN in lse, log probabilities,
  *   entropy, loss and all of its gradient.
+ *   A row's sums are cut into as many pieces as its length, the number of rows and the call ask for: equal calls give equal
+ *   bits, the same row in calls of other shapes may round otherwise.
  *   A token id below 0 says that there is none; one >= vocab is taken for none too and, if out_of_range is not NULL, bit 0
  *   of that device int is set (never cleared).
  */
