@@ -239,10 +239,11 @@ __device__ __forceinline__ float rho_of(float m, const Geometry& g) { return m <
 
 struct Sums { float m, s, w; };               // max x, sum 2^y, sum 2^y y against rho_of(m)
 
-// A sum against the reference rho moved to that of a maximum m.
+// A sum against the reference rho moved to that of a maximum m, which is no lower; but the sum of nothing (0, or NaN) stands
+// against 0, from where a power of two could be infinite.
 template <bool W>
 __device__ __forceinline__ void move(float& s, float& w, float rho, float m, const Geometry& g) {
-  const float d = rho - rho_of(m, g), f = ex2(d);
+  const float d = rho - rho_of(m, g), f = ex2(fminf(d, 0.f));
   if (W) w = f * fmaf(s, fmaxf(d, -1e30f), w);
   s *= f;
 }
