@@ -153,6 +153,8 @@ def distill(x, ids, teacher, rest, temperature=1.0, scale=1.0, dloss=None):
         outside[[e[0] for e in entries]] = False
         lo = l[outside]
         log_rest = -np.inf if not len(lo) or lo.max() == -np.inf else lo.max() + np.log(np.exp(lo - lo.max()).sum())
+        zo = x[r][outside] / temperature                # the rest's shares by itself: beside far larger logits l has lost their digits
+        eo = np.exp(zo - zo.max()) if log_rest != -np.inf else np.zeros(len(zo))
         kl = sum(qj * (np.log(qj) - l[i]) for (i, _), qj in zip(entries, q) if qj != 0)
         if qr > 0:
             kl += qr * (np.log(qr) - log_rest)
@@ -163,7 +165,7 @@ def distill(x, ids, teacher, rest, temperature=1.0, scale=1.0, dloss=None):
         for (i, _), qj in zip(entries, q):
             d[i] -= qj
         if qr > 0 and log_rest != -np.inf:
-            d[outside] -= qr * np.exp(lo - log_rest)
+            d[outside] -= qr * eo / eo.sum()
         f = (1.0 if dloss is None else dloss[r]) * scale / temperature
         dx[r] = d * f if f != 0 else 0.0
     return loss, dx

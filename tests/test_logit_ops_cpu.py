@@ -102,6 +102,18 @@ def test_rows_without_weight_and_impossible_tokens():
     assert loss[0] == inf and (dx[0, 2:] == 0).all() and np.isfinite(dx).all()
 
 
+@pytest.mark.parametrize("mask", [-1e9, -1e12, -1e15, -1e18, -1e30])
+def test_a_rest_of_equal_masked_tokens_shares_alike(mask):
+    """The rest's shares are those of its own softmax, whatever the distance to the listed tokens."""
+    x = np.full((2, 12), mask)
+    x[:, :3] = [0.5, 1.0, -1.0]
+    x[1, 11] += mask * 1e-3
+    ids, t = np.array([[0, 1, 2]] * 2), np.log([[0.25, 0.125, 0.125]] * 2)
+    loss, dx = O.distill(x, ids, t, True)
+    assert np.allclose(dx[0, 3:], -0.5 / 9, rtol=1e-12) and np.allclose(dx[1, 3:11], -0.5 / 8, rtol=1e-12) and abs(dx[1, 11]) <= 1e-12
+    assert np.isclose(loss[0], -0.5 * mask, rtol=1e-6) and np.abs(dx.sum(1)).max() <= 1e-12
+
+
 # ------------------------------------------------------------------------------------------------ refusals
 L = lp._lib
 
