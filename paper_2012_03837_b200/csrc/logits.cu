@@ -436,9 +436,12 @@ struct Ref {
                                                               far(m_ != -INFINITY && !(fabsf(m_) * g.c <= FAR)) {}
   __device__ __forceinline__ bool apart(float x) const { return far || fabsf(x) * c > FAR; }
   __device__ __forceinline__ float y(float x) const { return far ? (x - m) * c : fmaf(x, c, -rho); }
-  // (x - m) / T, of a masked token's lowest value too, and v above it
+  // (x - m) / T, of a masked token's lowest value too
   __device__ __forceinline__ float nat(float x) const { return apart(x) ? (x - m) * inv_t : fmaf(x, c, -rho) * LN2; }
-  __device__ __forceinline__ float above(float v, float x) const { return apart(x) ? v - (x - m) * inv_t : fmaf(-fmaf(x, c, -rho), LN2, v); }
+  // how far v lies above it, times q: that may be a number of 32 bits where the distance is none
+  __device__ __forceinline__ float above(float q, float v, float x) const {
+    return apart(x) ? (float)(q * (v + ((double)m - x) * inv_t)) : q * fmaf(-fmaf(x, c, -rho), LN2, v);
+  }
 };
 
 extern __shared__ uint4 dynamic[];
@@ -1214,7 +1217,7 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
 #pragma unroll
       for (int i = 0; i < PER_LANE; ++i) {
         if (i >= used) break;
-        if (now.id[i] >= 0 && !(w.q[i] == 0.f)) part += w.q[i] * s.ref.above(w.lq[i], now.x[i]);
+        if (now.id[i] >= 0 && !(w.q[i] == 0.f)) part += s.ref.above(w.q[i], w.lq[i], now.x[i]);
       }
       part = warp_sum(part);
       const double LN2D = 0.693147180559945309417;

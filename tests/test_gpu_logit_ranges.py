@@ -172,3 +172,26 @@ def test_rows_below_zero_of_which_warps_hold_no_token(level, vocab, dt):
     x[4] = np.where(np.arange(vocab) >= vocab - 3, x[4], -np.inf)
     for T in (1.0, 0.5):
         check(put(x, DT[dt][0]), T, g)
+
+
+# ------------------------------------------------------------------------------------------------ losses near the type's end
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+def test_a_loss_is_finite_where_a_log_probability_is_not(dt):
+    """A listed token of the type's lowest values: log p may be below fp32's range, a small weight times it is not."""
+    x = np.zeros((4, 500))
+    x[0, 7], x[1, 7], x[2, 7], x[3, 7] = -3.0e38, -3.3e38, -2.0e38, -INF
+    t = put(x, DT[dt][0])
+    x = np64(t)
+    ids = np.array([[7, 3]] * 4, dtype=np.int32)
+    q = np.array([[0.05, 0.6], [0.2, 0.7], [1e-30, 0.5], [1e-42, 0.5]])      # the last: a weight below the normal numbers, no probability
+    te = np.log(q).astype(np.float32)
+    for T in (0.75, 0.25):
+        for rest in (False, True):
+            use = te if rest else (te * np.float32(T)).astype(np.float32)
+            loss = torch.zeros(4, device="cuda")
+            lp.lp_distill(int(rest), t, cu(ids, torch.int32), cu(use), loss=loss, temperature=T)
+            with np.errstate(all="ignore"):
+                want, _ = O.distill(x, ids, use.astype(np.float64), rest, T)
+            assert np.isfinite(want[:3].astype(np.float32)).all() and np.isinf(want[3])
+            # of a weight: its exponential of an argument up to 70, in the first form a quotient; of a distance: three roundings
+            close(np64(loss), want, np.abs(np.where(np.isfinite(want), want, 0.0)) * (2 * EXP + 3 * U * 70 + 16 * U) + 72 * U + 4 * EXP, (T, rest))
