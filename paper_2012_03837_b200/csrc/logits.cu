@@ -2,7 +2,8 @@
 // gradient, and distillation from a teacher's top logits.
 //
 // x: a row, c = log2(e) / T, y_j = x_j c - rho with rho = fl(c max x): the reference of all powers of two, the same for all
-// terms, so that its rounding cancels.  S = sum 2^y_j, W = sum 2^y_j y_j:
+// terms, so that its rounding cancels; it is at most 2 while |rho| <= FAR, so the powers stay well within 32 bits.
+// S = sum 2^y_j, W = sum 2^y_j y_j:
 //   log p_j = y_j ln 2 - log S      lse = rho ln 2 + log S      entropy H = log S - ln 2 W / S
 //   gradient of a logp_tok + b H + g lse:
 //     dx_j = 2^y_j (k0 + k1 y_j) + a/T 1[j = tok],  k0 = (g - a + b ln 2 W / S) / (T S),  k1 = -b ln 2 / (T S)
@@ -11,8 +12,8 @@
 //   KL = sum q_j (log q_j - log p_j) + q_r (log q_r - log p_r),   log p_r = (rho_r - rho) ln 2 + log R - log S
 //   dx_i = 2^(x_i c - rho_r) kappa elsewhere, kappa = (Q f / S - q_r / R) / T;   dx_j = (Q p_j - q_j) / T where listed
 // Sums are in fp32 in a fixed order; what a row hands out is rounded from them once (the loss, a small difference of
-// logarithms, by way of 64 bits).  Rows whose |rho| is above FAR (the type's lowest value in every place, infinities) take the
-// differences before the factor, one element at a time.
+// logarithms, by way of 64 bits).  Rows whose |rho| is above FAR (masked tokens' value in every place, infinities; ordinary logits
+// only below temperatures of 1e-5) take the differences before the factor, one element at a time.
 //
 // What bounds it: memory, and close behind it the 16 exponentials a clock of an SM (one per logit, two with a gradient: 57 and
 // 114 us of the 82 and 164 that 8192 x 32768 bf16 take to pass) and the instructions (5.5 a logit for a sum, 11 with a gradient).
@@ -45,8 +46,11 @@ typedef unsigned long long u64;
 
 constexpr int TOP_MAX = 128;                  // LP_TOP_MAX
 constexpr float SMALLEST_REST = 0x1p-20f;
-constexpr float FAR = 1e12f;                  // LOWEST c is far below -FAR for every temperature
-constexpr double LOWEST = -1e20;
+// The border, in powers of two, from where a row is far.  fl(c max x) is off by half a unit in its last place: by 2 at 2^26 (by 64 at
+// 2^31, where a sum starts to overflow or vanish).  At the smallest temperature, 2^-20, logits of 44 lie at the border.
+constexpr float FAR = 0x1p26f;
+constexpr double LOWEST = -0x1p27;            // below it a logit is masked, unless the row has nothing above -FAR
+constexpr float BEYOND = 1e12f;               // from here on an error of 2 is rounding, and soon x c no number of 32 bits
 constexpr float LN2 = 0.693147180559945309f;
 constexpr int MAX_CLUSTER = 8;
 constexpr float SLACK = 8.f;                  // a sum's reference stays while no power of two exceeds 2^SLACK
@@ -434,9 +438,10 @@ struct Ref {
   bool far;
   __device__ __forceinline__ Ref(float m_, const Geometry& g) : m(m_), rho(rho_of(m_, g)), c(g.c), inv_t(g.inv_t),
                                                               far(m_ != -INFINITY && !(fabsf(m_) * g.c <= FAR)) {}
-  __device__ __forceinline__ bool apart(float x) const { return far || fabsf(x) * c > FAR; }
+  __device__ __forceinline__ bool apart(float x) const { return far || fabsf(x) * c > BEYOND; }
   __device__ __forceinline__ float y(float x) const { return far ? (x - m) * c : fmaf(x, c, -rho); }
-  // (x - m) / T, of a masked token's lowest value too
+  __device__ __forceinline__ float own() const { return y(m); }         // the maximum's: what rho is off by
+  // y ln 2, of a masked token's lowest value too
   __device__ __forceinline__ float nat(float x) const { return apart(x) ? (x - m) * inv_t : fmaf(x, c, -rho) * LN2; }
   // how far v lies above it, times q: that may be a number of 32 bits where the distance is none
   __device__ __forceinline__ float above(float q, float v, float x) const {
@@ -968,9 +973,15 @@ struct Weighed {
     f = factor(ro);
     S = o.s * f + l.student * factor(Ref(l.most, g));
   }
+  // Either reference may be far.  Two that are not are multiples of one unit, whose difference is all there is; otherwise the
+  // maximum of b stands in one sum as 2^own and has to stand in the other as 2^y.
+  __device__ __forceinline__ bool near(const Ref& b) const { return !b.far && !ref.far; }
   __device__ __forceinline__ float factor(const Ref& b) const {
-    // a far maximum below one that is not is a masked token's
-    return b.m == -INFINITY || (b.far && !ref.far) ? 0.f : ex2(ref.far ? (b.m - ref.m) * b.c : b.rho - ref.rho);
+    return b.m == -INFINITY ? 0.f : ex2(near(b) ? b.rho - ref.rho : ref.y(b.m) - b.own());
+  }
+  __device__ __forceinline__ double log_factor(const Ref& b) const {     // of b.m above -infinity
+    const double ln2 = 0.693147180559945309417;
+    return near(b) ? ((double)b.rho - (double)ref.rho) * ln2 : (double)ref.nat(b.m) - (double)b.own() * ln2;
   }
 };
 
@@ -1225,7 +1236,7 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
       if (a.rest) {
         const Ref rl(l.most, g);
         if (s.ref.far || s.ro.far || rl.far || o.s == 0.f || l.student == 0.f) {
-          logr = o.s == 0.f ? -(double)INFINITY : (s.ref.far || s.ro.far ? (double)((o.m - s.ref.m) * g.inv_t) : ((double)s.ro.rho - (double)s.ref.rho) * LN2D) + log_wide(o.s) - logs;
+          logr = o.s == 0.f ? -(double)INFINITY : s.log_factor(s.ro) + log_wide(o.s) - logs;
         } else {
           // both from one ratio of the listed to the others, whose rounding they then share: it enters the loss by p_r - q_r only
           const double apart = (double)rl.rho - (double)s.ro.rho;
@@ -1299,7 +1310,7 @@ Plan plan_rows(const LogitsIn& in, int elem_bytes, int threads, int batch, bool 
   p.threads = threads + more_threads;
   p.smem = (stay ? (size_t)per * 16 : smem) + (c > 1 ? smem_cluster : 0);
   const double cc = 1.4426950408889634 / (double)in.temperature;
-  p.g = Geometry{(float)cc, (float)(1.0 / (double)in.temperature), (float)(LOWEST * std::min(1.0, 1.0 / cc)), (float)(SLACK / cc), c, per,
+  p.g = Geometry{(float)cc, (float)(1.0 / (double)in.temperature), (float)(LOWEST / cc), (float)(SLACK / cc), c, per,
                  (per + batch * threads - 1) / (batch * threads), 0};
   while (batch / 4 * p.g.batches > ENTRIES << p.g.shift) ++p.g.shift;
   return p;

@@ -195,3 +195,169 @@ def test_a_loss_is_finite_where_a_log_probability_is_not(dt):
             assert np.isfinite(want[:3].astype(np.float32)).all() and np.isinf(want[3])
             # of a weight: its exponential of an argument up to 70, in the first form a quotient; of a distance: three roundings
             close(np64(loss), want, np.abs(np.where(np.isfinite(want), want, 0.0)) * (2 * EXP + 3 * U * 70 + 16 * U) + 72 * U + 4 * EXP, (T, rest))
+
+
+# ------------------------------------------------------------------------------------------------ values of any size
+TEMPERATURES = [0.5, 0.699999988079071, 0.75, 1.0, 1.5, 2.0]
+
+
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+@pytest.mark.parametrize("left", ["half", "tenth", "five"])
+@pytest.mark.parametrize("mask", [-1e7, -1e8, -1e9, -1e10, -1e12, -1e15, -1e18, -1e22])
+def test_masks_of_a_finite_value(mask, left, dt):
+    g = np.random.default_rng(int(7 * np.log10(-mask)))
+    for i, T in enumerate(TEMPERATURES):
+        rows, vocab = [(3, 1003), (2, 9011), (4, 250)][i % 3]
+        x = 3.0 * g.standard_normal((rows, vocab))
+        allowed = None
+        if left == "five":
+            allowed = np.stack([g.permutation(vocab)[:5] for _ in range(rows)])
+            y = np.full_like(x, mask)
+            np.put_along_axis(y, allowed, np.take_along_axis(x, allowed, 1), 1)
+            x = y
+        else:
+            x[g.random(x.shape) < (0.5 if left == "half" else 0.9)] = mask
+        x[-1, g.integers(0, vocab, 3)] = -np.inf            # beside the other kind of mask
+        t = put(x, DT[dt][0], 1, 1)
+        check(t, T, g)
+        if allowed is not None:                             # the teacher's rest is nothing but masked tokens
+            check_distillation(t, T, g, listed=allowed)
+
+
+LARGEST = [1e5, 1e6, 1e7, 2.3e7, 4.6e7, 4.7e7, 9e7, 1e8, 1e9, 5e9, 1e10, 1e11, 5e11, 1e12, 1e13, 1e20, 1e30]
+
+
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("vocab", [77, 4100])
+def test_largest_logits_of_any_size(vocab, sign, dt):
+    """Rows whose other logits are at most a few steps of the type lower, and rows with ordinary ones beside the largest."""
+    g = np.random.default_rng(vocab + sign)
+    for unit in (1.0, 8.0):                                 # the largest and the temperature, together: more rows about the border
+        x = np.zeros((2 * len(LARGEST), vocab))
+        for i, M in enumerate(LARGEST):
+            top = float(torch.tensor(sign * M * unit).to(DT[dt][0]))
+            step = abs(top) * 2 * DT[dt][1]
+            x[2 * i] = top - step * g.integers(0, 5, vocab)
+            x[2 * i, g.integers(0, vocab)] = top
+            x[2 * i + 1] = (3.0 if sign > 0 else 2 * top) + g.standard_normal(vocab)
+            x[2 * i + 1, g.integers(0, vocab)] = top
+        for T in (unit, 3.0 * unit):
+            check(put(x, DT[dt][0], 3, 0), T, g)
+
+
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+def test_small_temperatures(dt):
+    g = np.random.default_rng(11)
+    for T, sizes in ((2.0 ** -20, [1.0, 10.0, 22.0, 30.0, 43.0, 45.0, 60.0, 3008.0, 19968.0, 3e4, 1e5]), (2.0 ** -14, [13.0, 2800.0, 3000.0, 3e5]),
+                     (1e-4, [4000.0, 5000.0, 1e6])):
+        x = np.zeros((2 * len(sizes), 2050))
+        for i, M in enumerate(sizes):
+            for j, s in enumerate((M, -M)):
+                top = float(torch.tensor(s).to(DT[dt][0]))
+                x[2 * i + j] = top - abs(top) * 2 * DT[dt][1] * g.integers(0, 3, 2050) - T * g.integers(0, 9, 2050)
+        check(put(x, DT[dt][0]), float(np.float32(T)), g)
+
+
+@pytest.mark.parametrize("T", [1.0, 2.0, 16.0, 2.0 ** 20])
+@pytest.mark.parametrize("vocab", [60, 1500])
+def test_listed_tokens_and_the_rest_on_both_sides_of_the_border(vocab, T):
+    """Where a row's references stop being rounded multiples of its maximum, above 0 and below: the listed tokens' largest
+    logit, the others', both or none beyond it, a few steps of the type apart."""
+    g = np.random.default_rng(vocab)
+    x, ids = [], []
+    for power in range(24, 32):                             # of two, in units of ln 2 T
+        for sign in (1, -1):
+            border = np.float32(sign * 2.0 ** power * np.log(2.0) * T)
+            step = float(np.spacing(np.abs(border)))
+            for up in (-2, -1, 0, 1, 2):
+                for gap in (-1, 0, 1):
+                    listed = g.permutation(vocab)[:7]
+                    r = float(border) + step * (up - g.integers(0, 3, vocab))
+                    r[listed] += gap * step
+                    x.append(r)
+                    ids.append(listed)
+    x, ids = np.stack(x), np.stack(ids)
+    check_distillation(put(x, torch.float32), T, g, listed=ids)
+
+
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(1500, 700), (700, 33000), (5, 200003)])
+def test_many_rows_with_masks_and_levels_of_all_kinds(rows, vocab, dt):
+    """Rows of all sizes of values after one another in the same blocks, and long ones over clusters of blocks: against the
+    same expressions in 64 bits on the GPU."""
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    T, us = 0.75, DT[dt][1]
+    x = 2.0 * torch.randn(rows, vocab, generator=g, device="cuda")
+    levels = torch.tensor([0.0, -200.0, 3e4, -1e6, 3.4e7, -3.6e7, 1e9, -1e10, 4e11, 0.0], device="cuda")
+    x += levels[torch.arange(rows, device="cuda") % 10][:, None]
+    masks = torch.tensor([-1e10, -INF, -1e12, -1e18, -3e38, -1e9, -INF], device="cuda")
+    hidden = torch.rand(rows, vocab, generator=g, device="cuda") < 0.9
+    hidden[3::4] = False
+    t = torch.where(hidden, masks[torch.arange(rows, device="cuda") % 7][:, None], x).to(DT[dt][0])
+    z = t.double()
+    m = z.max(1, keepdim=True).values
+    y = (z - m) / T
+    s = y.exp().sum(1, keepdim=True)
+    l, d = y - s.log(), (vocab / 256 + 64) * U + EXP
+    p = l.exp()
+    far = torch.where(p > 0, -y, 0.0)
+    mean = (p * far).sum(1, keepdim=True)
+    e_logs = d + 5 * U * mean + 8 * U + 2 * U * s.log()
+    e_l = e_logs + 5 * U * y.abs() + 2 * U * l.abs()
+    rel = e_logs + 5 * U * far + EXP + 8 * U
+    H = -(p * torch.where(p > 0, l, 0.0)).sum(1, keepdim=True)
+    e_h = e_logs + (6 * d + 8 * U) * (1 + mean) + 5 * U * ((p * far * far).sum(1, keepdim=True) + mean * mean) + 12 * U + 2 * U * H
+    lse, e_lse = m / T + s.log(), e_logs + 3 * U * (m / T).abs() + U * (m / T + s.log()).abs()
+    f32 = lambda *n: torch.full(n, 7.0, device="cuda")
+    tok = torch.randint(0, vocab, (rows,), generator=g, device="cuda")
+    tok[::3] = z.argmax(1)[::3]
+    at, tok = tok[:, None], tok.int()
+
+    def near(got, want, tol, what):
+        over = want.float().isinf()
+        assert torch.equal(torch.where(over, got.float(), 0.0), torch.where(over, want.float(), 0.0)), what
+        gap = torch.where(over, -1.0, (got.double() - want).abs() - tol)
+        assert (gap <= 0).all(), (what, gap.max(), (gap > 0).nonzero()[:5])
+
+    for k in (0, 12):
+        o = dict(logp=f32(rows), entropy=f32(rows), lse=f32(rows))
+        if k:
+            o.update(top_ids=torch.zeros(rows, k, dtype=torch.int32, device="cuda"), top_logp=f32(rows, k))
+        lp.lp_token_logprobs(t, tok, temperature=T, **o)
+        near(o["logp"], l.gather(1, at)[:, 0], e_l.gather(1, at)[:, 0], "logp")
+        near(o["entropy"], H[:, 0], e_h[:, 0], "entropy")
+        near(o["lse"], lse[:, 0], e_lse[:, 0], "lse")
+        if k:
+            order = torch.sort(t.float(), dim=1, descending=True, stable=True).indices[:, :k]
+            assert torch.equal(o["top_ids"].long(), order)
+            near(o["top_logp"], l.gather(1, order), e_l.gather(1, order), "top_logp")
+    a, b = torch.randn(rows, generator=g, device="cuda"), torch.randn(rows, generator=g, device="cuda")
+    for with_b in (False, True):
+        b1 = b.double()[:, None] if with_b else torch.zeros(rows, 1, dtype=torch.float64, device="cuda")
+        a1 = a.double()[:, None]
+        lz = torch.where(p > 0, l, 0.0)
+        want = -a1 * p - b1 * p * (lz + H)
+        want.scatter_add_(1, at, a1)
+        k0 = a1.abs() + b1.abs() * (H + 3)
+        tol = p * (rel * (k0 + b1.abs() * (lz.abs() + 3)) + b1.abs() * (torch.where(p > 0, e_l, 0.0) + e_h) + 8 * U * k0) + TINY * (k0 + 200 * b1.abs())
+        tol.scatter_add_(1, at, 8 * U * (a1.abs() + k0))
+        dx = torch.full_like(t, 5.0)
+        lp.lp_token_logprobs_backward(t, tok, dlogp=a, dentropy=b if with_b else None, dlogits=dx, temperature=T)
+        near(dx, want / T, tol / T + us * (want / T).abs() * (1 + us), ("gradient", with_b))
+    some = slice(0, min(rows, 70))                          # of distillation the first rows, seven of each kind
+    ids = torch.rand(rows, vocab, generator=g, device="cuda").topk(5).indices
+    te = (torch.rand(rows, 5, generator=g, device="cuda") * 0.15 + 0.01).log()
+    for rest in (False, True):
+        loss, dx = f32(rows), torch.full_like(t, 5.0)
+        lp.lp_distill(int(rest), t, ids.int(), te, loss=loss, dlogits=dx, temperature=T)
+        xs, i, v = np64(t[some]), ids[some].int().cpu().numpy(), te[some].cpu().numpy()
+        with np.errstate(all="ignore"):
+            w_loss, w_dx = O.distill(xs, i, v.astype(np.float64), rest, T)
+            tl, tg = distill_bounds(xs, bounds(xs, T), i, v, rest, T, 1.0)
+        close(np64(loss)[some], w_loss, tl, ("loss", rest))
+        close(np64(dx)[some], w_dx, tg + us * np.abs(w_dx) * (1 + us), ("gradient", rest))
+        assert torch.isfinite(dx.float()).all()
+        again = f32(rows)
+        lp.lp_distill(int(rest), t, ids.int(), te, loss=again, temperature=T)
+        assert torch.equal(again, loss) and not torch.isnan(loss).any()
