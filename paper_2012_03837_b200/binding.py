@@ -576,6 +576,22 @@ def _logits(t, what: str, of=None):
 _logits_codes = {}
 
 
+def _ids(t, rows: int, what: str) -> int:
+    """Entries per row of a matrix of token ids."""
+    if getattr(t, "ndim", 0) != 2 or t.shape[0] != rows:
+        raise LpError(-2, f"{what} must be a matrix [rows, k]")
+    return t.shape[1]
+
+
+def _beside(t, kind, ids, what: str):
+    """Device address of the values that go with ids: a matrix of their shape (those of a wider one would belong to other
+    tokens), or a raw address."""
+    shape = getattr(t, "shape", None)
+    if shape is not None and shape != ids.shape:
+        raise LpError(-2, f"{what} must have the shape of its ids, {tuple(ids.shape)}, not {tuple(shape)}")
+    return _buffer(t, kind, ids.shape[0] * ids.shape[1], what)
+
+
 def lp_token_logprobs(logits, tokens=None, logp=None, entropy=None, lse=None, top_ids=None, top_logp=None, temperature: float = 1.0,
                       out_of_range=None, stream=None) -> None:
     """Log probabilities of given tokens, entropy, log-sum-exp and the top alternatives of every row of `logits`, a CUDA
@@ -583,17 +599,18 @@ def lp_token_logprobs(logits, tokens=None, logp=None, entropy=None, lse=None, to
     fp32 [rows]; top_ids int32 and top_logp fp32 [rows, top_k]; outputs that are not wanted are None."""
     code, x, ld, (rows, vocab) = _logits(logits, "lp_token_logprobs: logits")
     _, i32, f32, _, _ = _kinds
-    k = 0
+    k, tops = 0, None
     if top_ids is not None:
-        if top_ids.ndim != 2 or top_ids.shape[0] != rows:
-            raise LpError(-2, "lp_token_logprobs: top_ids must be [rows, top_k]")
-        k = top_ids.shape[1]
+        k = _ids(top_ids, rows, "lp_token_logprobs: top_ids")
+        tops = _beside(top_logp, f32, top_ids, "lp_token_logprobs: top_logp")
+    elif top_logp is not None:
+        tops = _buffer(top_logp, f32, 0, "lp_token_logprobs: top_logp")
     _check(None, _lib.lp_token_logprobs(code, x, ld, _buffer(tokens, i32, rows, "lp_token_logprobs: tokens"),
                                         _buffer(logp, f32, rows, "lp_token_logprobs: logp"),
                                         _buffer(entropy, f32, rows, "lp_token_logprobs: entropy"),
                                         _buffer(lse, f32, rows, "lp_token_logprobs: lse"),
                                         _buffer(top_ids, i32, rows * k, "lp_token_logprobs: top_ids"),
-                                        _buffer(top_logp, f32, rows * k, "lp_token_logprobs: top_logp"), k, rows, vocab, temperature,
+                                        tops, k, rows, vocab, temperature,
                                         _buffer(out_of_range, i32, 1, "lp_token_logprobs: out_of_range"), stream))
 
 
@@ -622,11 +639,9 @@ def lp_distill(form: int, logits, teacher_ids, teacher, loss=None, dloss=None, d
     if dlogits is not None:
         _, dx, ld_out, _ = _logits(dlogits, "lp_distill: dlogits", logits)
     _, i32, f32, _, _ = _kinds
-    if getattr(teacher_ids, "ndim", 0) != 2 or teacher_ids.shape[0] != rows:
-        raise LpError(-2, "lp_distill: teacher_ids must be [rows, k]")
-    k = teacher_ids.shape[1]
+    k = _ids(teacher_ids, rows, "lp_distill: teacher_ids")
     _check(None, _lib.lp_distill(form, code, x, ld, _buffer(teacher_ids, i32, rows * k, "lp_distill: teacher_ids"),
-                                 _buffer(teacher, f32, rows * k, "lp_distill: teacher"), k, _buffer(loss, f32, rows, "lp_distill: loss"),
+                                 _beside(teacher, f32, teacher_ids, "lp_distill: teacher"), k, _buffer(loss, f32, rows, "lp_distill: loss"),
                                  _buffer(dloss, f32, rows, "lp_distill: dloss"), dx, ld_out, rows, vocab, temperature, scale,
                                  _buffer(out_of_range, i32, 1, "lp_distill: out_of_range"), stream))
 

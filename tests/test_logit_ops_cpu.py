@@ -208,3 +208,24 @@ def test_binding_checks_types_sizes_and_strides():
     # one row may have any stride, a column of single logits any step
     refused("INVALID_ARG", lambda: lp.lp_token_logprobs(X((1, V), b16, (7, 1))), says="output")
     refused("INVALID_ARG", lambda: lp.lp_token_logprobs(X((R, 1), b16, (5, 5))), says="output")
+
+
+def test_values_beside_ids_have_their_shape():
+    """Values of a wider (longer, turned) matrix than the ids' would belong to other tokens."""
+    import torch
+    i32, f32, b16 = torch.int32, torch.float32, torch.bfloat16
+    X = OnDevice
+    R, V, k = 4, 40, 8
+    x, ids, out = X((R, V), b16), X((R, k), i32), X((R,), f32)
+    for shape in ((R, 32), (R + 1, k), (k, R), (R * k,), (R, k, 1), (2, R, k), (R, k - 1)):
+        v = X(shape, f32)
+        refused("SHAPE", lambda: lp.lp_token_logprobs(x, top_ids=ids, top_logp=v), says="top_logp")
+        refused("SHAPE", lambda: lp.lp_distill(lp.LP_DISTILL_TOP, x, ids, v, loss=out), says="teacher")
+    refused("SHAPE", lambda: lp.lp_token_logprobs(x, top_ids=256, top_logp=X((R, k), f32)), says="top_ids")      # an address says no shape
+    refused("SHAPE", lambda: lp.lp_distill(lp.LP_DISTILL_TOP, x, 256, X((R, k), f32), loss=out), says="teacher_ids")
+    # the first entries of a longer list, as a view: strided
+    refused("SHAPE", lambda: lp.lp_distill(lp.LP_DISTILL_TOP, x, ids, X((R, k), f32, (2 * k, 1)), loss=out), says="teacher")
+    # as they should be, or an address: the entry's own checks come next
+    for v in (X((R, k), f32), 256):
+        refused("INVALID_ARG", lambda: lp.lp_token_logprobs(x, top_ids=ids, top_logp=v, temperature=0.0), says="temperature")
+        refused("INVALID_ARG", lambda: lp.lp_distill(lp.LP_DISTILL_TOP, x, ids, v, loss=out, temperature=0.0), says="temperature")
