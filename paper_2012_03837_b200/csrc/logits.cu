@@ -30,7 +30,6 @@
 // 1031 x 50021 fp32 with 5 alternatives 36 (32); 1000 x 131071 bf16 distillation from 128 entries and a rest 125 (80).
 #include <algorithm>
 #include <atomic>
-#include <cfloat>
 #include <cstddef>
 
 #include <cooperative_groups.h>
@@ -445,7 +444,7 @@ struct Ref {
   __device__ __forceinline__ float nat(float x) const { return apart(x) ? (x - m) * inv_t : fmaf(x, c, -rho) * LN2; }
   // how far v lies above it, times q: that may be a number of 32 bits where the distance is none
   __device__ __forceinline__ float above(float q, float v, float x) const {
-    return apart(x) ? (float)(q * (v + ((double)m - x) * inv_t)) : q * fmaf(-fmaf(x, c, -rho), LN2, v);
+    return apart(x) ? fmaf(q * (0.5f * m - 0.5f * x), 2.f * inv_t, q * v) : q * fmaf(-fmaf(x, c, -rho), LN2, v);
   }
 };
 
@@ -461,20 +460,6 @@ __device__ __forceinline__ void cluster_started() {
     __syncwarp();
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
   }
-}
-
-// log v to about 3e-8 whatever its size: the exponent's part in 64 bits.
-__device__ __forceinline__ double log_wide(float v) {
-  if (!(v >= FLT_MIN && v <= FLT_MAX)) return (double)logf(v);
-  const int bits = __float_as_int(v) - 0x3f400000, e = bits >> 23;       // v = 2^e f, f from 0.75 to 1.5
-  return (double)e * 0.693147180559945309417 + (double)logf(__int_as_float((bits & 0x7fffff) + 0x3f400000));
-}
-
-// exp v to about 3e-8 of itself (expf: 1e-7, and a teacher's rest is what 1 lacks of many): 2^n (1 + (e^r - 1)), the 1 in 64 bits.
-__device__ __forceinline__ double exp_wide(float v) {
-  if (!(fabsf(v) < 80.f)) return (double)expf(v);
-  const float n = rintf(v * 1.44269504f), r = fmaf(n, -1.42860677e-6f, fmaf(n, -0.693145752f, v));     // ln 2 in two parts
-  return (1.0 + (double)expm1f(r)) * (double)__int_as_float(((int)n + 127) << 23);
 }
 
 // A token id, or -1 where there is none.
@@ -1077,7 +1062,7 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
   }
 
   struct Entries { int id[PER_LANE]; float t[PER_LANE], x[PER_LANE]; };       // token, teacher's value, student's logit
-  struct Weights { float q[PER_LANE], lq[PER_LANE]; double all, shift; unsigned first; bool twins; };   // log q = lq - shift, all: sum q
+  struct Weights { float q[PER_LANE], lq[PER_LANE]; double mass; unsigned first; bool twins; };     // q = exp(lq) by mass, or in REST by 1
   const int used = (a.k + 31) / 32;                      // entries per lane
   auto read = [&](long long r, Entries& e) {
 #pragma unroll
@@ -1123,7 +1108,7 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
       claim[i] = -1;
       w.q[i] = 0.f;
       if (i >= used) continue;
-      const double v = e.t[i] == -INFINITY ? 0.0 : a.rest ? exp_wide(e.t[i]) : (double)expf((e.t[i] - mt) * by);
+      const double v = e.t[i] == -INFINITY ? 0.0 : a.rest ? exp((double)e.t[i]) : (double)expf((e.t[i] - mt) * by);
       w.q[i] = (float)v;
       mass += v;
       if (e.id[i] < 0) continue;
@@ -1137,8 +1122,7 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
     }
     for (int o = 16; o > 0; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
     const float scale = a.rest ? 1.f : 1.f / (float)mass;
-    w.all = a.rest ? mass : mass == mass ? 1.0 : mass;
-    w.shift = a.rest || !a.loss ? 0.0 : log_wide((float)mass);
+    w.mass = mass;
 #pragma unroll
     for (int i = 0; i < PER_LANE; ++i) {
       if (i >= used) break;
@@ -1223,7 +1207,7 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
     if (!a.dx && a.rest && has_next) patch(next, later);
     const Weighed s(o, l, a.rest, g);
     if (a.loss && rank == 0) {
-      // sum q ((lq - y ln 2) + (log S - shift)): what the logarithms are large in they share with one another
+      // sum q ((lq - y ln 2) + (log S - log mass)): what the logarithms are large in they share with one another
       float part = 0.f;
 #pragma unroll
       for (int i = 0; i < PER_LANE; ++i) {
@@ -1231,23 +1215,31 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
         if (now.id[i] >= 0 && !(w.q[i] == 0.f)) part += s.ref.above(w.q[i], w.lq[i], now.x[i]);
       }
       part = warp_sum(part);
+      // A logarithm in 64 bits per lane, all at once: of S, of the others' sum, of the listed ones', of the rest, of the teacher's sum.
       const double LN2D = 0.693147180559945309417;
-      double logs = log_wide(s.S), logr = 0.0;           // log S, log p_r
+      const double mine = log(lane == 0 ? (double)s.S : lane == 1 ? (double)o.s : lane == 2 ? (double)l.student : lane == 3 ? (double)l.qr : w.mass);
+      auto log_of = [&](int i) { return __shfl_sync(0xffffffffu, mine, i); };
+      double logs = log_of(0), loss;
       if (a.rest) {
         const Ref rl(l.most, g);
+        const double log_o = log_of(1), log_l = log_of(2), log_q = log_of(3);
+        double logr;                                       // log p_r
         if (s.ref.far || s.ro.far || rl.far || o.s == 0.f || l.student == 0.f) {
-          logr = o.s == 0.f ? -(double)INFINITY : s.log_factor(s.ro) + log_wide(o.s) - logs;
+          logr = o.s == 0.f ? -(double)INFINITY : s.log_factor(s.ro) + log_o - logs;
         } else {
           // both from one ratio of the listed to the others, whose rounding they then share: it enters the loss by p_r - q_r only
           const double apart = (double)rl.rho - (double)s.ro.rho;
           const float u = l.student / o.s * ex2((float)apart), v = o.s / l.student * ex2((float)-apart);
-          const double lr = log_wide(o.s) + ((double)s.ro.rho - (double)s.ref.rho) * LN2D;
-          logs = u <= 1.f ? lr + (double)log1pf(u) : log_wide(l.student) + ((double)rl.rho - (double)s.ref.rho) * LN2D + (double)log1pf(v);
+          const double lr = log_o + ((double)s.ro.rho - (double)s.ref.rho) * LN2D;
+          logs = u <= 1.f ? lr + (double)log1pf(u) : log_l + ((double)rl.rho - (double)s.ref.rho) * LN2D + (double)log1pf(v);
           logr = u <= 1.f ? -(double)log1pf(u) : lr - logs;
         }
+        loss = (double)part + w.mass * logs;
+        if (l.qr > 0.f) loss += (double)l.qr * (log_q - logr);
+      } else {
+        loss = (double)part + (logs - log_of(4));
       }
-      double loss = s.S == 0.f ? (double)INFINITY : (double)part + w.all * (logs - w.shift);
-      if (l.qr > 0.f && s.S != 0.f) loss += (double)l.qr * (log_wide(l.qr) - logr);
+      if (s.S == 0.f) loss = (double)INFINITY;
       if (lane == 0) a.loss[r] = l.any ? (float)((double)a.scale * loss) : 0.f;
     }
     if (a.dx) {

@@ -361,3 +361,35 @@ def test_many_rows_with_masks_and_levels_of_all_kinds(rows, vocab, dt):
         again = f32(rows)
         lp.lp_distill(int(rest), t, ids.int(), te, loss=again, temperature=T)
         assert torch.equal(again, loss) and not torch.isnan(loss).any()
+
+
+# ------------------------------------------------------------------------------------------------ what lacks of 1
+@pytest.mark.parametrize("rest", [3e-6, 1e-4, 0.02])
+@pytest.mark.parametrize("k", [1, 40, 128])
+def test_a_small_rest_keeps_its_digits(k, rest):
+    """A teacher's rest is what its entries lack of 1.  Its entries' exponentials and their sum are in 64 bits, so that of the
+    rest only the rounding to 32 bits is left; where the student has next to no probability elsewhere, the gradient there is
+    the teacher's rest shared by the student's odds."""
+    g = np.random.default_rng(k)
+    rows, vocab, T = 6, 700, 1.0
+    x = g.standard_normal((rows, vocab))
+    ids = np.stack([g.permutation(vocab)[:k] for _ in range(rows)]).astype(np.int32)
+    np.put_along_axis(x, ids, 40.0 + g.standard_normal((rows, k)), 1)
+    t = put(x, torch.float32)
+    x = np64(t)
+    q = g.random((rows, k)) + 0.01
+    q *= (1.0 - rest) / q.sum(1, keepdims=True)
+    te = np.log(q).astype(np.float32)
+    lack = 1.0 - np.exp(te.astype(np.float64)).sum(1)       # of the rounded entries
+    loss, dx = torch.zeros(rows, device="cuda"), torch.zeros_like(t)
+    lp.lp_distill(lp.LP_DISTILL_REST, t, cu(ids, torch.int32), cu(te), loss=loss, dlogits=dx, temperature=T)
+    want, w_dx = O.distill(x, ids, te.astype(np.float64), True, T)
+    xo = x.copy()
+    np.put_along_axis(xo, ids, -np.inf, 1)
+    E = bounds(xo, T)
+    # the rest rounded, the others' sum, the power, the factor of both and its product; p elsewhere, at most 1e-12, is in full
+    tol = lack[:, None] * E["p"] * (E["rel"] + E["e_logs"] + 8 * U) + 1e-12 * E["p"]
+    got = np64(dx)
+    outside = np.isfinite(xo)
+    assert (np.abs(got - w_dx) <= tol)[outside].all(), (np.abs(got / w_dx - 1) * outside).max()
+    assert (lack > 2.0 ** -20).all() and np.isfinite(want).all()
