@@ -1120,6 +1120,7 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
       else w.twins = true;
       w.first |= 1u << i;
     }
+    __syncwarp();                                        // the claims are made before any is cleared, l.id is written before it is searched
     for (int o = 16; o > 0; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
     const float scale = a.rest ? 1.f : 1.f / (float)mass;
     w.mass = mass;

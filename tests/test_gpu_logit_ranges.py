@@ -393,3 +393,38 @@ def test_a_small_rest_keeps_its_digits(k, rest):
     outside = np.isfinite(xo)
     assert (np.abs(got - w_dx) <= tol)[outside].all(), (np.abs(got / w_dx - 1) * outside).max()
     assert (lack > 2.0 ** -20).all() and np.isfinite(want).all()
+
+
+# ------------------------------------------------------------------------------------------------ tokens in several entries
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("rows,vocab", [(3000, 300), (1300, 9000)])
+def test_tokens_in_several_entries_of_many_rows(rows, vocab, rest):
+    """Every block finds the doubles of row after row with the same table of claims, rows of doubles beside rows of none."""
+    g = np.random.default_rng(vocab)
+    k = 128
+    x = g.standard_normal((rows, vocab)).astype(np.float32)
+    ids = np.stack([g.permutation(vocab)[:k] for _ in range(rows)]).astype(np.int32)
+    for r in range(rows):
+        if r % 3:
+            ids[r] = ids[r, g.integers(0, (1, 3, 60)[r % 3], k)]
+    q = g.random((rows, k)) + 0.01
+    te = np.log(q / q.sum(1, keepdims=True) * 0.8).astype(np.float32)
+    t = cu(x)
+    runs = []
+    for _ in range(3):
+        loss, dx = torch.zeros(rows, device="cuda"), torch.zeros_like(t)
+        lp.lp_distill(int(rest), t, cu(ids, torch.int32), cu(te), loss=loss, dlogits=dx)
+        runs.append((loss, dx))
+    assert all(torch.equal(a, loss) and torch.equal(b, dx) for a, b in runs)
+    # the doubles' weights together: rows in 64 bits
+    z, at, v = t.double(), cu(ids, torch.int64), cu(te).double()
+    w = v.exp() if rest else torch.softmax(v, 1)
+    mass = torch.zeros_like(z).scatter_add_(1, at, w)
+    inside = torch.zeros_like(z, dtype=torch.bool).scatter_(1, at, True)
+    share = torch.softmax(z.masked_fill(inside, -INF), 1)
+    lack = (1 - w.sum(1, keepdim=True)) if rest else torch.zeros(rows, 1, dtype=torch.float64, device="cuda")
+    want = (w.sum(1, keepdim=True) + lack) * torch.softmax(z, 1) - mass - lack * share
+    # p and a share: their sums' terms and powers of |y| < 10; a weight: its power of |y| < 12, its quotient, 128 additions
+    d = (vocab / 256 + 64) * U + 2 * EXP + 3 * U * 24 + 16 * U
+    tol = (torch.softmax(z, 1) + lack * share) * d + mass * (2 * EXP + 3 * U * 12 + 140 * U)
+    assert ((dx.double() - want).abs() <= tol).all()
