@@ -10,7 +10,7 @@ import torch
 
 from oracle import lm_ops as O
 from paper_2012_03837_b200 import binding as lp
-from tests.test_gpu_logit_ops import DT, EXP, INF, U, close, cu, errors, np64, put
+from tests.test_gpu_logit_ops import DT, EXP, INF, MANY, U, between, close, cu, errors, many_rows, matrix, np64, put, same
 
 pytestmark = pytest.mark.gpu
 TINY = 2.0 ** -118                     # powers below 2^-126 are 0, against a reference off by up to 2^3, with margin
@@ -428,3 +428,49 @@ def test_tokens_in_several_entries_of_many_rows(rows, vocab, rest):
     d = (vocab / 256 + 64) * U + 2 * EXP + 3 * U * 24 + 16 * U
     tol = (torch.softmax(z, 1) + lack * share) * d + mass * (2 * EXP + 3 * U * 12 + 140 * U)
     assert ((dx.double() - want).abs() <= tol).all()
+
+
+# ------------------------------------------------------------------------------------------------ every row of many
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,vocab,pad,off", MANY)
+def test_log_sum_exp_of_every_row_and_its_gradient(rows, vocab, pad, off, dt):
+    """Rows that a block takes after its first, of all kinds in turn."""
+    g, t = many_rows(rows, vocab, pad, off, dt, rows + 2)
+    us, T = DT[dt][1], 1.25
+    z = t.double()
+    m = z.max(1, keepdim=True).values
+    some = m > -INF
+    y = torch.where(some, (z - m) / T, -INF)
+    p = torch.softmax(y, 1).nan_to_num(0.0)
+    log_s = torch.logsumexp(y, 1, keepdim=True)
+    want = torch.where(some, m / T + log_s, -INF)[:, 0]
+    far = torch.where(p > 0, -y, 0.0)
+    mean = (p * far).sum(1, keepdim=True)
+    e_logs = (vocab / 256 + 64) * U + EXP + 5 * U * mean + 8 * U + 2 * U * log_s.abs().nan_to_num(0.0, posinf=0.0)
+    e_lse = (e_logs + 3 * U * (m / T).abs())[:, 0] + U * want.abs()
+    for k in (0, min(5, vocab)):
+        lse, o = torch.full((rows,), 7.0, device="cuda"), {}
+        if k:
+            o = dict(top_ids=torch.zeros(rows, k, dtype=torch.int32, device="cuda"), top_logp=torch.zeros(rows, k, device="cuda"))
+        lp.lp_token_logprobs(t, lse=lse, temperature=T, **o)
+        same(lse, want, torch.where(torch.isfinite(want), e_lse, 0.0), ("lse", k))
+    a, b, c = (cu(g.standard_normal(rows)) for _ in range(3))
+    tok = cu(g.integers(0, vocab, rows), torch.int32)
+    at = tok.long()[:, None]
+    l = torch.where(p > 0, y - log_s, 0.0)
+    H = -(p * l).sum(1, keepdim=True)
+    rel = e_logs + 5 * U * far + EXP + 8 * U
+    e_h = e_logs + (6 * EXP + 6 * (vocab / 256 + 64) * U + 8 * U) * (1 + mean) + 5 * U * ((p * far * far).sum(1, keepdim=True) + mean * mean) + 12 * U + 2 * U * H
+    for which in ("c", "abc"):
+        a1, b1, c1 = (v.double()[:, None] if n in which else torch.zeros(rows, 1, dtype=torch.float64, device="cuda") for n, v in zip("abc", (a, b, c)))
+        grad = (c1 - a1) * p - b1 * p * (l + H)
+        grad.scatter_add_(1, at, a1)
+        k0 = a1.abs() + c1.abs() + b1.abs() * (H + 3)
+        tol = p * (rel * (k0 + b1.abs() * (l.abs() + 3)) + b1.abs() * (e_logs + 5 * U * far + 2 * U * l.abs() + e_h) + 8 * U * k0) + TINY * (k0 + 200 * b1.abs())
+        tol.scatter_add_(1, at, 8 * U * (a1.abs() + k0))
+        grad, tol = torch.where(some, grad, 0.0) / T, tol / T
+        dx = matrix(rows, vocab, t.dtype, pad, off, 5.0)
+        kw = dict(dlogp=a, dentropy=b) if which == "abc" else {}
+        lp.lp_token_logprobs_backward(t, tok if kw else None, dlse=c, dlogits=dx, temperature=T, **kw)
+        same(dx, grad, tol + us * grad.abs() * (1 + us), which)
+        assert (between(dx) == 5.0).all()
