@@ -439,7 +439,6 @@ struct Ref {
                                                               far(m_ != -INFINITY && !(fabsf(m_) * g.c <= FAR)) {}
   __device__ __forceinline__ bool apart(float x) const { return far || fabsf(x) * c > BEYOND; }
   __device__ __forceinline__ float y(float x) const { return far ? (x - m) * c : fmaf(x, c, -rho); }
-  __device__ __forceinline__ float own() const { return y(m); }         // the maximum's: what rho is off by
   // y ln 2, of a masked token's lowest value too
   __device__ __forceinline__ float nat(float x) const { return apart(x) ? (x - m) * inv_t : fmaf(x, c, -rho) * LN2; }
   // how far v lies above it, times q: that may be a number of 32 bits where the distance is none
@@ -958,15 +957,13 @@ struct Weighed {
     f = factor(ro);
     S = o.s * f + l.student * factor(Ref(l.most, g));
   }
-  // Either reference may be far.  Two that are not are multiples of one unit, whose difference is all there is; otherwise the
-  // maximum of b stands in one sum as 2^own and has to stand in the other as 2^y.
-  __device__ __forceinline__ bool near(const Ref& b) const { return !b.far && !ref.far; }
-  __device__ __forceinline__ float factor(const Ref& b) const {
-    return b.m == -INFINITY ? 0.f : ex2(near(b) ? b.rho - ref.rho : ref.y(b.m) - b.own());
+  // What the powers of b's sum are lower by than those of ref's, in 64 bits where either is far: a far maximum times c need not be
+  // a number of 32 bits.
+  __device__ __forceinline__ double apart(const Ref& b) const {
+    return (b.far ? (double)b.m * b.c : (double)b.rho) - (ref.far ? (double)ref.m * ref.c : (double)ref.rho);
   }
-  __device__ __forceinline__ double log_factor(const Ref& b) const {     // of b.m above -infinity
-    const double ln2 = 0.693147180559945309417;
-    return near(b) ? ((double)b.rho - (double)ref.rho) * ln2 : (double)ref.nat(b.m) - (double)b.own() * ln2;
+  __device__ __forceinline__ float factor(const Ref& b) const {
+    return b.m == -INFINITY ? 0.f : ex2(b.far || ref.far ? (float)apart(b) : b.rho - ref.rho);
   }
 };
 
@@ -1226,13 +1223,13 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
         const double log_o = log_of(1), log_l = log_of(2), log_q = log_of(3);
         double logr;                                       // log p_r
         if (s.ref.far || s.ro.far || rl.far || o.s == 0.f || l.student == 0.f) {
-          logr = o.s == 0.f ? -(double)INFINITY : s.log_factor(s.ro) + log_o - logs;
+          logr = o.s == 0.f ? -(double)INFINITY : s.apart(s.ro) * LN2D + log_o - logs;
         } else {
           // both from one ratio of the listed to the others, whose rounding they then share: it enters the loss by p_r - q_r only
-          const double apart = (double)rl.rho - (double)s.ro.rho;
-          const float u = l.student / o.s * ex2((float)apart), v = o.s / l.student * ex2((float)-apart);
-          const double lr = log_o + ((double)s.ro.rho - (double)s.ref.rho) * LN2D;
-          logs = u <= 1.f ? lr + (double)log1pf(u) : log_l + ((double)rl.rho - (double)s.ref.rho) * LN2D + (double)log1pf(v);
+          const float up = rl.rho - s.ro.rho;
+          const float u = l.student / o.s * ex2(up), v = o.s / l.student * ex2(-up);
+          const double lr = log_o + s.apart(s.ro) * LN2D;
+          logs = u <= 1.f ? lr + (double)log1pf(u) : log_l + s.apart(rl) * LN2D + (double)log1pf(v);
           logr = u <= 1.f ? -(double)log1pf(u) : lr - logs;
         }
         loss = (double)part + w.mass * logs;

@@ -197,6 +197,30 @@ def test_a_loss_is_finite_where_a_log_probability_is_not(dt):
             close(np64(loss), want, np.abs(np.where(np.isfinite(want), want, 0.0)) * (2 * EXP + 3 * U * 70 + 16 * U) + 72 * U + 4 * EXP, (T, rest))
 
 
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+def test_a_loss_is_finite_where_the_rests_log_probability_is_not(dt):
+    """All but the listed tokens at the type's lowest values: log p of the rest is below fp32's range, its weight times it is not."""
+    g = np.random.default_rng(4)
+    x = np.full((3, 600), -3.3e38)
+    x[1] = -2.0e38
+    ids = np.stack([g.permutation(600)[:3] for _ in range(3)]).astype(np.int32)
+    np.put_along_axis(x, ids, g.standard_normal((3, 3)), 1)
+    np.put_along_axis(x[2:], ids[2:], np.array([[1e37, 0.5e37, -1e37]]), 1)
+    t = put(x, DT[dt][0])
+    x = np64(t)
+    te = np.log([[0.5, 0.3, 0.15], [0.3, 0.2, 0.2], [0.4, 0.2, 0.35]]).astype(np.float32)
+    for T in (0.75, 0.5, 0.25):
+        loss, dx = torch.zeros(3, device="cuda"), torch.zeros_like(t)
+        lp.lp_distill(lp.LP_DISTILL_REST, t, cu(ids, torch.int32), cu(te), loss=loss, dlogits=dx, temperature=T)
+        want, w_dx = O.distill(x, ids, te.astype(np.float64), True, T)
+        fits = want < 3.0e38
+        assert fits[:2].all() or T == 0.25
+        # the rest: 64 bits rounded once; the listed tokens' distances, three roundings each; c, one
+        close(np64(loss)[fits], want[fits], want[fits] * 32 * U)
+        # the others' sum, 600 equal terms, their shares and p of the listed ones: orders of one
+        close(np64(dx), w_dx, (np.abs(w_dx) + (w_dx != 0) * 1e-3) * (72 * U + 4 * EXP) + DT[dt][1] * np.abs(w_dx) * 1.01, T)
+
+
 # ------------------------------------------------------------------------------------------------ values of any size
 TEMPERATURES = [0.5, 0.699999988079071, 0.75, 1.0, 1.5, 2.0]
 
