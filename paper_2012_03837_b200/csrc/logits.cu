@@ -813,7 +813,7 @@ __device__ __forceinline__ void gradient(const Piece<T, NT, B>& p, uint4* buf, f
   constexpr int N = Vec<T>::N;
   auto one = [&](float x, int j) {
     const float y = ref.y(W && !ref.far ? max_nan(x, g.lo) : x), e = ex2(y);
-    return (e == 0.f && k0 == k0 ? 0.f : W ? e * fmaf(k1, y, k0) : e * k0) + (j == t ? at_t : 0.f);
+    return (W && e != 0.f ? e * fmaf(k1, y, k0) : e * k0) + (j == t ? at_t : 0.f);       // y may be infinite
   };
   if (p.edge >= 0) dst[p.edge] = from_f<T>(one(edge, p.edge));
   if (ref.far) {

@@ -498,3 +498,41 @@ def test_log_sum_exp_of_every_row_and_its_gradient(rows, vocab, pad, off, dt):
         lp.lp_token_logprobs_backward(t, tok if kw else None, dlse=c, dlogits=dx, temperature=T, **kw)
         same(dx, grad, tol + us * grad.abs() * (1 + us), which)
         assert (between(dx) == 5.0).all()
+
+
+# ------------------------------------------------------------------------------------------------ gradients that are no numbers
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+@pytest.mark.parametrize("value", [INF, -INF, float("nan")])
+def test_an_incoming_gradient_that_is_no_number_spoils_its_whole_row(value, dt):
+    """0 times infinity is NaN for a masked token too, wherever in the row it stands and however the row is aligned."""
+    g = np.random.default_rng(8)
+    rows, vocab = 6, 77
+    x = g.standard_normal((rows, vocab))
+    x[:, g.random(vocab) < 0.4] = -np.inf
+    x[:, [0, 40, 76]], x[:, 1] = -np.inf, 0.5
+    x[4] = np.where(np.isinf(x[4]), -np.inf, -3.0e38)       # a far row
+    x[5] = -np.inf                                          # no token: nothing comes of it
+    tok = np.full(rows, 1, dtype=np.int32)
+    f = lambda *v: cu(np.array(v, dtype=np.float32))
+    dlogp, other, dloss = f(1, value, 2, 1, value, value), f(1, 0, value, 1, 0, 0), f(1, value, 0, 1, value, value)
+    for off in range(4):
+        t = put(x, DT[dt][0], 1, off)
+        dx = matrix(rows, vocab, DT[dt][0], 2, off, 5.0)
+        for kw, rows_spoilt in ((dict(dlogp=dlogp), (1, 4)), (dict(dlse=other), (2,)), (dict(dlogp=dlogp, dentropy=other), (1, 2, 4)),
+                                (dict(dlogp=dlogp, dentropy=other, dlse=other), (1, 2, 4))):
+            lp.lp_token_logprobs_backward(t, cu(tok, torch.int32), dlogits=dx, **kw)
+            got = np64(dx)
+            masked = np.isinf(x)
+            for r in range(rows):
+                bad = ~np.isfinite(got[r])
+                assert bad.all() if r in rows_spoilt else not bad.any(), (off, r, tuple(kw))
+                if r in rows_spoilt:
+                    assert np.isnan(got[r][masked[r]]).all(), (off, r, tuple(kw))
+            assert (got[5] == 0).all()
+        ids, te = cu(np.array([[3, 1]] * rows), torch.int32), cu(np.log(np.full((rows, 2), 0.25)))
+        for form in (lp.LP_DISTILL_TOP, lp.LP_DISTILL_REST):
+            lp.lp_distill(form, t, ids, te, dlogits=dx, dloss=dloss)
+            got = np64(dx)
+            for r in (0, 2, 3, 5):
+                assert np.isfinite(got[r]).all()
+            assert np.isnan(got[1][np.isinf(x[1]) & (np.arange(vocab) != 3)]).all() and not np.isfinite(got[1]).any()
