@@ -576,20 +576,21 @@ def _logits(t, what: str, of=None):
 _logits_codes = {}
 
 
-def _ids(t, rows: int, what: str) -> int:
-    """Entries per row of a matrix of token ids."""
-    if getattr(t, "ndim", 0) != 2 or t.shape[0] != rows:
+def _ids(t, rows: int, what: str):
+    """Shape of a matrix of token ids."""
+    shape = getattr(t, "shape", ())
+    if len(shape) != 2 or shape[0] != rows:
         raise LpError(-2, f"{what} must be a matrix [rows, k]")
-    return t.shape[1]
+    return shape
 
 
-def _beside(t, kind, ids, what: str):
-    """Device address of the values that go with ids: a matrix of their shape (those of a wider one would belong to other
-    tokens), or a raw address."""
-    shape = getattr(t, "shape", None)
-    if shape is not None and shape != ids.shape:
-        raise LpError(-2, f"{what} must have the shape of its ids, {tuple(ids.shape)}, not {tuple(shape)}")
-    return _buffer(t, kind, ids.shape[0] * ids.shape[1], what)
+def _beside(t, kind, ids, n: int, what: str):
+    """Device address of the n values that go with ids of the shape `ids`: a matrix of the same (those of a wider one would
+    belong to other tokens), or a raw address."""
+    shape = getattr(t, "shape", ids)
+    if shape != ids:
+        raise LpError(-2, f"{what} must have the shape of its ids, {tuple(ids)}, not {tuple(shape)}")
+    return _buffer(t, kind, n, what)
 
 
 def lp_token_logprobs(logits, tokens=None, logp=None, entropy=None, lse=None, top_ids=None, top_logp=None, temperature: float = 1.0,
@@ -601,8 +602,9 @@ def lp_token_logprobs(logits, tokens=None, logp=None, entropy=None, lse=None, to
     _, i32, f32, _, _ = _kinds
     k, tops = 0, None
     if top_ids is not None:
-        k = _ids(top_ids, rows, "lp_token_logprobs: top_ids")
-        tops = _beside(top_logp, f32, top_ids, "lp_token_logprobs: top_logp")
+        shape = _ids(top_ids, rows, "lp_token_logprobs: top_ids")
+        k = shape[1]
+        tops = _beside(top_logp, f32, shape, rows * k, "lp_token_logprobs: top_logp")
     elif top_logp is not None:
         tops = _buffer(top_logp, f32, 0, "lp_token_logprobs: top_logp")
     _check(None, _lib.lp_token_logprobs(code, x, ld, _buffer(tokens, i32, rows, "lp_token_logprobs: tokens"),
@@ -639,9 +641,10 @@ def lp_distill(form: int, logits, teacher_ids, teacher, loss=None, dloss=None, d
     if dlogits is not None:
         _, dx, ld_out, _ = _logits(dlogits, "lp_distill: dlogits", logits)
     _, i32, f32, _, _ = _kinds
-    k = _ids(teacher_ids, rows, "lp_distill: teacher_ids")
+    shape = _ids(teacher_ids, rows, "lp_distill: teacher_ids")
+    k = shape[1]
     _check(None, _lib.lp_distill(form, code, x, ld, _buffer(teacher_ids, i32, rows * k, "lp_distill: teacher_ids"),
-                                 _beside(teacher, f32, teacher_ids, "lp_distill: teacher"), k, _buffer(loss, f32, rows, "lp_distill: loss"),
+                                 _beside(teacher, f32, shape, rows * k, "lp_distill: teacher"), k, _buffer(loss, f32, rows, "lp_distill: loss"),
                                  _buffer(dloss, f32, rows, "lp_distill: dloss"), dx, ld_out, rows, vocab, temperature, scale,
                                  _buffer(out_of_range, i32, 1, "lp_distill: out_of_range"), stream))
 
