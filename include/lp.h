@@ -472,12 +472,13 @@ lp_status lp_linear_attention_bf16(int form, const lp_linattn_desc* desc, void* 
  *   x: a row of logits; z = x / temperature, 2^-20 <= temperature <= 2^20; p = softmax(z); lse = log sum exp(z).  A logit
  *   of -infinity is a masked token: probability 0, no part in the entropy, gradient 0.  A row of them alone: lse and log
  *   probabilities are -infinity, entropy and gradients 0.  A row with a NaN or +infinity: NaN in lse, log probabilities,
- *   entropy, loss and all of its gradient.  So does an incoming gradient that is infinite or NaN for its row's gradient, masked
- *   tokens among it.  Finite logits may have any size: a large negative number masks a token as far as its own power goes.
+ *   entropy, loss and all of its gradient.  An incoming gradient that is infinite or NaN leaves no number in its row's gradient
+ *   (NaN for masked tokens).  Finite logits may have any size; a large negative number in place of -infinity masks a token as
+ *   far as its own probability goes.
  *   A row's sums are cut into as many pieces as its length, the number of rows and the call ask for: equal calls give equal
  *   bits, the same row in calls of other shapes may round otherwise.
  *   A token id below 0 says that there is none; one >= vocab is taken for none too and, if out_of_range is not NULL, bit 0
- *   of that device int is set (never cleared).
+ *   of that device int is set (never cleared).  Tokens are looked at where logp (dlogp) is given.
  */
 #define LP_LOGITS_VOCAB_MAX (1 << 18)
 #define LP_TOP_MAX 128

@@ -24,7 +24,9 @@
 //   Rows that are only read (logprobs_kernel) stream through a ring of two batches, whatever their length.
 //   Rows that need a second pass (gradients, distillation) stay in shared memory: pieces of up to 65 KB, three blocks to an SM;
 //   as the second pass leaves a batch, the next row's takes its place.  A cluster of up to eight blocks shares a longer row and
-//   exchanges its sums through distributed shared memory; so do blocks that share a row because rows are few.
+//   exchanges its sums through distributed shared memory; so do blocks that share a row because rows are few.  Above 133120 fp32
+//   logits eight pieces are longer, up to 128 KB, and one or two blocks on an SM (512 x 262144: gradient 321 us against 164 to pass,
+//   distillation 282; 512 x 133120: 100 and 100 against 83).
 // Measured, replayed from a graph, against the bytes at 6.54 TB/s: 8192 x 32768 bf16 log probabilities 85 us (82), with entropy
 // 89 (82), with 64 alternatives 158 (83), gradient with entropy 179 (164), distillation with gradient 190 (165), with a rest 208;
 // 1031 x 50021 fp32 with 5 alternatives 36 (32); 1000 x 131071 bf16 distillation from 128 entries and a rest 125 (80).
@@ -345,7 +347,8 @@ struct Running {
   }
 };
 
-// The same against the row's maximum, for far rows, one element after the other, without the `k` tokens of `skip`.
+// The same against the row's maximum, for far rows, one element after the other, without the `k` tokens of `skip`, each of them compared
+// with each: 8192 x 32768 bf16 360 us (84 if not far), gradient 641 (178), distillation 820 (212), beside a rest and 64 entries 6300 (229).
 template <typename T, int NT, int B, bool W>
 __device__ __noinline__ Sums sweep_far(const Piece<T, NT, B> p, const Geometry g, float m, float edge, const int* skip = nullptr, int k = 0) {
   Sums a{m, 0.f, 0.f};
@@ -1276,7 +1279,11 @@ __global__ void __launch_bounds__(NT + 32, NT == STAY ? 4 : 1) distill_kernel(co
 }
 
 // ---------------------------------------------------------------------------------------------- launches
-constexpr int PIECE = 4160;                   // vectors of a staying piece that let three blocks share an SM
+// Vectors of a staying piece at most: 65 KB, so that three blocks share an SM.  Pieces to 4400 would fit three times too: with that limit
+// bf16 rows of 34000 take 101 us instead of 111 (gradient) and 119 instead of 142 (distillation), but those of 100300 110 instead of
+// 105 and fp32 rows of 16700 211 instead of 191.
+constexpr int PIECE = 4160;
+constexpr int SMS = 148;                      // of a B200, and not asked of the device: a row's cut, and with it its bits, goes by sizes alone
 
 struct Plan {
   Geometry g;
@@ -1293,8 +1300,8 @@ Plan plan_rows(const LogitsIn& in, int elem_bytes, int threads, int batch, bool 
   auto split = [&](int blocks, int vectors) {
     while (threads > FEW && 2 * c <= MAX_CLUSTER && (long long)in.rows * c < blocks && all / (2 * c) >= vectors) c *= 2;
   };
-  split(4 * 148, 4096);
-  if (!top) split(148, 1024);
+  split(4 * SMS, 4096);
+  if (!top) split(SMS, 1024);
   const int per = (all + c - 1) / c;
   p.rows = in.rows;
   p.threads = threads + more_threads;
@@ -1350,7 +1357,7 @@ struct Residency {
 };
 
 // Rows of at most `limit` bytes, enough of them to give every warp of the device one.
-bool short_rows(const LogitsIn& in, size_t elem_bytes, size_t limit) { return in.vocab * elem_bytes <= limit && in.rows >= 148 * 8; }
+bool short_rows(const LogitsIn& in, size_t elem_bytes, size_t limit) { return in.vocab * elem_bytes <= limit && in.rows >= SMS * 8; }
 
 template <typename... KArgs, typename A>
 cudaError_t run(void (*kernel)(KArgs...), Residency& residency, const Plan& p, cudaStream_t s, const A& a) {
@@ -1376,9 +1383,12 @@ cudaError_t run_logprobs(const LogprobsArgs& a, cudaStream_t s) {
     if (p.g.cluster > 1) return run_logprobs<T, NT, W, true, TOP>(a, p, s);
   return run_logprobs<T, NT, W, false, TOP>(a, p, s);
 }
+// A warp leaves 64 maxima to find a bound for its alternatives with, which is close for up to half as many: 32 of 2048 bf16 logits in
+// 16384 rows take 61 us against 104 with four warps per row, 64 of them 354 against 128.
+constexpr int TOP_OF_A_WARP = 32;
 template <typename T, bool W>
 cudaError_t run_logprobs(const LogprobsArgs& a, cudaStream_t s) {
-  if (short_rows(a.in, sizeof(T), 16384) && a.top_k <= FEW) return a.top_k > 0 ? run_logprobs<T, FEW, W, true>(a, s) : run_logprobs<T, FEW, W, false>(a, s);
+  if (short_rows(a.in, sizeof(T), 16384) && a.top_k <= TOP_OF_A_WARP) return a.top_k > 0 ? run_logprobs<T, FEW, W, true>(a, s) : run_logprobs<T, FEW, W, false>(a, s);
   return a.top_k > 0 ? run_logprobs<T, STREAM, W, true>(a, s) : run_logprobs<T, STREAM, W, false>(a, s);
 }
 template <typename T, int NT, bool W, bool CL>
