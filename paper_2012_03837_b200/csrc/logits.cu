@@ -28,7 +28,7 @@
 //   logits eight pieces are longer, up to 128 KB, and one or two blocks on an SM (512 x 262144: gradient 321 us against 164 to pass,
 //   distillation 282; 512 x 133120: 100 and 100 against 83).
 // Measured, replayed from a graph, against the bytes at 6.54 TB/s: 8192 x 32768 bf16 log probabilities 85 us (82), with entropy
-// 89 (82), with 64 alternatives 158 (83), gradient with entropy 179 (164), distillation with gradient 190 (165), with a rest 208;
+// 89 (82), with 64 alternatives 158 (83), gradient with entropy 179 (164), distillation with gradient 190 (165), with a rest 209;
 // 1031 x 50021 fp32 with 5 alternatives 36 (32); 1000 x 131071 bf16 distillation from 128 entries and a rest 125 (80).
 #include <algorithm>
 #include <atomic>
@@ -960,8 +960,7 @@ struct Weighed {
     f = factor(ro);
     S = o.s * f + l.student * factor(Ref(l.most, g));
   }
-  // What the powers of b's sum are lower by than those of ref's, in 64 bits where either is far: a far maximum times c need not be
-  // a number of 32 bits.
+  // b's reference above ref's, in powers of two: in 64 bits, as a far row's, its maximum times c, need be no number of 32 bits.
   __device__ __forceinline__ double apart(const Ref& b) const {
     return (b.far ? (double)b.m * b.c : (double)b.rho) - (ref.far ? (double)ref.m * ref.c : (double)ref.rho);
   }

@@ -536,3 +536,26 @@ def test_an_incoming_gradient_that_is_no_number_spoils_its_whole_row(value, dt):
             for r in (0, 2, 3, 5):
                 assert np.isfinite(got[r]).all()
             assert np.isnan(got[1][np.isinf(x[1]) & (np.arange(vocab) != 3)]).all() and not np.isfinite(got[1]).any()
+
+
+# ------------------------------------------------------------------------------------------------ few tokens to choose from
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,vocab,k", [(2000, 300, 32), (7, 9000, 128), (3, 131071, 16), (20, 200003, 128)])
+def test_more_alternatives_asked_for_than_tokens_left(rows, vocab, k, dt):
+    """A grammar's few tokens first, then the masked ones by ascending id, in one block and over several, whatever the mask."""
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    x = torch.randn(rows, vocab, generator=g, device="cuda")
+    keep = torch.zeros(rows, vocab, dtype=torch.bool, device="cuda")
+    for r in range(rows):
+        n = (0, 1, 5, 100, 5)[r % 5]
+        at = torch.randint(0, vocab, (n,), generator=g, device="cuda") if r % 5 < 3 else torch.arange(n, device="cuda") + vocab // 3
+        keep[r, at.clamp(max=vocab - 1)] = True
+    for mask in (-INF, -1e10, 0.0):
+        t = put(np.zeros((rows, vocab)), DT[dt][0], 1, 1)
+        t.copy_(torch.where(keep, x, mask))
+        ids, tops = torch.zeros(rows, k, dtype=torch.int32, device="cuda"), torch.zeros(rows, k, device="cuda")
+        lp.lp_token_logprobs(t, top_ids=ids, top_logp=tops)
+        want = torch.sort(t.float(), dim=1, descending=True, stable=True).indices[:, :k]
+        assert torch.equal(ids.long(), want), mask
+        none = torch.isinf(torch.gather(t, 1, want))
+        assert (tops[none] == -INF).all() and torch.isfinite(tops[~none]).all()
